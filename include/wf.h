@@ -30,6 +30,14 @@
  *   wf_ctx_set_batch        replica batch limit B_q (Eq. 11, Section 3.5)
  *   wf_ctx_destroy, wf_strerror, wf_last_error
  *
+ * What an execution grant (Section 3.2) turns into on a replica, where admitted
+ * activations run as rows of a paged KV cache:
+ *
+ *   wf_decode_create, wf_decode_status, wf_decode_destroy
+ *   wf_kv_extend            admission by free blocks, block tables and slots of a step's tokens
+ *   wf_beam_select          beam search's selection over beams and vocabulary
+ *   wf_kv_reorder           rows put in the selection's order: tables, last blocks, freed blocks
+ *
  * Conventions.
  *   - Times are int64 microseconds, memory int32 MiB; every output is an
  *     exact integer.
@@ -492,6 +500,185 @@ int wf_ctx_set_eval_path(wf_ctx *ctx, int32_t path);
  * WF_EINVAL for a value outside 0..64 or such a problem.
  */
 int wf_ctx_set_batch(wf_ctx *ctx, int32_t batch);
+
+/* ------------------------------------------------------------------------
+ * Rows of a replica's paged KV cache, and beam search over them.
+ *
+ * The cache's memory is n_blocks blocks of block_tokens tokens.  A row (one
+ * sequence; under beam search one hypothesis) lists its blocks in a table:
+ * token position p of row r lies in block table[r][p / block_tokens], at
+ * p % block_tokens.  The paper's runtime leaves this to its serving engine
+ * (Section 4.1); Eq. 11's memory check is the same admission in MiB.
+ * ------------------------------------------------------------------------ */
+
+typedef struct wf_decode wf_decode;
+
+/* Largest sizes of the calls on a wf_decode, which sizes its scratch. */
+typedef struct {
+    int32_t max_rows;        /* 1..65536 */
+    int32_t max_row_blocks;  /* table width of wf_kv_reorder, >= 0 (0: not called); max_rows * max_row_blocks < 2^31 */
+    int32_t max_vocab;       /* of wf_beam_select, 0..2^24 (0: not called) */
+    int32_t max_keep;        /* of wf_beam_select, 0..64 */
+} wf_decode_limits;
+
+/*
+ * Scratch for the calls below on device `device`: about 4 bytes per table
+ * cell of the limits and, for the selection, up to (8 * max_keep + 8) bytes
+ * per row and 8,192 tokens of vocabulary.  The calls allocate nothing more.
+ * One wf_decode serves one stream at a time.  Returns WF_OK, WF_EINVAL,
+ * WF_ENOMEM or WF_ECUDA.
+ */
+int wf_decode_create(const wf_decode_limits *limits, int device, wf_decode **out);
+
+/*
+ * Synchronize `stream` and report (then clear) what earlier calls found on
+ * the device: WF_EINVAL when a table or the ring named a block outside the
+ * cache (its copy was left out), else WF_OK.
+ */
+int wf_decode_status(wf_decode *d, void *stream);
+
+/* Release the scratch (NULL is a no-op). */
+void wf_decode_destroy(wf_decode *d);
+
+/*
+ * The rows' tables and the pool of free blocks; DEVICE pointers, caller-owned.
+ *   table[r * table_stride / 4 + j]: block j of row r; row r holds the first
+ *     ceil(len[r] / block_tokens) entries, the others are unspecified.
+ *   ring[(i mod n_blocks)] for ends[0] <= i < ends[1]: the free block ids,
+ *     taken at ends[0] and given back at ends[1] (both >= 0, never wrapped).
+ *     The caller starts with ring = 0..n_blocks-1 and ends = {0, n_blocks}.
+ */
+typedef struct {
+    int32_t rows;          /* 1..65536 */
+    int32_t row_blocks;    /* width of the table, >= 1 */
+    int32_t block_tokens;  /* >= 1 */
+    int32_t n_blocks;      /* 1..2^31-2 */
+    int32_t *table;
+    int64_t table_stride;  /* bytes, a multiple of 4, >= 4 * row_blocks */
+    int32_t *len;          /* [rows] tokens cached */
+    int32_t *ring;         /* [n_blocks] */
+    int64_t *ends;         /* [2] */
+} wf_kv;
+
+/* Status bits of a row (wf_kv_step.status, wf_kv_reorder). */
+enum {
+    WF_KV_LONG = 1u,     /* a negative length or more tokens than a table row holds: the row is left out */
+    WF_KV_BLOCKS = 2u,   /* waits: the free blocks end before it (extend); its last tokens were lost (reorder) */
+    WF_KV_TOKENS = 4u,   /* waits: max_tokens ends before it */
+    WF_KV_PARENT = 1u    /* reorder: the parent is no row of the group; treated as -1 */
+};
+
+/* What wf_kv_extend writes; DEVICE pointers, caller-owned. */
+typedef struct {
+    int64_t max_tokens;  /* tokens of a step, 1..2^31-2 */
+    int64_t *slot;       /* [max_tokens] cache slot of each new token: block * block_tokens + place; -1 past the last */
+    int32_t *pos;        /* [max_tokens] its position in its row; 0 past the last */
+    int32_t *row;        /* [max_tokens] its row; -1 past the last */
+    int32_t *start;      /* [rows + 1] the first token of each row in this step; start[rows]: tokens in all */
+    int32_t *len;        /* [rows] tokens cached once the step has run (may be kv->len) */
+    int64_t *ends;       /* [2] the pool's ends afterwards (may be kv->ends) */
+    uint32_t *status;    /* [rows] WF_KV_* bits */
+} wf_kv_step;
+
+/*
+ * A step's tokens: row r has len[r] tokens cached and asks for add[r] more
+ * (DEVICE int32 [rows]): a whole prompt, a chunk of one, one token, none.
+ * Rows are admitted in their order until the blocks that they need exceed
+ * the free ones or their tokens exceed max_tokens; that row and those
+ * after it wait (a line: the caller orders rows by priority).  A row that a
+ * table row cannot hold is passed over (WF_KV_LONG).  For the admitted
+ * rows, missing blocks are taken from the ring in the order of rows and
+ * appended to kv->table; every new token's slot, position and row are
+ * written, and the places up to max_tokens are filled (-1, 0, -1), so that a
+ * captured graph of this size can run behind the call.
+ * out->len and out->ends may be the inputs themselves (the state then moves
+ * on); no other output may overlap an input.  Asynchronous on `stream`; no
+ * allocation.  Returns WF_EINVAL for null pointers and sizes out of range.
+ */
+int wf_kv_extend(wf_decode *d, const wf_kv *kv, const int32_t *add, const wf_kv_step *out, void *stream);
+
+/* Element types of the logits (wf_beam.dtype). */
+enum { WF_F32 = 0, WF_F16 = 1, WF_BF16 = 2 };
+
+/*
+ * One step of beam search: `groups` searches of `beams` rows each; row
+ * g * beams + k is beam k of search g.  DEVICE pointers.
+ */
+typedef struct {
+    int32_t groups;        /* >= 1; groups * beams <= max_rows */
+    int32_t beams;         /* 1..32 */
+    int32_t vocab;         /* 1..max_vocab */
+    int32_t keep;          /* candidates returned for each search, 1..max_keep */
+    int32_t dtype;         /* WF_F32, WF_F16 or WF_BF16 */
+    int32_t eos;           /* the token that ends a hypothesis, or -1 */
+    const void *logits;    /* [groups * beams][vocab], aligned to its elements */
+    int64_t logits_stride; /* bytes between rows, a multiple of the element size */
+    const float *score;    /* [groups * beams] log probability so far; -inf: an empty beam, its logits are not read */
+} wf_beam;
+
+typedef struct {
+    float *score;        /* [groups][keep] */
+    int32_t *parent;     /* [groups][keep] row (0..groups*beams-1) that the candidate continues */
+    int32_t *token;      /* [groups][keep] */
+    float *next_score;   /* [groups][beams], and the next two: the first `beams` candidates that do not end, in */
+    int32_t *next_parent; /* order: the next step's rows (next_parent is wf_kv_reorder's parent).  All three or none */
+    int32_t *next_token; /* may be NULL */
+} wf_beam_out;
+
+/*
+ * The `keep` best continuations of each search: candidate (k, v) has the sum
+ *   score[k] + log softmax(logits[k])[v]
+ * in 32-bit floating point, (x - max) - log(sum of exp(x - max)) added to the
+ * score; best first.  Equal sums: the lower beam first, in a beam the larger
+ * logit, then the lower token.  A logit of -inf or NaN is masked: no
+ * candidate, no part of the sum; a row with a logit of +inf shares its
+ * probability among those.  A row that is masked throughout, or whose score
+ * is -inf or NaN, has no candidates.  Places without a candidate hold score
+ * -inf, parent -1 and token -1.  No output may overlap an input.  The
+ * result does not depend on the order of arrival of the GPU's blocks.
+ * Asynchronous on `stream`; no allocation.  WF_EINVAL as above.
+ */
+int wf_beam_select(wf_decode *d, const wf_beam *in, const wf_beam_out *out, void *stream);
+
+/*
+ * The cache's memory, for copies of blocks: `planes` arrays (a layer's keys,
+ * its values, ...), each [n_blocks][block_tokens][token_bytes]; DEVICE.
+ */
+typedef struct {
+    void *base;
+    int32_t planes;        /* >= 1 */
+    int32_t reserved;      /* 0 */
+    int64_t plane_stride;  /* bytes between planes, >= n_blocks * block_tokens * token_bytes */
+    int64_t token_bytes;   /* >= 1 */
+} wf_kv_cache;
+
+/*
+ * The rows in the order that a selection chose: rows come in groups of
+ * `group` (1..32, dividing rows), and new row r of a group continues the old
+ * row parent[r] (DEVICE int32 [rows]) of the same group, or nothing (-1).
+ * parent = -1 throughout a group gives all its blocks back.  Rows share
+ * blocks with rows of their group only, and then at the same place of the
+ * table (as this call leaves them); lengths beyond the table's width count
+ * as the width.
+ *   - to->table's row r gets the parent's entries, to->len[r] its length
+ *     (entries past a row's blocks keep what they held);
+ *   - a block that no new row of its group holds is free;
+ *   - a last block that is partly filled and that several new rows of the
+ *     group hold stays with the lowest of them; each other row gets a block of its own,
+ *     the group's freed ones first (by place in the table, then by old row),
+ *     then from the ring, in the order of rows, and the tokens it holds are copied in every
+ *     plane of `cache` (NULL: no copies made); copies[r] = {from, to}, or
+ *     {-1, -1};
+ *   - freed blocks that are left go to the ring, by group.
+ * Blocks freed in this call serve other groups from the next call on.  If the
+ * ring runs out, a row is cut to its whole blocks and gets WF_KV_BLOCKS.
+ * *to has the sizes and the ring of *kv; its table, len and ends may be
+ * those of *kv too (each the same memory or disjoint).  copies: DEVICE int32
+ * [rows][2]; status: DEVICE uint32 [rows].  Asynchronous on `stream`; no
+ * allocation.  WF_EINVAL as above.
+ */
+int wf_kv_reorder(wf_decode *d, const wf_kv *kv, int32_t group, const int32_t *parent, const wf_kv *to,
+                  const wf_kv_cache *cache, int32_t *copies, uint32_t *status, void *stream);
 
 /* Release every device and host allocation of the context (NULL is a no-op). */
 void wf_ctx_destroy(wf_ctx *ctx);

@@ -1,0 +1,41 @@
+// Internal definitions of the calls on a replica's rows: cache bookkeeping
+// (wf_kv.cu) and beam selection (wf_beam.cu).
+#pragma once
+
+#include "wf_internal.cuh"
+
+// Per-call scratch, one device allocation made by wf_decode_create.
+struct wf_decode {
+    int device;
+    int sms;
+    wf_decode_limits lim;
+    void *mem;
+    int *err;              // device error word (wf_decode_status)
+    uint32_t *ticket;      // [1 + 2 * max_rows] arrivals of CTAs; every call leaves them 0
+    int32_t *sums;         // [3 * max_rows + 3] extend's sums where shared memory does not hold them
+    // reorder
+    int32_t *freed;        // [max_rows][row blocks rounded up to a tile] ids of a tile's freed blocks
+    int32_t *tile_freed;   // [groups][tiles] their count
+    uint32_t *tile_copy;   // [groups][tiles] rows that need a copy of a block of this tile
+    int32_t *copy_from;    // [max_rows] the block that a row's copy is made from
+    int4 *group_plan;      // [groups] {first position in the ring's tail, in its head, blocks used for copies, blocks freed}
+    int64_t *ring_was;     // [2] head and tail before the call
+    int4 *pairs;           // [max_rows] {from, to, tokens, 0}
+    uint32_t *n_pairs;
+    // select
+    float2 *part;          // [lists] a chunk's maximum and its sum of exponentials
+    uint64_t *list;        // [lists][max_keep] a chunk's best, best first
+    uint64_t *row_key;     // [max_rows][max_keep]
+    int32_t *row_token;    // [max_rows][max_keep]
+    int64_t lists;
+};
+
+constexpr int kTileCols = 256;     // columns of the tables that a CTA of the reorder takes
+constexpr int kMaxGroup = 32;      // rows of a group, beams
+constexpr int kMaxKeep = 64;
+
+int64_t wf_beam_lists(int64_t rows, int64_t vocab);
+int wf_launch_extend(wf_decode *d, const wf_kv *kv, const int32_t *add, const wf_kv_step *out, cudaStream_t st);
+int wf_launch_reorder(wf_decode *d, const wf_kv *kv, int32_t group, const int32_t *parent, const wf_kv *to,
+                      const wf_kv_cache *cache, int32_t *copies, uint32_t *status, cudaStream_t st);
+int wf_launch_select(wf_decode *d, const wf_beam *in, const wf_beam_out *out, cudaStream_t st);

@@ -26,7 +26,9 @@ EXPORTS = ("wf_problem_check", "wf_ctx_create", "wf_forecast_readiness", "wf_eva
            "wf_eval_plans_static", "wf_mutate_plans", "wf_merge_elite", "wf_local_search",
            "wf_construct_plans", "wf_ctx_set_reclaim", "wf_ctx_check_wait_expiry", "wf_eval_plans_phi",
            "wf_topk_phi", "wf_static_status", "wf_ctx_set_eval_path",
-           "wf_ctx_set_batch", "wf_eval_topk_host", "wf_ctx_reserve_host")
+           "wf_ctx_set_batch", "wf_eval_topk_host", "wf_ctx_reserve_host",
+           "wf_decode_create", "wf_decode_status", "wf_decode_destroy", "wf_kv_extend", "wf_beam_select",
+           "wf_kv_reorder")
 
 
 class WfError(RuntimeError):
@@ -60,6 +62,39 @@ class wf_plans(ctypes.Structure):
 class wf_eval_out(ctypes.Structure):
     _fields_ = [("makespan_us", ctypes.c_void_p), ("p95_us", ctypes.c_void_p),
                 ("gpu_us", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
+class wf_decode_limits(ctypes.Structure):
+    _fields_ = [("max_rows", ctypes.c_int32), ("max_row_blocks", ctypes.c_int32), ("max_vocab", ctypes.c_int32),
+                ("max_keep", ctypes.c_int32)]
+
+
+class wf_kv(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("row_blocks", ctypes.c_int32), ("block_tokens", ctypes.c_int32),
+                ("n_blocks", ctypes.c_int32), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("len", ctypes.c_void_p), ("ring", ctypes.c_void_p), ("ends", ctypes.c_void_p)]
+
+
+class wf_kv_step(ctypes.Structure):
+    _fields_ = [("max_tokens", ctypes.c_int64), ("slot", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+                ("row", ctypes.c_void_p), ("start", ctypes.c_void_p), ("len", ctypes.c_void_p),
+                ("ends", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
+class wf_beam(ctypes.Structure):
+    _fields_ = [("groups", ctypes.c_int32), ("beams", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("keep", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eos", ctypes.c_int32),
+                ("logits", ctypes.c_void_p), ("logits_stride", ctypes.c_int64), ("score", ctypes.c_void_p)]
+
+
+class wf_beam_out(ctypes.Structure):
+    _fields_ = [("score", ctypes.c_void_p), ("parent", ctypes.c_void_p), ("token", ctypes.c_void_p),
+                ("next_score", ctypes.c_void_p), ("next_parent", ctypes.c_void_p), ("next_token", ctypes.c_void_p)]
+
+
+class wf_kv_cache(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("planes", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("plane_stride", ctypes.c_int64), ("token_bytes", ctypes.c_int64)]
 
 
 _lib = None
@@ -98,6 +133,12 @@ def load_library():
         "wf_ctx_set_batch": ([p, i32], ctypes.c_int),
         "wf_eval_topk_host": ([p, p, i32, p, p, p, p, p, p], ctypes.c_int),
         "wf_ctx_reserve_host": ([p], ctypes.c_int),
+        "wf_decode_create": ([p, ctypes.c_int, p], ctypes.c_int),
+        "wf_decode_status": ([p, p], ctypes.c_int),
+        "wf_decode_destroy": ([p], None),
+        "wf_kv_extend": ([p, p, p, p, p], ctypes.c_int),
+        "wf_beam_select": ([p, p, p, p], ctypes.c_int),
+        "wf_kv_reorder": ([p, p, i32, p, p, p, p, p, p], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
@@ -465,3 +506,174 @@ def wf_static_status(stream=None):
     """Synchronize the stream and report (then clear) the device-side outcome
     of the last wf_eval_plans_static call on the current device."""
     _check(load_library().wf_static_status(_stream_handle(stream)), "wf_static_status")
+
+
+# ---------------------------------------------------------------------------
+# Rows of a replica's paged KV cache, and beam search over them
+# ---------------------------------------------------------------------------
+
+KV_LONG, KV_BLOCKS, KV_TOKENS, KV_PARENT = 1, 2, 4, 1
+
+
+def _tensor(t, name: str, dtype: str, shape=None, device: int | None = None):
+    """t, checked: a contiguous device tensor of this type (and shape, and device)."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise WfError(WF_EINVAL, name, "is not a device tensor")
+    if t.dtype != getattr(torch, dtype) or not t.is_contiguous():
+        raise WfError(WF_EINVAL, name, f"is {t.dtype}, or not contiguous; expected contiguous {dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise WfError(WF_EINVAL, name, f"has shape {tuple(t.shape)}; expected {tuple(shape)}")
+    if device is not None and t.device.index != device:
+        raise WfError(WF_EINVAL, name, f"is on {t.device}; expected device {device}")
+    return t
+
+
+class Decode:
+    """Owns a wf_decode: the scratch of the calls below, for calls of up to these sizes."""
+
+    def __init__(self, max_rows: int, max_row_blocks: int = 0, max_vocab: int = 0, max_keep: int = 0, device: int = 0):
+        self.limits = wf_decode_limits(int(max_rows), int(max_row_blocks), int(max_vocab), int(max_keep))
+        self.device = int(device)
+        self.ptr = ctypes.c_void_p()
+        _check(load_library().wf_decode_create(ctypes.byref(self.limits), self.device, ctypes.byref(self.ptr)),
+               "wf_decode_create")
+
+    def close(self):
+        if self.ptr:
+            load_library().wf_decode_destroy(self.ptr)
+            self.ptr = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def wf_decode_status(decode: Decode, stream=None):
+    _check(load_library().wf_decode_status(decode.ptr, _stream_handle(stream)), "wf_decode_status")
+
+
+class Kv:
+    """The rows' block tables and the pool of free blocks (a wf_kv): device
+    tensors table [rows, >= row_blocks] int32 (its rows may be strided), len
+    [rows] int32, ring [n_blocks] int32, ends [2] int64.  The tensors are fixed for
+    the object's life; their contents are not."""
+
+    def __init__(self, table, len, ring, ends, block_tokens: int, row_blocks: int | None = None):
+        import torch
+        if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.dtype != torch.int32 \
+                or table.device.type != "cuda" or table.stride(1) != 1:
+            raise WfError(WF_EINVAL, "table", "is not a device int32 tensor [rows, blocks] with contiguous rows")
+        rows, dev = table.shape[0], table.device.index
+        if row_blocks is not None and not 1 <= row_blocks <= table.shape[1]:
+            raise WfError(WF_EINVAL, "row_blocks", f"{row_blocks} of a table {table.shape[1]} wide")
+        self.table, self.block_tokens = table, int(block_tokens)
+        self.len = _tensor(len, "len", "int32", (rows,), dev)
+        self.ring = _tensor(ring, "ring", "int32", (ring.numel(),), dev)
+        self.ends = _tensor(ends, "ends", "int64", (2,), dev)
+        self.rows, self.row_blocks, self.device = rows, int(row_blocks or table.shape[1]), dev
+        stride = table.stride(0) if rows > 1 else max(table.stride(0), table.shape[1])
+        self.c = wf_kv(rows, self.row_blocks, self.block_tokens, ring.numel(), table.data_ptr(),
+                       4 * stride, len.data_ptr(), ring.data_ptr(), ends.data_ptr())
+
+    @staticmethod
+    def empty(rows: int, row_blocks: int, block_tokens: int, n_blocks: int, device="cuda"):
+        """Rows without tokens, and every block free."""
+        import torch
+        return Kv(torch.full((rows, row_blocks), -1, dtype=torch.int32, device=device),
+                  torch.zeros(rows, dtype=torch.int32, device=device),
+                  torch.arange(n_blocks, dtype=torch.int32, device=device),
+                  torch.tensor([0, n_blocks], dtype=torch.int64, device=device), block_tokens)
+
+
+class KvStep:
+    """wf_kv_extend's outputs.  With `kv` given, len and ends are the
+    rows' own: the call then moves their state on."""
+
+    def __init__(self, rows: int, max_tokens: int, kv: Kv | None = None, device="cuda"):
+        import torch
+        mk = lambda n, dt: torch.empty(n, dtype=dt, device=device)
+        self.max_tokens, self.rows = int(max_tokens), int(rows)
+        self.slot, self.pos, self.row = mk(max_tokens, torch.int64), mk(max_tokens, torch.int32), mk(max_tokens, torch.int32)
+        self.start, self.status = mk(rows + 1, torch.int32), mk(rows, torch.int32)
+        self.len = kv.len if kv else mk(rows, torch.int32)
+        self.ends = kv.ends if kv else mk(2, torch.int64)
+        self.c = wf_kv_step(self.max_tokens, self.slot.data_ptr(), self.pos.data_ptr(), self.row.data_ptr(),
+                            self.start.data_ptr(), self.len.data_ptr(), self.ends.data_ptr(), self.status.data_ptr())
+
+
+def wf_kv_extend(decode: Decode, kv: Kv, add, out: KvStep, stream=None):
+    """A step's tokens: block tables and slots.  add: device int32 [rows]."""
+    if out.rows != kv.rows:
+        raise WfError(WF_EINVAL, "wf_kv_extend", f"outputs for {out.rows} rows, {kv.rows} given")
+    _tensor(add, "add", "int32", (kv.rows,), kv.device)
+    _check(load_library().wf_kv_extend(decode.ptr, ctypes.byref(kv.c), add.data_ptr(), ctypes.byref(out.c),
+                                       _stream_handle(stream)), "wf_kv_extend")
+
+
+class BeamOut:
+    """wf_beam_select's outputs: score, parent, token [groups, keep] and next_* [groups, beams]."""
+
+    def __init__(self, groups: int, beams: int, keep: int, device="cuda"):
+        import torch
+        mk = lambda n, dt: torch.empty((groups, n), dtype=dt, device=device)
+        self.groups, self.beams, self.keep = int(groups), int(beams), int(keep)
+        self.score, self.parent, self.token = mk(keep, torch.float32), mk(keep, torch.int32), mk(keep, torch.int32)
+        self.next_score, self.next_parent, self.next_token = (mk(beams, torch.float32), mk(beams, torch.int32),
+                                                              mk(beams, torch.int32))
+        self.c = wf_beam_out(self.score.data_ptr(), self.parent.data_ptr(), self.token.data_ptr(),
+                             self.next_score.data_ptr(), self.next_parent.data_ptr(), self.next_token.data_ptr())
+
+
+_DTYPES = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2}
+
+
+def wf_beam_select(decode: Decode, logits, score, out: BeamOut, eos: int = -1, stream=None):
+    """One step of beam search.  logits: device [groups * beams, vocab] in
+    float32, float16 or bfloat16 (rows may be strided); score: device float32 with
+    groups * beams elements."""
+    rows = out.groups * out.beams
+    dtype = _DTYPES.get(str(logits.dtype))
+    if dtype is None or logits.dim() != 2 or logits.shape[0] != rows or logits.device.type != "cuda" \
+            or (logits.stride(1) != 1 and logits.shape[1] > 1):
+        raise WfError(WF_EINVAL, "logits", f"{logits.dtype} {tuple(logits.shape)}; expected {rows} rows of float32, "
+                                           "float16 or bfloat16 with contiguous elements on the device")
+    _tensor(score, "score", "float32", None, logits.device.index)
+    if score.numel() != rows:
+        raise WfError(WF_EINVAL, "score", f"has {score.numel()} elements; expected {rows}")
+    c = wf_beam(out.groups, out.beams, logits.shape[1], out.keep, dtype, int(eos), logits.data_ptr(),
+                logits.stride(0) * logits.element_size(), score.data_ptr())
+    _check(load_library().wf_beam_select(decode.ptr, ctypes.byref(c), ctypes.byref(out.c), _stream_handle(stream)),
+           "wf_beam_select")
+
+
+class KvMoves:
+    """wf_kv_reorder's outputs beside the rows: copies [rows, 2] (from, to) and status [rows]."""
+
+    def __init__(self, rows: int, device="cuda"):
+        import torch
+        self.copies = torch.empty((rows, 2), dtype=torch.int32, device=device)
+        self.status = torch.empty(rows, dtype=torch.int32, device=device)
+
+
+def wf_kv_reorder(decode: Decode, kv: Kv, group: int, parent, to: Kv, out: KvMoves, cache=None, stream=None):
+    """The rows in the order of a selection.  parent: device int32 with a row
+    (or -1) for each row; to: the rows afterwards (kv itself, or another Kv on the same ring);
+    cache: a contiguous device tensor [planes, n_blocks, block_tokens, ...] or None."""
+    _tensor(parent, "parent", "int32", None, kv.device)
+    if parent.numel() != kv.rows or out.status.numel() != kv.rows:
+        raise WfError(WF_EINVAL, "wf_kv_reorder", f"parent or outputs for other than {kv.rows} rows")
+    cc = None
+    if cache is not None:
+        if cache.device.type != "cuda" or not cache.is_contiguous() or cache.dim() < 3 \
+                or tuple(cache.shape[1:3]) != (kv.c.n_blocks, kv.block_tokens):
+            raise WfError(WF_EINVAL, "cache", f"{tuple(cache.shape)}; expected contiguous [planes, {kv.c.n_blocks}, "
+                                              f"{kv.block_tokens}, ...] on the device")
+        plane = cache.stride(0) * cache.element_size()
+        cc = ctypes.byref(wf_kv_cache(cache.data_ptr(), cache.shape[0], 0, plane,
+                                      plane // (kv.c.n_blocks * kv.block_tokens)))
+    _check(load_library().wf_kv_reorder(decode.ptr, ctypes.byref(kv.c), int(group), parent.data_ptr(),
+                                        ctypes.byref(to.c), cc, out.copies.data_ptr(), out.status.data_ptr(),
+                                        _stream_handle(stream)), "wf_kv_reorder")
