@@ -523,8 +523,8 @@ typedef struct {
 
 /*
  * Scratch for the calls below on device `device`: about 4 bytes per table
- * cell of the limits and, for the selection, up to (8 * max_keep + 8) bytes
- * per row and 8,192 tokens of vocabulary.  The calls allocate nothing more.
+ * cell of the limits and, for the selection, 4 bytes per row and 128 tokens of
+ * vocabulary (at most 16 KiB a row).  The calls allocate nothing more.
  * One wf_decode serves one stream at a time.  Returns WF_OK, WF_EINVAL,
  * WF_ENOMEM or WF_ECUDA.
  */
@@ -613,7 +613,7 @@ typedef struct {
     int32_t eos;           /* the token that ends a hypothesis, or -1 */
     const void *logits;    /* [groups * beams][vocab], aligned to its elements */
     int64_t logits_stride; /* bytes between rows, a multiple of the element size */
-    const float *score;    /* [groups * beams] log probability so far; -inf: an empty beam, its logits are not read */
+    const float *score;    /* [groups * beams] log probability so far; -inf: an empty beam, whose logits do not count */
 } wf_beam;
 
 typedef struct {

@@ -1,24 +1,25 @@
 // Beam search's selection over beams and vocabulary (wf_beam_select).
 //
 // A candidate's sum is score + (x - m) - log Z, with a row's maximum m and
-// Z = sum of exp(x - m).  Within a row the order of the sums is that of the
-// logits, so the row's `keep` best logits can be found in the pass that makes
-// m and Z, before either is known:
+// Z = sum of exp(x - m).  One launch that reads the logits once:
 //
-//   1. a CTA takes a chunk of a row into registers (one read of the logits),
-//      makes the chunk's maximum and sum of exponentials, and lists the
-//      chunk's `keep` best logits;
-//   2. the last CTA of a row joins its chunks: m, Z, the row's best;
-//   3. the last CTA of a search joins its rows by their sums.
+//   1. The rows' logits, taken as one long run of units (a line of 512 bytes,
+//      a warp's load, or several), are dealt out evenly to the warps.  A warp
+//      sums the exponentials of its part of a row and keeps the maximum of
+//      every unit; no barrier, no choice of candidates.
+//   2. The last CTA of a search joins: m and Z of its rows, the sums of the
+//      units' maxima, and a bound that at least `keep` of those reach.  Only the units that
+//      reach it hold candidates that count, so only those are read again.
 //
-// All in one launch.  A list of the best n of many: the threads' own maxima,
-// taken over 32 or 64 classes of threads, have a n-th largest; at least n
-// values reach it and few more do (the classes hold interleaved values, so the
-// n-th largest of their maxima is near the n-th largest of all).  Those are gathered
-// and ranked by comparing each with all.  Where many values are equal (a mask of
-// the type's lowest value) the gathering repeats with 64-bit keys that order
-// equal values by their place, and where even that gathers too many the n-th
-// largest key is found bit by bit.
+// The exponentials are summed relative to a value near the start of the
+// warp's part: a sum relative to any value is as exact as one relative to
+// the maximum as long as it stays within a float's range, and a row where it
+// did not is summed again by the join.
+//
+// The bound: the threads' maxima, over 32 or 64 classes of threads, have a
+// keep-th largest.  The classes hold interleaved units, so few more than `keep`
+// reach it, unless many are equal (a mask of one low value); then the keys that
+// order equal sums by their place make the bound.
 #include <algorithm>
 
 #include <cuda_bf16.h>
@@ -31,7 +32,12 @@ namespace {
 constexpr uint32_t kFull = 0xFFFFFFFFu;
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kCap = 512;      // values gathered before they are ranked
+constexpr int kCap = 512;      // keys gathered before they are ranked
+constexpr int kStep = 4;       // lines that a warp has in flight, and as many in work
+constexpr int kSum = 64;       // steps whose exponentials are summed before that sum joins the warp's
+constexpr int kUnits = 4096;   // units of a search, but for one a row more
+constexpr int kPick = 128;     // units that the join reads again, at most, before it orders them by key
+constexpr int kPerSm = 4;      // CTAs an SM
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Whole numbers in the order of the floats; -0 counts as 0.
@@ -43,141 +49,161 @@ __device__ __forceinline__ uint32_t order_of(float x)
 
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
 
-// A key: the value's order above the complement of its place, so that the
-// larger key is the larger value, of equal ones the first.  0: no value.
-__device__ __forceinline__ uint64_t key_of(float x, uint32_t place) { return (uint64_t)order_of(x) << 32 | (uint32_t)~place; }
-__device__ __forceinline__ uint32_t place_of(uint64_t key) { return ~(uint32_t)key; }
-__device__ __forceinline__ float value_of_key(uint64_t key) { return value_of((uint32_t)(key >> 32)); }
+// What candidates (and units, by their maxima) are ordered by, the larger
+// key first: hi by sum, then lower beam; lo by logit, then lower place
+// (token, or unit in the row).  hi = 0: none.
+struct Key {
+    uint64_t hi, lo;
+};
+__device__ __forceinline__ bool operator>(const Key &a, const Key &b) { return a.hi > b.hi || (a.hi == b.hi && a.lo > b.lo); }
+__device__ __forceinline__ Key shuffle(const Key &k, int o)
+{
+    return {__shfl_xor_sync(kFull, k.hi, o), __shfl_xor_sync(kFull, k.lo, o)};
+}
 
-// The warp's values in descending order, lane 0 the largest.
-template <class T>
-__device__ __forceinline__ T warp_sorted(T v)
+// The warp's keys in descending order, lane 0 the largest.
+__device__ __noinline__ Key warp_sorted(Key v)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll 1
+        for (int o = size >> 1; o > 0; o >>= 1) {
+            const Key w = shuffle(v, o);
+            const bool first = (lane & o) == 0, down = size == 32 || (lane & size) == 0;
+            if ((first == down) == (w > v)) v = w;
+        }
+    return v;
+}
+
+__device__ __forceinline__ float warp_sorted(float v)
 {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int size = 2; size <= 32; size <<= 1)
 #pragma unroll
         for (int o = size >> 1; o > 0; o >>= 1) {
-            const T w = __shfl_xor_sync(kFull, v, o);
+            const float w = __shfl_xor_sync(kFull, v, o);
             const bool first = (lane & o) == 0, down = size == 32 || (lane & size) == 0;
-            v = first == down ? (v > w ? v : w) : (v > w ? w : v);
+            v = first == down ? fmaxf(v, w) : fminf(v, w);
         }
     return v;
 }
 
 struct Shared {
     union {
-        float f[kWarps][32];
-        uint64_t k[kWarps][32];
-    } best;                   // the threads' largest values
-    uint64_t got[kCap];       // gathered keys
-    uint64_t sorted[kMaxKeep];
-    uint32_t count;
-    uint32_t tally;
+        Key best[kWarps][32];  // the threads' best
+        float most[kWarps][32];
+    };
+    Key got[kCap];           // gathered keys
+    Key sorted[kMaxKeep];    // the best, in order; hi = 0 past the last
+    union {
+        float unit[kUnits + kMaxGroup];  // the units' maxima, then their sums
+        struct {
+            uint4 aside[kCap];           // vectors with a candidate that reaches the bound
+            int2 aside_of[kCap];         // ... their beam and the token of their first element
+        };
+    };
+    int32_t pick[kPick];     // units that are read again, counted over the search
+    float cut;               // the bound
+    Key bound;
+    uint32_t count, n_aside;
+    uint32_t again;          // rows whose exponentials are summed again
+    float3 stat[kMaxGroup];  // a row's maximum, log Z and score
     float sum[kWarps];
-    float2 stat[kMaxGroup];
     bool last;
 };
 
-// A value that at least n of the CTA's values reach (the lowest one, if there
-// are fewer): v is each thread's largest.  top: the largest of all.
-template <class T>
-__device__ __forceinline__ T reached(T v, T (*best)[32], int n, T &top)
+// Each of the count keys in sm.got finds its place among them, four threads a
+// key; the n best go to sm.sorted.
+__device__ __noinline__ void rank_keys(Shared &sm, int count, int n)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    best[warp][lane] = v;
+    const int tid = threadIdx.x;
+    if (tid < n) sm.sorted[tid] = {0, 0};
     __syncthreads();
-    T even = best[0][lane], odd = best[1][lane];
-#pragma unroll
-    for (int w = 2; w < kWarps; w += 2) {
-        const T x = best[w][lane], y = best[w + 1][lane];
-        even = x > even ? x : even;
-        odd = y > odd ? y : odd;
-    }
-    const T both = warp_sorted(even > odd ? even : odd);
-    top = __shfl_sync(kFull, both, 0);
-    if (n <= 32) return __shfl_sync(kFull, both, n - 1);
-    const T least = warp_sorted(even > odd ? odd : even);
-    return __shfl_sync(kFull, least, 31);
-}
-
-// Ranks sm.got[0, count) and leaves the n largest keys, in order, in
-// sm.sorted; what is missing is 0.
-__device__ void rank_keys(Shared &sm, int count, int n)
-{
-    for (int i = threadIdx.x; i < n; i += kThreads) sm.sorted[i] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < count; i += kThreads) {
-        const uint64_t key = sm.got[i];
+    for (int i = tid >> 2; i < (count + 7) / 8 * 8; i += kThreads / 4) {
+        const Key k = i < count ? sm.got[i] : Key{0, 0};
         int ahead = 0;
-        for (int j = 0; j < count; ++j) ahead += sm.got[j] > key;
-        if (ahead < n) sm.sorted[ahead] = key;
+#pragma unroll 4
+        for (int j = tid & 3; j < count; j += 4) ahead += sm.got[j] > k;
+        ahead += __shfl_xor_sync(kFull, ahead, 1);
+        ahead += __shfl_xor_sync(kFull, ahead, 2);
+        if (i < count && (tid & 3) == 0 && ahead < n) sm.sorted[ahead] = k;
     }
     __syncthreads();
 }
 
-// Gathers the CTA's keys that are at least t (0 is no key); each(f) calls f
-// with every key of this thread.  Returns how many there are; no more than
-// kCap are kept.
+// The n best of the CTA's keys, to sm.sorted: each(f) calls f with every key
+// of this thread, and can be called again.
 template <class Each>
-__device__ __forceinline__ int gather(Shared &sm, const Each &each, uint64_t t)
+__device__ __noinline__ void best_keys(Shared &sm, int n, const Each &each)
 {
-    if (threadIdx.x == 0) sm.count = 0;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    Key mine = {0, 0};
+    each([&](const Key &k) { if (k > mine) mine = k; });
     __syncthreads();
-    each([&](uint64_t key) {
-        if (key >= t && key) {
+    sm.best[warp][lane] = mine;
+    __syncthreads();
+    if (warp == 0) {
+        Key even = sm.best[0][lane], odd = sm.best[1][lane];
+        for (int w = 2; w < kWarps; w += 2) {
+            const Key x = sm.best[w][lane], y = sm.best[w + 1][lane];
+            if (x > even) even = x;
+            if (y > odd) odd = y;
+        }
+        // The n-th best of 32 classes; of 64 (two sorted halves) from n = 17 on, the least of those beyond 32.
+        Key sorted;
+        if (n <= 16) {
+            sorted = warp_sorted(even > odd ? even : odd);
+        } else if (n <= 32) {
+            const Key x = warp_sorted(even), y = warp_sorted(odd);
+            const Key z = {__shfl_sync(kFull, y.hi, 31 - lane), __shfl_sync(kFull, y.lo, 31 - lane)};
+            sorted = warp_sorted(x > z ? x : z);
+        } else {
+            sorted = warp_sorted(even > odd ? odd : even);
+        }
+        if (lane == min(n, 32) - 1) sm.bound = sorted;
+        if (lane == 0) sm.count = 0;
+    }
+    __syncthreads();
+    Key bound = sm.bound;
+    for (int round = 0; round < 4; ++round) {
+        each([&](const Key &k) {
+            if (!k.hi || bound > k) return;
             const uint32_t at = atomicAdd(&sm.count, 1u);
-            if (at < kCap) sm.got[at] = key;
-        }
-    });
-    __syncthreads();
-    return (int)sm.count;
-}
-
-// The n largest of the CTA's keys, in order, in sm.sorted.
-template <class Each>
-__device__ void best_keys(Shared &sm, const Each &each, int n)
-{
-    uint64_t mine = 0, top;
-    each([&](uint64_t key) { mine = key > mine ? key : mine; });
-    __syncthreads();
-    uint64_t t = reached(mine, sm.best.k, n, top);
-    int count = gather(sm, each, t);
-    if (count > kCap) {
-        // Bit by bit: the largest key that n keys reach.
-        t = 0;
-        for (int bit = 63; bit >= 0; --bit) {
-            const uint64_t cand = t | 1ull << bit;
-            uint32_t c = 0;
-            each([&](uint64_t key) { c += key >= cand; });
-            c = __reduce_add_sync(kFull, c);
-            __syncthreads();
-            if (threadIdx.x == 0) sm.tally = 0;
-            __syncthreads();
-            if ((threadIdx.x & 31) == 0) atomicAdd(&sm.tally, c);
-            __syncthreads();
-            if (sm.tally >= (uint32_t)n) t = cand;
-        }
-        count = gather(sm, each, t);
+            if (at < kCap) sm.got[at] = k;
+        });
+        __syncthreads();
+        const int came = (int)sm.count;
+        rank_keys(sm, min(came, kCap), n);
+        if (came <= kCap) return;
+        // An order that defeats the classes: the n-th of those that were kept is a better bound.
+        bound = sm.sorted[n - 1];
+        if (tid == 0) sm.count = 0;
+        __syncthreads();
     }
-    rank_keys(sm, count, n);
-}
-
-// Arrival of one CTA; true for the last of n, which resets the count.
-__device__ __forceinline__ bool last_arrival(Shared &sm, uint32_t *ticket, uint32_t n)
-{
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        sm.last = atomicAdd(ticket, 1u) == n - 1;
-        if (sm.last) *ticket = 0;
+    // Still too many: one after the other.
+    Key last = {~0ull, ~0ull};
+    for (int r = 0; r < n; ++r) {
+        Key next = {0, 0};
+        each([&](const Key &k) { if (last > k && k > next) next = k; });
+#pragma unroll 1
+        for (int o = 16; o > 0; o >>= 1) {
+            const Key w = shuffle(next, o);
+            if (w > next) next = w;
+        }
+        __syncthreads();
+        if (lane == 0) sm.best[0][warp] = next;
+        __syncthreads();
+        last = {0, 0};
+        for (int w = 0; w < kWarps; ++w)
+            if (sm.best[0][w] > last) last = sm.best[0][w];
+        if (tid == 0) sm.sorted[r] = last;
     }
     __syncthreads();
-    if (sm.last) __threadfence();
-    return sm.last;
 }
 
-// The elements of a 16-byte vector as floats.
+// The elements of a 16-byte vector as floats, and their maximum (NaN passed over).
 template <int kType>
 struct Elems;
 template <>
@@ -188,7 +214,11 @@ struct Elems<WF_F32> {
     {
         x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
     }
-    static __device__ __forceinline__ uint32_t lowest() { return 0xFF800000u; }  // -inf
+    static __device__ __forceinline__ float most(const uint4 &v)
+    {
+        return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    }
+    static __device__ __forceinline__ uint32_t masked() { return 0xFF800000u; }  // -inf
 };
 template <>
 struct Elems<WF_F16> {
@@ -204,7 +234,14 @@ struct Elems<WF_F16> {
             x[2 * i + 1] = f.y;
         }
     }
-    static __device__ __forceinline__ uint32_t lowest() { return 0xFC00FC00u; }
+    static __device__ __forceinline__ float most(const uint4 &v)
+    {
+        const __half2 m = __hmax2(__hmax2(*(const __half2 *)&v.x, *(const __half2 *)&v.y),
+                                  __hmax2(*(const __half2 *)&v.z, *(const __half2 *)&v.w));
+        const float2 f = __half22float2(m);
+        return fmaxf(f.x, f.y);
+    }
+    static __device__ __forceinline__ uint32_t masked() { return 0xFC00FC00u; }
 };
 template <>
 struct Elems<WF_BF16> {
@@ -219,7 +256,14 @@ struct Elems<WF_BF16> {
             x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
         }
     }
-    static __device__ __forceinline__ uint32_t lowest() { return 0xFF80FF80u; }
+    static __device__ __forceinline__ float most(const uint4 &v)
+    {
+        const __nv_bfloat162 m = __hmax2(__hmax2(*(const __nv_bfloat162 *)&v.x, *(const __nv_bfloat162 *)&v.y),
+                                         __hmax2(*(const __nv_bfloat162 *)&v.z, *(const __nv_bfloat162 *)&v.w));
+        const uint32_t w = *(const uint32_t *)&m;
+        return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+    }
+    static __device__ __forceinline__ uint32_t masked() { return 0xFF80FF80u; }
 };
 
 // 2^x, 0 below the smallest normal number.
@@ -238,287 +282,529 @@ __device__ __forceinline__ float element(const typename Elems<kType>::type *p)
     return kType == WF_F16 ? __half2float(__ushort_as_half((unsigned short)h)) : __uint_as_float(h << 16);
 }
 
-// The rare chunks, from memory once more (the registers of the common path
-// stay few): its sum of exponentials with infinities, NaN or masks of the type's lowest value ...
-template <int kType>
-__device__ __noinline__ float chunk_sum(const typename Elems<kType>::type *base, int lo, int hi, float m)
-{
-    float s = 0;
-    for (int t = lo + threadIdx.x; t < hi; t += kThreads) {
-        const float x = element<kType>(base + t);
-        s += x == m ? 1.0f : isnan(x) ? 0.0f : exp2f((x - m) * kLog2e);
-    }
-    return s;
-}
-
-// ... and its best where too many values reach the bound (equal values).
-template <int kType>
-__device__ __noinline__ void chunk_keys(Shared &sm, const typename Elems<kType>::type *base, int lo, int hi, int n)
-{
-    best_keys(sm, [&](auto f) {
-        for (int t = lo + threadIdx.x; t < hi; t += kThreads) {
-            const float x = element<kType>(base + t);
-            f(x > -INFINITY ? key_of(x, (uint32_t)t) : 0ull);
-        }
-    }, n);
-}
-
 struct SelectArgs {
     wf_beam in;
     wf_beam_out out;
-    int chunks;             // of a row
-    float2 *part;
-    uint64_t *list, *row_key;
-    int32_t *row_token;
-    uint32_t *row_ticket, *group_ticket;
+    int row_lines, unit_lines, row_units;
+    int warp_units;         // units of a warp
+    int parts;              // warps that share a row, at most
+    int units;              // of all rows
+    uint32_t unit_magic;    // i / row_units = (i * unit_magic) >> 32 for the units of a search
+    float4 *part;           // [rows][parts] {reference, sum of exponentials, maximum}
+    float *most;            // [rows][row_units] the units' maxima
+    uint32_t *ticket;       // [groups]
 };
 
 __device__ __forceinline__ bool live_score(float s) { return s > -INFINITY; }  // neither -inf nor NaN
 
-// Step 1: the chunk of kVecs vectors a thread.
-template <int kType, int kVecs>
-__device__ void chunk_best(const SelectArgs &a, Shared &sm, int row, int chunk)
+// A row's tokens; its first vector, on a 16-byte boundary, starts `lead` elements before them.
+template <int kType>
+__device__ __forceinline__ const typename Elems<kType>::type *row_base(const SelectArgs &a, int row, int &lead)
 {
-    using E = Elems<kType>;
-    using T = typename E::type;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = a.in.keep, V = a.in.vocab;
-    const T *base = (const T *)((const uint8_t *)a.in.logits + (int64_t)row * a.in.logits_stride);
-    // Vectors lie on 16-byte boundaries; element e of vector j is token j * E::n + e - lead.
-    const int lead = (int)(((uintptr_t)base & 15) / sizeof(T));
-    uint4 v[kVecs];
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        const int t0 = ((chunk * kVecs + i) * kThreads + tid) * E::n - lead;
-        if (t0 >= 0 && t0 + E::n <= V) {
-            v[i] = __ldcs((const uint4 *)(base + t0));
-        } else {
-            uint32_t w[4] = {E::lowest(), E::lowest(), E::lowest(), E::lowest()};
-#pragma unroll
-            for (int e = 0; e < E::n; ++e) {
-                if (t0 + e < 0 || t0 + e >= V) continue;
-                if (sizeof(T) == 4) {
-                    w[e & 3] = ((const uint32_t *)base)[t0 + e];
-                } else {
-                    const uint32_t h = ((const uint16_t *)base)[t0 + e];
-                    w[e >> 1] = e & 1 ? (w[e >> 1] & 0xFFFFu) | h << 16 : (w[e >> 1] & 0xFFFF0000u) | h;
-                }
-            }
-            v[i] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-    }
-    float mine = -INFINITY;  // fmaxf passes NaN over
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        float x[E::n];
-        E::get(v[i], x);
-#pragma unroll
-        for (int e = 0; e < E::n; ++e) mine = fmaxf(mine, x[e]);
-    }
-    float m;
-    const float t = reached(mine, sm.best.f, n, m);
-    if (tid == 0) sm.count = 0;
-    __syncthreads();
-    // exp(x - m) = 2^(x log2e - c) * 2^(c - m log2e) with c = m log2e rounded: the first takes one operation, the second
-    // is the same for all.
-    const float c = m * kLog2e;
-    const bool plain = fabsf(m) < 1e30f;
-    const int t00 = (chunk * kVecs * kThreads + tid) * E::n - lead;
-    float s = 0;
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        float x[E::n];
-        E::get(v[i], x);
-#pragma unroll
-        for (int e = 0; e < E::n; ++e) {
-            s += exp2_fast(fmaf(x[e], kLog2e, -c));
-            if (x[e] >= t && x[e] > -INFINITY) {
-                const uint32_t at = atomicAdd(&sm.count, 1u);
-                if (at < kCap) sm.got[at] = key_of(x[e], (uint32_t)(t00 + i * kThreads * E::n + e));
-            }
-        }
-    }
-    s *= exp2f(-fmaf(m, kLog2e, -c));
-    const int lo = max(chunk * kVecs * kThreads * E::n - lead, 0), hi = min((chunk + 1) * kVecs * kThreads * E::n - lead, V);
-    // A NaN in one thread's values leaves its sum NaN; it then sums its share of the chunk's tokens again, so all do.
-    if (__syncthreads_or(!plain || isnan(s))) s = m > -INFINITY ? chunk_sum<kType>(base, lo, hi, m) : 0.0f;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
-    if (lane == 0) sm.sum[warp] = s;
-    __syncthreads();
-    const int count = (int)sm.count;
-    if (count > kCap) {  // many equal values
-        chunk_keys<kType>(sm, base, lo, hi, n);
-    } else {
-        rank_keys(sm, count, n);
-    }
-    const int64_t at = (int64_t)row * a.chunks + chunk;
-    for (int i = tid; i < n; i += kThreads) a.list[at * n + i] = sm.sorted[i];
-    if (tid == 0) {
-        float sum = 0;
-        for (int w = 0; w < kWarps; ++w) sum += sm.sum[w];
-        a.part[at] = make_float2(m, sum);
-    }
+    const uint8_t *p = (const uint8_t *)a.in.logits + (int64_t)row * a.in.logits_stride;
+    lead = (int)(((uintptr_t)p & 15) / sizeof(typename Elems<kType>::type));
+    return (const typename Elems<kType>::type *)p;
 }
 
-// Step 2: a row's maximum, log Z and best, from its chunks.
-__device__ void row_best(const SelectArgs &a, Shared &sm, int row, float score)
+// A vector that lies in its row in part, or not at all: masked where there is no token.
+template <int kType>
+__device__ __noinline__ uint4 load_edge(const typename Elems<kType>::type *base, int t0, int V)
 {
-    const int tid = threadIdx.x, n = a.in.keep, C = a.chunks;
-    const int64_t at = (int64_t)row * C;
-    if (tid < 32) {
-        float m = -INFINITY, z = 0;
-        for (int c = tid; c < C; c += 32) m = fmaxf(m, __ldcg(&a.part[at + c]).x);
+    using E = Elems<kType>;
+    uint32_t w[4] = {E::masked(), E::masked(), E::masked(), E::masked()};
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, o));
-        for (int c = tid; c < C; c += 32) {
-            const float2 p = __ldcg(&a.part[at + c]);
-            z += p.x == m ? p.y : p.y * exp2f((p.x - m) * kLog2e);
+    for (int e = 0; e < E::n; ++e) {
+        if (t0 + e < 0 || t0 + e >= V) continue;
+        if (E::n == 4) {
+            w[e & 3] = ((const uint32_t *)base)[t0 + e];
+        } else {
+            const uint32_t h = ((const uint16_t *)base)[t0 + e];
+            w[e >> 1] = e & 1 ? (w[e >> 1] & 0xFFFFu) | h << 16 : (w[e >> 1] & 0xFFFF0000u) | h;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ float warp_max(float x)  // NaN passed over
+{
+    float y;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Units [u0, u1) of a row, by one warp: their maxima and the sum of their
+// exponentials.  kOne: a unit is a line; else it is one or more steps.
+template <int kType, bool kOne>
+__device__ __forceinline__ void take_part(const SelectArgs &a, int row, int u0, int u1, int64_t at)
+{
+    using E = Elems<kType>;
+    constexpr int kLine = 32 * E::n;
+    const int lane = threadIdx.x & 31, V = a.in.vocab, unit_lines = kOne ? 1 : a.unit_lines;
+    int lead;
+    const auto *base = row_base<kType>(a, row, lead);
+    const int i0 = u0 * unit_lines, i1 = min(u1 * unit_lines, a.row_lines);
+    // Lines of tokens only; the row's first and last may hold fewer.
+    const int whole0 = lead ? 1 : 0, whole1 = min(i1, (V + lead) / kLine);
+    const auto *mine = base + (lane * E::n - lead);
+    const auto load = [&](uint4 (&v)[kStep], int i) {
+        if (i >= whole0 && i + kStep <= whole1) {
+#pragma unroll
+            for (int u = 0; u < kStep; ++u) v[u] = __ldcs((const uint4 *)(mine + (int64_t)i * kLine + u * kLine));
+        } else {
+#pragma unroll
+            for (int u = 0; u < kStep; ++u) {
+                if (i + u >= whole0 && i + u < whole1) v[u] = __ldcs((const uint4 *)(mine + (int64_t)(i + u) * kLine));
+                else if (i + u < i1) v[u] = load_edge<kType>(base, (i + u) * kLine + lane * E::n - lead, V);
+                else v[u] = make_uint4(E::masked(), E::masked(), E::masked(), E::masked());
+            }
+        }
+    };
+    float *most = a.most + (int64_t)row * a.row_units + u0;
+    const float score = a.in.score[row];
+    uint4 v[kStep], next[kStep];
+    load(v, i0);
+    if (!live_score(score)) {  // an empty beam
+        for (int u = lane; u < u1 - u0; u += 32) most[u] = -INFINITY;
+        if (lane == 0) a.part[at] = make_float4(0.0f, 0.0f, -INFINITY, 0.0f);
+        return;
+    }
+    // exp(x - ref) = 2^(x log2e - c), c = ref log2e rounded: one operation each; what the rounding shifts is known to
+    // the join.  Where the part starts with a mask, 0 is the reference.
+    float first = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) first = fmaxf(first, E::most(v[u]));
+    first = warp_max(first);
+    const float c = fabsf(first) < 1e4f ? first * kLog2e : 0.0f;
+    float sum = 0, all = -INFINITY, unit = -INFINITY;
+    int left = unit_lines;
+    for (int i = i0; i < i1;) {
+        float s0 = 0, s1 = 0;
+        const int until = min(i1, i + kSum * kStep);
+#pragma unroll 1
+        for (; i < until; i += kStep) {
+            load(next, i + kStep);
+            float top[kStep];
+#pragma unroll
+            for (int u = 0; u < kStep; ++u) {
+                float x[E::n];
+                E::get(v[u], x);
+#pragma unroll
+                for (int e = 0; e < E::n; e += 2) {
+                    s0 += exp2_fast(fmaf(x[e], kLog2e, -c));
+                    s1 += exp2_fast(fmaf(x[e + 1], kLog2e, -c));
+                }
+                top[u] = E::most(v[u]);
+                v[u] = next[u];
+            }
+            if (kOne) {
+                float put = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < kStep; ++u) {
+                    top[u] = warp_max(top[u]);
+                    all = fmaxf(all, top[u]);
+                    put = lane == u ? top[u] : put;
+                }
+                if (lane < kStep && i + lane < i1) most[i - i0 + lane] = put;
+            } else {
+#pragma unroll
+                for (int u = 0; u < kStep; ++u) unit = fmaxf(unit, top[u]);
+                left -= kStep;
+                if (left == 0 || i + kStep >= i1) {
+                    unit = warp_max(unit);
+                    if (lane == 0) *most = unit;
+                    ++most;
+                    all = fmaxf(all, unit);
+                    unit = -INFINITY;
+                    left = unit_lines;
+                }
+            }
+        }
+        sum += s0 + s1;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
+    if (lane == 0) a.part[at] = make_float4(c, sum, all, 0.0f);
+}
+
+// The beam of a search's unit.
+__device__ __forceinline__ int unit_beam(const SelectArgs &a, int i) { return a.row_units == 1 ? i : (int)__umulhi((uint32_t)i, a.unit_magic); }
+
+// The first warp of a row's parts, and their number.
+__device__ __forceinline__ int first_part(const SelectArgs &a, int row) { return (int)((uint32_t)(row * a.row_units) / (uint32_t)a.warp_units); }
+__device__ __forceinline__ int row_parts(const SelectArgs &a, int row)
+{
+    return (int)((uint32_t)((row + 1) * a.row_units - 1) / (uint32_t)a.warp_units) - first_part(a, row) + 1;
+}
+
+// What a part adds to Z, for the row's maximum m; NaN where that cannot be told.
+__device__ __forceinline__ float part_sum(const float4 &q, float m)
+{
+    // With 0 as the reference, a small sum may lack what fell below the smallest number: nothing to Z if the part's maximum
+    // lies far below the row's.
+    if (q.x == 0.0f && !(q.y > 1e-20f)) return q.z < m - 60.0f ? 0.0f : q.z > -INFINITY ? NAN : 0.0f;
+    return q.y * exp2f(fmaf(-m, kLog2e, q.x));
+}
+
+// The rows' maxima, log Z and scores, to sm.stat, and the units' maxima, to sm.unit.
+template <int kType>
+__device__ __forceinline__ void row_stats(const SelectArgs &a, Shared &sm, int group)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.in.beams, V = a.in.vocab;
+    // A warp takes every kWarps-th row: the first parts of all of them are loaded at once.
+    constexpr int kRows = kMaxGroup / kWarps;
+    const float4 none = make_float4(0.0f, 0.0f, -INFINITY, 0.0f);
+    float4 q[kRows];
+    float score[kRows];
+    int parts[kRows];
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+        const int row = group * K + warp + j * kWarps;
+        parts[j] = warp + j * kWarps < K ? row_parts(a, row) : 0;
+        q[j] = lane < parts[j] ? __ldcg(&a.part[(int64_t)row * a.parts + lane]) : none;
+        score[j] = parts[j] ? a.in.score[row] : 0.0f;
+    }
+    // The units' maxima meanwhile.
+    const int units = K * a.row_units;
+    const float *most = a.most + (int64_t)group * units;
+    for (int i0 = tid; i0 < units; i0 += 8 * kThreads) {
+        float x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[u] = i0 + u * kThreads < units ? __ldcg(&most[i0 + u * kThreads]) : 0.0f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (i0 + u * kThreads < units) sm.unit[i0 + u * kThreads] = x[u];
+    }
+    if (tid == 0) { sm.again = 0; sm.count = 0; sm.n_aside = 0; }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+        if (!parts[j]) continue;
+        const float4 *part = a.part + (int64_t)(group * K + warp + j * kWarps) * a.parts;
+        float m = q[j].z;
+        for (int p = lane + 32; p < parts[j]; p += 32) m = fmaxf(m, __ldcg(&part[p]).z);
+        m = warp_max(m);
+        float z = 0;
+        if (m > -INFINITY) {
+            z = part_sum(q[j], m);
+            for (int p = lane + 32; p < parts[j]; p += 32) z += part_sum(__ldcg(&part[p]), m);
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(kFull, z, o);
-        if (tid == 0) sm.stat[0] = make_float2(m, logf(z));
-    }
-    // The lists' places interleave: neighbouring threads hold the same rank of neighbouring chunks.
-    best_keys(sm, [&](auto f) {
-        for (int i = tid; i < n * C; i += kThreads) f(__ldcg(&a.list[(at + i % C) * n + i / C]));
-    }, n);
-    const float2 stat = sm.stat[0];
-    const int place0 = row % a.in.beams * n;
-    for (int i = tid; i < n; i += kThreads) {
-        const uint64_t key = sm.sorted[i];
-        uint64_t out = 0;
-        if (key && live_score(score)) {
-            const float x = value_of_key(key);
-            const float sum = score + ((x == stat.x ? 0.0f : x - stat.x) - stat.y);
-            if (sum > -INFINITY) out = key_of(sum, (uint32_t)(place0 + i));
+        if (lane == 0) {
+            sm.stat[warp + j * kWarps] = make_float3(m, logf(z), score[j]);
+            if (m > -INFINITY && !(z >= 0.5f && z < INFINITY)) atomicOr(&sm.again, 1u << (warp + j * kWarps));  // (the maximum alone gives 1)
         }
-        a.row_key[(int64_t)row * n + i] = out;
-        a.row_token[(int64_t)row * n + i] = (int32_t)place_of(key);
+    }
+    __syncthreads();
+    // Rows with infinities, NaN or sums that left a float's range.
+    for (uint32_t rows = sm.again; rows; rows &= rows - 1) {
+        const int k = __ffs((int)rows) - 1;
+        int lead;
+        const auto *base = row_base<kType>(a, group * K + k, lead);
+        const float m = sm.stat[k].x;
+        float s = 0;
+        for (int t0 = tid; t0 < V; t0 += 8 * kThreads) {
+            float x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = t0 + u * kThreads < V ? element<kType>(base + t0 + u * kThreads) : -INFINITY;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += x[u] == m ? 1.0f : x[u] > -INFINITY ? exp2f((x[u] - m) * kLog2e) : 0.0f;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+        if (lane == 0) sm.sum[warp] = s;
+        __syncthreads();
+        if (tid == 0) {
+            float z = 0;
+            for (int w = 0; w < kWarps; ++w) z += sm.sum[w];
+            sm.stat[k].y = logf(z);
+        }
+        __syncthreads();
     }
 }
 
-// Step 3: a search's best and the next step's rows.
-__device__ void group_best(const SelectArgs &a, Shared &sm, int group)
+// The sum of a logit of a beam.
+__device__ __forceinline__ float sum_of(const float3 &stat, float x) { return stat.z + ((x == stat.x ? 0.0f : x - stat.x) - stat.y); }
+
+// Its key: {0, 0} if it is no candidate.
+__device__ __forceinline__ Key key_of(const Shared &sm, int k, float x, uint32_t place)
 {
-    const int tid = threadIdx.x, n = a.in.keep, K = a.in.beams;
-    const int64_t first = (int64_t)group * K * n;
-    best_keys(sm, [&](auto f) {
-        for (int i = tid; i < n * K; i += kThreads) f(__ldcg(&a.row_key[first + (i % K) * n + i / K]));
-    }, n);
-    // Warp 0: two candidates a lane, `goes` those that do not end.
-    if (tid >= 32) return;
-    int put = 0;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        const int i = i0 + tid;
-        const uint64_t key = i < n ? sm.sorted[i] : 0;
-        float score = -INFINITY;
-        int32_t parent = -1, token = -1;
-        if (key) {
-            const uint32_t place = place_of(key);
-            score = value_of_key(key);
-            parent = group * K + (int32_t)(place / (uint32_t)n);
-            token = __ldcg(&a.row_token[first + place]);
-        }
-        if (i < n) {
-            a.out.score[(int64_t)group * n + i] = score;
-            a.out.parent[(int64_t)group * n + i] = parent;
-            a.out.token[(int64_t)group * n + i] = token;
-        }
-        const bool goes = key && token != a.in.eos;
-        const uint32_t mask = __ballot_sync(kFull, goes);
-        const int at = put + __popc(mask & ((1u << tid) - 1u));
-        if (a.out.next_score && goes && at < K) {
-            a.out.next_score[(int64_t)group * K + at] = score;
-            a.out.next_parent[(int64_t)group * K + at] = parent;
-            a.out.next_token[(int64_t)group * K + at] = token;
-        }
-        put += __popc(mask);
-    }
-    for (int at = put + tid; a.out.next_score && at < K; at += 32) {
-        a.out.next_score[(int64_t)group * K + at] = -INFINITY;
-        a.out.next_parent[(int64_t)group * K + at] = -1;
-        a.out.next_token[(int64_t)group * K + at] = -1;
-    }
+    const float sum = sum_of(sm.stat[k], x);
+    if (!(x > -INFINITY) || !(sum > -INFINITY)) return {0, 0};
+    return {(uint64_t)order_of(sum) << 32 | (uint32_t)~k, (uint64_t)order_of(x) << 32 | (uint32_t)~place};
 }
 
-template <int kType, int kVecs>
-__global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a)
+// Line l of the picked units: the row's tokens, this lane's first token, its beam.
+template <int kType>
+__device__ __forceinline__ const typename Elems<kType>::type *picked_line(const SelectArgs &a, const Shared &sm, int group, int l, int2 &of)
 {
-    __shared__ Shared sm;
-    const int row = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
-    const float score = a.in.score[row];
-    if (live_score(score)) {
-        chunk_best<kType, kVecs>(a, sm, row, chunk);
-    } else {  // an empty beam: nothing is read
-        const int64_t at = (int64_t)row * a.chunks + chunk;
-        for (int i = threadIdx.x; i < a.in.keep; i += kThreads) a.list[at * a.in.keep + i] = 0;
-        if (threadIdx.x == 0) a.part[at] = make_float2(-INFINITY, 0.0f);
+    const int unit = sm.pick[l / a.unit_lines], k = unit_beam(a, unit);
+    const int i = (unit - k * a.row_units) * a.unit_lines + l % a.unit_lines;
+    int lead;
+    const auto *base = row_base<kType>(a, group * a.in.beams + k, lead);
+    of = make_int2(k, (i * 32 + (int)(threadIdx.x & 31)) * Elems<kType>::n - lead);
+    return base;
+}
+
+// A load without a branch around it, so that several stay in flight.
+__device__ __forceinline__ void load_if(bool ok, const void *from, uint4 &v)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %4, 0;\n\t@p ld.global.v4.u32 {%0, %1, %2, %3}, [%5];\n\t}"
+                 : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w) : "r"((int)ok), "l"(from));
+}
+
+// Calls f(beam, logit, token) for this lane's share of the picked units; a
+// warp takes every kWarps-th of their lines.
+template <int kType, class F>
+__device__ __forceinline__ void each_token(const SelectArgs &a, const Shared &sm, int group, int picked, const F &f)
+{
+    using E = Elems<kType>;
+    for (int l = (int)threadIdx.x >> 5; l < picked * a.unit_lines; l += kWarps) {
+        int2 of;
+        float x[E::n];
+        const auto *base = picked_line<kType>(a, sm, group, l, of);
+        E::get(of.y >= 0 && of.y + E::n <= a.in.vocab ? *(const uint4 *)(base + of.y) : load_edge<kType>(base, of.y, a.in.vocab), x);
+#pragma unroll
+        for (int e = 0; e < E::n; ++e) f(of.x, x[e], (uint32_t)(of.y + e));
     }
-    if (!last_arrival(sm, &a.row_ticket[row], (uint32_t)a.chunks)) return;
-    row_best(a, sm, row, score);
-    const int group = row / a.in.beams;
-    if (!last_arrival(sm, &a.group_ticket[group], (uint32_t)a.in.beams)) return;
-    group_best(a, sm, group);
-}
-
-constexpr int kMaxVecs = 8;
-constexpr int64_t kFill = 304;  // CTAs that fill the machine (two an SM)
-
-int chunks_of(int64_t vocab, int es, int vecs)
-{
-    const int64_t per = 16 / es, vectors = (vocab + 2 * (per - 1)) / per;  // a row may start inside a vector
-    return (int)((vectors + (int64_t)vecs * kThreads - 1) / ((int64_t)vecs * kThreads));
-}
-
-// Vectors of a thread: as many as leave enough CTAs to fill the machine.
-int vecs_of(int64_t rows, int64_t vocab, int es)
-{
-    int vecs = kMaxVecs;
-    while (vecs > 1 && rows * chunks_of(vocab, es, vecs) < kFill) vecs >>= 1;
-    return vecs;
 }
 
 template <int kType>
-void launch(const SelectArgs &a, int vecs, cudaStream_t st)
+__device__ __forceinline__ void join(const SelectArgs &a, Shared &sm, int group)
 {
-    const unsigned ctas = (unsigned)(a.in.groups * a.in.beams * a.chunks);
-    switch (vecs) {
-    case 1: select_kernel<kType, 1><<<ctas, kThreads, 0, st>>>(a); break;
-    case 2: select_kernel<kType, 2><<<ctas, kThreads, 0, st>>>(a); break;
-    case 4: select_kernel<kType, 4><<<ctas, kThreads, 0, st>>>(a); break;
-    default: select_kernel<kType, kMaxVecs><<<ctas, kThreads, 0, st>>>(a); break;
+    using E = Elems<kType>;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = a.in.keep, units = a.in.beams * a.row_units;
+    const float *most = a.most + (int64_t)group * units;
+    row_stats<kType>(a, sm, group);
+    // The bound, and the units that reach it.
+    float top = -INFINITY;
+#pragma unroll 4
+    for (int i = tid; i < units; i += kThreads) {
+        const float x = sm.unit[i], sum = x > -INFINITY ? sum_of(sm.stat[unit_beam(a, i)], x) : -INFINITY;
+        sm.unit[i] = sum;
+        top = fmaxf(top, sum);
     }
+    sm.most[warp][lane] = top;
+    __syncthreads();
+    if (warp == 0) {
+        float even = sm.most[0][lane], odd = sm.most[1][lane];
+#pragma unroll
+        for (int w = 2; w < kWarps; w += 2) {
+            even = fmaxf(even, sm.most[w][lane]);
+            odd = fmaxf(odd, sm.most[w + 1][lane]);
+        }
+        // The n-th largest of 32 classes; of 64 (the 32 largest of two sorted halves) from n = 17 on, the least of
+        // those beyond 32.
+        float sorted = warp_sorted(n <= 16 ? fmaxf(even, odd) : n <= 32 ? even : fminf(even, odd));
+        if (n > 16 && n <= 32) sorted = warp_sorted(fmaxf(sorted, __shfl_sync(kFull, warp_sorted(odd), 31 - lane)));
+        if (lane == min(n, 32) - 1) sm.cut = fmaxf(sorted, -3.402823466e38f);  // (a sum of -inf is no candidate)
+    }
+    __syncthreads();
+    float cut = sm.cut;
+    for (int i = tid; i < units; i += kThreads) {
+        if (!(sm.unit[i] >= cut)) continue;
+        const uint32_t at = atomicAdd(&sm.count, 1u);
+        if (at < kPick) sm.pick[at] = i;
+    }
+    __syncthreads();
+    int picked = (int)sm.count;
+    if (picked > kPick) {  // many equal, or a loose bound for many: exactly the n best
+        best_keys(sm, n, [&](auto f) {
+            for (int i = tid; i < units; i += kThreads) {
+                const int k = unit_beam(a, i);
+                f(key_of(sm, k, __ldcg(&most[i]), (uint32_t)(i - k * a.row_units)));
+            }
+        });
+        picked = 0;
+        while (picked < n && sm.sorted[picked].hi) ++picked;
+        if (tid < picked) sm.pick[tid] = (int)~(uint32_t)sm.sorted[tid].hi * a.row_units + (int)~(uint32_t)sm.sorted[tid].lo;
+        if (picked == n) cut = value_of((uint32_t)(sm.sorted[n - 1].hi >> 32));
+    }
+    __syncthreads();
+    if (tid == 0) sm.count = 0;
+    // Their vectors that reach the bound, kBatch lines of a warp at once; then those vectors' candidates; those in order.
+    constexpr int kBatch = 8;
+    for (int l0 = warp; l0 < picked * a.unit_lines; l0 += kBatch * kWarps) {
+        uint4 v[kBatch];
+        int2 of[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int l = min(l0 + u * kWarps, picked * a.unit_lines - 1);
+            const auto *base = picked_line<kType>(a, sm, group, l, of[u]);
+            v[u] = make_uint4(E::masked(), E::masked(), E::masked(), E::masked());
+            if (l0 + u * kWarps > l) of[u].y = a.in.vocab;
+            load_if(of[u].y >= 0 && of[u].y + E::n <= a.in.vocab, base + of[u].y, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)  // the rows' ends
+            if (of[u].y < a.in.vocab && (of[u].y < 0 || of[u].y + E::n > a.in.vocab)) {
+                int lead;
+                v[u] = load_edge<kType>(row_base<kType>(a, group * a.in.beams + of[u].x, lead), of[u].y, a.in.vocab);
+            }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const float x = E::most(v[u]);
+            if (!(x > -INFINITY) || !(sum_of(sm.stat[of[u].x], x) >= cut)) continue;
+            const uint32_t at = atomicAdd(&sm.n_aside, 1u);
+            if (at < kCap) { sm.aside[at] = v[u]; sm.aside_of[at] = of[u]; }
+        }
+    }
+    __syncthreads();
+    const int aside = (int)sm.n_aside;
+    for (int i = tid; i < min(aside, kCap) * E::n; i += kThreads) {
+        const float x = element<kType>((const typename E::type *)sm.aside + i);
+        const int2 of = sm.aside_of[i / E::n];
+        if (!(x > -INFINITY) || !(sum_of(sm.stat[of.x], x) >= cut)) continue;
+        const uint32_t at = atomicAdd(&sm.count, 1u);
+        if (at < kCap) sm.got[at] = key_of(sm, of.x, x, (uint32_t)(of.y + i % E::n));
+    }
+    __syncthreads();
+    const int count = (int)sm.count;
+    if (aside <= kCap && count <= kCap)
+        rank_keys(sm, count, n);
+    else
+        best_keys(sm, n, [&](auto f) {
+            each_token<kType>(a, sm, group, picked, [&](int k, float x, uint32_t token) { f(key_of(sm, k, x, token)); });
+        });
+}
+
+// A search's outputs, from sm.sorted, by warp 0.
+__device__ void write_group(const SelectArgs &a, const Shared &sm, int group)
+{
+    const int lane = threadIdx.x, n = a.in.keep, K = a.in.beams;
+    const int64_t out = (int64_t)group * n, next = (int64_t)group * K;
+    int put = 0;
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        const int i = i0 + lane;
+        const Key key = i < n ? sm.sorted[i] : Key{0, 0};
+        const float score = key.hi ? value_of((uint32_t)(key.hi >> 32)) : -INFINITY;
+        const int32_t parent = key.hi ? group * K + (int32_t)~(uint32_t)key.hi : -1, token = key.hi ? (int32_t)~(uint32_t)key.lo : -1;
+        if (i < n) {
+            a.out.score[out + i] = score;
+            a.out.parent[out + i] = parent;
+            a.out.token[out + i] = token;
+        }
+        const bool goes = key.hi && token != a.in.eos;
+        const uint32_t mask = __ballot_sync(kFull, goes);
+        const int at = put + __popc(mask & ((1u << lane) - 1u));
+        if (a.out.next_score && goes && at < K) {
+            a.out.next_score[next + at] = score;
+            a.out.next_parent[next + at] = parent;
+            a.out.next_token[next + at] = token;
+        }
+        put += __popc(mask);
+    }
+    if (a.out.next_score && put + lane < K) {  // (K is at most 32)
+        a.out.next_score[next + put + lane] = -INFINITY;
+        a.out.next_parent[next + put + lane] = -1;
+        a.out.next_token[next + put + lane] = -1;
+    }
+}
+
+// Arrival of one CTA; true for the last of n, which resets the count.  The
+// barrier hands what the CTA has written to the thread that makes it known
+// to the others.
+__device__ __forceinline__ bool last_arrival(Shared &sm, uint32_t *ticket, uint32_t n)
+{
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        sm.last = atomicAdd(ticket, 1u) == n - 1;
+        if (sm.last) *ticket = 0;
+        __threadfence();
+    }
+    __syncthreads();
+    return sm.last;
+}
+
+template <int kType, bool kOne>
+__global__ void __launch_bounds__(kThreads, kPerSm) select_kernel(const __grid_constant__ SelectArgs a)
+{
+    __shared__ Shared sm;
+    const int cta_units = kWarps * a.warp_units, warp = (int)threadIdx.x >> 5, w = (int)blockIdx.x * kWarps + warp;
+    const int begin = (int)blockIdx.x * cta_units, end = min(begin + cta_units, a.units);
+    int u = min(begin + warp * a.warp_units, end);
+    const int u_end = min(u + a.warp_units, end);
+    while (u < u_end) {
+        const int row = u / a.row_units, row0 = row * a.row_units, stop = min(u_end, row0 + a.row_units);
+        take_part<kType, kOne>(a, row, u - row0, stop - row0, (int64_t)row * a.parts + (w - first_part(a, row)));
+        u = stop;
+    }
+    // Join the searches whose last CTA this is.
+    const int group_units = a.row_units * a.in.beams;
+    for (int group = begin / group_units; group * group_units < end; ++group) {
+        const int g0 = group * group_units;
+        const uint32_t ctas = (uint32_t)(g0 + group_units - 1) / (uint32_t)cta_units - (uint32_t)g0 / (uint32_t)cta_units + 1;
+        if (last_arrival(sm, &a.ticket[group], ctas)) {
+            join<kType>(a, sm, group);
+            if (threadIdx.x < 32) write_group(a, sm, group);
+        }
+    }
+}
+
+// How the rows are cut.  Warps: as many as the machine holds at once.  Units:
+// a line where the warps have few, a step (kStep lines, a quarter of the
+// reductions) where they have at least kLong, more steps where a search would have more
+// than kUnits.
+constexpr int kLong = 8;
+
+bool deal(SelectArgs &a, int es, int sms)
+{
+    const int64_t per = 16 / es, rows = (int64_t)a.in.groups * a.in.beams, warps = (int64_t)sms * kPerSm * kWarps;
+    const int64_t vectors = (a.in.vocab + 2 * (per - 1)) / per;  // a row may start inside a vector
+    const int64_t row_lines = (vectors + 31) / 32;
+    int64_t unit_lines = (row_lines * a.in.beams + kUnits - 1) / kUnits;
+    if (unit_lines > 1 || rows * row_lines >= kLong * warps) unit_lines = (unit_lines + kStep - 1) / kStep * kStep;
+    const int64_t row_units = (row_lines + unit_lines - 1) / unit_lines, units = rows * row_units;
+    const int64_t warp_units = (units + warps - 1) / warps;
+    a.row_lines = (int)row_lines;
+    a.unit_lines = (int)unit_lines;
+    a.row_units = (int)row_units;
+    a.units = (int)units;
+    a.warp_units = (int)warp_units;
+    a.parts = (int)((row_units + warp_units - 1) / warp_units) + 1;
+    // A search has at most kUnits + kMaxGroup units: i * (2^32 / row_units, rounded up) is off by less than 1 / row_units.
+    a.unit_magic = (uint32_t)(((1ull << 32) + (uint64_t)row_units - 1) / (uint64_t)row_units);  // (row_units = 1: not used)
+    return units + kWarps * warp_units < INT32_MAX;
+}
+
+template <int kType>
+int launch(const SelectArgs &a, cudaStream_t st)
+{
+    const int cta_units = kWarps * a.warp_units;
+    const unsigned ctas = (unsigned)((a.units + cta_units - 1) / cta_units);
+    if (a.unit_lines == 1) select_kernel<kType, true><<<ctas, kThreads, 0, st>>>(a);
+    else select_kernel<kType, false><<<ctas, kThreads, 0, st>>>(a);
+    return wf_cuda_check(cudaGetLastError(), "select launch");
 }
 
 }  // namespace
 
-// Lists that any call of at most `rows` rows and `vocab` tokens needs: with
-// kMaxVecs vectors a thread, its rows' chunks; with fewer, twice vecs would not have
-// filled the machine, so at most twice that many CTAs and one more a row.
-int64_t wf_beam_lists(int64_t rows, int64_t vocab)
+// Scratch of any call of at most these sizes.  Parts: rows * parts, where the
+// rows' units make at most as many parts as there are warps, one more a row
+// for the rounding up and one for a row's first cut.  Units: a row's share of
+// kUnits and one for the rounding up, or its lines.
+void wf_beam_scratch(int64_t rows, int64_t vocab, int sms, int64_t *parts, int64_t *units)
 {
-    const int64_t full = rows * chunks_of(vocab, 4, kMaxVecs);
-    return std::max(full, 2 * kFill + rows);
+    *parts = (int64_t)sms * kPerSm * kWarps + 2 * rows;
+    *units = rows * std::min<int64_t>((vocab + 6) / 128 + 1, kUnits + 1);
 }
 
 int wf_launch_select(wf_decode *d, const wf_beam *in, const wf_beam_out *out, cudaStream_t st)
 {
-    const int es = in->dtype == WF_F32 ? 4 : 2;
-    const int64_t rows = (int64_t)in->groups * in->beams;
-    const int vecs = vecs_of(rows, in->vocab, es);
     SelectArgs a;
     a.in = *in;
     a.out = *out;
-    a.chunks = chunks_of(in->vocab, es, vecs);
+    if (!deal(a, in->dtype == WF_F32 ? 4 : 2, d->sms))
+        return wf_set_error(WF_EINVAL, "wf_beam_select: %d x %d rows of %d logits pass 2^31 units", in->groups, in->beams, in->vocab);
     a.part = d->part;
-    a.list = d->list;
-    a.row_key = d->row_key;
-    a.row_token = d->row_token;
-    a.row_ticket = d->ticket + 1;
-    a.group_ticket = d->ticket + 1 + d->lim.max_rows;
-    if (rows * a.chunks > d->lists) return wf_set_error(WF_EINVAL, "wf_beam_select: %lld lists exceed the scratch", (long long)(rows * a.chunks));
-    if (in->dtype == WF_F32) launch<WF_F32>(a, vecs, st);
-    else if (in->dtype == WF_F16) launch<WF_F16>(a, vecs, st);
-    else launch<WF_BF16>(a, vecs, st);
-    return wf_cuda_check(cudaGetLastError(), "select launch");
+    a.most = d->most;
+    a.ticket = d->ticket + 1;
+    const int64_t parts = (int64_t)in->groups * in->beams * a.parts;
+    if (parts > d->parts || a.units > d->units)
+        return wf_set_error(WF_EINVAL, "wf_beam_select: %lld parts and %d units exceed the scratch", (long long)parts, a.units);
+    if (in->dtype == WF_F32) return launch<WF_F32>(a, st);
+    if (in->dtype == WF_F16) return launch<WF_F16>(a, st);
+    return launch<WF_BF16>(a, st);
 }

@@ -32,27 +32,26 @@ extern "C" int wf_decode_create(const wf_decode_limits *lim, int device, wf_deco
     d->device = device;
     d->lim = *lim;
     rc = wf_cuda_check(cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, device), "device attributes");
+    if (rc) { wf_decode_destroy(d); return rc; }
 
-    const int64_t rows = lim->max_rows, keep = lim->max_keep;
+    const int64_t rows = lim->max_rows;
     const int64_t tiles = (lim->max_row_blocks + kTileCols - 1) / kTileCols;
-    d->lists = lim->max_vocab && keep ? wf_beam_lists(rows, lim->max_vocab) : 0;
+    if (lim->max_vocab && lim->max_keep) wf_beam_scratch(rows, lim->max_vocab, d->sms, &d->parts, &d->units);
     size_t at = 0;
     auto place = [&](size_t bytes) {
         const size_t here = at;
         at += (bytes + 255) / 256 * 256;
         return here;
     };
-    const size_t o_err = place(64), o_ticket = place(4 * (1 + 2 * (size_t)rows));
+    const size_t o_err = place(64), o_ticket = place(4 * (1 + (size_t)rows));
     const size_t zeroed = at;
     const size_t o_sums = place(4 * (3 * (size_t)rows + 3));
     const size_t o_freed = place(4 * (size_t)(rows * tiles * kTileCols));
     const size_t o_tf = place(4 * (size_t)(rows * tiles)), o_tc = place(4 * (size_t)(rows * tiles));
     const size_t o_cf = place(4 * (size_t)rows);
     const size_t o_plan = place(16 * (size_t)rows), o_was = place(16), o_pairs = place(16 * (size_t)rows);
-    const size_t o_np = place(4), o_part = place(8 * (size_t)d->lists), o_list = place(8 * (size_t)(d->lists * keep));
-    const size_t o_key = place(8 * (size_t)(d->lists ? rows * keep : 0));
-    const size_t o_tok = place(4 * (size_t)(d->lists ? rows * keep : 0));
-    if (!rc) rc = wf_cuda_check(cudaMalloc(&d->mem, at), "cudaMalloc(decode scratch)");
+    const size_t o_np = place(4), o_part = place(16 * (size_t)d->parts), o_most = place(4 * (size_t)d->units);
+    rc = wf_cuda_check(cudaMalloc(&d->mem, at), "cudaMalloc(decode scratch)");
     if (!rc) rc = wf_cuda_check(cudaMemset(d->mem, 0, zeroed), "clear the decode scratch");
     if (rc) { wf_decode_destroy(d); return rc; }
     uint8_t *m = (uint8_t *)d->mem;
@@ -67,10 +66,8 @@ extern "C" int wf_decode_create(const wf_decode_limits *lim, int device, wf_deco
     d->ring_was = (int64_t *)(m + o_was);
     d->pairs = (int4 *)(m + o_pairs);
     d->n_pairs = (uint32_t *)(m + o_np);
-    d->part = (float2 *)(m + o_part);
-    d->list = (uint64_t *)(m + o_list);
-    d->row_key = (uint64_t *)(m + o_key);
-    d->row_token = (int32_t *)(m + o_tok);
+    d->part = (float4 *)(m + o_part);
+    d->most = (float *)(m + o_most);
     // The clearing runs on the default stream; the calls may use any other.
     rc = wf_cuda_check(cudaDeviceSynchronize(), "cudaDeviceSynchronize");
     if (rc) { wf_decode_destroy(d); return rc; }

@@ -11,7 +11,7 @@ struct wf_decode {
     wf_decode_limits lim;
     void *mem;
     int *err;              // device error word (wf_decode_status)
-    uint32_t *ticket;      // [1 + 2 * max_rows] arrivals of CTAs; every call leaves them 0
+    uint32_t *ticket;      // [1 + max_rows] arrivals of CTAs; every call leaves them 0
     int32_t *sums;         // [3 * max_rows + 3] extend's sums where shared memory does not hold them
     // reorder
     int32_t *freed;        // [max_rows][row blocks rounded up to a tile] ids of a tile's freed blocks
@@ -23,18 +23,16 @@ struct wf_decode {
     int4 *pairs;           // [max_rows] {from, to, tokens, 0}
     uint32_t *n_pairs;
     // select
-    float2 *part;          // [lists] a chunk's maximum and its sum of exponentials
-    uint64_t *list;        // [lists][max_keep] a chunk's best, best first
-    uint64_t *row_key;     // [max_rows][max_keep]
-    int32_t *row_token;    // [max_rows][max_keep]
-    int64_t lists;
+    float4 *part;          // [parts] a warp's part of a row: reference, sum of exponentials, maximum
+    float *most;           // [units] the maximum of each unit of the rows
+    int64_t parts, units;
 };
 
 constexpr int kTileCols = 256;     // columns of the tables that a CTA of the reorder takes
 constexpr int kMaxGroup = 32;      // rows of a group, beams
 constexpr int kMaxKeep = 64;
 
-int64_t wf_beam_lists(int64_t rows, int64_t vocab);
+void wf_beam_scratch(int64_t rows, int64_t vocab, int sms, int64_t *parts, int64_t *units);
 int wf_launch_extend(wf_decode *d, const wf_kv *kv, const int32_t *add, const wf_kv_step *out, cudaStream_t st);
 int wf_launch_reorder(wf_decode *d, const wf_kv *kv, int32_t group, const int32_t *parent, const wf_kv *to,
                       const wf_kv_cache *cache, int32_t *copies, uint32_t *status, cudaStream_t st);

@@ -240,7 +240,7 @@ __device__ void write_tokens(const ExtendArgs &a, const RowSums &s, uint32_t tok
     }
 }
 
-__global__ void __launch_bounds__(kExtThreads) extend_kernel(ExtendArgs a)
+__global__ void __launch_bounds__(kExtThreads) extend_kernel(const __grid_constant__ ExtendArgs a)
 {
     extern __shared__ int32_t rows_sm[];
     const RowSums s{rows_sm, rows_sm + a.rows + 1, rows_sm + 2 * a.rows + 1};
@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(kExtThreads) extend_kernel(ExtendArgs a)
 
 // More rows than shared memory holds: one CTA makes the sums in global memory
 // for the kernel after it.
-__global__ void __launch_bounds__(kExtThreads) extend_sums_kernel(ExtendArgs a, int32_t *sums)
+__global__ void __launch_bounds__(kExtThreads) extend_sums_kernel(const __grid_constant__ ExtendArgs a, int32_t *sums)
 {
     const RowSums s{sums + 2, sums + 3 + a.rows, sums + 3 + 2 * a.rows};
     const int64_t head = a.ends[0], tail = a.ends[1];
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(kExtThreads) extend_sums_kernel(ExtendArgs a, 
     }
 }
 
-__global__ void __launch_bounds__(kExtThreads) extend_fill_kernel(ExtendArgs a, int32_t *sums)
+__global__ void __launch_bounds__(kExtThreads) extend_fill_kernel(const __grid_constant__ ExtendArgs a, int32_t *sums)
 {
     const RowSums s{sums + 2, sums + 3 + a.rows, sums + 3 + 2 * a.rows};
     write_tokens(a, s, (uint32_t)sums[0], (uint32_t)sums[1]);
@@ -397,7 +397,7 @@ __device__ void plan_groups(const ReorderArgs &a)
     }
 }
 
-__global__ void __launch_bounds__(kColThreads) reorder_tables_kernel(ReorderArgs a)
+__global__ void __launch_bounds__(kColThreads) reorder_tables_kernel(const __grid_constant__ ReorderArgs a)
 {
     extern __shared__ int32_t cells[];  // [group][kTileCols]
     __shared__ int had[kMaxGroup], from[kMaxGroup];
@@ -481,7 +481,7 @@ __device__ __forceinline__ int32_t freed_id(const ReorderArgs &a, int g, int i)
     return -1;
 }
 
-__global__ void __launch_bounds__(kMoveThreads) reorder_moves_kernel(ReorderArgs a)
+__global__ void __launch_bounds__(kMoveThreads) reorder_moves_kernel(const __grid_constant__ ReorderArgs a)
 {
     const int g = blockIdx.x, tid = threadIdx.x, K = a.group;
     const uint32_t n = (uint32_t)a.n_blocks;

@@ -161,9 +161,13 @@ def _check(code: int, where: str):
         raise WfError(code, where, detail)
 
 
-def _stream_handle(stream) -> int | None:
+def _stream_handle(stream, device: int | None = None) -> int | None:
+    """The cudaStream_t of a stream object or handle; None: torch's current
+    stream (of `device`, or of the current device)."""
     if stream is None:
         import torch
+        if device is not None:  # the handle alone: a Stream object takes longer to make than a launch
+            return torch._C._cuda_getCurrentRawStream(device) or None
         return torch.cuda.current_stream().cuda_stream or None
     if isinstance(stream, int):
         return stream or None
@@ -515,17 +519,13 @@ def wf_static_status(stream=None):
 KV_LONG, KV_BLOCKS, KV_TOKENS, KV_PARENT = 1, 2, 4, 1
 
 
-def _tensor(t, name: str, dtype: str, shape=None, device: int | None = None):
-    """t, checked: a contiguous device tensor of this type (and shape, and device)."""
+def _tensor(t, name: str, dtype: str, n: int, device: int):
+    """t, checked: n contiguous elements of this type on the device."""
     import torch
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
-        raise WfError(WF_EINVAL, name, "is not a device tensor")
-    if t.dtype != getattr(torch, dtype) or not t.is_contiguous():
-        raise WfError(WF_EINVAL, name, f"is {t.dtype}, or not contiguous; expected contiguous {dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise WfError(WF_EINVAL, name, f"has shape {tuple(t.shape)}; expected {tuple(shape)}")
-    if device is not None and t.device.index != device:
-        raise WfError(WF_EINVAL, name, f"is on {t.device}; expected device {device}")
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is getattr(torch, dtype) and t.is_contiguous()
+            and t.numel() == n and t.get_device() == device):
+        what = f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
+        raise WfError(WF_EINVAL, name, f"is {what}; expected {n} contiguous {dtype} on cuda:{device}")
     return t
 
 
@@ -570,9 +570,9 @@ class Kv:
         if row_blocks is not None and not 1 <= row_blocks <= table.shape[1]:
             raise WfError(WF_EINVAL, "row_blocks", f"{row_blocks} of a table {table.shape[1]} wide")
         self.table, self.block_tokens = table, int(block_tokens)
-        self.len = _tensor(len, "len", "int32", (rows,), dev)
-        self.ring = _tensor(ring, "ring", "int32", (ring.numel(),), dev)
-        self.ends = _tensor(ends, "ends", "int64", (2,), dev)
+        self.len = _tensor(len, "len", "int32", rows, dev)
+        self.ring = _tensor(ring, "ring", "int32", ring.numel(), dev)
+        self.ends = _tensor(ends, "ends", "int64", 2, dev)
         self.rows, self.row_blocks, self.device = rows, int(row_blocks or table.shape[1]), dev
         stride = table.stride(0) if rows > 1 else max(table.stride(0), table.shape[1])
         self.c = wf_kv(rows, self.row_blocks, self.block_tokens, ring.numel(), table.data_ptr(),
@@ -608,9 +608,9 @@ def wf_kv_extend(decode: Decode, kv: Kv, add, out: KvStep, stream=None):
     """A step's tokens: block tables and slots.  add: device int32 [rows]."""
     if out.rows != kv.rows:
         raise WfError(WF_EINVAL, "wf_kv_extend", f"outputs for {out.rows} rows, {kv.rows} given")
-    _tensor(add, "add", "int32", (kv.rows,), kv.device)
+    _tensor(add, "add", "int32", kv.rows, kv.device)
     _check(load_library().wf_kv_extend(decode.ptr, ctypes.byref(kv.c), add.data_ptr(), ctypes.byref(out.c),
-                                       _stream_handle(stream)), "wf_kv_extend")
+                                       _stream_handle(stream, kv.device)), "wf_kv_extend")
 
 
 class BeamOut:
@@ -634,19 +634,17 @@ def wf_beam_select(decode: Decode, logits, score, out: BeamOut, eos: int = -1, s
     """One step of beam search.  logits: device [groups * beams, vocab] in
     float32, float16 or bfloat16 (rows may be strided); score: device float32 with
     groups * beams elements."""
-    rows = out.groups * out.beams
-    dtype = _DTYPES.get(str(logits.dtype))
-    if dtype is None or logits.dim() != 2 or logits.shape[0] != rows or logits.device.type != "cuda" \
+    rows, dtype = out.groups * out.beams, _DTYPES.get(str(logits.dtype))
+    if dtype is None or not logits.is_cuda or logits.dim() != 2 or logits.shape[0] != rows \
             or (logits.stride(1) != 1 and logits.shape[1] > 1):
         raise WfError(WF_EINVAL, "logits", f"{logits.dtype} {tuple(logits.shape)}; expected {rows} rows of float32, "
                                            "float16 or bfloat16 with contiguous elements on the device")
-    _tensor(score, "score", "float32", None, logits.device.index)
-    if score.numel() != rows:
-        raise WfError(WF_EINVAL, "score", f"has {score.numel()} elements; expected {rows}")
-    c = wf_beam(out.groups, out.beams, logits.shape[1], out.keep, dtype, int(eos), logits.data_ptr(),
+    device = logits.get_device()
+    _tensor(score, "score", "float32", rows, device)
+    c = wf_beam(out.groups, out.beams, logits.shape[1], out.keep, dtype, eos, logits.data_ptr(),
                 logits.stride(0) * logits.element_size(), score.data_ptr())
-    _check(load_library().wf_beam_select(decode.ptr, ctypes.byref(c), ctypes.byref(out.c), _stream_handle(stream)),
-           "wf_beam_select")
+    _check(load_library().wf_beam_select(decode.ptr, ctypes.byref(c), ctypes.byref(out.c),
+                                         _stream_handle(stream, device)), "wf_beam_select")
 
 
 class KvMoves:
@@ -654,6 +652,7 @@ class KvMoves:
 
     def __init__(self, rows: int, device="cuda"):
         import torch
+        self.rows = int(rows)
         self.copies = torch.empty((rows, 2), dtype=torch.int32, device=device)
         self.status = torch.empty(rows, dtype=torch.int32, device=device)
 
@@ -662,12 +661,12 @@ def wf_kv_reorder(decode: Decode, kv: Kv, group: int, parent, to: Kv, out: KvMov
     """The rows in the order of a selection.  parent: device int32 with a row
     (or -1) for each row; to: the rows afterwards (kv itself, or another Kv on the same ring);
     cache: a contiguous device tensor [planes, n_blocks, block_tokens, ...] or None."""
-    _tensor(parent, "parent", "int32", None, kv.device)
-    if parent.numel() != kv.rows or out.status.numel() != kv.rows:
-        raise WfError(WF_EINVAL, "wf_kv_reorder", f"parent or outputs for other than {kv.rows} rows")
+    _tensor(parent, "parent", "int32", kv.rows, kv.device)
+    if out.rows != kv.rows:
+        raise WfError(WF_EINVAL, "wf_kv_reorder", f"outputs for {out.rows} rows, {kv.rows} given")
     cc = None
     if cache is not None:
-        if cache.device.type != "cuda" or not cache.is_contiguous() or cache.dim() < 3 \
+        if cache.get_device() != kv.device or not cache.is_contiguous() or cache.dim() < 3 \
                 or tuple(cache.shape[1:3]) != (kv.c.n_blocks, kv.block_tokens):
             raise WfError(WF_EINVAL, "cache", f"{tuple(cache.shape)}; expected contiguous [planes, {kv.c.n_blocks}, "
                                               f"{kv.block_tokens}, ...] on the device")
@@ -676,4 +675,4 @@ def wf_kv_reorder(decode: Decode, kv: Kv, group: int, parent, to: Kv, out: KvMov
                                       plane // (kv.c.n_blocks * kv.block_tokens)))
     _check(load_library().wf_kv_reorder(decode.ptr, ctypes.byref(kv.c), int(group), parent.data_ptr(),
                                         ctypes.byref(to.c), cc, out.copies.data_ptr(), out.status.data_ptr(),
-                                        _stream_handle(stream)), "wf_kv_reorder")
+                                        _stream_handle(stream, kv.device)), "wf_kv_reorder")
