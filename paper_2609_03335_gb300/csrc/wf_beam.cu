@@ -109,7 +109,10 @@ struct Shared {
     Key bound;
     uint32_t count, n_aside;
     uint32_t again;          // rows whose exponentials are summed again
-    float3 stat[kMaxGroup];  // a row's maximum, log Z and score
+    uint32_t live;           // the search's rows that have a score
+    int warp_units;
+    float score[kMaxGroup];
+    float4 stat[kMaxGroup];  // a row's maximum, log Z and score
     float sum[kWarps];
     bool last;
 };
@@ -286,11 +289,10 @@ struct SelectArgs {
     wf_beam in;
     wf_beam_out out;
     int row_lines, unit_lines, row_units;
-    int warp_units;         // units of a warp
-    int parts;              // warps that share a row, at most
-    int units;              // of all rows
+    int ctas;               // of a search
+    int warp_units;         // units of a warp; 0: as the search's live rows give
     uint32_t unit_magic;    // i / row_units = (i * unit_magic) >> 32 for the units of a search
-    float4 *part;           // [rows][parts] {reference, sum of exponentials, maximum}
+    float4 *part;           // [groups][ctas * kWarps + beams] {reference, sum of exponentials, maximum}
     float *most;            // [rows][row_units] the units' maxima
     uint32_t *ticket;       // [groups]
 };
@@ -333,13 +335,14 @@ __device__ __forceinline__ float warp_max(float x)  // NaN passed over
 }
 
 // Units [u0, u1) of a row, by one warp: their maxima and the sum of their
-// exponentials.  kOne: a unit is a line; else it is one or more steps.
-template <int kType, bool kOne>
-__device__ __forceinline__ void take_part(const SelectArgs &a, int row, int u0, int u1, int64_t at)
+// exponentials.  kUnit: lines of a unit (1 or 2), or kStep for one or more
+// steps.
+template <int kType, int kUnit>
+__device__ __forceinline__ void take_part(const SelectArgs &a, int row, int u0, int u1, float4 *part)
 {
     using E = Elems<kType>;
     constexpr int kLine = 32 * E::n;
-    const int lane = threadIdx.x & 31, V = a.in.vocab, unit_lines = kOne ? 1 : a.unit_lines;
+    const int lane = threadIdx.x & 31, V = a.in.vocab, unit_lines = kUnit < kStep ? kUnit : a.unit_lines;
     int lead;
     const auto *base = row_base<kType>(a, row, lead);
     const int i0 = u0 * unit_lines, i1 = min(u1 * unit_lines, a.row_lines);
@@ -360,14 +363,8 @@ __device__ __forceinline__ void take_part(const SelectArgs &a, int row, int u0, 
         }
     };
     float *most = a.most + (int64_t)row * a.row_units + u0;
-    const float score = a.in.score[row];
     uint4 v[kStep], next[kStep];
     load(v, i0);
-    if (!live_score(score)) {  // an empty beam
-        for (int u = lane; u < u1 - u0; u += 32) most[u] = -INFINITY;
-        if (lane == 0) a.part[at] = make_float4(0.0f, 0.0f, -INFINITY, 0.0f);
-        return;
-    }
     // exp(x - ref) = 2^(x log2e - c), c = ref log2e rounded: one operation each; what the rounding shifts is known to
     // the join.  Where the part starts with a mask, 0 is the reference.
     float first = -INFINITY;
@@ -396,15 +393,18 @@ __device__ __forceinline__ void take_part(const SelectArgs &a, int row, int u0, 
                 top[u] = E::most(v[u]);
                 v[u] = next[u];
             }
-            if (kOne) {
+            if (kUnit < kStep) {
+                constexpr int kHere = kStep / kUnit;  // units of a step
                 float put = -INFINITY;
 #pragma unroll
-                for (int u = 0; u < kStep; ++u) {
-                    top[u] = warp_max(top[u]);
-                    all = fmaxf(all, top[u]);
-                    put = lane == u ? top[u] : put;
+                for (int u = 0; u < kHere; ++u) {
+                    float x = top[u * kUnit];
+                    if (kUnit == 2) x = fmaxf(x, top[u * kUnit + 1]);
+                    x = warp_max(x);
+                    all = fmaxf(all, x);
+                    put = lane == u ? x : put;
                 }
-                if (lane < kStep && i + lane < i1) most[i - i0 + lane] = put;
+                if (lane < kHere && i + lane * kUnit < i1) most[(i - i0) / kUnit + lane] = put;
             } else {
 #pragma unroll
                 for (int u = 0; u < kStep; ++u) unit = fmaxf(unit, top[u]);
@@ -423,26 +423,21 @@ __device__ __forceinline__ void take_part(const SelectArgs &a, int row, int u0, 
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
-    if (lane == 0) a.part[at] = make_float4(c, sum, all, 0.0f);
+    if (lane == 0) *part = make_float4(c, sum, all, 0.0f);
 }
 
 // The beam of a search's unit.
 __device__ __forceinline__ int unit_beam(const SelectArgs &a, int i) { return a.row_units == 1 ? i : (int)__umulhi((uint32_t)i, a.unit_magic); }
 
-// The first warp of a row's parts, and their number.
-__device__ __forceinline__ int first_part(const SelectArgs &a, int row) { return (int)((uint32_t)(row * a.row_units) / (uint32_t)a.warp_units); }
-__device__ __forceinline__ int row_parts(const SelectArgs &a, int row)
+// A search's warps share its rows one after the other, each warp_units units;
+// a warp's part of the j-th row is number (warp of the search) + j.
+struct Parts {
+    int first, count;
+};
+__device__ __forceinline__ Parts row_parts(const SelectArgs &a, int j, int warp_units)
 {
-    return (int)((uint32_t)((row + 1) * a.row_units - 1) / (uint32_t)a.warp_units) - first_part(a, row) + 1;
-}
-
-// What a part adds to Z, for the row's maximum m; NaN where that cannot be told.
-__device__ __forceinline__ float part_sum(const float4 &q, float m)
-{
-    // With 0 as the reference, a small sum may lack what fell below the smallest number: nothing to Z if the part's maximum
-    // lies far below the row's.
-    if (q.x == 0.0f && !(q.y > 1e-20f)) return q.z < m - 60.0f ? 0.0f : q.z > -INFINITY ? NAN : 0.0f;
-    return q.y * exp2f(fmaf(-m, kLog2e, q.x));
+    const int first = (int)((uint32_t)(j * a.row_units) / (uint32_t)warp_units);
+    return {first + j, (int)((uint32_t)((j + 1) * a.row_units - 1) / (uint32_t)warp_units) - first + 1};
 }
 
 // The rows' maxima, log Z and scores, to sm.stat, and the units' maxima, to sm.unit.
@@ -450,53 +445,60 @@ template <int kType>
 __device__ __forceinline__ void row_stats(const SelectArgs &a, Shared &sm, int group)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.in.beams, V = a.in.vocab;
-    // A warp takes every kWarps-th row: the first parts of all of them are loaded at once.
-    constexpr int kRows = kMaxGroup / kWarps;
-    const float4 none = make_float4(0.0f, 0.0f, -INFINITY, 0.0f);
-    float4 q[kRows];
-    float score[kRows];
-    int parts[kRows];
+    if (tid == 0) { sm.again = 0; sm.count = 0; sm.n_aside = 0; }
+    constexpr int kLoads = 4;  // parts that a lane loads at once
+    const float4 none = make_float4(0.0f, 0.0f, -INFINITY, 0.0f), *parts = a.part + (int64_t)group * (a.ctas * kWarps + K);
+    const auto parts_of = [&](int k) {
+        const uint32_t live = sm.live;
+        return live >> k & 1u ? row_parts(a, a.warp_units ? k : __popc(live & ((1u << k) - 1u)), sm.warp_units) : Parts{0, 0};
+    };
+    // The first of them before the units' maxima, so that both are under way together.
+    Parts at = warp < K ? parts_of(warp) : Parts{0, 0};
+    float4 q[kLoads];
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
-        const int row = group * K + warp + j * kWarps;
-        parts[j] = warp + j * kWarps < K ? row_parts(a, row) : 0;
-        q[j] = lane < parts[j] ? __ldcg(&a.part[(int64_t)row * a.parts + lane]) : none;
-        score[j] = parts[j] ? a.in.score[row] : 0.0f;
-    }
-    // The units' maxima meanwhile.
+    for (int u = 0; u < kLoads; ++u) q[u] = lane + 32 * u < at.count ? __ldcg(&parts[at.first + lane + 32 * u]) : none;
     const int units = K * a.row_units;
     const float *most = a.most + (int64_t)group * units;
-    for (int i0 = tid; i0 < units; i0 += 8 * kThreads) {
-        float x[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) x[u] = i0 + u * kThreads < units ? __ldcg(&most[i0 + u * kThreads]) : 0.0f;
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (i0 + u * kThreads < units) sm.unit[i0 + u * kThreads] = x[u];
-    }
-    if (tid == 0) { sm.again = 0; sm.count = 0; sm.n_aside = 0; }
+#pragma unroll 4
+    for (int i = tid; i < units; i += kThreads) sm.unit[i] = __ldcg(&most[i]);
     __syncthreads();
+#pragma unroll 1
+    for (int k = warp; k < K; k += kWarps) {
+        if (k != warp) {
+            at = parts_of(k);
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
-        if (!parts[j]) continue;
-        const float4 *part = a.part + (int64_t)(group * K + warp + j * kWarps) * a.parts;
-        float m = q[j].z;
-        for (int p = lane + 32; p < parts[j]; p += 32) m = fmaxf(m, __ldcg(&part[p]).z);
-        m = warp_max(m);
-        float z = 0;
-        if (m > -INFINITY) {
-            z = part_sum(q[j], m);
-            for (int p = lane + 32; p < parts[j]; p += 32) z += part_sum(__ldcg(&part[p]), m);
+            for (int u = 0; u < kLoads; ++u) q[u] = lane + 32 * u < at.count ? __ldcg(&parts[at.first + lane + 32 * u]) : none;
         }
+        // Each lane's parts by their own maximum, then the lanes' by the row's.
+        float m = -INFINITY, z = 0, doubt = -INFINITY;
+#pragma unroll 1
+        for (int p = lane; p < at.count; p += 32) {
+            const float4 now = q[0];
+            if (now.z > m) {
+                z = m > -INFINITY ? z * exp2f((m - now.z) * kLog2e) : 0.0f;
+                m = now.z;
+            }
+            // With 0 as the reference, a small sum may lack what fell below the smallest number.
+            if (now.x == 0.0f && !(now.y > 1e-20f)) doubt = fmaxf(doubt, now.z);
+            else z += now.y * exp2f(fmaf(-m, kLog2e, now.x));
+#pragma unroll
+            for (int u = 0; u + 1 < kLoads; ++u) q[u] = q[u + 1];
+            q[kLoads - 1] = p + 32 * kLoads < at.count ? __ldcg(&parts[at.first + p + 32 * kLoads]) : none;
+        }
+        const float most_of = warp_max(m);
+        if (m < most_of) z = m > -INFINITY ? z * exp2f((m - most_of) * kLog2e) : 0.0f;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(kFull, z, o);
+        doubt = warp_max(doubt);
         if (lane == 0) {
-            sm.stat[warp + j * kWarps] = make_float3(m, logf(z), score[j]);
-            if (m > -INFINITY && !(z >= 0.5f && z < INFINITY)) atomicOr(&sm.again, 1u << (warp + j * kWarps));  // (the maximum alone gives 1)
+            sm.stat[k] = make_float4(most_of, logf(z), sm.score[k], 0.0f);  // (an empty beam: a maximum of -inf)
+            // The maximum alone gives Z = 1.  What a doubtful part lacks is nothing beside that if its maximum lies far below.
+            if (most_of > -INFINITY && (!(z >= 0.5f && z < INFINITY) || doubt >= most_of - 60.0f)) atomicOr(&sm.again, 1u << k);
         }
     }
     __syncthreads();
     // Rows with infinities, NaN or sums that left a float's range.
+#pragma unroll 1
     for (uint32_t rows = sm.again; rows; rows &= rows - 1) {
         const int k = __ffs((int)rows) - 1;
         int lead;
@@ -524,25 +526,31 @@ __device__ __forceinline__ void row_stats(const SelectArgs &a, Shared &sm, int g
 }
 
 // The sum of a logit of a beam.
-__device__ __forceinline__ float sum_of(const float3 &stat, float x) { return stat.z + ((x == stat.x ? 0.0f : x - stat.x) - stat.y); }
+__device__ __forceinline__ float sum_of(const float4 &stat, float x) { return stat.z + ((x == stat.x ? 0.0f : x - stat.x) - stat.y); }
 
 // Its key: {0, 0} if it is no candidate.
 __device__ __forceinline__ Key key_of(const Shared &sm, int k, float x, uint32_t place)
 {
-    const float sum = sum_of(sm.stat[k], x);
-    if (!(x > -INFINITY) || !(sum > -INFINITY)) return {0, 0};
+    const float4 stat = sm.stat[k];
+    const float sum = sum_of(stat, x);
+    if (!(stat.x > -INFINITY) || !(x > -INFINITY) || !(sum > -INFINITY)) return {0, 0};
     return {(uint64_t)order_of(sum) << 32 | (uint32_t)~k, (uint64_t)order_of(x) << 32 | (uint32_t)~place};
 }
 
-// Line l of the picked units: the row's tokens, this lane's first token, its beam.
-template <int kType>
-__device__ __forceinline__ const typename Elems<kType>::type *picked_line(const SelectArgs &a, const Shared &sm, int group, int l, int2 &of)
+// Item l of the picked units, kLines lines of one: the row's tokens, this
+// lane's first token, its beam, and how many of the lines there are.
+template <int kType, int kLines>
+__device__ __forceinline__ const typename Elems<kType>::type *picked_lines(const SelectArgs &a, const Shared &sm, int group, int l, int &k,
+                                                                           int &t0, int &lines)
 {
-    const int unit = sm.pick[l / a.unit_lines], k = unit_beam(a, unit);
-    const int i = (unit - k * a.row_units) * a.unit_lines + l % a.unit_lines;
+    const int items = kLines < kStep ? 1 : a.unit_lines / kStep, j = items == 1 ? l : l / items;
+    const int unit = sm.pick[j];
+    k = unit_beam(a, unit);
+    const int i = (unit - k * a.row_units) * a.unit_lines + (l - j * items) * kLines;
+    lines = min(kLines, a.row_lines - i);
     int lead;
     const auto *base = row_base<kType>(a, group * a.in.beams + k, lead);
-    of = make_int2(k, (i * 32 + (int)(threadIdx.x & 31)) * Elems<kType>::n - lead);
+    t0 = (i * 32 + (int)(threadIdx.x & 31)) * Elems<kType>::n - lead;
     return base;
 }
 
@@ -554,22 +562,24 @@ __device__ __forceinline__ void load_if(bool ok, const void *from, uint4 &v)
 }
 
 // Calls f(beam, logit, token) for this lane's share of the picked units; a
-// warp takes every kWarps-th of their lines.
-template <int kType, class F>
-__device__ __forceinline__ void each_token(const SelectArgs &a, const Shared &sm, int group, int picked, const F &f)
+// warp takes every kWarps-th of their items.
+template <int kType, int kLines, class F>
+__device__ __forceinline__ void each_token(const SelectArgs &a, const Shared &sm, int group, int items, const F &f)
 {
     using E = Elems<kType>;
-    for (int l = (int)threadIdx.x >> 5; l < picked * a.unit_lines; l += kWarps) {
-        int2 of;
-        float x[E::n];
-        const auto *base = picked_line<kType>(a, sm, group, l, of);
-        E::get(of.y >= 0 && of.y + E::n <= a.in.vocab ? *(const uint4 *)(base + of.y) : load_edge<kType>(base, of.y, a.in.vocab), x);
+    for (int l = (int)threadIdx.x >> 5; l < items; l += kWarps) {
+        int k, t0, lines;
+        const auto *base = picked_lines<kType, kLines>(a, sm, group, l, k, t0, lines);
+        for (int u = 0; u < lines; ++u, t0 += 32 * E::n) {
+            float x[E::n];
+            E::get(t0 >= 0 && t0 + E::n <= a.in.vocab ? *(const uint4 *)(base + t0) : load_edge<kType>(base, t0, a.in.vocab), x);
 #pragma unroll
-        for (int e = 0; e < E::n; ++e) f(of.x, x[e], (uint32_t)(of.y + e));
+            for (int e = 0; e < E::n; ++e) f(k, x[e], (uint32_t)(t0 + e));
+        }
     }
 }
 
-template <int kType>
+template <int kType, int kLines>
 __device__ __forceinline__ void join(const SelectArgs &a, Shared &sm, int group)
 {
     using E = Elems<kType>;
@@ -580,7 +590,8 @@ __device__ __forceinline__ void join(const SelectArgs &a, Shared &sm, int group)
     float top = -INFINITY;
 #pragma unroll 4
     for (int i = tid; i < units; i += kThreads) {
-        const float x = sm.unit[i], sum = x > -INFINITY ? sum_of(sm.stat[unit_beam(a, i)], x) : -INFINITY;
+        const float4 stat = sm.stat[unit_beam(a, i)];
+        const float x = sm.unit[i], sum = stat.x > -INFINITY && x > -INFINITY ? sum_of(stat, x) : -INFINITY;
         sm.unit[i] = sum;
         top = fmaxf(top, sum);
     }
@@ -623,30 +634,38 @@ __device__ __forceinline__ void join(const SelectArgs &a, Shared &sm, int group)
     __syncthreads();
     if (tid == 0) sm.count = 0;
     // Their vectors that reach the bound, kBatch lines of a warp at once; then those vectors' candidates; those in order.
-    constexpr int kBatch = 8;
-    for (int l0 = warp; l0 < picked * a.unit_lines; l0 += kBatch * kWarps) {
+    constexpr int kBatch = 8, kItems = kBatch / kLines;
+    const int items = picked * (kLines < kStep ? 1 : a.unit_lines / kStep);
+    for (int l0 = warp; l0 < items; l0 += kItems * kWarps) {
         uint4 v[kBatch];
-        int2 of[kBatch];
+        int k[kItems], t0[kItems], lines[kItems];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const int l = min(l0 + u * kWarps, picked * a.unit_lines - 1);
-            const auto *base = picked_line<kType>(a, sm, group, l, of[u]);
-            v[u] = make_uint4(E::masked(), E::masked(), E::masked(), E::masked());
-            if (l0 + u * kWarps > l) of[u].y = a.in.vocab;
-            load_if(of[u].y >= 0 && of[u].y + E::n <= a.in.vocab, base + of[u].y, v[u]);
+        for (int j = 0; j < kItems; ++j) {
+            const int l = l0 + j * kWarps;
+            const auto *base = picked_lines<kType, kLines>(a, sm, group, min(l, items - 1), k[j], t0[j], lines[j]);
+            if (l >= items) lines[j] = 0;
+#pragma unroll
+            for (int u = 0; u < kLines; ++u) {
+                const int t = t0[j] + u * 32 * E::n;
+                v[j * kLines + u] = make_uint4(E::masked(), E::masked(), E::masked(), E::masked());
+                load_if(u < lines[j] && t >= 0 && t + E::n <= a.in.vocab, base + t, v[j * kLines + u]);
+            }
         }
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u)  // the rows' ends
-            if (of[u].y < a.in.vocab && (of[u].y < 0 || of[u].y + E::n > a.in.vocab)) {
-                int lead;
-                v[u] = load_edge<kType>(row_base<kType>(a, group * a.in.beams + of[u].x, lead), of[u].y, a.in.vocab);
-            }
+        for (int j = 0; j < kItems; ++j) {
+            const float4 stat = sm.stat[k[j]];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const float x = E::most(v[u]);
-            if (!(x > -INFINITY) || !(sum_of(sm.stat[of[u].x], x) >= cut)) continue;
-            const uint32_t at = atomicAdd(&sm.n_aside, 1u);
-            if (at < kCap) { sm.aside[at] = v[u]; sm.aside_of[at] = of[u]; }
+            for (int u = 0; u < kLines; ++u) {
+                const int t = t0[j] + u * 32 * E::n;
+                uint4 &w = v[j * kLines + u];
+                int lead;
+                if (u < lines[j] && t < a.in.vocab && (t < 0 || t + E::n > a.in.vocab))  // a row's end
+                    w = load_edge<kType>(row_base<kType>(a, group * a.in.beams + k[j], lead), t, a.in.vocab);
+                const float x = E::most(w);
+                if (!(x > -INFINITY) || !(sum_of(stat, x) >= cut)) continue;
+                const uint32_t at = atomicAdd(&sm.n_aside, 1u);
+                if (at < kCap) { sm.aside[at] = w; sm.aside_of[at] = make_int2(k[j], t); }
+            }
         }
     }
     __syncthreads();
@@ -664,7 +683,7 @@ __device__ __forceinline__ void join(const SelectArgs &a, Shared &sm, int group)
         rank_keys(sm, count, n);
     else
         best_keys(sm, n, [&](auto f) {
-            each_token<kType>(a, sm, group, picked, [&](int k, float x, uint32_t token) { f(key_of(sm, k, x, token)); });
+            each_token<kType, kLines>(a, sm, group, items, [&](int k, float x, uint32_t token) { f(key_of(sm, k, x, token)); });
         });
 }
 
@@ -718,76 +737,86 @@ __device__ __forceinline__ bool last_arrival(Shared &sm, uint32_t *ticket, uint3
     return sm.last;
 }
 
-template <int kType, bool kOne>
+template <int kType, int kUnit>
 __global__ void __launch_bounds__(kThreads, kPerSm) select_kernel(const __grid_constant__ SelectArgs a)
 {
     __shared__ Shared sm;
-    const int cta_units = kWarps * a.warp_units, warp = (int)threadIdx.x >> 5, w = (int)blockIdx.x * kWarps + warp;
-    const int begin = (int)blockIdx.x * cta_units, end = min(begin + cta_units, a.units);
-    int u = min(begin + warp * a.warp_units, end);
-    const int u_end = min(u + a.warp_units, end);
+    const int lane = threadIdx.x & 31, warp = (int)threadIdx.x >> 5, K = a.in.beams;
+    const int group = (int)blockIdx.x / a.ctas, w = ((int)blockIdx.x % a.ctas) * kWarps + warp;
+    const float score = lane < K ? a.in.score[group * K + lane] : -INFINITY;
+    // With few units a warp the rows are shared out as they are, so that no load waits for the scores; with many, the
+    // live ones are: a search's first step has one.
+    uint32_t live = kFull;
+    int warp_units = a.warp_units, rows = K;
+    if (!warp_units) {
+        live = __ballot_sync(kFull, live_score(score));
+        rows = __popc(live);
+        warp_units = max(1, (rows * a.row_units + a.ctas * kWarps - 1) / (a.ctas * kWarps));
+    }
+    float4 *parts = a.part + (int64_t)group * (a.ctas * kWarps + K);
+    int u = w * warp_units;
+    const int u_end = min(u + warp_units, rows * a.row_units);
     while (u < u_end) {
-        const int row = u / a.row_units, row0 = row * a.row_units, stop = min(u_end, row0 + a.row_units);
-        take_part<kType, kOne>(a, row, u - row0, stop - row0, (int64_t)row * a.parts + (w - first_part(a, row)));
+        const int j = unit_beam(a, u), row0 = j * a.row_units, stop = min(u_end, row0 + a.row_units);
+        const int k = a.warp_units ? j : (int)__fns(live, 0, j + 1);
+        take_part<kType, kUnit>(a, group * K + k, u - row0, stop - row0, &parts[w + j]);
         u = stop;
     }
-    // Join the searches whose last CTA this is.
-    const int group_units = a.row_units * a.in.beams;
-    for (int group = begin / group_units; group * group_units < end; ++group) {
-        const int g0 = group * group_units;
-        const uint32_t ctas = (uint32_t)(g0 + group_units - 1) / (uint32_t)cta_units - (uint32_t)g0 / (uint32_t)cta_units + 1;
-        if (last_arrival(sm, &a.ticket[group], ctas)) {
-            join<kType>(a, sm, group);
-            if (threadIdx.x < 32) write_group(a, sm, group);
-        }
+    if (warp == 0) {
+        sm.score[lane] = score;
+        live = __ballot_sync(kFull, live_score(score));
+        if (lane == 0) { sm.live = live; sm.warp_units = warp_units; }
     }
+    if (!last_arrival(sm, &a.ticket[group], (uint32_t)a.ctas)) return;
+    join<kType, kUnit>(a, sm, group);
+    if (warp == 0) write_group(a, sm, group);
 }
 
-// How the rows are cut.  Warps: as many as the machine holds at once.  Units:
-// a line where the warps have few, a step (kStep lines, a quarter of the
-// reductions) where they have at least kLong, more steps where a search would have more
-// than kUnits.
+// How the rows are cut.  CTAs: a search has its own, so that none is the last
+// of two; as many in all as the machine holds at once, or up to twice that where the
+// rounding down would leave much of it idle.  Units: a line where a warp has
+// few, two where it has at least kLong (half the reductions), steps where a
+// search would have more than kUnits.
 constexpr int kLong = 8;
 
 bool deal(SelectArgs &a, int es, int sms)
 {
-    const int64_t per = 16 / es, rows = (int64_t)a.in.groups * a.in.beams, warps = (int64_t)sms * kPerSm * kWarps;
+    const int64_t per = 16 / es, K = a.in.beams, groups = a.in.groups, most = (int64_t)sms * kPerSm;
     const int64_t vectors = (a.in.vocab + 2 * (per - 1)) / per;  // a row may start inside a vector
-    const int64_t row_lines = (vectors + 31) / 32;
-    int64_t unit_lines = (row_lines * a.in.beams + kUnits - 1) / kUnits;
-    if (unit_lines > 1 || rows * row_lines >= kLong * warps) unit_lines = (unit_lines + kStep - 1) / kStep * kStep;
-    const int64_t row_units = (row_lines + unit_lines - 1) / unit_lines, units = rows * row_units;
-    const int64_t warp_units = (units + warps - 1) / warps;
+    const int64_t row_lines = (vectors + 31) / 32, lines = K * row_lines;
+    int64_t ctas = groups * 4 <= most ? most / groups : (most + groups - 1) / groups;
+    int64_t unit = (lines + kUnits - 1) / kUnits;
+    if (unit == 1 && lines >= kLong * ctas * kWarps) unit = 2;
+    if (unit > 2) unit = (unit + kStep - 1) / kStep * kStep;
+    const int64_t row_units = (row_lines + unit - 1) / unit, units = K * row_units;
+    const int64_t warp_units = std::max<int64_t>(1, (units + ctas * kWarps - 1) / (ctas * kWarps));
     a.row_lines = (int)row_lines;
-    a.unit_lines = (int)unit_lines;
+    a.unit_lines = (int)unit;
     a.row_units = (int)row_units;
-    a.units = (int)units;
-    a.warp_units = (int)warp_units;
-    a.parts = (int)((row_units + warp_units - 1) / warp_units) + 1;
-    // A search has at most kUnits + kMaxGroup units: i * (2^32 / row_units, rounded up) is off by less than 1 / row_units.
+    a.ctas = (int)((units + warp_units * kWarps - 1) / (warp_units * kWarps));
+    a.warp_units = warp_units * unit >= kLong ? 0 : (int)warp_units;
+    // i * (2^32 / row_units, rounded up) is off by less than 1 / row_units for the units of a search, kUnits + kMaxGroup at most.
     a.unit_magic = (uint32_t)(((1ull << 32) + (uint64_t)row_units - 1) / (uint64_t)row_units);  // (row_units = 1: not used)
-    return units + kWarps * warp_units < INT32_MAX;
+    return groups * a.ctas < INT32_MAX;
 }
 
 template <int kType>
 int launch(const SelectArgs &a, cudaStream_t st)
 {
-    const int cta_units = kWarps * a.warp_units;
-    const unsigned ctas = (unsigned)((a.units + cta_units - 1) / cta_units);
-    if (a.unit_lines == 1) select_kernel<kType, true><<<ctas, kThreads, 0, st>>>(a);
-    else select_kernel<kType, false><<<ctas, kThreads, 0, st>>>(a);
+    const unsigned ctas = (unsigned)(a.in.groups * a.ctas);
+    if (a.unit_lines == 1) select_kernel<kType, 1><<<ctas, kThreads, 0, st>>>(a);
+    else if (a.unit_lines == 2) select_kernel<kType, 2><<<ctas, kThreads, 0, st>>>(a);
+    else select_kernel<kType, kStep><<<ctas, kThreads, 0, st>>>(a);
     return wf_cuda_check(cudaGetLastError(), "select launch");
 }
 
 }  // namespace
 
-// Scratch of any call of at most these sizes.  Parts: rows * parts, where the
-// rows' units make at most as many parts as there are warps, one more a row
-// for the rounding up and one for a row's first cut.  Units: a row's share of
-// kUnits and one for the rounding up, or its lines.
+// Scratch of any call of at most these sizes.  Parts: a search's warps and
+// one more a row; the searches' CTAs are at most twice what the machine holds, or one each.  Units: a row's share of kUnits and one for the rounding up, or its lines.
 void wf_beam_scratch(int64_t rows, int64_t vocab, int sms, int64_t *parts, int64_t *units)
 {
-    *parts = (int64_t)sms * kPerSm * kWarps + 2 * rows;
+    *parts = std::max<int64_t>(2 * (int64_t)sms * kPerSm, rows) * kWarps + rows;
     *units = rows * std::min<int64_t>((vocab + 6) / 128 + 1, kUnits + 1);
 }
 
@@ -796,14 +825,14 @@ int wf_launch_select(wf_decode *d, const wf_beam *in, const wf_beam_out *out, cu
     SelectArgs a;
     a.in = *in;
     a.out = *out;
-    if (!deal(a, in->dtype == WF_F32 ? 4 : 2, d->sms))
-        return wf_set_error(WF_EINVAL, "wf_beam_select: %d x %d rows of %d logits pass 2^31 units", in->groups, in->beams, in->vocab);
+    const bool ok = deal(a, in->dtype == WF_F32 ? 4 : 2, d->sms);
     a.part = d->part;
     a.most = d->most;
     a.ticket = d->ticket + 1;
-    const int64_t parts = (int64_t)in->groups * in->beams * a.parts;
-    if (parts > d->parts || a.units > d->units)
-        return wf_set_error(WF_EINVAL, "wf_beam_select: %lld parts and %d units exceed the scratch", (long long)parts, a.units);
+    const int64_t parts = (int64_t)in->groups * ((int64_t)a.ctas * kWarps + in->beams);
+    const int64_t units = (int64_t)in->groups * in->beams * a.row_units;
+    if (!ok || parts > d->parts || units > d->units)
+        return wf_set_error(WF_EINVAL, "wf_beam_select: %lld parts and %lld units exceed the scratch", (long long)parts, (long long)units);
     if (in->dtype == WF_F32) return launch<WF_F32>(a, st);
     if (in->dtype == WF_F16) return launch<WF_F16>(a, st);
     return launch<WF_BF16>(a, st);
