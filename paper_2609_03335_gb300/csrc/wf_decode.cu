@@ -48,9 +48,9 @@ extern "C" int wf_decode_create(const wf_decode_limits *lim, int device, wf_deco
     const size_t o_sums = place(4 * (3 * (size_t)rows + 3));
     const size_t o_freed = place(4 * (size_t)(rows * tiles * kTileCols));
     const size_t o_tf = place(4 * (size_t)(rows * tiles)), o_tc = place(4 * (size_t)(rows * tiles));
-    const size_t o_cf = place(4 * (size_t)rows);
-    const size_t o_plan = place(16 * (size_t)rows), o_was = place(16), o_pairs = place(16 * (size_t)rows);
-    const size_t o_np = place(4), o_part = place(16 * (size_t)d->parts), o_most = place(4 * (size_t)d->units);
+    const size_t o_from = place(8 * (size_t)rows), o_rows = place(4 * (size_t)rows), o_gc = place(4 * (size_t)rows);
+    const size_t o_plan = place(16 * (size_t)rows), o_was = place(16), o_nc = place(4);
+    const size_t o_part = place(16 * (size_t)d->parts), o_most = place(4 * (size_t)d->units);
     rc = wf_cuda_check(cudaMalloc(&d->mem, at), "cudaMalloc(decode scratch)");
     if (!rc) rc = wf_cuda_check(cudaMemset(d->mem, 0, zeroed), "clear the decode scratch");
     if (rc) { wf_decode_destroy(d); return rc; }
@@ -61,11 +61,12 @@ extern "C" int wf_decode_create(const wf_decode_limits *lim, int device, wf_deco
     d->freed = (int32_t *)(m + o_freed);
     d->tile_freed = (int32_t *)(m + o_tf);
     d->tile_copy = (uint32_t *)(m + o_tc);
-    d->copy_from = (int32_t *)(m + o_cf);
+    d->copy_from = (int2 *)(m + o_from);
+    d->copy_rows = (int32_t *)(m + o_rows);
+    d->n_copies = (int32_t *)(m + o_nc);
+    d->group_copy = (uint32_t *)(m + o_gc);
     d->group_plan = (int4 *)(m + o_plan);
     d->ring_was = (int64_t *)(m + o_was);
-    d->pairs = (int4 *)(m + o_pairs);
-    d->n_pairs = (uint32_t *)(m + o_np);
     d->part = (float4 *)(m + o_part);
     d->most = (float *)(m + o_most);
     // The clearing runs on the default stream; the calls may use any other.

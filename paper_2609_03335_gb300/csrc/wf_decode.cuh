@@ -17,11 +17,12 @@ struct wf_decode {
     int32_t *freed;        // [max_rows][row blocks rounded up to a tile] ids of a tile's freed blocks
     int32_t *tile_freed;   // [groups][tiles] their count
     uint32_t *tile_copy;   // [groups][tiles] rows that need a copy of a block of this tile
-    int32_t *copy_from;    // [max_rows] the block that a row's copy is made from
-    int4 *group_plan;      // [groups] {first position in the ring's tail, in its head, blocks used for copies, blocks freed}
+    int2 *copy_from;       // [max_rows] the block that a row's copy is made from, its tokens
+    int32_t *copy_rows;    // [max_rows] the rows with copies
+    int32_t *n_copies;
+    uint32_t *group_copy;  // [groups] rows with copies
+    int4 *group_plan;      // [groups] {first place in the ring's tail, in its head, freed blocks used for copies, first copy}
     int64_t *ring_was;     // [2] head and tail before the call
-    int4 *pairs;           // [max_rows] {from, to, tokens, 0}
-    uint32_t *n_pairs;
     // select
     float4 *part;          // [parts] a warp's part of a row: reference, sum of exponentials, maximum
     float *most;           // [units] the maximum of each unit of the rows

@@ -44,7 +44,8 @@ __device__ __forceinline__ bool last_arrival(uint32_t *ticket, uint32_t n)
 // ---------------------------------------------------------------------------
 
 constexpr int kExtThreads = 512;
-constexpr int kTok = 4;         // consecutive tokens of a thread
+constexpr int kTok = 2;         // consecutive tokens of a lane: its slots fill 16 bytes, so a warp's stores whole sectors
+constexpr int kRegRows = 4;     // rows of a thread that the sums keep in registers
 constexpr int kSmemRows = 16384; // rows whose sums every CTA makes and holds (12 bytes each)
 
 struct ExtendArgs {
@@ -56,7 +57,7 @@ struct ExtendArgs {
     uint32_t max_tokens;
     wf_kv_step out;
     uint32_t *ticket;
-    bool wide;       // slot, pos and row take 16-byte stores
+    bool wide;       // the outputs take a lane's tokens in one store each
 };
 
 // What a token needs of its row: the first token's place in the step, the
@@ -74,37 +75,58 @@ __device__ __forceinline__ uint32_t blocks_of(uint32_t x, uint32_t bs, int shift
     return q + (q * bs != x);
 }
 
+// What a row asks for: tokens (-1: the row is passed over) and blocks.
+__device__ __forceinline__ int2 row_needs(const ExtendArgs &a, int32_t len, int32_t add)
+{
+    if (len < 0 || add < 0) return make_int2(-1, 0);
+    const uint32_t had = blocks_of((uint32_t)len, a.bs, a.shift), then = blocks_of((uint32_t)len + (uint32_t)add, a.bs, a.shift);
+    return then <= (uint32_t)a.width ? make_int2(add, (int)(then - had)) : make_int2(-1, 0);
+}
+
 // The sums of every row, by one CTA; returns the step's tokens and blocks.
 // first: this CTA also writes the rows' outputs that no input may share.
-__device__ void row_sums(const ExtendArgs &a, const RowSums &s, uint32_t avail, bool first, uint32_t &tokens,
-                         uint32_t &blocks)
+// A thread takes `per` consecutive rows: kPer of them in registers, or, for
+// kPer = 0, any number staged in s.
+template <int kPer>
+__device__ __forceinline__ void row_sums(const ExtendArgs &a, const RowSums &s, uint32_t avail, bool first, uint32_t &tokens,
+                                         uint32_t &blocks)
 {
     __shared__ uint2 warp_sum[kExtThreads / 32];
     __shared__ uint2 cut;  // tokens and blocks before the row that ends the line
-    __shared__ uint2 all;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    // Needs, staged in place: start = tokens (negative: the row is passed over), base = blocks.
-    for (int r = tid; r < a.rows; r += kExtThreads) {
-        const int32_t len = a.len[r], add = a.add[r];
-        int32_t t = -1, b = 0;
-        if (len >= 0 && add >= 0) {
-            const uint32_t had = blocks_of((uint32_t)len, a.bs, a.shift);
-            const uint32_t then = blocks_of((uint32_t)len + (uint32_t)add, a.bs, a.shift);
-            if (then <= (uint32_t)a.width) { t = add; b = (int32_t)(then - had); }
+    const int per = kPer ? kPer : (a.rows + kExtThreads - 1) / kExtThreads;
+    const int r0 = min(tid * per, a.rows), r1 = min(r0 + per, a.rows);
+    int32_t len[kPer ? kPer : 1];
+    int2 need[kPer ? kPer : 1];
+    if (kPer) {
+        int32_t add[kPer ? kPer : 1];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            len[i] = r0 + i < r1 ? a.len[r0 + i] : 0;
+            add[i] = r0 + i < r1 ? a.add[r0 + i] : 0;
         }
-        s.start[r] = t;
-        s.base[r] = b;
-        s.delta[r] = len;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) need[i] = row_needs(a, len[i], add[i]);
+    } else {
+        for (int r = tid; r < a.rows; r += kExtThreads) {
+            const int32_t l = a.len[r];
+            const int2 n = row_needs(a, l, a.add[r]);
+            s.start[r] = n.x;
+            s.base[r] = n.y;
+            s.delta[r] = l;
+        }
     }
     if (tid == 0) cut = make_uint2(kSat, kSat);
-    __syncthreads();
-    const int per = (a.rows + kExtThreads - 1) / kExtThreads;
-    const int r0 = min(tid * per, a.rows), r1 = min(r0 + per, a.rows);
+    if (!kPer) __syncthreads();
+    const auto needs = [&](int r) { return kPer ? need[r - r0] : make_int2(s.start[r], s.base[r]); };
     uint2 sum = make_uint2(0, 0);
-    for (int r = r0; r < r1; ++r) {
-        sum.x = sat_add(sum.x, (uint32_t)max(s.start[r], 0));
-        sum.y = sat_add(sum.y, (uint32_t)s.base[r]);
-    }
+#pragma unroll
+    for (int i = 0; i < (kPer ? kPer : 1); ++i)
+        for (int r = r0 + i; r < (kPer ? r0 + i + 1 : r1); ++r) {
+            const int2 n = kPer ? need[i] : needs(r);
+            sum.x = sat_add(sum.x, (uint32_t)max(n.x, 0));
+            sum.y = sat_add(sum.y, (uint32_t)n.y);
+        }
     uint2 inc = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -117,36 +139,53 @@ __device__ void row_sums(const ExtendArgs &a, const RowSums &s, uint32_t avail, 
     if (lane == 0) before = make_uint2(0, 0);
     if (lane == 31) warp_sum[warp] = inc;
     __syncthreads();
-    uint2 w = make_uint2(0, 0);
-    for (int i = 0; i < warp; ++i) { w.x = sat_add(w.x, warp_sum[i].x); w.y = sat_add(w.y, warp_sum[i].y); }
-    before.x = sat_add(before.x, w.x);
-    before.y = sat_add(before.y, w.y);
-    if (tid == kExtThreads - 1) all = make_uint2(sat_add(before.x, sum.x), sat_add(before.y, sum.y));
-    // The line ends at the one row that is the first past a limit.
+    // The warps' sums, scanned by every warp for itself.
+    uint2 w = lane < kExtThreads / 32 ? warp_sum[lane] : make_uint2(0, 0);
+#pragma unroll
+    for (int o = 1; o < kExtThreads / 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(kFull, w.x, o), y = __shfl_up_sync(kFull, w.y, o);
+        if (lane >= o) { w.x = sat_add(w.x, x); w.y = sat_add(w.y, y); }
+    }
+    const uint2 all = make_uint2(__shfl_sync(kFull, w.x, kExtThreads / 32 - 1), __shfl_sync(kFull, w.y, kExtThreads / 32 - 1));
+    if (warp) {
+        before.x = sat_add(before.x, __shfl_sync(kFull, w.x, warp - 1));
+        before.y = sat_add(before.y, __shfl_sync(kFull, w.y, warp - 1));
+    }
+    // The line ends at the one row that is the first past a limit.  If all fit there is none.
+    tokens = all.x;
+    blocks = all.y;
+    if (all.x > a.max_tokens || all.y > avail) {
+        uint2 at = before;
+#pragma unroll
+        for (int i = 0; i < (kPer ? kPer : 1); ++i)
+            for (int r = r0 + i; r < (kPer ? min(r0 + i + 1, r1) : r1); ++r) {
+                const int2 n = kPer ? need[i] : needs(r);
+                const uint2 next = make_uint2(sat_add(at.x, (uint32_t)max(n.x, 0)), sat_add(at.y, (uint32_t)n.y));
+                if ((next.x > a.max_tokens || next.y > avail) && at.x <= a.max_tokens && at.y <= avail) cut = at;
+                at = next;
+            }
+        __syncthreads();
+        tokens = cut.x;
+        blocks = cut.y;
+    }
     uint2 at = before;
-    for (int r = r0; r < r1; ++r) {
-        const uint2 next = make_uint2(sat_add(at.x, (uint32_t)max(s.start[r], 0)), sat_add(at.y, (uint32_t)s.base[r]));
-        if ((next.x > a.max_tokens || next.y > avail) && at.x <= a.max_tokens && at.y <= avail) cut = at;
-        at = next;
-    }
-    __syncthreads();
-    tokens = min(cut.x, all.x);
-    blocks = min(cut.y, all.y);
-    at = before;
-    for (int r = r0; r < r1; ++r) {
-        const int32_t t = s.start[r], b = s.base[r], len = s.delta[r];
-        const uint2 next = make_uint2(sat_add(at.x, (uint32_t)max(t, 0)), sat_add(at.y, (uint32_t)b));
-        const bool late_t = next.x > a.max_tokens, late_b = next.y > avail;
-        const int32_t start = (int32_t)(late_t || late_b ? tokens : at.x);
-        s.start[r] = start;
-        s.delta[r] = len - start;
-        s.base[r] = (int32_t)(at.y - blocks_of((uint32_t)max(len, 0), a.bs, a.shift));
-        if (first) {
-            a.out.start[r] = start;
-            a.out.status[r] = t < 0 ? WF_KV_LONG : (late_b ? WF_KV_BLOCKS : 0u) | (late_t ? WF_KV_TOKENS : 0u);
+#pragma unroll
+    for (int i = 0; i < (kPer ? kPer : 1); ++i)
+        for (int r = r0 + i; r < (kPer ? min(r0 + i + 1, r1) : r1); ++r) {
+            const int2 n = kPer ? need[i] : needs(r);
+            const int32_t l = kPer ? len[i] : s.delta[r];
+            const uint2 next = make_uint2(sat_add(at.x, (uint32_t)max(n.x, 0)), sat_add(at.y, (uint32_t)n.y));
+            const bool late_t = next.x > a.max_tokens, late_b = next.y > avail;
+            const int32_t start = (int32_t)(late_t || late_b ? tokens : at.x);
+            s.start[r] = start;
+            s.delta[r] = l - start;
+            s.base[r] = (int32_t)(at.y - blocks_of((uint32_t)max(l, 0), a.bs, a.shift));
+            if (first) {
+                a.out.start[r] = start;
+                a.out.status[r] = n.x < 0 ? WF_KV_LONG : (late_b ? WF_KV_BLOCKS : 0u) | (late_t ? WF_KV_TOKENS : 0u);
+            }
+            at = next;
         }
-        at = next;
-    }
     if (tid == 0) {
         s.start[a.rows] = (int32_t)tokens;
         if (first) a.out.start[a.rows] = (int32_t)tokens;
@@ -156,9 +195,9 @@ __device__ void row_sums(const ExtendArgs &a, const RowSums &s, uint32_t avail, 
 
 // The row of token t < tokens: the last one whose start is at most t and
 // that has tokens, found as the first whose successor starts after t.
-__device__ __forceinline__ int row_of(const int32_t *start, int rows, int32_t t)
+__device__ __forceinline__ int row_of(const int32_t *start, int lo, int rows, int32_t t)
 {
-    int lo = 0, hi = rows - 1;
+    int hi = rows - 1;
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         if (start[mid + 1] > t) hi = mid;
@@ -167,79 +206,148 @@ __device__ __forceinline__ int row_of(const int32_t *start, int rows, int32_t t)
     return lo;
 }
 
-// The tokens of the step, kTok consecutive ones a thread.
-__device__ void write_tokens(const ExtendArgs &a, const RowSums &s, uint32_t tokens, uint32_t h0)
+__device__ __forceinline__ void store_tokens(const ExtendArgs &a, uint32_t t0, const int64_t (&slot)[kTok], const int32_t (&pos)[kTok],
+                                             const int32_t (&row)[kTok])
 {
-    const uint32_t n = (uint32_t)a.n_blocks, bs = (uint32_t)a.bs;
-    const int64_t quads = ((int64_t)a.max_tokens + kTok - 1) / kTok;
-    for (int64_t q = (int64_t)blockIdx.x * kExtThreads + threadIdx.x; q < quads;
-         q += (int64_t)gridDim.x * kExtThreads) {
-        const uint32_t t0 = (uint32_t)(q * kTok);
-        int64_t slot[kTok];
-        int32_t pos[kTok], row[kTok];
-        int r = t0 < tokens ? row_of(s.start, a.rows, (int32_t)t0) : 0;
-        uint32_t end = 0, blk = 0, off = 0, id = 0;
-        bool fresh = true;
+    if (a.wide && t0 + kTok <= a.max_tokens) {
+        *(longlong2 *)(a.out.slot + t0) = make_longlong2(slot[0], slot[1]);
+        *(int2 *)(a.out.pos + t0) = make_int2(pos[0], pos[1]);
+        *(int2 *)(a.out.row + t0) = make_int2(row[0], row[1]);
+    } else {
 #pragma unroll
         for (int i = 0; i < kTok; ++i) {
-            const uint32_t t = t0 + i;
-            if (t >= tokens) {
-                slot[i] = -1;
-                pos[i] = 0;
-                row[i] = -1;
-                continue;
-            }
-            if (i > 0 && t >= end) {
-                do ++r; while ((uint32_t)s.start[r + 1] <= t);
-                fresh = true;
-            }
-            const uint32_t p = t + (uint32_t)s.delta[r];
-            bool load = true;
-            if (fresh) {
-                end = (uint32_t)s.start[r + 1];
-                blk = a.shift >= 0 ? p >> a.shift : p / bs;
-                off = p - blk * bs;
-                fresh = false;
-            } else if (++off == bs) {
-                off = 0;
-                ++blk;
-            } else {
-                load = false;
-            }
-            if (load) {
-                // A block before the row's first new one holds cached tokens: it is in the table.  A new one's first
-                // token has off 0 and is always new.
-                const uint32_t len = (uint32_t)(s.start[r] + s.delta[r]);
-                if (blk * bs < len) {
-                    id = (uint32_t)a.table[r * a.stride + blk];
-                } else {
-                    uint32_t at = h0 + (uint32_t)s.base[r] + blk;
-                    if (at >= n) at -= n;
-                    id = (uint32_t)__ldg(&a.ring[at]);
-                    if (off == 0) a.table[r * a.stride + blk] = (int32_t)id;
-                }
-            }
-            slot[i] = (int64_t)(int32_t)id * bs + off;
-            pos[i] = (int32_t)p;
-            row[i] = r;
-        }
-        if (a.wide && t0 + kTok <= a.max_tokens) {
-            *(longlong2 *)(a.out.slot + t0) = make_longlong2(slot[0], slot[1]);
-            *(longlong2 *)(a.out.slot + t0 + 2) = make_longlong2(slot[2], slot[3]);
-            *(int4 *)(a.out.pos + t0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
-            *(int4 *)(a.out.row + t0) = make_int4(row[0], row[1], row[2], row[3]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kTok; ++i) {
-                if (t0 + i >= a.max_tokens) break;
-                a.out.slot[t0 + i] = slot[i];
-                a.out.pos[t0 + i] = pos[i];
-                a.out.row[t0 + i] = row[i];
-            }
+            if (t0 + i >= a.max_tokens) break;
+            a.out.slot[t0 + i] = slot[i];
+            a.out.pos[t0 + i] = pos[i];
+            a.out.row[t0 + i] = row[i];
         }
     }
 }
 
+// Where block blk of row r is named: in the table if it holds cached tokens
+// (its first token comes before len), else at its place in the ring.
+__device__ __forceinline__ const int32_t *block_name(const ExtendArgs &a, const RowSums &s, int r, uint32_t blk, uint32_t len, uint32_t h0)
+{
+    if (blk * (uint32_t)a.bs < len) return a.table + (r * a.stride + blk);
+    uint32_t at = h0 + (uint32_t)s.base[r] + blk;
+    if (at >= (uint32_t)a.n_blocks) at -= (uint32_t)a.n_blocks;
+    return a.ring + at;
+}
+
+// kChunks times 64 tokens of row r, from this lane's first token t0 on: a
+// lane's tokens lie in one block or two neighbouring ones, whose names are
+// loaded for all chunks before any is used.
+template <int kChunks>
+__device__ __forceinline__ void row_chunks(const ExtendArgs &a, const RowSums &s, int r, uint32_t t0, uint32_t h0)
+{
+    constexpr uint32_t kChunk = 32 * kTok;
+    const uint32_t bs = (uint32_t)a.bs, n = (uint32_t)a.n_blocks;
+    const uint32_t p0 = t0 + (uint32_t)s.delta[r], len = (uint32_t)(s.start[r] + s.delta[r]);
+    const uint32_t ring0 = h0 + (uint32_t)s.base[r];
+    int32_t *const cells = a.table + r * a.stride;
+    uint32_t off[kChunks];
+    int32_t id[kChunks], id2[kChunks];
+#pragma unroll
+    for (int u = 0; u < kChunks; ++u) {
+        const uint32_t p = p0 + u * kChunk, blk = a.shift >= 0 ? p >> a.shift : p / bs;
+        off[u] = p - blk * bs;
+        uint32_t at = ring0 + blk, at2 = ring0 + blk + 1;
+        if (at >= n) at -= n;
+        if (at2 >= n) at2 -= n;
+        const bool two = off[u] + kTok > bs;  // the last tokens lie in the next block, a new one
+        id[u] = *(blk * bs < len ? cells + blk : a.ring + at);  // (its first token cached: the table names it)
+        id2[u] = two ? __ldg(&a.ring[at2]) : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < kChunks; ++u) {
+        const uint32_t p = p0 + u * kChunk, blk = a.shift >= 0 ? p >> a.shift : p / bs;
+        const bool two = off[u] + kTok > bs;
+        const int next_at = (int)(bs - off[u]);
+        if (off[u] == 0) cells[blk] = id[u];  // the block's first token: the table gets its name
+        if (two) cells[blk + 1] = id2[u];
+        const int64_t here = (int64_t)id[u] * bs + off[u], there = (int64_t)id2[u] * bs - next_at;
+        int64_t slot[kTok];
+#pragma unroll
+        for (int i = 0; i < kTok; ++i) slot[i] = (two && i >= next_at ? there : here) + i;
+        const uint32_t t = t0 + u * kChunk;
+        *(longlong2 *)(a.out.slot + t) = make_longlong2(slot[0], slot[1]);
+        *(int2 *)(a.out.pos + t) = make_int2((int)p, (int)p + 1);
+        *(int2 *)(a.out.row + t) = make_int2(r, r);
+    }
+}
+
+// The tokens of the step, 64 a warp at a time and kTok consecutive ones a
+// lane; where they lie in one row, without a search.
+__device__ __forceinline__ void write_tokens(const ExtendArgs &a, const RowSums &s, uint32_t tokens, uint32_t h0)
+{
+    constexpr uint32_t kChunk = 32 * kTok;
+    constexpr int kFast = 8;  // chunks of a row at once
+    const uint32_t bs = (uint32_t)a.bs, lane = threadIdx.x & 31;
+    // A CTA takes a run of the step, its warps in turn kFast chunks of it (one, where that gives each warp some).
+    const uint32_t chunks = (a.max_tokens + kChunk - 1) / kChunk;
+    const uint32_t size = chunks >= gridDim.x * (kExtThreads / 32) * kFast ? kFast : 1, batches = (chunks + size - 1) / size;
+    const uint32_t run = (batches + gridDim.x - 1) / gridDim.x;
+    const uint32_t b0 = min(blockIdx.x * run, batches), b1 = min(b0 + run, batches);
+    int r = 0;
+    for (uint32_t b = b0 + (threadIdx.x >> 5); b < b1; b += kExtThreads / 32)
+    for (uint32_t c = b * size, c1 = min(c + size, chunks); c < c1; ++c) {
+        const uint32_t first = c * kChunk, t0 = first + lane * kTok;
+        int64_t slot[kTok];
+        int32_t pos[kTok], row[kTok];
+        if (first >= tokens) {
+#pragma unroll
+            for (int i = 0; i < kTok; ++i) { slot[i] = -1; pos[i] = 0; row[i] = -1; }
+        } else {
+            if ((uint32_t)s.start[r + 1] <= first) r = row_of(s.start, r + 1, a.rows, (int32_t)first);  // (first < tokens: there is one)
+            const uint32_t left = (uint32_t)s.start[r + 1] - first;
+            if (left >= kFast * kChunk && c + kFast <= c1 && bs >= kTok && a.wide) {
+                row_chunks<kFast>(a, s, r, first + lane * kTok, h0);
+                c += kFast - 1;
+                continue;
+            }
+            if (left >= kChunk && bs >= kTok && a.wide) {
+                row_chunks<1>(a, s, r, first + lane * kTok, h0);
+                continue;
+            }
+            {
+                // Each token's row, then all their blocks' names at once.
+                const int32_t *name[kTok];
+                int32_t *cell[kTok];
+                uint32_t off[kTok];
+                int q = t0 < tokens ? row_of(s.start, r, a.rows, (int32_t)t0) : r;
+#pragma unroll
+                for (int i = 0; i < kTok; ++i) {
+                    const uint32_t t = t0 + i;
+                    name[i] = nullptr;
+                    cell[i] = nullptr;
+                    off[i] = 0;
+                    pos[i] = 0;
+                    row[i] = -1;
+                    if (t >= tokens) continue;
+                    while ((uint32_t)s.start[q + 1] <= t) ++q;
+                    const uint32_t p = t + (uint32_t)s.delta[q], blk = a.shift >= 0 ? p >> a.shift : p / bs;
+                    off[i] = p - blk * bs;
+                    name[i] = block_name(a, s, q, blk, (uint32_t)(s.start[q] + s.delta[q]), h0);
+                    if (off[i] == 0) cell[i] = a.table + (q * a.stride + blk);
+                    pos[i] = (int32_t)p;
+                    row[i] = q;
+                }
+                int32_t id[kTok];
+#pragma unroll
+                for (int i = 0; i < kTok; ++i) id[i] = name[i] ? *name[i] : 0;
+#pragma unroll
+                for (int i = 0; i < kTok; ++i) {
+                    if (cell[i]) *cell[i] = id[i];
+                    slot[i] = name[i] ? (int64_t)id[i] * bs + off[i] : -1;
+                }
+                r = __shfl_sync(kFull, q, 31);
+            }
+        }
+        store_tokens(a, t0, slot, pos, row);
+    }
+}
+
+template <int kPer>
 __global__ void __launch_bounds__(kExtThreads) extend_kernel(const __grid_constant__ ExtendArgs a)
 {
     extern __shared__ int32_t rows_sm[];
@@ -247,7 +355,7 @@ __global__ void __launch_bounds__(kExtThreads) extend_kernel(const __grid_consta
     const int64_t head = a.ends[0], tail = a.ends[1];
     const uint32_t avail = (uint32_t)max(0ll, min((long long)(tail - head), (long long)a.n_blocks));
     uint32_t tokens, blocks;
-    row_sums(a, s, avail, blockIdx.x == 0, tokens, blocks);
+    row_sums<kPer>(a, s, avail, blockIdx.x == 0, tokens, blocks);
     // Every CTA has read the lengths and the ends once the last one is here: they may be written, in place too.
     if (last_arrival(a.ticket, gridDim.x)) {
         for (int r = threadIdx.x; r < a.rows; r += kExtThreads)
@@ -268,7 +376,7 @@ __global__ void __launch_bounds__(kExtThreads) extend_sums_kernel(const __grid_c
     const int64_t head = a.ends[0], tail = a.ends[1];
     const uint32_t avail = (uint32_t)max(0ll, min((long long)(tail - head), (long long)a.n_blocks));
     uint32_t tokens, blocks;
-    row_sums(a, s, avail, true, tokens, blocks);
+    row_sums<0>(a, s, avail, true, tokens, blocks);
     for (int r = threadIdx.x; r < a.rows; r += kExtThreads)
         a.out.len[r] = s.start[r] + s.delta[r] + (s.start[r + 1] - s.start[r]);
     if (threadIdx.x == 0) {
@@ -289,15 +397,20 @@ __global__ void __launch_bounds__(kExtThreads) extend_fill_kernel(const __grid_c
 // Reorder
 // ---------------------------------------------------------------------------
 //
-// A CTA takes a group's rows over a tile of table columns: a thread per
-// column reads the old rows' entries into shared memory, writes the new
-// rows' in their place (all are read before any is written, so in place too),
-// and marks the entries that no new row holds: sharing stays within a
-// column, so a column decides alone.  The tile's freed ids are listed in
-// order, the rows whose last block lies in the tile say whether they need a
-// copy, and the last CTA to arrive sums freed blocks and copies over the
-// groups.  A second kernel gives the freed ids back and names the copies' blocks, a
-// third copies.
+// 1. A CTA takes a group's rows over a tile of table columns: a thread per
+//    column reads the old rows' entries into shared memory, writes the new
+//    rows' in their place (all are read before any is written, so in place too),
+//    and marks the entries that no new row holds: sharing stays within a
+//    column, so a column decides alone.  The tile's freed ids are listed in
+//    order, the rows whose last block lies in the tile say whether they need a
+//    copy, and the last CTA to arrive sums freed blocks and copies over the
+//    groups.
+// 2. With the sums, a CTA per group gives its freed ids back and writes its rows'
+//    lengths and last blocks, while other CTAs, which find a copy's blocks by
+//    the same sums, copy.
+//
+// The second kernel is launched while the first runs and waits for it on the
+// GPU, which hides most of a launch.
 
 constexpr int kColThreads = kTileCols;
 
@@ -312,20 +425,21 @@ struct ReorderArgs {
     uint32_t *status;
     // scratch
     int32_t *freed, *tile_freed;
-    int32_t *copy_from;
-    uint32_t *tile_copy, *ticket, *n_pairs;
-    int4 *group_plan, *pairs;
+    int2 *copy_from;            // per row: the block that its copy is made from, its tokens
+    int32_t *copy_rows, *n_copies;  // the rows with copies, in order
+    uint32_t *tile_copy, *group_copy, *ticket;
+    int4 *group_plan;           // {first place in the ring's tail, in its head, freed blocks used for copies, first copy}
     int64_t *ring_was;
     int *err;
 };
 
 // Length of an old row within the table's width, and the blocks it holds.
-__device__ __forceinline__ int64_t row_len(const ReorderArgs &a, int64_t row)
+__device__ __forceinline__ uint32_t row_len(const ReorderArgs &a, int64_t row)
 {
-    return min((int64_t)max(a.len[row], 0), (int64_t)a.width * a.bs);
+    return (uint32_t)min((int64_t)max(a.len[row], 0), (int64_t)a.width * a.bs);
 }
 
-__device__ __forceinline__ int row_blocks(const ReorderArgs &a, int64_t len) { return (int)((len + a.bs - 1) / a.bs); }
+__device__ __forceinline__ int row_blocks(const ReorderArgs &a, uint32_t len) { return (int)((len + (uint32_t)a.bs - 1) / (uint32_t)a.bs); }
 
 // The old row that row `row` of group g continues, counted in the group, or -1.
 __device__ __forceinline__ int row_parent(const ReorderArgs &a, int g, int k, bool &bad)
@@ -336,97 +450,132 @@ __device__ __forceinline__ int row_parent(const ReorderArgs &a, int g, int k, bo
     return ok ? (int)p : -1;
 }
 
-// Exclusive sum of v over the CTA's threads; total: the sum of all.
-__device__ __forceinline__ int block_before(int v, int &total)
+// Exclusive sums of v over the CTA's threads; total: the sums of all.
+__device__ __noinline__ int3 block_before(int3 v, int3 &total)
 {
-    __shared__ int warps[32];
+    __shared__ int3 warps[kColThreads / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int inc = v;
-#pragma unroll
+    int3 inc = v;
+#pragma unroll 1
     for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(kFull, inc, o);
-        if (lane >= o) inc += x;
+        const int x = __shfl_up_sync(kFull, inc.x, o), y = __shfl_up_sync(kFull, inc.y, o), z = __shfl_up_sync(kFull, inc.z, o);
+        if (lane >= o) { inc.x += x; inc.y += y; inc.z += z; }
     }
     __syncthreads();
     if (lane == 31) warps[warp] = inc;
     __syncthreads();
-    int before = 0;
-    total = 0;
-    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) {
-        if (w < warp) before += warps[w];
-        total += warps[w];
+    int3 before = make_int3(inc.x - v.x, inc.y - v.y, inc.z - v.z);
+    total = make_int3(0, 0, 0);
+#pragma unroll 1
+    for (int w = 0; w < kColThreads / 32; ++w) {
+        const int3 s = warps[w];
+        if (w < warp) { before.x += s.x; before.y += s.y; before.z += s.z; }
+        total.x += s.x;
+        total.y += s.y;
+        total.z += s.z;
     }
-    return before + inc - v;
+    return before;
 }
 
-// The groups' shares of the ring, by the last CTA of the tables' kernel.
-__device__ void plan_groups(const ReorderArgs &a)
+// The groups' shares of the ring, by the last CTA of the tables' kernel; sums:
+// two words a group for kTileCols / 2 * group groups at a time.
+__device__ void plan_groups(const ReorderArgs &a, int32_t *sums)
 {
-    const int per = (a.groups + kColThreads - 1) / kColThreads;
-    const int g0 = min((int)threadIdx.x * per, a.groups), g1 = min(g0 + per, a.groups);
-    int give = 0, take = 0;
-    for (int g = g0; g < g1; ++g) {
-        int f = 0, c = 0;
-        for (int t = 0; t < a.tiles; ++t) {
-            f += __ldcg(&a.tile_freed[(int64_t)g * a.tiles + t]);
-            c += __popc(__ldcg(&a.tile_copy[(int64_t)g * a.tiles + t]));
+    const int tid = threadIdx.x, chunk = kTileCols / 2 * a.group;
+    const int64_t head = a.ends[0], tail = a.ends[1];
+    int3 at = make_int3(0, 0, 0);  // given back, taken, copies
+    for (int c0 = 0; c0 < a.groups; c0 += chunk) {
+        const int n = min(chunk, a.groups - c0);
+        __syncthreads();
+        for (int i = tid; i < 2 * n; i += kColThreads) sums[i] = 0;
+        __syncthreads();
+        // Freed blocks and rows with copies: each row's last block lies in one tile.
+        for (int i = tid; i < n * a.tiles; i += kColThreads) {
+            const int freed = __ldcg(&a.tile_freed[(int64_t)c0 * a.tiles + i]);
+            const uint32_t copy = __ldcg(&a.tile_copy[(int64_t)c0 * a.tiles + i]);
+            const int g = a.tiles == 1 ? i : i / a.tiles;
+            if (freed) atomicAdd(&sums[2 * g], freed);
+            if (copy) atomicOr(&sums[2 * g + 1], (int)copy);
         }
-        a.group_plan[g] = make_int4(0, 0, min(f, c), f);
-        give += max(f - c, 0);
-        take += max(c - f, 0);
-        a.group_plan[g].x = f - c;
+        __syncthreads();
+        const int per = (n + kColThreads - 1) / kColThreads, g0 = min(tid * per, n), g1 = min(g0 + per, n);
+        int3 mine = make_int3(0, 0, 0), all;
+#pragma unroll 1
+        for (int g = g0; g < g1; ++g) {
+            const int f = sums[2 * g], c = __popc((uint32_t)sums[2 * g + 1]);
+            mine.x += max(f - c, 0);
+            mine.y += max(c - f, 0);
+            mine.z += c;
+        }
+        int3 here = block_before(mine, all);
+        here.x += at.x;
+        here.y += at.y;
+        here.z += at.z;
+#pragma unroll 1
+        for (int g = g0; g < g1; ++g) {
+            const uint32_t mask = (uint32_t)sums[2 * g + 1];
+            const int f = sums[2 * g], c = __popc(mask);
+            a.group_plan[c0 + g] = make_int4(here.x, here.y, min(f, c), here.z);
+            a.group_copy[c0 + g] = mask;
+            for (uint32_t m = mask; m; m &= m - 1) a.copy_rows[here.z++] = (c0 + g) * a.group + __ffs((int)m) - 1;
+            here.x += max(f - c, 0);
+            here.y += max(c - f, 0);
+        }
+        at.x += all.x;
+        at.y += all.y;
+        at.z += all.z;
     }
-    int gives, takes;
-    int give_at = block_before(give, gives), take_at = block_before(take, takes);
-    for (int g = g0; g < g1; ++g) {
-        int4 p = a.group_plan[g];
-        const int net = p.x;
-        p.x = give_at;
-        p.y = take_at;
-        a.group_plan[g] = p;
-        give_at += max(net, 0);
-        take_at += max(-net, 0);
-    }
-    if (threadIdx.x == 0) {
-        const int64_t head = a.ends[0], tail = a.ends[1];
+    if (tid == 0) {
         a.ring_was[0] = head;
         a.ring_was[1] = tail;
-        a.to_ends[0] = head + min((int64_t)takes, max(tail - head, (int64_t)0));
-        a.to_ends[1] = tail + gives;
-        *a.n_pairs = 0;
+        a.to_ends[0] = head + min((int64_t)at.y, max(tail - head, (int64_t)0));
+        a.to_ends[1] = tail + at.x;
+        *a.n_copies = at.z;
     }
 }
 
 __global__ void __launch_bounds__(kColThreads) reorder_tables_kernel(const __grid_constant__ ReorderArgs a)
 {
     extern __shared__ int32_t cells[];  // [group][kTileCols]
-    __shared__ int had[kMaxGroup], from[kMaxGroup];
+    __shared__ int had[kMaxGroup], from[kMaxGroup], part[kMaxGroup];  // blocks, parent, tokens in a partly filled last block
     __shared__ uint32_t goes_on, copied;
     const int g = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, tid = threadIdx.x, K = a.group;
     const int64_t row0 = (int64_t)g * K;
+    asm volatile("griddepcontrol.launch_dependents;");
     if (tid < 32) {
         bool bad;
         const int p = tid < K ? row_parent(a, g, tid, bad) : -1;
         if (tid < K) {
+            const uint32_t len = row_len(a, row0 + tid);
             from[tid] = p;
-            had[tid] = row_blocks(a, row_len(a, row0 + tid));
+            had[tid] = row_blocks(a, len);
+            part[tid] = (int)(len % (uint32_t)a.bs);
         }
         const uint32_t on = __reduce_or_sync(kFull, p >= 0 ? 1u << p : 0u);
         if (tid == 0) goes_on = on;
     }
     __syncthreads();
     const int j = tile * kTileCols + tid;
-    for (int k = 0; k < K; ++k) cells[k * kTileCols + tid] = j < had[k] ? a.table[(row0 + k) * a.stride + j] : -1;
+    const int32_t *column = a.table + row0 * a.stride + j;
+#pragma unroll 4
+    for (int k = 0; k < K; ++k, column += a.stride) {  // (copies, which no register waits for)
+        int32_t *cell = &cells[k * kTileCols + tid];
+        if (j < had[k])
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(cell)), "l"(column) : "memory");
+        else
+            *cell = -1;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
     // The rows whose last block lies here, is partly filled and is a lower row's too: they will get one of their own.
     if (tid < 32) {
         bool mine = false;
         int last = 0;
-        int32_t id = -1;
+        int32_t id = -1, rest = 0;
         if (tid < K && from[tid] >= 0) {
-            const int64_t n = row_len(a, row0 + from[tid]);
+            rest = part[from[tid]];
             last = had[from[tid]] - 1;
-            mine = n % a.bs != 0 && last / kTileCols == tile;
+            mine = rest != 0 && last / kTileCols == tile;
             if (mine) id = cells[from[tid] * kTileCols + last % kTileCols];
         }
         const uint32_t in = __ballot_sync(kFull, mine);
@@ -434,7 +583,7 @@ __global__ void __launch_bounds__(kColThreads) reorder_tables_kernel(const __gri
         if (mine) {
             const uint32_t same = __match_any_sync(in, (unsigned long long)(uint32_t)last << 32 | (uint32_t)id);
             copy = (same & ((1u << tid) - 1u)) != 0;
-            if (copy) a.copy_from[row0 + tid] = id;
+            if (copy) a.copy_from[row0 + tid] = make_int2(id, rest);
         }
         const uint32_t mask = __ballot_sync(kFull, copy);
         if (tid == 0) copied = mask;
@@ -442,6 +591,7 @@ __global__ void __launch_bounds__(kColThreads) reorder_tables_kernel(const __gri
     __syncthreads();
     // The new rows.  A row that goes on in its own place needs no write.
     const bool in_place = a.table == a.to_table;
+#pragma unroll 4
     for (int k = 0; k < K; ++k) {
         const int p = from[k];
         if (p < 0 || j >= had[p] || (in_place && p == k) || ((copied >> k & 1u) && j == had[p] - 1)) continue;
@@ -449,87 +599,117 @@ __global__ void __launch_bounds__(kColThreads) reorder_tables_kernel(const __gri
     }
     // Freed: an old row's entry that no row that goes on holds, and no lower one of those that end.
     uint32_t free_mask = 0;
-    for (int k = 0; k < K; ++k) {
-        if ((goes_on >> k & 1u) || j >= had[k]) continue;
+#pragma unroll 1
+    for (uint32_t ends = ~goes_on & (uint32_t)((1ull << K) - 1); ends; ends &= ends - 1) {
+        const int k = __ffs((int)ends) - 1;
         const int32_t id = cells[k * kTileCols + tid];
-        bool held = false;
-        for (int q = 0; q < K; ++q)
-            held |= q != k && j < had[q] && ((goes_on >> q & 1u) || q < k) && cells[q * kTileCols + tid] == id;
-        if (!held) free_mask |= 1u << k;
+        bool held = id < 0;  // no entry
+#pragma unroll 2
+        for (uint32_t others = goes_on | (ends ^ (ends - 1)) >> 1; others; others &= others - 1)
+            held |= cells[(__ffs((int)others) - 1) * kTileCols + tid] == id;
+        free_mask |= (uint32_t)!held << k;
     }
-    int freed;
-    int at = block_before(__popc(free_mask), freed);
+    int3 all;
+    int at = block_before(make_int3(__popc(free_mask), 0, 0), all).x;
+    const int freed = all.x;
     int32_t *list = a.freed + ((int64_t)g * a.tiles + tile) * kTileCols * K;
     for (uint32_t m = free_mask; m; m &= m - 1) list[at++] = cells[(__ffs((int)m) - 1) * kTileCols + tid];
     if (tid == 0) {
         a.tile_copy[(int64_t)g * a.tiles + tile] = copied;
         a.tile_freed[(int64_t)g * a.tiles + tile] = freed;
     }
-    if (last_arrival(a.ticket, (uint32_t)(a.groups * a.tiles))) plan_groups(a);
+    if (last_arrival(a.ticket, (uint32_t)(a.groups * a.tiles))) plan_groups(a, cells);
 }
 
-constexpr int kMoveThreads = 128;
+constexpr int kFinishThreads = 256;
+constexpr int kPiece = 16384;  // bytes of a plane's block that a CTA copies at once
 
-// Freed block i of a group, from the tiles' lists.
-__device__ __forceinline__ int32_t freed_id(const ReorderArgs &a, int g, int i)
+// Freed block i of a group (i < 0: none), from the tiles' lists; a whole warp
+// calls it, each lane for its own i.
+__device__ __forceinline__ int32_t freed_block(const ReorderArgs &a, int g, int i)
 {
-    for (int t = 0; t < a.tiles; ++t) {
-        const int n = a.tile_freed[(int64_t)g * a.tiles + t];
-        if (i < n) return a.freed[((int64_t)g * a.tiles + t) * kTileCols * a.group + i];
-        i -= n;
+    const int lane = threadIdx.x & 31;
+    int32_t id = -1;
+    for (int t0 = 0, before = 0; t0 < a.tiles; t0 += 32) {
+        const int n = t0 + lane < a.tiles ? a.tile_freed[(int64_t)g * a.tiles + t0 + lane] : 0;
+        int inc = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(kFull, inc, o);
+            if (lane >= o) inc += x;
+        }
+        int tile = -1, at = 0;
+        for (int t = 0; t < min(32, a.tiles - t0); ++t) {
+            const int end = before + __shfl_sync(kFull, inc, t), begin = end - __shfl_sync(kFull, n, t);
+            if (i >= begin && i < end) { tile = t0 + t; at = i - begin; }
+        }
+        if (tile >= 0) id = a.freed[((int64_t)g * a.tiles + tile) * kTileCols * a.group + at];
+        before += __shfl_sync(kFull, inc, 31);
+        if (!__any_sync(kFull, i >= before)) break;
     }
-    return -1;
+    return id;
 }
 
-__global__ void __launch_bounds__(kMoveThreads) reorder_moves_kernel(const __grid_constant__ ReorderArgs a)
+// The block that the copy of row k of group g goes to, by a whole warp; false
+// for the lanes without a copy or whose copy finds the ring run out.
+__device__ __forceinline__ bool copy_block(const ReorderArgs &a, int g, bool copies, int k, uint32_t mask, const int4 &plan, int64_t head,
+                                           int64_t tail, int32_t &to)
 {
-    const int g = blockIdx.x, tid = threadIdx.x, K = a.group;
-    const uint32_t n = (uint32_t)a.n_blocks;
+    const int i = copies ? __popc(mask & ((1u << k) - 1u)) : -1;
+    to = freed_block(a, g, i < plan.z ? i : -1);
+    if (i < plan.z) return copies;
+    const int64_t at = (int64_t)plan.y + i - plan.z;
+    if (at >= tail - head) return false;
+    to = a.ring[((uint64_t)head + at) % (uint32_t)a.n_blocks];
+    return true;
+}
+
+// A group: its freed blocks back to the ring, its rows' lengths, last blocks and outputs.
+__device__ __forceinline__ void finish_group(const ReorderArgs &a, int g)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.group;
+    const uint32_t n = (uint32_t)a.n_blocks, mask = a.group_copy[g];
     const int4 plan = a.group_plan[g];
     const int64_t head = a.ring_was[0], tail = a.ring_was[1];
-    // Give back what the copies do not use.
+    // What the copies do not use goes back; a warp takes every eighth tile.
     const uint32_t tail0 = (uint32_t)((uint64_t)tail % n);
-    int before = 0;
-    for (int t = 0; t < a.tiles; ++t) {
-        const int c = a.tile_freed[(int64_t)g * a.tiles + t];
-        const int32_t *list = a.freed + ((int64_t)g * a.tiles + t) * kTileCols * K;
-        for (int i = tid; i < c; i += kMoveThreads) {
-            const int rest = before + i - plan.z;
-            if (rest < 0) continue;
-            a.ring[((uint64_t)tail0 + plan.x + rest) % n] = list[i];
+    for (int t0 = 0, before = 0; t0 < a.tiles; t0 += 32) {
+        const int c = t0 + lane < a.tiles ? a.tile_freed[(int64_t)g * a.tiles + t0 + lane] : 0;
+        int inc = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(kFull, inc, o);
+            if (lane >= o) inc += x;
         }
-        before += c;
+        for (int t = warp; t < min(32, a.tiles - t0); t += kFinishThreads / 32) {
+            const int count = __shfl_sync(kFull, c, t), first = before + __shfl_sync(kFull, inc, t) - count - plan.z;
+            const int32_t *list = a.freed + ((int64_t)g * a.tiles + t0 + t) * kTileCols * K;
+            for (int i = lane; i < count; i += 32)
+                if (first + i >= 0) a.ring[((uint64_t)tail0 + plan.x + first + i) % n] = list[i];
+        }
+        before += __shfl_sync(kFull, inc, 31);
     }
-    if (tid >= 32) return;
-    uint32_t copy = 0;
-    for (int t = 0; t < a.tiles; ++t) copy |= a.tile_copy[(int64_t)g * a.tiles + t];
-    if (tid >= K) return;
-    const int64_t row = (int64_t)g * K + tid;
-    bool bad;
-    const int p = row_parent(a, g, tid, bad);
+    if (warp) return;
+    const bool here = lane < K, copies = here && (mask >> lane & 1u);
+    const int64_t row = (int64_t)g * K + lane;
+    bool bad = false;
+    const int p = here ? row_parent(a, g, lane, bad) : -1;
     uint32_t status = bad ? WF_KV_PARENT : 0;
     // The parents' lengths are read before any is written: to_len may be len.
-    int64_t len = p >= 0 ? row_len(a, (int64_t)g * K + p) : 0;
-    __syncwarp(K == 32 ? kFull : (1u << K) - 1u);
+    uint32_t len = p >= 0 ? row_len(a, (int64_t)g * K + p) : 0;
+    int32_t to = -1;
+    const bool found = copy_block(a, g, copies, lane, mask, plan, head, tail, to);  // (a whole warp's call)
+    __syncwarp();
+    if (!here) return;
     int2 move = make_int2(-1, -1);
-    if (copy >> tid & 1u) {
-        const int i = __popc(copy & ((1u << tid) - 1u));
-        int32_t *cell = &a.to_table[row * a.to_stride + row_blocks(a, len) - 1];  // left to this kernel
-        const int64_t in_ring = (int64_t)plan.y + i - plan.z;
-        if (i >= plan.z && in_ring >= tail - head) {
-            status |= WF_KV_BLOCKS;
-            len -= len % a.bs;
-        } else {
-            const int32_t src = a.copy_from[row];
-            const int32_t dst = i < plan.z ? freed_id(a, g, i) : a.ring[((uint64_t)head + in_ring) % n];
-            *cell = dst;
-            if ((uint32_t)src < n && (uint32_t)dst < n) {
-                move = make_int2(src, dst);
-                a.pairs[atomicAdd(a.n_pairs, 1u)] = make_int4(src, dst, (int)(len % a.bs), 0);
-            } else {
-                *a.err = 1;
-            }
-        }
+    if (found) {
+        a.to_table[row * a.to_stride + row_blocks(a, len) - 1] = to;  // left to this kernel
+        const int32_t from = a.copy_from[row].x;
+        if ((uint32_t)from < n && (uint32_t)to < n) move = make_int2(from, to);
+        else *a.err = 1;
+    } else if (copies) {
+        status |= WF_KV_BLOCKS;
+        len -= len % (uint32_t)a.bs;
     }
     a.to_len[row] = (int32_t)len;
     a.copies[2 * row] = move.x;
@@ -537,34 +717,64 @@ __global__ void __launch_bounds__(kMoveThreads) reorder_moves_kernel(const __gri
     a.status[row] = status;
 }
 
-constexpr int kCopyThreads = 256;
-constexpr int kPiece = 16384;  // bytes of a plane's block that a CTA copies at once
-
-// T: the widest type that the cache's addresses are aligned to.
+// CTAs [0, groups) finish a group each; the others copy.  T: the widest type
+// that the cache's addresses are aligned to.  A copying CTA takes a run of
+// pieces, those of a copy one after the other.
 template <class T>
-__global__ void __launch_bounds__(kCopyThreads) copy_kernel(wf_kv_cache c, int64_t block_bytes, int pieces, const int4 *pairs,
-                                                            const uint32_t *n_pairs)
+__global__ void __launch_bounds__(kFinishThreads) reorder_finish_kernel(const __grid_constant__ ReorderArgs a,
+                                                                        const __grid_constant__ wf_kv_cache c, int64_t block_bytes,
+                                                                        int pieces)
 {
-    const int64_t items = (int64_t)*n_pairs * c.planes * pieces;
-    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-        const int piece = (int)(it % pieces);
-        const int64_t rest = it / pieces;
-        const int4 m = pairs[rest / c.planes];
-        const int64_t end = min((int64_t)m.z * c.token_bytes, (int64_t)(piece + 1) * kPiece);
-        uint8_t *plane = (uint8_t *)c.base + (rest % c.planes) * c.plane_stride;
-        const T *src = (const T *)(plane + m.x * block_bytes + (int64_t)piece * kPiece);
-        T *dst = (T *)(plane + m.y * block_bytes + (int64_t)piece * kPiece);
-        const int n = (int)((end - (int64_t)piece * kPiece) / (int64_t)sizeof(T));
-        int i = threadIdx.x;
-        for (; i + 3 * kCopyThreads < n; i += 4 * kCopyThreads) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if ((int)blockIdx.x < a.groups) {
+        finish_group(a, (int)blockIdx.x);
+        return;
+    }
+    const int64_t each = (int64_t)c.planes * pieces, items = *a.n_copies * each, ctas = (int)gridDim.x - a.groups;
+    const int64_t run = (items + ctas - 1) / ctas, it0 = ((int)blockIdx.x - a.groups) * run, it1 = min(it0 + run, items);
+    const int64_t head = a.ring_was[0], tail = a.ring_was[1];
+    int64_t copy = -1;
+    int32_t from = 0, to = 0;
+    int64_t bytes = 0;
+    for (int64_t it = it0; it < it1; ++it) {
+        if (it / each != copy) {
+            copy = it / each;
+            const int row = a.copy_rows[copy], g = row / a.group;
+            const int2 src = a.copy_from[row];
+            const bool found = copy_block(a, g, true, row - g * a.group, a.group_copy[g], a.group_plan[g], head, tail, to);
+            from = src.x;
+            bytes = found && (uint32_t)from < (uint32_t)a.n_blocks && (uint32_t)to < (uint32_t)a.n_blocks ? src.y * c.token_bytes : 0;
+        }
+        const int64_t rest = it - copy * each, plane = rest / pieces, first = (rest - plane * pieces) * kPiece;
+        const int n = (int)((min(bytes, first + kPiece) - first) / (int64_t)sizeof(T));  // (no more than 0: nothing to copy)
+        uint8_t *base = (uint8_t *)c.base + plane * c.plane_stride + first;
+        const T *src = (const T *)(base + from * block_bytes);
+        T *dst = (T *)(base + to * block_bytes);
+        for (int i = threadIdx.x; i < n; i += 4 * kFinishThreads) {
             T v[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = src[i + u * kCopyThreads];
+            for (int u = 0; u < 4; ++u)
+                if (i + u * kFinishThreads < n) v[u] = src[i + u * kFinishThreads];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) dst[i + u * kCopyThreads] = v[u];
+            for (int u = 0; u < 4; ++u)
+                if (i + u * kFinishThreads < n) dst[i + u * kFinishThreads] = v[u];
         }
-        for (; i < n; i += kCopyThreads) dst[i] = src[i];
     }
+}
+
+template <class T>
+int launch_finish(const ReorderArgs &a, const wf_kv_cache &c, int64_t block_bytes, int pieces, unsigned copiers, cudaStream_t st)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)a.groups + copiers);
+    cfg.blockDim = dim3(kFinishThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return wf_cuda_check(cudaLaunchKernelEx(&cfg, reorder_finish_kernel<T>, a, c, block_bytes, pieces), "reorder finish launch");
 }
 
 }  // namespace
@@ -595,26 +805,25 @@ int wf_launch_reorder(wf_decode *d, const wf_kv *kv, int32_t group, const int32_
     a.freed = d->freed;
     a.tile_freed = d->tile_freed;
     a.tile_copy = d->tile_copy;
+    a.group_copy = d->group_copy;
     a.copy_from = d->copy_from;
+    a.copy_rows = d->copy_rows;
+    a.n_copies = d->n_copies;
     a.ticket = d->ticket;
-    a.n_pairs = d->n_pairs;
     a.group_plan = d->group_plan;
-    a.pairs = d->pairs;
     a.ring_was = d->ring_was;
     a.err = d->err;
     reorder_tables_kernel<<<(unsigned)(a.groups * a.tiles), kColThreads, 4 * (size_t)group * kTileCols, st>>>(a);
-    reorder_moves_kernel<<<(unsigned)a.groups, kMoveThreads, 0, st>>>(a);
-    if (cache) {
-        const int64_t block = cache->token_bytes * kv->block_tokens;
-        const int pieces = (int)((block + kPiece - 1) / kPiece);
-        const uint64_t bits = (uintptr_t)cache->base | (uint64_t)cache->token_bytes | (cache->planes > 1 ? (uint64_t)cache->plane_stride : 0);
-        const int64_t most = (int64_t)a.rows * cache->planes * pieces;
-        const unsigned ctas = (unsigned)std::min<int64_t>(most, 8 * d->sms);
-        if (bits % 16 == 0) copy_kernel<uint4><<<ctas, kCopyThreads, 0, st>>>(*cache, block, pieces, a.pairs, a.n_pairs);
-        else if (bits % 4 == 0) copy_kernel<uint32_t><<<ctas, kCopyThreads, 0, st>>>(*cache, block, pieces, a.pairs, a.n_pairs);
-        else copy_kernel<uint8_t><<<ctas, kCopyThreads, 0, st>>>(*cache, block, pieces, a.pairs, a.n_pairs);
-    }
-    return wf_cuda_check(cudaGetLastError(), "reorder launch");
+    int rc = wf_cuda_check(cudaGetLastError(), "reorder launch");
+    if (rc) return rc;
+    if (!cache) return launch_finish<uint32_t>(a, wf_kv_cache{}, 0, 0, 0, st);
+    const int64_t block = cache->token_bytes * kv->block_tokens;
+    const int pieces = (int)((block + kPiece - 1) / kPiece);
+    const uint64_t bits = (uintptr_t)cache->base | (uint64_t)cache->token_bytes | (cache->planes > 1 ? (uint64_t)cache->plane_stride : 0);
+    const unsigned copiers = (unsigned)std::min<int64_t>((int64_t)a.rows * cache->planes * pieces, 8 * d->sms);
+    if (bits % 16 == 0) return launch_finish<uint4>(a, *cache, block, pieces, copiers, st);
+    if (bits % 4 == 0) return launch_finish<uint32_t>(a, *cache, block, pieces, copiers, st);
+    return launch_finish<uint8_t>(a, *cache, block, pieces, copiers, st);
 }
 
 int wf_launch_extend(wf_decode *d, const wf_kv *kv, const int32_t *add, const wf_kv_step *out, cudaStream_t st)
@@ -634,7 +843,7 @@ int wf_launch_extend(wf_decode *d, const wf_kv *kv, const int32_t *add, const wf
     a.max_tokens = (uint32_t)out->max_tokens;
     a.out = *out;
     a.ticket = d->ticket;
-    a.wide = (((uintptr_t)out->slot | (uintptr_t)out->pos | (uintptr_t)out->row) & 15) == 0;
+    a.wide = ((uintptr_t)out->slot & 15) == 0 && (((uintptr_t)out->pos | (uintptr_t)out->row) & 7) == 0;
     const int64_t ctas = ((int64_t)a.max_tokens + kTok * kExtThreads - 1) / (kTok * kExtThreads);
     const unsigned grid = (unsigned)std::min<int64_t>(ctas, 2 * d->sms);
     if (a.rows > kSmemRows) {
@@ -643,9 +852,13 @@ int wf_launch_extend(wf_decode *d, const wf_kv *kv, const int32_t *add, const wf
         return wf_cuda_check(cudaGetLastError(), "extend launch");
     }
     const size_t smem = 4 * (3 * (size_t)a.rows + 1);
-    int rc = wf_cuda_check(cudaFuncSetAttribute(extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem),
-                           "extend smem attribute");
-    if (rc) return rc;
-    extend_kernel<<<grid, kExtThreads, smem, st>>>(a);
+    if (a.rows <= kRegRows * kExtThreads) {
+        extend_kernel<kRegRows><<<grid, kExtThreads, smem, st>>>(a);
+    } else {
+        const int rc = wf_cuda_check(cudaFuncSetAttribute(extend_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem),
+                                     "extend smem attribute");
+        if (rc) return rc;
+        extend_kernel<0><<<grid, kExtThreads, smem, st>>>(a);
+    }
     return wf_cuda_check(cudaGetLastError(), "extend launch");
 }
