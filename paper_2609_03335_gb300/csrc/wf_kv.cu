@@ -417,7 +417,9 @@ __global__ void __launch_bounds__(kExtThreads) extend_fill_kernel(const __grid_c
 //    the same sums, copy.
 //
 // The second kernel is launched while the first runs and waits for it on the
-// GPU, which hides most of a launch.
+// GPU, which hides most of a launch.  (Its CTAs could each make the sums for
+// themselves and spare the first kernel its arrivals: 1 us less where nothing
+// is copied, 2.5 us more where much is.)
 
 constexpr int kColThreads = kTileCols;
 
@@ -545,6 +547,7 @@ __global__ void __launch_bounds__(kColThreads) reorder_tables_kernel(const __gri
 {
     extern __shared__ int32_t cells[];  // [group][kTileCols]
     __shared__ int had[kMaxGroup], from[kMaxGroup], part[kMaxGroup];  // blocks, parent, tokens in a partly filled last block
+    __shared__ int put[kMaxGroup];                                    // entries of the new row that are written here
     __shared__ uint32_t goes_on, copied;
     const int g = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, tid = threadIdx.x, K = a.group;
     const int64_t row0 = (int64_t)g * K;
@@ -594,16 +597,15 @@ __global__ void __launch_bounds__(kColThreads) reorder_tables_kernel(const __gri
         }
         const uint32_t mask = __ballot_sync(kFull, copy);
         if (tid == 0) copied = mask;
+        // A row that goes on in its own place needs no write; a block of its own is named later.
+        if (tid < K) put[tid] = from[tid] < 0 || (a.table == a.to_table && from[tid] == tid) ? 0 : last + 1 - (int)copy;
     }
     __syncthreads();
-    // The new rows.  A row that goes on in its own place needs no write.
-    const bool in_place = a.table == a.to_table;
+    // The new rows.
+    int32_t *to = a.to_table + row0 * a.to_stride + j;
 #pragma unroll 4
-    for (int k = 0; k < K; ++k) {
-        const int p = from[k];
-        if (p < 0 || j >= had[p] || (in_place && p == k) || ((copied >> k & 1u) && j == had[p] - 1)) continue;
-        a.to_table[(row0 + k) * a.to_stride + j] = cells[p * kTileCols + tid];
-    }
+    for (int k = 0; k < K; ++k, to += a.to_stride)
+        if (j < put[k]) *to = cells[from[k] * kTileCols + tid];
     // Freed: an old row's entry that no row that goes on holds, and no lower one of those that end.
     uint32_t free_mask = 0;
 #pragma unroll 1
@@ -616,11 +618,14 @@ __global__ void __launch_bounds__(kColThreads) reorder_tables_kernel(const __gri
             held |= cells[(__ffs((int)others) - 1) * kTileCols + tid] == id;
         free_mask |= (uint32_t)!held << k;
     }
-    int3 all;
-    int at = block_before(make_int3(__popc(free_mask), 0, 0), all).x;
-    const int freed = all.x;
-    int32_t *list = a.freed + ((int64_t)g * a.tiles + tile) * kTileCols * K;
-    for (uint32_t m = free_mask; m; m &= m - 1) list[at++] = cells[(__ffs((int)m) - 1) * kTileCols + tid];
+    int freed = 0;
+    if (__syncthreads_or(free_mask != 0)) {
+        int3 all;
+        int at = block_before(make_int3(__popc(free_mask), 0, 0), all).x;
+        freed = all.x;
+        int32_t *list = a.freed + ((int64_t)g * a.tiles + tile) * kTileCols * K;
+        for (uint32_t m = free_mask; m; m &= m - 1) list[at++] = cells[(__ffs((int)m) - 1) * kTileCols + tid];
+    }
     if (tid == 0) {
         a.tile_copy[(int64_t)g * a.tiles + tile] = copied;
         a.tile_freed[(int64_t)g * a.tiles + tile] = freed;
@@ -633,19 +638,21 @@ constexpr int kPiece = 16384;  // bytes of a plane's block that a CTA copies at 
 
 // Freed block i of a group (i < 0: none), from the tiles' lists; a whole warp
 // calls it, each lane for its own i.
-__device__ __forceinline__ int32_t freed_block(const ReorderArgs &a, int g, int i)
+__device__ __noinline__ int32_t freed_block(const ReorderArgs &a, int g, int i)
 {
+    const int32_t *tiles = a.tile_freed + (int64_t)g * a.tiles;
     const int lane = threadIdx.x & 31;
     int32_t id = -1;
     for (int t0 = 0, before = 0; t0 < a.tiles; t0 += 32) {
-        const int n = t0 + lane < a.tiles ? a.tile_freed[(int64_t)g * a.tiles + t0 + lane] : 0;
+        const int n = t0 + lane < a.tiles ? tiles[t0 + lane] : 0;
         int inc = n;
-#pragma unroll
+#pragma unroll 1
         for (int o = 1; o < 32; o <<= 1) {
             const int x = __shfl_up_sync(kFull, inc, o);
             if (lane >= o) inc += x;
         }
         int tile = -1, at = 0;
+#pragma unroll 1
         for (int t = 0; t < min(32, a.tiles - t0); ++t) {
             const int end = before + __shfl_sync(kFull, inc, t), begin = end - __shfl_sync(kFull, n, t);
             if (i >= begin && i < end) { tile = t0 + t; at = i - begin; }
@@ -657,22 +664,27 @@ __device__ __forceinline__ int32_t freed_block(const ReorderArgs &a, int g, int 
     return id;
 }
 
-// The block that the copy of row k of group g goes to, by a whole warp; false
-// for the lanes without a copy or whose copy finds the ring run out.
-__device__ __forceinline__ bool copy_block(const ReorderArgs &a, int g, bool copies, int k, uint32_t mask, const int4 &plan, int64_t head,
-                                           int64_t tail, int32_t &to)
+// The block that copy i of group g (i < 0: none) goes to, by a whole warp;
+// false for the lanes without a copy or whose copy finds the ring run out.
+__device__ __forceinline__ bool copy_block(const ReorderArgs &a, const int4 &plan, int g, int i, int64_t head, int64_t tail, int32_t &to)
 {
-    const int i = copies ? __popc(mask & ((1u << k) - 1u)) : -1;
     to = freed_block(a, g, i < plan.z ? i : -1);
-    if (i < plan.z) return copies;
+    if (i < plan.z) return i >= 0;
     const int64_t at = (int64_t)plan.y + i - plan.z;
     if (at >= tail - head) return false;
     to = a.ring[((uint64_t)head + at) % (uint32_t)a.n_blocks];
     return true;
 }
 
+// A row of a group: its parent (-1: none, bad: not of the group) and the parent's length.
+struct RowFrom {
+    int parent;
+    bool bad;
+    uint32_t len;
+};
+
 // A group: its freed blocks back to the ring, its rows' lengths, last blocks and outputs.
-__device__ __forceinline__ void finish_group(const ReorderArgs &a, int g)
+__device__ __forceinline__ void finish_group(const ReorderArgs &a, int g, const RowFrom &from)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.group;
     const uint32_t n = (uint32_t)a.n_blocks, mask = a.group_copy[g];
@@ -699,20 +711,15 @@ __device__ __forceinline__ void finish_group(const ReorderArgs &a, int g)
     if (warp) return;
     const bool here = lane < K, copies = here && (mask >> lane & 1u);
     const int64_t row = (int64_t)g * K + lane;
-    bool bad = false;
-    const int p = here ? row_parent(a, g, lane, bad) : -1;
-    uint32_t status = bad ? WF_KV_PARENT : 0;
-    // The parents' lengths are read before any is written: to_len may be len.
-    uint32_t len = p >= 0 ? row_len(a, (int64_t)g * K + p) : 0;
+    uint32_t status = from.bad ? WF_KV_PARENT : 0, len = from.len;
+    const int32_t block = copies ? a.copy_from[row].x : -1;
     int32_t to = -1;
-    const bool found = copy_block(a, g, copies, lane, mask, plan, head, tail, to);  // (a whole warp's call)
-    __syncwarp();
+    const bool found = copy_block(a, plan, g, copies ? __popc(mask & ((1u << lane) - 1u)) : -1, head, tail, to);
     if (!here) return;
     int2 move = make_int2(-1, -1);
     if (found) {
         a.to_table[row * a.to_stride + row_blocks(a, len) - 1] = to;  // left to this kernel
-        const int32_t from = a.copy_from[row].x;
-        if ((uint32_t)from < n && (uint32_t)to < n) move = make_int2(from, to);
+        if ((uint32_t)block < n && (uint32_t)to < n) move = make_int2(block, to);
         else *a.err = 1;
     } else if (copies) {
         status |= WF_KV_BLOCKS;
@@ -732,39 +739,48 @@ __global__ void __launch_bounds__(kFinishThreads) reorder_finish_kernel(const __
                                                                         const __grid_constant__ wf_kv_cache c, int64_t block_bytes,
                                                                         int pieces)
 {
+    const int group = (int)blockIdx.x < a.groups ? (int)blockIdx.x : -1, lane = threadIdx.x & 31;
+    // What the first kernel does not write is read while it runs.  (All parents' lengths are, before any is written: to_len may be len.)
+    RowFrom from = {-1, false, 0};
+    if (group >= 0 && threadIdx.x < 32 && lane < a.group) {
+        from.parent = row_parent(a, group, lane, from.bad);
+        if (from.parent >= 0) from.len = row_len(a, (int64_t)group * a.group + from.parent);
+    }
+    __syncwarp();
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if ((int)blockIdx.x < a.groups) {
-        finish_group(a, (int)blockIdx.x);
+    if (group >= 0) {
+        finish_group(a, group, from);
         return;
     }
     const int64_t each = (int64_t)c.planes * pieces, items = *a.n_copies * each, ctas = (int)gridDim.x - a.groups;
     const int64_t run = (items + ctas - 1) / ctas, it0 = ((int)blockIdx.x - a.groups) * run, it1 = min(it0 + run, items);
     const int64_t head = a.ring_was[0], tail = a.ring_was[1];
-    int64_t copy = -1;
-    int32_t from = 0, to = 0;
+    int copy = -1;
+    int2 src = make_int2(0, 0);
+    int32_t to = 0;
     int64_t bytes = 0;
     for (int64_t it = it0; it < it1; ++it) {
-        if (it / each != copy) {
-            copy = it / each;
+        if ((int)(it / each) != copy) {
+            copy = (int)(it / each);
             const int row = a.copy_rows[copy], g = row / a.group;
-            const int2 src = a.copy_from[row];
-            const bool found = copy_block(a, g, true, row - g * a.group, a.group_copy[g], a.group_plan[g], head, tail, to);
-            from = src.x;
-            bytes = found && (uint32_t)from < (uint32_t)a.n_blocks && (uint32_t)to < (uint32_t)a.n_blocks ? src.y * c.token_bytes : 0;
+            const int4 plan = a.group_plan[g];
+            src = a.copy_from[row];
+            const bool found = copy_block(a, plan, g, copy - plan.w, head, tail, to);
+            bytes = found && (uint32_t)src.x < (uint32_t)a.n_blocks && (uint32_t)to < (uint32_t)a.n_blocks ? src.y * c.token_bytes : 0;
         }
         const int64_t rest = it - copy * each, plane = rest / pieces, first = (rest - plane * pieces) * kPiece;
         const int n = (int)((min(bytes, first + kPiece) - first) / (int64_t)sizeof(T));  // (no more than 0: nothing to copy)
         uint8_t *base = (uint8_t *)c.base + plane * c.plane_stride + first;
-        const T *src = (const T *)(base + from * block_bytes);
-        T *dst = (T *)(base + to * block_bytes);
+        const T *from_at = (const T *)(base + src.x * block_bytes);
+        T *to_at = (T *)(base + to * block_bytes);
         for (int i = threadIdx.x; i < n; i += 4 * kFinishThreads) {
             T v[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-                if (i + u * kFinishThreads < n) v[u] = src[i + u * kFinishThreads];
+                if (i + u * kFinishThreads < n) v[u] = from_at[i + u * kFinishThreads];
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-                if (i + u * kFinishThreads < n) dst[i + u * kFinishThreads] = v[u];
+                if (i + u * kFinishThreads < n) to_at[i + u * kFinishThreads] = v[u];
         }
     }
 }
