@@ -334,6 +334,57 @@ def test_select_repeats_and_scratch_is_left_clean():
         assert all(np.array_equal(u, v) for u, v in zip(a, b))
 
 
+@pytest.mark.parametrize("dtype,groups,beams,vocab,keep", [
+    ("bfloat16", 1, 32, 200_003, 64), ("float32", 2, 16, 65537, 32), ("float16", 1, 1, 1 << 24, 8), ("float32", 500, 1, 999, 3),
+    ("bfloat16", 700, 2, 513, 4), ("bfloat16", 5, 7, 30000, 17)])
+def test_select_over_few_and_many_units(dtype, groups, beams, vocab, keep):
+    """Searches cut into units of one line, of two, of many; more searches than the machine holds at once."""
+    wf = lib()
+    rng = np.random.default_rng(vocab)
+    logits = logits_of(rng, groups * beams, vocab, dtype)
+    score = dev((-rng.random(groups * beams) * 9).astype(np.float32))
+    check_select(logits, score, beams, keep, run_select(wf, logits, score, beams, keep))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("vocab", [700, 70001])
+def test_select_sums_that_leave_a_floats_range(dtype, vocab):
+    """Exponentials relative to a value at the start of a row's part that says little about the rest: masked, far
+    below it, far above it."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(17)
+    x = logits_of(rng, 8, vocab, dtype)
+    x[0] -= 200
+    x[1, :vocab // 2] = -math.inf
+    x[1] -= 95
+    x[2, :vocab // 3] -= 60
+    x[2, vocab // 2:] += 300
+    x[3, :64] = -math.inf
+    x[3, 64:] -= 93
+    x[4] = -20000.0 + x[4]
+    x[5, ::2] = torch.finfo(x.dtype).min
+    x[6] += 9000
+    x[7, vocab // 2:] = -math.inf
+    score = torch.zeros(8, device="cuda")
+    check_select(x, score, 2, 8, run_select(wf, x, score, 2, 8))
+
+
+def test_select_first_step_reads_the_live_beams_alone():
+    """One live beam of each search, the others empty with logits of NaN."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(2)
+    for groups, beams, vocab in ((3, 4, 500), (20, 8, 40_000)):
+        x = logits_of(rng, groups * beams, vocab, "bfloat16")
+        score = torch.full((groups * beams,), -math.inf, device="cuda")
+        score[beams // 2::beams] = -1.5
+        x[~(score > -math.inf)] = math.nan
+        out = run_select(wf, x, score, beams, 2 * beams)
+        check_select(x, score, beams, 2 * beams, out)
+        assert (host(out.parent) % beams == beams // 2).all()
+
+
 # ---------------------------------------------------------------------------
 # Reorder
 # ---------------------------------------------------------------------------
