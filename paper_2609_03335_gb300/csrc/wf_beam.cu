@@ -104,7 +104,7 @@ struct Shared {
             int2 aside_of[kCap];         // ... their beam and the token of their first element
         };
     };
-    int32_t pick[kPick];     // units that are read again, counted over the search
+    int32_t pick[kCap];      // units that reach the bound, counted over the search; at most kPick are read again
     float cut;               // the bound
     Key bound;
     uint32_t count, n_aside;
@@ -615,10 +615,42 @@ __device__ __forceinline__ void join(const SelectArgs &a, Shared &sm, int group)
     for (int i = tid; i < units; i += kThreads) {
         if (!(sm.unit[i] >= cut)) continue;
         const uint32_t at = atomicAdd(&sm.count, 1u);
-        if (at < kPick) sm.pick[at] = i;
+        if (at < kCap) sm.pick[at] = i;
     }
     __syncthreads();
     int picked = (int)sm.count;
+    if (picked > kPick && picked <= kCap) {
+        // A loose bound (the least of 64 classes, for more than 32): the n-th largest of these sums is the bound.
+        int mine[kCap / kThreads];
+        bool keep[kCap / kThreads];
+        float least = INFINITY;
+#pragma unroll
+        for (int u = 0; u < kCap / kThreads; ++u) {
+            const int j = tid + u * kThreads;
+            keep[u] = false;
+            if (j >= picked) continue;
+            mine[u] = sm.pick[j];
+            const float sum = sm.unit[mine[u]];
+            int ahead = 0;
+#pragma unroll 4
+            for (int i = 0; i < picked; ++i) ahead += sm.unit[sm.pick[i]] > sum;
+            keep[u] = ahead < n;  // (equal sums stay together)
+            if (keep[u]) least = fminf(least, sum);
+        }
+        __syncthreads();
+        if (tid == 0) sm.count = 0;
+        least = -warp_max(-least);
+        if (lane == 0) sm.sum[warp] = least;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) least = fminf(least, sm.sum[w]);
+#pragma unroll
+        for (int u = 0; u < kCap / kThreads; ++u)
+            if (keep[u]) sm.pick[atomicAdd(&sm.count, 1u)] = mine[u];
+        __syncthreads();
+        picked = (int)sm.count;
+        cut = least;
+    }
     if (picked > kPick) {  // many equal, or a loose bound for many: exactly the n best
         best_keys(sm, n, [&](auto f) {
             for (int i = tid; i < units; i += kThreads) {

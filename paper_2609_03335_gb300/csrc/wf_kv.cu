@@ -45,7 +45,7 @@ __device__ __forceinline__ bool last_arrival(uint32_t *ticket, uint32_t n)
 
 constexpr int kExtThreads = 512;
 constexpr int kTok = 2;         // consecutive tokens of a lane: its slots fill 16 bytes, so a warp's stores whole sectors
-constexpr int kRegRows = 4;     // rows of a thread that the sums keep in registers
+constexpr int kPer = 4;         // rows of a thread that are summed at once
 constexpr int kSmemRows = 16384; // rows whose sums every CTA makes and holds (12 bytes each)
 
 struct ExtendArgs {
@@ -84,110 +84,106 @@ __device__ __forceinline__ int2 row_needs(const ExtendArgs &a, int32_t len, int3
     return then <= (uint32_t)a.width ? make_int2(add, (int)(then - had)) : make_int2(-1, 0);
 }
 
-// The sums of every row, by one CTA; returns the step's tokens and blocks.
-// first: this CTA also writes the rows' outputs that no input may share.
-// A thread takes `per` consecutive rows: kPer of them in registers, or, for
-// kPer = 0, any number staged in s.
-template <int kPer>
-__device__ __forceinline__ void row_sums(const ExtendArgs &a, const RowSums &s, uint32_t avail, bool first, uint32_t &tokens,
-                                         uint32_t &blocks)
+// The sums of every row, by one CTA, kPer consecutive rows a thread at a time;
+// returns the step's tokens and blocks.  first: this CTA also writes the
+// rows' outputs; write_len: the new lengths too.
+__device__ __forceinline__ void row_sums(const ExtendArgs &a, const RowSums &s, uint32_t avail, bool first, bool write_len,
+                                         uint32_t &tokens, uint32_t &blocks)
 {
-    __shared__ uint2 warp_sum[kExtThreads / 32];
+    __shared__ uint2 warp_sum[2][kExtThreads / 32];
     __shared__ uint2 cut;  // tokens and blocks before the row that ends the line
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = kPer ? kPer : (a.rows + kExtThreads - 1) / kExtThreads;
-    const int r0 = min(tid * per, a.rows), r1 = min(r0 + per, a.rows);
-    int32_t len[kPer ? kPer : 1];
-    int2 need[kPer ? kPer : 1];
-    if (kPer) {
-        int32_t add[kPer ? kPer : 1];
+    int32_t next_len[kPer], next_add[kPer];
+    const auto load = [&](int r0) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            len[i] = r0 + i < r1 ? a.len[r0 + i] : 0;
-            add[i] = r0 + i < r1 ? a.add[r0 + i] : 0;
+            next_len[i] = r0 + i < a.rows ? a.len[r0 + i] : 0;
+            next_add[i] = r0 + i < a.rows ? a.add[r0 + i] : 0;
         }
+    };
+    load(tid * kPer);
+    uint2 carry = make_uint2(0, 0);  // asked for by the rows so far
+    bool over = false;
+    int turn = 0;
+    for (int lo = 0; lo < a.rows; lo += kPer * kExtThreads, turn ^= 1) {
+        const int r0 = lo + tid * kPer;
+        int32_t len[kPer];
+        int2 need[kPer];
+        uint2 sum = make_uint2(0, 0);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) need[i] = row_needs(a, len[i], add[i]);
-    } else {
-        for (int r = tid; r < a.rows; r += kExtThreads) {
-            const int32_t l = a.len[r];
-            const int2 n = row_needs(a, l, a.add[r]);
-            s.start[r] = n.x;
-            s.base[r] = n.y;
-            s.delta[r] = l;
+        for (int i = 0; i < kPer; ++i) {
+            len[i] = next_len[i];
+            need[i] = row_needs(a, len[i], next_add[i]);
+            sum.x = sat_add(sum.x, (uint32_t)max(need[i].x, 0));
+            sum.y = sat_add(sum.y, (uint32_t)need[i].y);
         }
-    }
-    if (tid == 0) cut = make_uint2(kSat, kSat);
-    if (!kPer) __syncthreads();
-    const auto needs = [&](int r) { return kPer ? need[r - r0] : make_int2(s.start[r], s.base[r]); };
-    uint2 sum = make_uint2(0, 0);
+        if (lo + kPer * kExtThreads < a.rows) load(r0 + kPer * kExtThreads);
+        uint2 inc = sum;
 #pragma unroll
-    for (int i = 0; i < (kPer ? kPer : 1); ++i)
-        for (int r = r0 + i; r < (kPer ? r0 + i + 1 : r1); ++r) {
-            const int2 n = kPer ? need[i] : needs(r);
-            sum.x = sat_add(sum.x, (uint32_t)max(n.x, 0));
-            sum.y = sat_add(sum.y, (uint32_t)n.y);
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(kFull, inc.x, o), y = __shfl_up_sync(kFull, inc.y, o);
+            if (lane >= o) { inc.x = sat_add(inc.x, x); inc.y = sat_add(inc.y, y); }
         }
-    uint2 inc = sum;
+        uint2 before;
+        before.x = __shfl_up_sync(kFull, inc.x, 1);
+        before.y = __shfl_up_sync(kFull, inc.y, 1);
+        if (lane == 0) before = make_uint2(0, 0);
+        if (lane == 31) warp_sum[turn][warp] = inc;
+        __syncthreads();
+        // The warps' sums, scanned by every warp for itself.
+        uint2 w = lane < kExtThreads / 32 ? warp_sum[turn][lane] : make_uint2(0, 0);
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t x = __shfl_up_sync(kFull, inc.x, o), y = __shfl_up_sync(kFull, inc.y, o);
-        if (lane >= o) { inc.x = sat_add(inc.x, x); inc.y = sat_add(inc.y, y); }
-    }
-    uint2 before;
-    before.x = __shfl_up_sync(kFull, inc.x, 1);
-    before.y = __shfl_up_sync(kFull, inc.y, 1);
-    if (lane == 0) before = make_uint2(0, 0);
-    if (lane == 31) warp_sum[warp] = inc;
-    __syncthreads();
-    // The warps' sums, scanned by every warp for itself.
-    uint2 w = lane < kExtThreads / 32 ? warp_sum[lane] : make_uint2(0, 0);
+        for (int o = 1; o < kExtThreads / 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(kFull, w.x, o), y = __shfl_up_sync(kFull, w.y, o);
+            if (lane >= o) { w.x = sat_add(w.x, x); w.y = sat_add(w.y, y); }
+        }
+        const uint2 here = make_uint2(__shfl_sync(kFull, w.x, kExtThreads / 32 - 1), __shfl_sync(kFull, w.y, kExtThreads / 32 - 1));
+        if (warp) {
+            before.x = sat_add(before.x, __shfl_sync(kFull, w.x, warp - 1));
+            before.y = sat_add(before.y, __shfl_sync(kFull, w.y, warp - 1));
+        }
+        before.x = sat_add(before.x, carry.x);
+        before.y = sat_add(before.y, carry.y);
+        carry.x = sat_add(carry.x, here.x);
+        carry.y = sat_add(carry.y, here.y);
+        // The line ends at the one row that is the first past a limit.
+        if (!over) {
+            tokens = carry.x;
+            blocks = carry.y;
+            if (carry.x > a.max_tokens || carry.y > avail) {
+                uint2 at = before;
 #pragma unroll
-    for (int o = 1; o < kExtThreads / 32; o <<= 1) {
-        const uint32_t x = __shfl_up_sync(kFull, w.x, o), y = __shfl_up_sync(kFull, w.y, o);
-        if (lane >= o) { w.x = sat_add(w.x, x); w.y = sat_add(w.y, y); }
-    }
-    const uint2 all = make_uint2(__shfl_sync(kFull, w.x, kExtThreads / 32 - 1), __shfl_sync(kFull, w.y, kExtThreads / 32 - 1));
-    if (warp) {
-        before.x = sat_add(before.x, __shfl_sync(kFull, w.x, warp - 1));
-        before.y = sat_add(before.y, __shfl_sync(kFull, w.y, warp - 1));
-    }
-    // The line ends at the one row that is the first past a limit.  If all fit there is none.
-    tokens = all.x;
-    blocks = all.y;
-    if (all.x > a.max_tokens || all.y > avail) {
+                for (int i = 0; i < kPer; ++i) {
+                    const uint2 next = make_uint2(sat_add(at.x, (uint32_t)max(need[i].x, 0)), sat_add(at.y, (uint32_t)need[i].y));
+                    if ((next.x > a.max_tokens || next.y > avail) && at.x <= a.max_tokens && at.y <= avail) cut = at;
+                    at = next;
+                }
+                __syncthreads();
+                tokens = cut.x;
+                blocks = cut.y;
+                over = true;
+            }
+        }
         uint2 at = before;
 #pragma unroll
-        for (int i = 0; i < (kPer ? kPer : 1); ++i)
-            for (int r = r0 + i; r < (kPer ? min(r0 + i + 1, r1) : r1); ++r) {
-                const int2 n = kPer ? need[i] : needs(r);
-                const uint2 next = make_uint2(sat_add(at.x, (uint32_t)max(n.x, 0)), sat_add(at.y, (uint32_t)n.y));
-                if ((next.x > a.max_tokens || next.y > avail) && at.x <= a.max_tokens && at.y <= avail) cut = at;
-                at = next;
-            }
-        __syncthreads();
-        tokens = cut.x;
-        blocks = cut.y;
-    }
-    uint2 at = before;
-#pragma unroll
-    for (int i = 0; i < (kPer ? kPer : 1); ++i)
-        for (int r = r0 + i; r < (kPer ? min(r0 + i + 1, r1) : r1); ++r) {
-            const int2 n = kPer ? need[i] : needs(r);
-            const int32_t l = kPer ? len[i] : s.delta[r];
-            const uint2 next = make_uint2(sat_add(at.x, (uint32_t)max(n.x, 0)), sat_add(at.y, (uint32_t)n.y));
+        for (int i = 0; i < kPer; ++i) {
+            const int r = r0 + i;
+            const uint2 next = make_uint2(sat_add(at.x, (uint32_t)max(need[i].x, 0)), sat_add(at.y, (uint32_t)need[i].y));
             const bool late_t = next.x > a.max_tokens, late_b = next.y > avail;
             const int32_t start = (int32_t)(late_t || late_b ? tokens : at.x);
-            s.start[r] = start;
-            s.delta[r] = l - start;
-            s.base[r] = (int32_t)(at.y - blocks_of((uint32_t)max(l, 0), a.bs, a.shift));
-            if (first) {
-                if (!a.in_place) a.out.len[r] = l + (late_t || late_b ? 0 : max(n.x, 0));
-                a.out.start[r] = start;
-                a.out.status[r] = n.x < 0 ? WF_KV_LONG : (late_b ? WF_KV_BLOCKS : 0u) | (late_t ? WF_KV_TOKENS : 0u);
+            if (r < a.rows) {
+                s.start[r] = start;
+                s.delta[r] = len[i] - start;
+                s.base[r] = (int32_t)(at.y - blocks_of((uint32_t)max(len[i], 0), a.bs, a.shift));
+                if (first) {
+                    if (write_len) a.out.len[r] = len[i] + (late_t || late_b ? 0 : max(need[i].x, 0));
+                    a.out.start[r] = start;
+                    a.out.status[r] = need[i].x < 0 ? WF_KV_LONG : (late_b ? WF_KV_BLOCKS : 0u) | (late_t ? WF_KV_TOKENS : 0u);
+                }
             }
             at = next;
         }
+    }
     if (tid == 0) {
         s.start[a.rows] = (int32_t)tokens;
         if (first) a.out.start[a.rows] = (int32_t)tokens;
@@ -349,7 +345,6 @@ __device__ __forceinline__ void write_tokens(const ExtendArgs &a, const RowSums 
     }
 }
 
-template <int kPer>
 __global__ void __launch_bounds__(kExtThreads) extend_kernel(const __grid_constant__ ExtendArgs a)
 {
     extern __shared__ int32_t rows_sm[];
@@ -357,7 +352,7 @@ __global__ void __launch_bounds__(kExtThreads) extend_kernel(const __grid_consta
     const int64_t head = a.ends[0], tail = a.ends[1];
     const uint32_t avail = (uint32_t)max(0ll, min((long long)(tail - head), (long long)a.n_blocks));
     uint32_t tokens, blocks;
-    row_sums<kPer>(a, s, avail, blockIdx.x == 0, tokens, blocks);
+    row_sums(a, s, avail, blockIdx.x == 0, !a.in_place, tokens, blocks);
     write_tokens(a, s, tokens, (uint32_t)((uint64_t)head % (uint32_t)a.n_blocks));
     if (!a.in_place) {
         if (blockIdx.x == 0 && threadIdx.x == 0) {
@@ -383,9 +378,7 @@ __global__ void __launch_bounds__(kExtThreads) extend_sums_kernel(const __grid_c
     const int64_t head = a.ends[0], tail = a.ends[1];
     const uint32_t avail = (uint32_t)max(0ll, min((long long)(tail - head), (long long)a.n_blocks));
     uint32_t tokens, blocks;
-    row_sums<0>(a, s, avail, true, tokens, blocks);
-    for (int r = threadIdx.x; r < a.rows; r += kExtThreads)
-        a.out.len[r] = s.start[r] + s.delta[r] + (s.start[r + 1] - s.start[r]);
+    row_sums(a, s, avail, true, true, tokens, blocks);  // (a row's length is read before it is written)
     if (threadIdx.x == 0) {
         sums[0] = (int32_t)tokens;
         sums[1] = (int32_t)((uint64_t)head % (uint32_t)a.n_blocks);
@@ -876,13 +869,11 @@ int wf_launch_extend(wf_decode *d, const wf_kv *kv, const int32_t *add, const wf
         return wf_cuda_check(cudaGetLastError(), "extend launch");
     }
     const size_t smem = 4 * (3 * (size_t)a.rows + 1);
-    if (a.rows <= kRegRows * kExtThreads) {
-        extend_kernel<kRegRows><<<grid, kExtThreads, smem, st>>>(a);
-    } else {
-        const int rc = wf_cuda_check(cudaFuncSetAttribute(extend_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem),
+    if (smem > 40 << 10) {
+        const int rc = wf_cuda_check(cudaFuncSetAttribute(extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem),
                                      "extend smem attribute");
         if (rc) return rc;
-        extend_kernel<0><<<grid, kExtThreads, smem, st>>>(a);
     }
+    extend_kernel<<<grid, kExtThreads, smem, st>>>(a);
     return wf_cuda_check(cudaGetLastError(), "extend launch");
 }
