@@ -630,7 +630,7 @@ typedef struct {
  *   score[k] + log softmax(logits[k])[v]
  * in 32-bit floating point, (x - max) - log(sum of exp(x - max)) added to the
  * score; best first.  Equal sums: the lower beam first, in a beam the larger
- * logit, then the lower token.  A logit of -inf or NaN is masked: no
+ * logit, then the lower token; beams with equal logits and scores have equal sums.  A logit of -inf or NaN is masked: no
  * candidate, no part of the sum; a row with a logit of +inf shares its
  * probability among those.  A row that is masked throughout, or whose score
  * is -inf or NaN, has no candidates.  Places without a candidate hold score

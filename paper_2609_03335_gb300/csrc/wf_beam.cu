@@ -90,6 +90,13 @@ __device__ __forceinline__ float warp_sorted(float v)
     return v;
 }
 
+// How a search's warps share its rows: each row is cut alike, so that equal rows
+// that lie alike in memory have equal sums to the last bit.  Part q of the j-th row is number j * of_row + q.
+struct Share {
+    int of_row;  // warps of a row (1: a warp may have several rows)
+    int units;   // units of a warp in a row
+};
+
 struct Shared {
     union {
         Key best[kWarps][32];  // the threads' best
@@ -110,7 +117,7 @@ struct Shared {
     uint32_t count, n_aside;
     uint32_t again;          // rows whose exponentials are summed again
     uint32_t live;           // the search's rows that have a score
-    int warp_units;
+    Share share;
     float score[kMaxGroup];
     float4 stat[kMaxGroup];  // a row's maximum, log Z and score
     float sum[kWarps];
@@ -290,9 +297,10 @@ struct SelectArgs {
     wf_beam_out out;
     int row_lines, unit_lines, row_units;
     int ctas;               // of a search
-    int warp_units;         // units of a warp; 0: as the search's live rows give
+    bool live_rows;         // the warps share the search's live rows, else all
     uint32_t unit_magic;    // i / row_units = (i * unit_magic) >> 32 for the units of a search
-    float4 *part;           // [groups][ctas * kWarps + beams] {reference, sum of exponentials, maximum}
+    int parts;              // places for parts of a search
+    float4 *part;           // [groups][parts] {reference, sum of exponentials, maximum}
     float *most;            // [rows][row_units] the units' maxima
     uint32_t *ticket;       // [groups]
 };
@@ -429,15 +437,11 @@ __device__ __forceinline__ void take_part(const SelectArgs &a, int row, int u0, 
 // The beam of a search's unit.
 __device__ __forceinline__ int unit_beam(const SelectArgs &a, int i) { return a.row_units == 1 ? i : (int)__umulhi((uint32_t)i, a.unit_magic); }
 
-// A search's warps share its rows one after the other, each warp_units units;
-// a warp's part of the j-th row is number (warp of the search) + j.
-struct Parts {
-    int first, count;
-};
-__device__ __forceinline__ Parts row_parts(const SelectArgs &a, int j, int warp_units)
+// How a search's warps share `rows` of its rows.
+__device__ __forceinline__ Share share_rows(const SelectArgs &a, int rows)
 {
-    const int first = (int)((uint32_t)(j * a.row_units) / (uint32_t)warp_units);
-    return {first + j, (int)((uint32_t)((j + 1) * a.row_units - 1) / (uint32_t)warp_units) - first + 1};
+    const int of_row = max(1, a.ctas * kWarps / max(rows, 1));
+    return {of_row, (a.row_units + of_row - 1) / of_row};
 }
 
 // The rows' maxima, log Z and scores, to sm.stat, and the units' maxima, to sm.unit.
@@ -447,16 +451,19 @@ __device__ __forceinline__ void row_stats(const SelectArgs &a, Shared &sm, int g
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.in.beams, V = a.in.vocab;
     if (tid == 0) { sm.again = 0; sm.count = 0; sm.n_aside = 0; }
     constexpr int kLoads = 4;  // parts that a lane loads at once
-    const float4 none = make_float4(0.0f, 0.0f, -INFINITY, 0.0f), *parts = a.part + (int64_t)group * (a.ctas * kWarps + K);
+    const float4 none = make_float4(0.0f, 0.0f, -INFINITY, 0.0f), *parts = a.part + (int64_t)group * a.parts;
+    const uint32_t live = sm.live;
+    const Share share = sm.share;
+    const int n_parts = (a.row_units + share.units - 1) / share.units;  // of a row
     const auto parts_of = [&](int k) {
-        const uint32_t live = sm.live;
-        return live >> k & 1u ? row_parts(a, a.warp_units ? k : __popc(live & ((1u << k) - 1u)), sm.warp_units) : Parts{0, 0};
+        const int j = a.live_rows ? __popc(live & ((1u << k) - 1u)) : k;
+        return live >> k & 1u ? make_int2(j * share.of_row, n_parts) : make_int2(0, 0);
     };
     // The first of them before the units' maxima, so that both are under way together.
-    Parts at = warp < K ? parts_of(warp) : Parts{0, 0};
+    int2 at = warp < K ? parts_of(warp) : make_int2(0, 0);  // {first, count}
     float4 q[kLoads];
 #pragma unroll
-    for (int u = 0; u < kLoads; ++u) q[u] = lane + 32 * u < at.count ? __ldcg(&parts[at.first + lane + 32 * u]) : none;
+    for (int u = 0; u < kLoads; ++u) q[u] = lane + 32 * u < at.y ? __ldcg(&parts[at.x + lane + 32 * u]) : none;
     const int units = K * a.row_units;
     const float *most = a.most + (int64_t)group * units;
 #pragma unroll 4
@@ -467,12 +474,12 @@ __device__ __forceinline__ void row_stats(const SelectArgs &a, Shared &sm, int g
         if (k != warp) {
             at = parts_of(k);
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u) q[u] = lane + 32 * u < at.count ? __ldcg(&parts[at.first + lane + 32 * u]) : none;
+            for (int u = 0; u < kLoads; ++u) q[u] = lane + 32 * u < at.y ? __ldcg(&parts[at.x + lane + 32 * u]) : none;
         }
         // Each lane's parts by their own maximum, then the lanes' by the row's.
         float m = -INFINITY, z = 0, doubt = -INFINITY;
 #pragma unroll 1
-        for (int p = lane; p < at.count; p += 32) {
+        for (int p = lane; p < at.y; p += 32) {
             const float4 now = q[0];
             if (now.z > m) {
                 z = m > -INFINITY ? z * exp2f((m - now.z) * kLog2e) : 0.0f;
@@ -483,7 +490,7 @@ __device__ __forceinline__ void row_stats(const SelectArgs &a, Shared &sm, int g
             else z += now.y * exp2f(fmaf(-m, kLog2e, now.x));
 #pragma unroll
             for (int u = 0; u + 1 < kLoads; ++u) q[u] = q[u + 1];
-            q[kLoads - 1] = p + 32 * kLoads < at.count ? __ldcg(&parts[at.first + p + 32 * kLoads]) : none;
+            q[kLoads - 1] = p + 32 * kLoads < at.y ? __ldcg(&parts[at.x + p + 32 * kLoads]) : none;
         }
         const float most_of = warp_max(m);
         if (m < most_of) z = m > -INFINITY ? z * exp2f((m - most_of) * kLog2e) : 0.0f;
@@ -497,9 +504,21 @@ __device__ __forceinline__ void row_stats(const SelectArgs &a, Shared &sm, int g
         }
     }
     __syncthreads();
-    // Rows with infinities, NaN or sums that left a float's range.
+    // Summed again, in the order of the tokens: rows with infinities, NaN or sums that left a float's range; and rows
+    // that may be equal to another (same score and maximum) if their sums are near each other but not the same, as where
+    // the rows' places in their 16 bytes differ.
+    uint32_t rows = sm.again;
+    {
+        const float4 stat = sm.stat[lane < K ? lane : 0];
+        const bool row = lane < K && stat.x > -INFINITY;
+        const uint64_t same = row ? (uint64_t)__float_as_uint(stat.z) << 32 | __float_as_uint(stat.x) : ~(uint64_t)lane;
+        const uint32_t like = __match_any_sync(kFull, (unsigned long long)same);
+        const float other = __shfl_sync(kFull, stat.y, __ffs((int)like) - 1);
+        const uint32_t off = __ballot_sync(kFull, row && stat.y != other && fabsf(stat.y - other) < 1e-3f);
+        rows |= __ballot_sync(kFull, row && (like & off));
+    }
 #pragma unroll 1
-    for (uint32_t rows = sm.again; rows; rows &= rows - 1) {
+    for (; rows; rows &= rows - 1) {
         const int k = __ffs((int)rows) - 1;
         int lead;
         const auto *base = row_base<kType>(a, group * K + k, lead);
@@ -779,25 +798,22 @@ __global__ void __launch_bounds__(kThreads, kPerSm) select_kernel(const __grid_c
     // With few units a warp the rows are shared out as they are, so that no load waits for the scores; with many, the
     // live ones are: a search's first step has one.
     uint32_t live = kFull;
-    int warp_units = a.warp_units, rows = K;
-    if (!warp_units) {
+    int rows = K;
+    if (a.live_rows) {
         live = __ballot_sync(kFull, live_score(score));
         rows = __popc(live);
-        warp_units = max(1, (rows * a.row_units + a.ctas * kWarps - 1) / (a.ctas * kWarps));
     }
-    float4 *parts = a.part + (int64_t)group * (a.ctas * kWarps + K);
-    int u = w * warp_units;
-    const int u_end = min(u + warp_units, rows * a.row_units);
-    while (u < u_end) {
-        const int j = unit_beam(a, u), row0 = j * a.row_units, stop = min(u_end, row0 + a.row_units);
-        const int k = a.warp_units ? j : (int)__fns(live, 0, j + 1);
-        take_part<kType, kUnit>(a, group * K + k, u - row0, stop - row0, &parts[w + j]);
-        u = stop;
+    const Share share = share_rows(a, rows);
+    float4 *parts = a.part + (int64_t)group * a.parts;
+    const int u0 = share.of_row > 1 ? w % share.of_row * share.units : 0, u1 = min(u0 + share.units, a.row_units);
+    for (int j = share.of_row > 1 ? w / share.of_row : w; j < rows && u0 < u1; j += a.ctas * kWarps) {
+        const int k = a.live_rows ? (int)__fns(live, 0, j + 1) : j;
+        take_part<kType, kUnit>(a, group * K + k, u0, u1, &parts[share.of_row > 1 ? w : j]);
     }
     if (warp == 0) {
         sm.score[lane] = score;
         live = __ballot_sync(kFull, live_score(score));
-        if (lane == 0) { sm.live = live; sm.warp_units = warp_units; }
+        if (lane == 0) { sm.live = live; sm.share = share; }
     }
     if (!last_arrival(sm, &a.ticket[group], (uint32_t)a.ctas)) return;
     join<kType, kUnit>(a, sm, group);
@@ -820,13 +836,16 @@ bool deal(SelectArgs &a, int es, int sms)
     int64_t unit = (lines + kUnits - 1) / kUnits;
     if (unit == 1 && lines >= kLong * ctas * kWarps) unit = 2;
     if (unit > 2) unit = (unit + kStep - 1) / kStep * kStep;
-    const int64_t row_units = (row_lines + unit - 1) / unit, units = K * row_units;
-    const int64_t warp_units = std::max<int64_t>(1, (units + ctas * kWarps - 1) / (ctas * kWarps));
+    const int64_t row_units = (row_lines + unit - 1) / unit;
+    // The warps that the rows, each cut alike, have a use for.
+    const int64_t of_row = std::max<int64_t>(1, ctas * kWarps / K), warp_units = (row_units + of_row - 1) / of_row;
+    if (of_row > 1) ctas = (K * ((row_units + warp_units - 1) / warp_units) + kWarps - 1) / kWarps;
     a.row_lines = (int)row_lines;
     a.unit_lines = (int)unit;
     a.row_units = (int)row_units;
-    a.ctas = (int)((units + warp_units * kWarps - 1) / (warp_units * kWarps));
-    a.warp_units = warp_units * unit >= kLong ? 0 : (int)warp_units;
+    a.ctas = (int)ctas;
+    a.parts = (int)std::max<int64_t>(ctas * kWarps, K);
+    a.live_rows = warp_units * unit >= kLong;
     // i * (2^32 / row_units, rounded up) is off by less than 1 / row_units for the units of a search, kUnits + kMaxGroup at most.
     a.unit_magic = (uint32_t)(((1ull << 32) + (uint64_t)row_units - 1) / (uint64_t)row_units);  // (row_units = 1: not used)
     return groups * a.ctas < INT32_MAX;
@@ -844,8 +863,9 @@ int launch(const SelectArgs &a, cudaStream_t st)
 
 }  // namespace
 
-// Scratch of any call of at most these sizes.  Parts: a search's warps and
-// one more a row; the searches' CTAs are at most twice what the machine holds, or one each.  Units: a row's share of kUnits and one for the rounding up, or its lines.
+// Scratch of any call of at most these sizes.  Parts: a search's warps, or its
+// rows; the searches' CTAs are at most twice what the machine holds, or one
+// each.  Units: a row's share of kUnits and one for the rounding up, or its lines.
 void wf_beam_scratch(int64_t rows, int64_t vocab, int sms, int64_t *parts, int64_t *units)
 {
     *parts = std::max<int64_t>(2 * (int64_t)sms * kPerSm, rows) * kWarps + rows;
@@ -861,7 +881,7 @@ int wf_launch_select(wf_decode *d, const wf_beam *in, const wf_beam_out *out, cu
     a.part = d->part;
     a.most = d->most;
     a.ticket = d->ticket + 1;
-    const int64_t parts = (int64_t)in->groups * ((int64_t)a.ctas * kWarps + in->beams);
+    const int64_t parts = (int64_t)in->groups * a.parts;
     const int64_t units = (int64_t)in->groups * in->beams * a.row_units;
     if (!ok || parts > d->parts || units > d->units)
         return wf_set_error(WF_EINVAL, "wf_beam_select: %lld parts and %lld units exceed the scratch", (long long)parts, (long long)units);

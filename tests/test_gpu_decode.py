@@ -301,6 +301,31 @@ def test_select_equal_values_go_to_the_first(dtype, keep):
             assert host(out.token)[0, 1] == 7 and host(out.parent)[0, 1] == 1
 
 
+@pytest.mark.parametrize("groups,beams,vocab,dtype", [(1, 3, 4097, "bfloat16"), (2, 5, 50257, "float16"), (30, 7, 9001, "float32"),
+                                                      (3, 32, 2000, "bfloat16"), (200, 6, 700, "bfloat16"), (9, 16, 40000, "bfloat16")])
+def test_select_equal_rows_have_equal_sums(groups, beams, vocab, dtype):
+    """Beams with the same logits and scores: to the last bit the same sums, so a logit's candidates go by beam, a
+    beam's by token."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(vocab)
+    x = logits_of(rng, groups, vocab, dtype).repeat_interleave(beams, 0).contiguous()
+    score = torch.full((groups * beams,), -3.7, device="cuda")
+    keep = min(64, 2 * beams)
+    out = run_select(wf, x, score, beams, keep)
+    parent, token, got = host(out.parent) % beams, host(out.token), host(out.score)
+    for g in range(groups):
+        row = host(x[g * beams].float())
+        want = []
+        for value in np.unique(row)[::-1]:
+            want += [(k, int(t)) for k in range(beams) for t in np.flatnonzero(row == value)]
+            if len(want) >= keep:
+                break
+        assert list(zip(parent[g].tolist(), token[g].tolist())) == want[:keep]
+        at = row[token[g]]
+        assert all(len(set(got[g][at == v].tolist())) == 1 for v in np.unique(at))
+
+
 def test_select_orders_that_defeat_the_bound():
     """Values whose large ones all lie with a few threads: more reach the bound than are gathered."""
     import torch
