@@ -299,6 +299,7 @@ struct SelectArgs {
     int ctas;               // of a search
     bool live_rows;         // the warps share the search's live rows, else all
     uint32_t unit_magic;    // i / row_units = (i * unit_magic) >> 32 for the units of a search
+    int most_of_row;        // warps of a row, at most: each has the lines that it loads at once
     int parts;              // places for parts of a search
     float4 *part;           // [groups][parts] {reference, sum of exponentials, maximum}
     float *most;            // [rows][row_units] the units' maxima
@@ -440,7 +441,7 @@ __device__ __forceinline__ int unit_beam(const SelectArgs &a, int i) { return a.
 // How a search's warps share `rows` of its rows.
 __device__ __forceinline__ Share share_rows(const SelectArgs &a, int rows)
 {
-    const int of_row = max(1, a.ctas * kWarps / max(rows, 1));
+    const int of_row = min(max(1, a.ctas * kWarps / max(rows, 1)), a.most_of_row);
     return {of_row, (a.row_units + of_row - 1) / of_row};
 }
 
@@ -509,13 +510,18 @@ __device__ __forceinline__ void row_stats(const SelectArgs &a, Shared &sm, int g
     // the rows' places in their 16 bytes differ.
     uint32_t rows = sm.again;
     {
+        // Each with every other, by rotation (a matching instruction takes longer for values that all differ).
         const float4 stat = sm.stat[lane < K ? lane : 0];
-        const bool row = lane < K && stat.x > -INFINITY;
-        const uint64_t same = row ? (uint64_t)__float_as_uint(stat.z) << 32 | __float_as_uint(stat.x) : ~(uint64_t)lane;
-        const uint32_t like = __match_any_sync(kFull, (unsigned long long)same);
-        const float other = __shfl_sync(kFull, stat.y, __ffs((int)like) - 1);
-        const uint32_t off = __ballot_sync(kFull, row && stat.y != other && fabsf(stat.y - other) < 1e-3f);
-        rows |= __ballot_sync(kFull, row && (like & off));
+        const uint32_t mark = __float_as_uint(stat.z) * 0x9E3779B1u ^ __float_as_uint(stat.x);
+        bool off = false;
+#pragma unroll 1
+        for (int d = 1; d < K; ++d) {
+            const int from = lane + d < K ? lane + d : lane + d - K;
+            const uint32_t its = __shfl_sync(kFull, mark, from);
+            const float z = __shfl_sync(kFull, stat.y, from);
+            off |= its == mark && z != stat.y && fabsf(z - stat.y) < 1e-3f;
+        }
+        rows |= __ballot_sync(kFull, off && lane < K && stat.x > -INFINITY);
     }
 #pragma unroll 1
     for (; rows; rows &= rows - 1) {
@@ -838,12 +844,14 @@ bool deal(SelectArgs &a, int es, int sms)
     if (unit > 2) unit = (unit + kStep - 1) / kStep * kStep;
     const int64_t row_units = (row_lines + unit - 1) / unit;
     // The warps that the rows, each cut alike, have a use for.
-    const int64_t of_row = std::max<int64_t>(1, ctas * kWarps / K), warp_units = (row_units + of_row - 1) / of_row;
-    if (of_row > 1) ctas = (K * ((row_units + warp_units - 1) / warp_units) + kWarps - 1) / kWarps;
+    const int64_t most_of_row = (row_lines + kStep - 1) / kStep;
+    const int64_t of_row = std::min(std::max<int64_t>(1, ctas * kWarps / K), most_of_row), warp_units = (row_units + of_row - 1) / of_row;
+    if (of_row == most_of_row || of_row > 1) ctas = std::min(ctas, (K * ((row_units + warp_units - 1) / warp_units) + kWarps - 1) / kWarps);
     a.row_lines = (int)row_lines;
     a.unit_lines = (int)unit;
     a.row_units = (int)row_units;
     a.ctas = (int)ctas;
+    a.most_of_row = (int)most_of_row;
     a.parts = (int)std::max<int64_t>(ctas * kWarps, K);
     a.live_rows = warp_units * unit >= kLong;
     // i * (2^32 / row_units, rounded up) is off by less than 1 / row_units for the units of a search, kUnits + kMaxGroup at most.
