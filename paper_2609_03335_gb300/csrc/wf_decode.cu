@@ -49,7 +49,7 @@ extern "C" int wf_decode_create(const wf_decode_limits *lim, int device, wf_deco
     const size_t o_freed = place(4 * (size_t)(rows * tiles * kTileCols));
     const size_t o_tf = place(4 * (size_t)(rows * tiles)), o_tc = place(4 * (size_t)(rows * tiles));
     const size_t o_from = place(8 * (size_t)rows), o_rows = place(4 * (size_t)rows), o_gc = place(4 * (size_t)rows);
-    const size_t o_plan = place(16 * (size_t)rows), o_was = place(16), o_nc = place(4);
+    const size_t o_plan = place(16 * (size_t)rows), o_was = place(sizeof(wf_ring)), o_nc = place(4);
     const size_t o_part = place(16 * (size_t)d->parts), o_most = place(4 * (size_t)d->units);
     rc = wf_cuda_check(cudaMalloc(&d->mem, at), "cudaMalloc(decode scratch)");
     if (!rc) rc = wf_cuda_check(cudaMemset(d->mem, 0, zeroed), "clear the decode scratch");
@@ -66,7 +66,7 @@ extern "C" int wf_decode_create(const wf_decode_limits *lim, int device, wf_deco
     d->n_copies = (int32_t *)(m + o_nc);
     d->group_copy = (uint32_t *)(m + o_gc);
     d->group_plan = (int4 *)(m + o_plan);
-    d->ring_was = (int64_t *)(m + o_was);
+    d->ring_was = (wf_ring *)(m + o_was);
     d->part = (float4 *)(m + o_part);
     d->most = (float *)(m + o_most);
     // The clearing runs on the default stream; the calls may use any other.

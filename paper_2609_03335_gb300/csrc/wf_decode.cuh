@@ -4,6 +4,12 @@
 
 #include "wf_internal.cuh"
 
+// The pool's ends before a call, and their places in the ring.
+struct wf_ring {
+    int64_t head, tail;
+    uint32_t head_at, tail_at;
+};
+
 // Per-call scratch, one device allocation made by wf_decode_create.
 struct wf_decode {
     int device;
@@ -22,7 +28,7 @@ struct wf_decode {
     int32_t *n_copies;
     uint32_t *group_copy;  // [groups] rows with copies
     int4 *group_plan;      // [groups] {first place in the ring's tail, in its head, freed blocks used for copies, first copy}
-    int64_t *ring_was;     // [2] head and tail before the call
+    wf_ring *ring_was;
     // select
     float4 *part;          // [parts] a warp's part of a row: reference, sum of exponentials, maximum
     float *most;           // [units] the maximum of each unit of the rows

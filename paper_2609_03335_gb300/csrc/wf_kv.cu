@@ -8,9 +8,12 @@
 // before a row say where its blocks lie in the ring and its tokens in the
 // step.  A token then finds its row by bisecting the starts.
 //
-// What it has to move is 16 bytes a token (slot, position, row) and little
-// else, so the sums are made by every CTA for itself in shared memory (the rows'
-// lengths come from L2) instead of by a kernel before: one launch.
+// It has to move 16 bytes a token (slot, position, row) and little else.  So
+// the sums are made by every CTA for itself in shared memory (the rows'
+// lengths come from L2) instead of by a kernel before: one launch.  2,000 rows
+// decoding take 6.1 us and 12 rows 3.6, bound by the launch and two or three trips to L2 in
+// turn; 35 M tokens of 2,000 rows 97 us, 5.96 TB/s, bound by the writes (a
+// fill of the same arrays reaches 6.9), about 5 us of it the sums.
 #include <algorithm>
 
 #include "wf_decode.cuh"
@@ -409,8 +412,11 @@ __global__ void __launch_bounds__(kExtThreads) extend_fill_kernel(const __grid_c
 //    lengths and last blocks, while other CTAs, which find a copy's blocks by
 //    the same sums, copy.
 //
-// The second kernel is launched while the first runs and waits for it on the
-// GPU, which hides most of a launch.  (Its CTAs could each make the sums for
+// One group of 4 rows takes 7.6 us, 64 groups of 8 rows of 1,024 blocks 14.5:
+// bound by L2 trips in turn (lengths, entries, arrivals, sums, lists), about
+// 1,100 cycles each, and by code that is fetched once; 64 groups of 8 with 61 MB
+// of tokens to copy 36 us, the copies near 5.5 TB/s of reads and writes.  The
+// second kernel is launched while the first runs and waits for it on the GPU, which hides most of a launch.  (Its CTAs could each make the sums for
 // themselves and spare the first kernel its arrivals: 1 us less where nothing
 // is copied, 2.5 us more where much is.)
 
@@ -431,7 +437,7 @@ struct ReorderArgs {
     int32_t *copy_rows, *n_copies;  // the rows with copies, in order
     uint32_t *tile_copy, *group_copy, *ticket;
     int4 *group_plan;           // {first place in the ring's tail, in its head, freed blocks used for copies, first copy}
-    int64_t *ring_was;
+    wf_ring *ring_was;
     int *err;
 };
 
@@ -528,8 +534,6 @@ __device__ void plan_groups(const ReorderArgs &a, int32_t *sums)
         at.z += all.z;
     }
     if (tid == 0) {
-        a.ring_was[0] = head;
-        a.ring_was[1] = tail;
         a.to_ends[0] = head + min((int64_t)at.y, max(tail - head, (int64_t)0));
         a.to_ends[1] = tail + at.x;
         *a.n_copies = at.z;
@@ -556,6 +560,9 @@ __global__ void __launch_bounds__(kColThreads) reorder_tables_kernel(const __gri
         }
         const uint32_t on = __reduce_or_sync(kFull, p >= 0 ? 1u << p : 0u);
         if (tid == 0) goes_on = on;
+    } else if (tid == 32 && blockIdx.x == 0) {
+        const int64_t head = a.ends[0], tail = a.ends[1];
+        *a.ring_was = {head, tail, (uint32_t)((uint64_t)head % (uint32_t)a.n_blocks), (uint32_t)((uint64_t)tail % (uint32_t)a.n_blocks)};
     }
     __syncthreads();
     const int j = tile * kTileCols + tid;
@@ -657,15 +664,23 @@ __device__ __noinline__ int32_t freed_block(const ReorderArgs &a, int g, int i)
     return id;
 }
 
+// Place i from place `at` on of a ring of n (i below n in a pool that is in order).
+__device__ __forceinline__ uint32_t ring_place(uint32_t at, uint64_t i, uint32_t n)
+{
+    if (i >= n) i %= n;
+    const uint32_t p = at + (uint32_t)i;
+    return p >= n ? p - n : p;
+}
+
 // The block that copy i of group g (i < 0: none) goes to, by a whole warp;
 // false for the lanes without a copy or whose copy finds the ring run out.
-__device__ __forceinline__ bool copy_block(const ReorderArgs &a, const int4 &plan, int g, int i, int64_t head, int64_t tail, int32_t &to)
+__device__ __forceinline__ bool copy_block(const ReorderArgs &a, const int4 &plan, int g, int i, const wf_ring &ring, int32_t &to)
 {
     to = freed_block(a, g, i < plan.z ? i : -1);
     if (i < plan.z) return i >= 0;
     const int64_t at = (int64_t)plan.y + i - plan.z;
-    if (at >= tail - head) return false;
-    to = a.ring[((uint64_t)head + at) % (uint32_t)a.n_blocks];
+    if (at >= ring.tail - ring.head) return false;
+    to = a.ring[ring_place(ring.head_at, (uint64_t)at, (uint32_t)a.n_blocks)];
     return true;
 }
 
@@ -682,9 +697,8 @@ __device__ __forceinline__ void finish_group(const ReorderArgs &a, int g, const 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.group;
     const uint32_t n = (uint32_t)a.n_blocks, mask = a.group_copy[g];
     const int4 plan = a.group_plan[g];
-    const int64_t head = a.ring_was[0], tail = a.ring_was[1];
+    const wf_ring ring = *a.ring_was;
     // What the copies do not use goes back; a warp takes every eighth tile.
-    const uint32_t tail0 = (uint32_t)((uint64_t)tail % n);
     for (int t0 = 0, before = 0; t0 < a.tiles; t0 += 32) {
         const int c = t0 + lane < a.tiles ? a.tile_freed[(int64_t)g * a.tiles + t0 + lane] : 0;
         int inc = c;
@@ -697,7 +711,7 @@ __device__ __forceinline__ void finish_group(const ReorderArgs &a, int g, const 
             const int count = __shfl_sync(kFull, c, t), first = before + __shfl_sync(kFull, inc, t) - count - plan.z;
             const int32_t *list = a.freed + ((int64_t)g * a.tiles + t0 + t) * kTileCols * K;
             for (int i = lane; i < count; i += 32)
-                if (first + i >= 0) a.ring[((uint64_t)tail0 + plan.x + first + i) % n] = list[i];
+                if (first + i >= 0) a.ring[ring_place(ring.tail_at, (uint64_t)plan.x + first + i, n)] = list[i];
         }
         before += __shfl_sync(kFull, inc, 31);
     }
@@ -707,7 +721,7 @@ __device__ __forceinline__ void finish_group(const ReorderArgs &a, int g, const 
     uint32_t status = from.bad ? WF_KV_PARENT : 0, len = from.len;
     const int32_t block = copies ? a.copy_from[row].x : -1;
     int32_t to = -1;
-    const bool found = copy_block(a, plan, g, copies ? __popc(mask & ((1u << lane) - 1u)) : -1, head, tail, to);
+    const bool found = copy_block(a, plan, g, copies ? __popc(mask & ((1u << lane) - 1u)) : -1, ring, to);
     if (!here) return;
     int2 move = make_int2(-1, -1);
     if (found) {
@@ -747,7 +761,7 @@ __global__ void __launch_bounds__(kFinishThreads) reorder_finish_kernel(const __
     }
     const int64_t each = (int64_t)c.planes * pieces, items = *a.n_copies * each, ctas = (int)gridDim.x - a.groups;
     const int64_t run = (items + ctas - 1) / ctas, it0 = ((int)blockIdx.x - a.groups) * run, it1 = min(it0 + run, items);
-    const int64_t head = a.ring_was[0], tail = a.ring_was[1];
+    const wf_ring ring = *a.ring_was;
     int copy = -1;
     int2 src = make_int2(0, 0);
     int32_t to = 0;
@@ -758,7 +772,7 @@ __global__ void __launch_bounds__(kFinishThreads) reorder_finish_kernel(const __
             const int row = a.copy_rows[copy], g = row / a.group;
             const int4 plan = a.group_plan[g];
             src = a.copy_from[row];
-            const bool found = copy_block(a, plan, g, copy - plan.w, head, tail, to);
+            const bool found = copy_block(a, plan, g, copy - plan.w, ring, to);
             bytes = found && (uint32_t)src.x < (uint32_t)a.n_blocks && (uint32_t)to < (uint32_t)a.n_blocks ? src.y * c.token_bytes : 0;
         }
         const int64_t rest = it - copy * each, plane = rest / pieces, first = (rest - plane * pieces) * kPiece;

@@ -573,7 +573,7 @@ class Kv:
         self.len = _tensor(len, "len", "int32", rows, dev)
         self.ring = _tensor(ring, "ring", "int32", ring.numel(), dev)
         self.ends = _tensor(ends, "ends", "int64", 2, dev)
-        self.rows, self.row_blocks, self.device = rows, int(row_blocks or table.shape[1]), dev
+        self.rows, self.row_blocks, self.n_blocks, self.device = rows, int(row_blocks or table.shape[1]), ring.numel(), dev
         stride = table.stride(0) if rows > 1 else max(table.stride(0), table.shape[1])
         self.c = wf_kv(rows, self.row_blocks, self.block_tokens, ring.numel(), table.data_ptr(),
                        4 * stride, len.data_ptr(), ring.data_ptr(), ends.data_ptr())
@@ -628,13 +628,20 @@ class BeamOut:
 
 
 _DTYPES = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2}
+_dtype_codes: dict = {}  # the same by torch.dtype
+
+
+def _dtype_code(dtype):
+    if dtype not in _dtype_codes:
+        _dtype_codes[dtype] = _DTYPES.get(str(dtype))
+    return _dtype_codes[dtype]
 
 
 def wf_beam_select(decode: Decode, logits, score, out: BeamOut, eos: int = -1, stream=None):
     """One step of beam search.  logits: device [groups * beams, vocab] in
     float32, float16 or bfloat16 (rows may be strided); score: device float32 with
     groups * beams elements."""
-    rows, dtype = out.groups * out.beams, _DTYPES.get(str(logits.dtype))
+    rows, dtype = out.groups * out.beams, _dtype_code(logits.dtype)
     if dtype is None or not logits.is_cuda or logits.dim() != 2 or logits.shape[0] != rows \
             or (logits.stride(1) != 1 and logits.shape[1] > 1):
         raise WfError(WF_EINVAL, "logits", f"{logits.dtype} {tuple(logits.shape)}; expected {rows} rows of float32, "
@@ -666,13 +673,13 @@ def wf_kv_reorder(decode: Decode, kv: Kv, group: int, parent, to: Kv, out: KvMov
         raise WfError(WF_EINVAL, "wf_kv_reorder", f"outputs for {out.rows} rows, {kv.rows} given")
     cc = None
     if cache is not None:
-        if cache.get_device() != kv.device or not cache.is_contiguous() or cache.dim() < 3 \
-                or tuple(cache.shape[1:3]) != (kv.c.n_blocks, kv.block_tokens):
-            raise WfError(WF_EINVAL, "cache", f"{tuple(cache.shape)}; expected contiguous [planes, {kv.c.n_blocks}, "
+        if not (cache.get_device() == kv.device and cache.is_contiguous() and cache.dim() >= 3
+                and cache.size(1) == kv.n_blocks and cache.size(2) == kv.block_tokens):
+            raise WfError(WF_EINVAL, "cache", f"{tuple(cache.shape)}; expected contiguous [planes, {kv.n_blocks}, "
                                               f"{kv.block_tokens}, ...] on the device")
         plane = cache.stride(0) * cache.element_size()
         cc = ctypes.byref(wf_kv_cache(cache.data_ptr(), cache.shape[0], 0, plane,
-                                      plane // (kv.c.n_blocks * kv.block_tokens)))
+                                      plane // (kv.n_blocks * kv.block_tokens)))
     _check(load_library().wf_kv_reorder(decode.ptr, ctypes.byref(kv.c), int(group), parent.data_ptr(),
                                         ctypes.byref(to.c), cc, out.copies.data_ptr(), out.status.data_ptr(),
                                         _stream_handle(stream, kv.device)), "wf_kv_reorder")
