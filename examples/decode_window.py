@@ -72,7 +72,8 @@ def decode(prob, device, batch, beams=4, steps=16, seed=0):
 
     scratch = wf.Decode(max_rows=rows, max_row_blocks=width, max_vocab=VOCAB, max_keep=2 * beams)
     kv = wf.Kv.empty(rows, width, BLOCK_TOKENS, n_blocks)
-    moves, found = wf.KvMoves(rows), wf.BeamOut(groups, beams, 2 * beams)
+    score = torch.full((rows,), -torch.inf, device="cuda")
+    moves, found = wf.KvMoves(rows), wf.BeamOut(groups, beams, 2 * beams, score)  # the scores move on in place
     heads = torch.arange(0, rows, beams, device="cuda")
 
     # The prompts, each in its search's first row.  A prompt that finds no blocks left waits: here it is left out.
@@ -89,7 +90,6 @@ def decode(prob, device, batch, beams=4, steps=16, seed=0):
     # The stand-in model: the sum of a row's cached vectors, kept as a running state.
     state = torch.zeros((rows, WIDTH), device="cuda")
     state.index_add_(0, prefill.row[used].long(), vectors[prefill.slot[used]])
-    score = torch.full((rows,), -torch.inf, device="cuda")
     score[heads] = torch.where(kv.len[heads] > 0, 0.0, -torch.inf)
     step = wf.KvStep(rows, rows, kv)
     parents, tokens = [], []
@@ -103,7 +103,6 @@ def decode(prob, device, batch, beams=4, steps=16, seed=0):
         live = step.row >= 0
         vectors[step.slot[live]] = embed[new[step.row[live].long()].long()]
         state = torch.where(alive[:, None], state[found.next_parent.view(-1).clamp(min=0).long()] + embed[new.clamp(min=0).long()], 0.0)
-        score = found.next_score.view(-1).clone()
         parents.append(found.next_parent.view(-1).clone())
         tokens.append(new)
     wf.wf_decode_status(scratch)

@@ -634,8 +634,9 @@ typedef struct {
  * candidate, no part of the sum; a row with a logit of +inf shares its
  * probability among those.  A row that is masked throughout, or whose score
  * is -inf or NaN, has no candidates.  Places without a candidate hold score
- * -inf, parent -1 and token -1.  No output may overlap an input.  The
- * result does not depend on the order of arrival of the GPU's blocks.
+ * -inf, parent -1 and token -1.  out->next_score may be in->score itself (the
+ * state then moves on); no other output may overlap an input.  The result does
+ * not depend on the order of arrival of the GPU's blocks.
  * Asynchronous on `stream`; no allocation.  WF_EINVAL as above.
  */
 int wf_beam_select(wf_decode *d, const wf_beam *in, const wf_beam_out *out, void *stream);

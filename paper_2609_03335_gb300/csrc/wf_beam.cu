@@ -20,15 +20,16 @@
 // keep-th largest.  The classes hold interleaved units, so few more than `keep`
 // reach it, unless many are equal (a mask of one low value); then the keys that
 // order equal sums by their place make the bound.
-// Measured: 64 searches of 8 beams over 131,072 bf16 tokens (134 MB) 32.7 us;
-// the last warp of step 1 ends at 22 us (6.1 TB/s, 70 warp instructions a
-// line at 25 % of the issue slots: bound by HBM), the join takes 7 us more, and the launch 2.
-// The join is bound by its chain: arrival, parts, units, the units read
-// again, each a trip to L2 or HBM of 1,100 to 1,900 cycles, and code that runs
+//
+// Measured: 64 searches of 8 beams over 131,072 bf16 tokens (134 MB) take 32.7
+// us; the last warp of step 1 ends at 22 us (6.1 TB/s; 68 warp instructions a
+// line, 40 % of the issue slots: bound by HBM), the join takes 7 us more, the
+// launch 2.  The join is bound by its chain (arrival, parts and units, the units
+// read again: trips to L2 or HBM of 1,100 to 1,900 cycles) and by code that runs
 // once a CTA, so what is not on its path stays out of line.  One search of 4
-// beams over 32,000 tokens, all join, takes 9.1 us.  Lists of candidates kept by each
-// CTA's part of a row, with a running bound, took 46 us for the large case: their sorting is 10 K
-// warp instructions a part, and its barriers leave the loads waiting.
+// beams over 32,000 tokens, all join, takes 9.1 us.  Lists of candidates that
+// each CTA's part of a row kept, with a running bound, took 46 us for the large
+// case: 10 K warp instructions a part, and barriers that leave the loads waiting.
 #include <algorithm>
 
 #include <cuda_bf16.h>
@@ -384,12 +385,13 @@ __device__ __forceinline__ void take_part(const SelectArgs &a, int row, int u0, 
     uint4 v[kStep], next[kStep];
     load(v, i0);
     // exp(x - ref) = 2^(x log2e - c), c = ref log2e rounded: one operation each; what the rounding shifts is known to
-    // the join.  Where the part starts with a mask, 0 is the reference.
+    // the join.  Where the part starts with a mask (-inf, or a value so low that the others would leave a float's
+    // range), 0 is the reference.
     float first = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kStep; ++u) first = fmaxf(first, E::most(v[u]));
     first = warp_max(first);
-    const float c = fabsf(first) < 1e4f ? first * kLog2e : 0.0f;
+    const float c = first > -80.0f && first < 1e4f ? first * kLog2e : 0.0f;
     float sum = 0, all = -INFINITY, unit = -INFINITY;
     int left = unit_lines;
     for (int i = i0; i < i1;) {

@@ -614,15 +614,20 @@ def wf_kv_extend(decode: Decode, kv: Kv, add, out: KvStep, stream=None):
 
 
 class BeamOut:
-    """wf_beam_select's outputs: score, parent, token [groups, keep] and next_* [groups, beams]."""
+    """wf_beam_select's outputs: score, parent, token [groups, keep] and next_* [groups, beams].
+    With `score` given (groups * beams float32), next_score is that tensor: the
+    scores then move on in place."""
 
-    def __init__(self, groups: int, beams: int, keep: int, device="cuda"):
+    def __init__(self, groups: int, beams: int, keep: int, score=None, device="cuda"):
         import torch
         mk = lambda n, dt: torch.empty((groups, n), dtype=dt, device=device)
         self.groups, self.beams, self.keep = int(groups), int(beams), int(keep)
         self.score, self.parent, self.token = mk(keep, torch.float32), mk(keep, torch.int32), mk(keep, torch.int32)
-        self.next_score, self.next_parent, self.next_token = (mk(beams, torch.float32), mk(beams, torch.int32),
-                                                              mk(beams, torch.int32))
+        self.next_score = mk(beams, torch.float32)
+        if score is not None:
+            _tensor(score, "score", "float32", groups * beams, self.score.get_device())
+            self.next_score = score.view(groups, beams)
+        self.next_parent, self.next_token = mk(beams, torch.int32), mk(beams, torch.int32)
         self.c = wf_beam_out(self.score.data_ptr(), self.parent.data_ptr(), self.token.data_ptr(),
                              self.next_score.data_ptr(), self.next_parent.data_ptr(), self.next_token.data_ptr())
 

@@ -341,6 +341,39 @@ def test_select_orders_that_defeat_the_bound():
             check_select(logits, score, 2, keep, run_select(wf, logits, score, 2, keep))
 
 
+@pytest.mark.parametrize("groups,beams,vocab", [(1, 3, 300), (40, 8, 30_000)])
+def test_select_scores_in_place(groups, beams, vocab):
+    """next_score may be the scores themselves, over steps."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(6)
+    d = wf.Decode(max_rows=groups * beams, max_vocab=vocab, max_keep=2 * beams)
+    score = dev((-rng.random(groups * beams)).astype(np.float32))
+    here, apart = wf.BeamOut(groups, beams, 2 * beams, score), wf.BeamOut(groups, beams, 2 * beams)
+    for _ in range(3):
+        x = logits_of(rng, groups * beams, vocab, "float32")
+        wf.wf_beam_select(d, x, score.clone(), apart)
+        wf.wf_beam_select(d, x, score, here)
+        for a, b in ((here.next_score.view(-1), apart.next_score.view(-1)), (here.token, apart.token), (here.next_parent, apart.next_parent)):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("mask", [-40.0, -100.0, -1000.0, -9999.0, -1e9])
+def test_select_masks_of_any_low_value(mask):
+    """Parts of rows that start with a mask of a finite value."""
+    wf = lib()
+    rng = np.random.default_rng(31)
+    for vocab in (3000, 60_000):
+        x = logits_of(rng, 6, vocab, "float32")
+        x[0, :vocab // 2] = mask
+        x[1, vocab // 7:] = mask
+        x[2, ::2] = mask
+        x[3] = mask
+        x[4, :vocab - 3] = mask
+        score = dev((-rng.random(6)).astype(np.float32))
+        check_select(x, score, 3, 6, run_select(wf, x, score, 3, 6))
+
+
 def test_select_repeats_and_scratch_is_left_clean():
     """Calls of different sizes in turn on one scratch, twice with the same result to the last bit."""
     import torch
