@@ -21,13 +21,13 @@
 // reach it, unless many are equal (a mask of one low value); then the keys that
 // order equal sums by their place make the bound.
 //
-// Measured: 64 searches of 8 beams over 131,072 bf16 tokens (134 MB) take 32.7
+// Measured: 64 searches of 8 beams over 131,072 bf16 tokens (134 MB) take 32.6
 // us; the last warp of step 1 ends at 22 us (6.1 TB/s; 68 warp instructions a
 // line, 40 % of the issue slots: bound by HBM), the join takes 7 us more, the
 // launch 2.  The join is bound by its chain (arrival, parts and units, the units
 // read again: trips to L2 or HBM of 1,100 to 1,900 cycles) and by code that runs
 // once a CTA, so what is not on its path stays out of line.  One search of 4
-// beams over 32,000 tokens, all join, takes 9.1 us.  Lists of candidates that
+// beams over 32,000 tokens, all join, takes 8.6 us.  Lists of candidates that
 // each CTA's part of a row kept, with a running bound, took 46 us for the large
 // case: 10 K warp instructions a part, and barriers that leave the loads waiting.
 #include <algorithm>
@@ -40,14 +40,18 @@
 namespace {
 
 constexpr uint32_t kFull = 0xFFFFFFFFu;
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 constexpr int kCap = 512;      // keys gathered before they are ranked
 constexpr int kStep = 4;       // lines that a warp has in flight, and as many in work
 constexpr int kSum = 64;       // steps whose exponentials are summed before that sum joins the warp's
 constexpr int kUnits = 4096;   // units of a search, but for one a row more
 constexpr int kPick = 128;     // units that the join reads again, at most, before it orders them by key
-constexpr int kPerSm = 3;      // CTAs an SM (80 registers; with 4 and 64, spills: 0.4 us more for one search, 0.7 for 16)
+
+// CTAs of 256 threads, three an SM (80 registers; with four and 64, spills:
+// 0.4 us more for one search, 0.7 for 16), which stream best; or, where the
+// join counts for more, of 512, one an SM.  deal() chooses.
+constexpr int kSmall = 256, kBig = 512;
+constexpr int per_sm(int threads) { return threads == kSmall ? 3 : 1; }
+
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Whole numbers in the order of the floats; -0 counts as 0.
@@ -107,7 +111,9 @@ struct Share {
     int units;   // units of a warp in a row
 };
 
+template <int kThreads>
 struct Shared {
+    static constexpr int kWarps = kThreads / 32;
     union {
         Key best[kWarps][32];  // the threads' best
         float most[kWarps][32];
@@ -136,7 +142,8 @@ struct Shared {
 
 // Each of the count keys in sm.got finds its place among them, four threads a
 // key; the n best go to sm.sorted.
-__device__ __noinline__ void rank_keys(Shared &sm, int count, int n)
+template <int kThreads>
+__device__ __noinline__ void rank_keys(Shared<kThreads> &sm, int count, int n)
 {
     const int tid = threadIdx.x;
     if (tid < n) sm.sorted[tid] = {0, 0};
@@ -155,9 +162,10 @@ __device__ __noinline__ void rank_keys(Shared &sm, int count, int n)
 
 // The n best of the CTA's keys, to sm.sorted: each(f) calls f with every key
 // of this thread, and can be called again.
-template <class Each>
-__device__ __noinline__ void best_keys(Shared &sm, int n, const Each &each)
+template <int kThreads, class Each>
+__device__ __noinline__ void best_keys(Shared<kThreads> &sm, int n, const Each &each)
 {
+    constexpr int kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     Key mine = {0, 0};
     each([&](const Key &k) { if (k > mine) mine = k; });
@@ -450,16 +458,19 @@ __device__ __forceinline__ void take_part(const SelectArgs &a, int row, int u0, 
 __device__ __forceinline__ int unit_beam(const SelectArgs &a, int i) { return a.row_units == 1 ? i : (int)__umulhi((uint32_t)i, a.unit_magic); }
 
 // How a search's warps share `rows` of its rows.
+template <int kThreads>
 __device__ __forceinline__ Share share_rows(const SelectArgs &a, int rows)
 {
+    constexpr int kWarps = kThreads / 32;
     const int of_row = min(max(1, a.ctas * kWarps / max(rows, 1)), a.most_of_row);
     return {of_row, (a.row_units + of_row - 1) / of_row};
 }
 
 // The rows' maxima, log Z and scores, to sm.stat, and the units' maxima, to sm.unit.
-template <int kType>
-__device__ __forceinline__ void row_stats(const SelectArgs &a, Shared &sm, int group)
+template <int kType, int kThreads>
+__device__ __forceinline__ void row_stats(const SelectArgs &a, Shared<kThreads> &sm, int group)
 {
+    constexpr int kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.in.beams, V = a.in.vocab;
     if (tid == 0) { sm.again = 0; sm.count = 0; sm.n_aside = 0; }
     constexpr int kLoads = 4;  // parts that a lane loads at once
@@ -565,7 +576,8 @@ __device__ __forceinline__ void row_stats(const SelectArgs &a, Shared &sm, int g
 __device__ __forceinline__ float sum_of(const float4 &stat, float x) { return stat.z + ((x == stat.x ? 0.0f : x - stat.x) - stat.y); }
 
 // Its key: {0, 0} if it is no candidate.
-__device__ __forceinline__ Key key_of(const Shared &sm, int k, float x, uint32_t place)
+template <int kThreads>
+__device__ __forceinline__ Key key_of(const Shared<kThreads> &sm, int k, float x, uint32_t place)
 {
     const float4 stat = sm.stat[k];
     const float sum = sum_of(stat, x);
@@ -575,9 +587,9 @@ __device__ __forceinline__ Key key_of(const Shared &sm, int k, float x, uint32_t
 
 // Item l of the picked units, kLines lines of one: the row's tokens, this
 // lane's first token, its beam, and how many of the lines there are.
-template <int kType, int kLines>
-__device__ __forceinline__ const typename Elems<kType>::type *picked_lines(const SelectArgs &a, const Shared &sm, int group, int l, int &k,
-                                                                           int &t0, int &lines)
+template <int kType, int kLines, int kThreads>
+__device__ __forceinline__ const typename Elems<kType>::type *picked_lines(const SelectArgs &a, const Shared<kThreads> &sm, int group, int l,
+                                                                           int &k, int &t0, int &lines)
 {
     const int items = kLines < kStep ? 1 : a.unit_lines / kStep, j = items == 1 ? l : l / items;
     const int unit = sm.pick[j];
@@ -599,10 +611,11 @@ __device__ __forceinline__ void load_if(bool ok, const void *from, uint4 &v)
 
 // Calls f(beam, logit, token) for this lane's share of the picked units; a
 // warp takes every kWarps-th of their items.
-template <int kType, int kLines, class F>
-__device__ __forceinline__ void each_token(const SelectArgs &a, const Shared &sm, int group, int items, const F &f)
+template <int kType, int kLines, int kThreads, class F>
+__device__ __forceinline__ void each_token(const SelectArgs &a, const Shared<kThreads> &sm, int group, int items, const F &f)
 {
     using E = Elems<kType>;
+    constexpr int kWarps = kThreads / 32;
     for (int l = (int)threadIdx.x >> 5; l < items; l += kWarps) {
         int k, t0, lines;
         const auto *base = picked_lines<kType, kLines>(a, sm, group, l, k, t0, lines);
@@ -615,10 +628,11 @@ __device__ __forceinline__ void each_token(const SelectArgs &a, const Shared &sm
     }
 }
 
-template <int kType, int kLines>
-__device__ __forceinline__ void join(const SelectArgs &a, Shared &sm, int group)
+template <int kType, int kLines, int kThreads>
+__device__ __forceinline__ void join(const SelectArgs &a, Shared<kThreads> &sm, int group)
 {
     using E = Elems<kType>;
+    constexpr int kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = a.in.keep, units = a.in.beams * a.row_units;
     const float *most = a.most + (int64_t)group * units;
     row_stats<kType>(a, sm, group);
@@ -702,7 +716,7 @@ __device__ __forceinline__ void join(const SelectArgs &a, Shared &sm, int group)
     __syncthreads();
     if (tid == 0) sm.count = 0;
     // Their vectors that reach the bound, kBatch lines of a warp at once; then those vectors' candidates; those in order.
-    constexpr int kBatch = 8, kItems = kBatch / kLines;
+    constexpr int kBatch = kThreads == kSmall ? 8 : 4, kItems = kBatch / kLines;
     const int items = picked * (kLines < kStep ? 1 : a.unit_lines / kStep);
     for (int l0 = warp; l0 < items; l0 += kItems * kWarps) {
         uint4 v[kBatch];
@@ -756,7 +770,8 @@ __device__ __forceinline__ void join(const SelectArgs &a, Shared &sm, int group)
 }
 
 // A search's outputs, from sm.sorted, by warp 0.
-__device__ void write_group(const SelectArgs &a, const Shared &sm, int group)
+template <int kThreads>
+__device__ void write_group(const SelectArgs &a, const Shared<kThreads> &sm, int group)
 {
     const int lane = threadIdx.x, n = a.in.keep, K = a.in.beams;
     const int64_t out = (int64_t)group * n, next = (int64_t)group * K;
@@ -792,7 +807,8 @@ __device__ void write_group(const SelectArgs &a, const Shared &sm, int group)
 // Arrival of one CTA; true for the last of n, which resets the count.  The
 // barrier hands what the CTA has written to the thread that makes it known
 // to the others.
-__device__ __forceinline__ bool last_arrival(Shared &sm, uint32_t *ticket, uint32_t n)
+template <int kThreads>
+__device__ __forceinline__ bool last_arrival(Shared<kThreads> &sm, uint32_t *ticket, uint32_t n)
 {
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -805,10 +821,11 @@ __device__ __forceinline__ bool last_arrival(Shared &sm, uint32_t *ticket, uint3
     return sm.last;
 }
 
-template <int kType, int kUnit>
-__global__ void __launch_bounds__(kThreads, kPerSm) select_kernel(const __grid_constant__ SelectArgs a)
+template <int kType, int kUnit, int kThreads>
+__global__ void __launch_bounds__(kThreads, per_sm(kThreads)) select_kernel(const __grid_constant__ SelectArgs a)
 {
-    __shared__ Shared sm;
+    constexpr int kWarps = kThreads / 32;
+    __shared__ Shared<kThreads> sm;
     const int lane = threadIdx.x & 31, warp = (int)threadIdx.x >> 5, K = a.in.beams;
     const int group = (int)blockIdx.x / a.ctas, w = ((int)blockIdx.x % a.ctas) * kWarps + warp;
     const float score = lane < K ? a.in.score[group * K + lane] : -INFINITY;
@@ -820,7 +837,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) select_kernel(const __grid_c
         live = __ballot_sync(kFull, live_score(score));
         rows = __popc(live);
     }
-    const Share share = share_rows(a, rows);
+    const Share share = share_rows<kThreads>(a, rows);
     float4 *parts = a.part + (int64_t)group * a.parts;
     const int u0 = share.of_row > 1 ? w % share.of_row * share.units : 0, u1 = min(u0 + share.units, a.row_units);
     for (int j = share.of_row > 1 ? w / share.of_row : w; j < rows && u0 < u1; j += a.ctas * kWarps) {
@@ -845,12 +862,23 @@ __global__ void __launch_bounds__(kThreads, kPerSm) select_kernel(const __grid_c
 // few, two where it has at least kLong (half the reductions), steps where a
 // search would have more than kUnits.
 constexpr int kLong = 8;
+// CTAs of 512 threads where every search has an SM and the logits are at most
+// kShort lines (33 MB): twice the warps for the join, half the parts to join.
+// us of 256 threads -> of 512: one search of 4 beams over 32,000 tokens 9.0 ->
+// 8.6, 16 of 4 over 50,257 12.1 -> 10.5, 16 of 12 over 60,000 17.7 -> 15.1, one
+// of 32 over 131,072 35.6 -> 25.3, 128 of 4 over 32,000 16.0 -> 15.2 (100 such
+// 14.1 -> 14.6).  With more logits the fewer bytes in flight weigh more: 64 of
+// 8 over 50,257 20.4 -> 20.2, 64 of 5 over 100,000 20.9 -> 22.4, 40 of 8 over
+// 131,072 24.5 -> 26.5, 64 of 8 32.5 -> 35.9.
+constexpr int64_t kShort = 65536;
 
-bool deal(SelectArgs &a, int es, int sms)
+bool deal(SelectArgs &a, int es, int sms, int &threads)
 {
-    const int64_t per = 16 / es, K = a.in.beams, groups = a.in.groups, most = (int64_t)sms * kPerSm;
+    const int64_t per = 16 / es, K = a.in.beams, groups = a.in.groups, rows = K * groups;
     const int64_t vectors = (a.in.vocab + 2 * (per - 1)) / per;  // a row may start inside a vector
     const int64_t row_lines = (vectors + 31) / 32, lines = K * row_lines;
+    threads = groups <= sms && rows * row_lines <= kShort ? kBig : kSmall;
+    const int64_t most = (int64_t)sms * per_sm(threads), kWarps = threads / 32;
     int64_t ctas = std::max<int64_t>(1, most / groups);
     int64_t unit = (lines + kUnits - 1) / kUnits;
     if (unit == 1 && lines >= kLong * ctas * kWarps) unit = 2;
@@ -872,23 +900,30 @@ bool deal(SelectArgs &a, int es, int sms)
     return groups * a.ctas < INT32_MAX;
 }
 
-template <int kType>
+template <int kType, int kThreads>
 int launch(const SelectArgs &a, cudaStream_t st)
 {
     const unsigned ctas = (unsigned)(a.in.groups * a.ctas);
-    if (a.unit_lines == 1) select_kernel<kType, 1><<<ctas, kThreads, 0, st>>>(a);
-    else if (a.unit_lines == 2) select_kernel<kType, 2><<<ctas, kThreads, 0, st>>>(a);
-    else select_kernel<kType, kStep><<<ctas, kThreads, 0, st>>>(a);
+    if (a.unit_lines == 1) select_kernel<kType, 1, kThreads><<<ctas, kThreads, 0, st>>>(a);
+    else if (a.unit_lines == 2) select_kernel<kType, 2, kThreads><<<ctas, kThreads, 0, st>>>(a);
+    else select_kernel<kType, kStep, kThreads><<<ctas, kThreads, 0, st>>>(a);
     return wf_cuda_check(cudaGetLastError(), "select launch");
+}
+
+template <int kType>
+int launch(const SelectArgs &a, int threads, cudaStream_t st)
+{
+    return threads == kSmall ? launch<kType, kSmall>(a, st) : launch<kType, kBig>(a, st);
 }
 
 }  // namespace
 
 // Scratch of any call of at most these sizes.  Parts: a search's warps, or its
-// rows; the searches' CTAs are at most what the machine holds, or one each.  Units: a row's share of kUnits and one for the rounding up, or its lines.
+// rows; the searches' CTAs are at most what the machine holds of either size, or
+// one each.  Units: a row's share of kUnits and one for the rounding up, or its lines.
 void wf_beam_scratch(int64_t rows, int64_t vocab, int sms, int64_t *parts, int64_t *units)
 {
-    *parts = std::max<int64_t>((int64_t)sms * kPerSm, rows) * kWarps + rows;
+    *parts = std::max({(int64_t)sms * per_sm(kSmall) * (kSmall / 32), rows * (kSmall / 32), (int64_t)sms * per_sm(kBig) * (kBig / 32)});
     *units = rows * std::min<int64_t>((vocab + 6) / 128 + 1, kUnits + 1);
 }
 
@@ -897,7 +932,8 @@ int wf_launch_select(wf_decode *d, const wf_beam *in, const wf_beam_out *out, cu
     SelectArgs a;
     a.in = *in;
     a.out = *out;
-    const bool ok = deal(a, in->dtype == WF_F32 ? 4 : 2, d->sms);
+    int threads;
+    const bool ok = deal(a, in->dtype == WF_F32 ? 4 : 2, d->sms, threads);
     a.part = d->part;
     a.most = d->most;
     a.ticket = d->ticket + 1;
@@ -905,7 +941,7 @@ int wf_launch_select(wf_decode *d, const wf_beam *in, const wf_beam_out *out, cu
     const int64_t units = (int64_t)in->groups * in->beams * a.row_units;
     if (!ok || parts > d->parts || units > d->units)
         return wf_set_error(WF_EINVAL, "wf_beam_select: %lld parts and %lld units exceed the scratch", (long long)parts, (long long)units);
-    if (in->dtype == WF_F32) return launch<WF_F32>(a, st);
-    if (in->dtype == WF_F16) return launch<WF_F16>(a, st);
-    return launch<WF_BF16>(a, st);
+    if (in->dtype == WF_F32) return launch<WF_F32>(a, threads, st);
+    if (in->dtype == WF_F16) return launch<WF_F16>(a, threads, st);
+    return launch<WF_BF16>(a, threads, st);
 }

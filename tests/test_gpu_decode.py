@@ -443,6 +443,61 @@ def test_select_first_step_reads_the_live_beams_alone():
         assert (host(out.parent) % beams == beams // 2).all()
 
 
+@pytest.mark.parametrize("groups,beams,vocab,keep,dtype", [
+    (160, 3, 1003, 6, "float16"), (160, 4, 8200, 8, "bfloat16"), (170, 2, 3001, 33, "float32"), (153, 1, 1, 2, "float32"),
+    (152, 2, 257, 3, "bfloat16"), (10, 32, 60_001, 64, "bfloat16"), (6, 32, 100_001, 40, "float32"), (65, 8, 70_000, 16, "float16"),
+    (64, 8, 65_520, 16, "bfloat16"), (63, 8, 65_520, 16, "bfloat16")])
+def test_select_on_both_sides_of_the_ctas_sizes(groups, beams, vocab, keep, dtype):
+    """More searches than SMs, or many logits, beside one less."""
+    wf = lib()
+    rng = np.random.default_rng(groups + vocab)
+    logits = logits_of(rng, groups * beams, vocab, dtype)
+    score = dev((-rng.random(groups * beams) * 9).astype(np.float32))
+    check_select(logits, score, beams, keep, run_select(wf, logits, score, beams, keep))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("vocab,offset", [(700, 0), (1003, 3), (4097, 1)])
+def test_select_of_many_searches_masks_infinities_and_order(dtype, vocab, offset):
+    """More searches than SMs: views that start anywhere, masks, infinities, NaN, parts far apart, equal values, values
+    whose large ones lie with a few threads."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(vocab)
+    t, groups, beams, keep = getattr(torch, dtype), 165, 2, 8
+    low = torch.finfo(t).min
+    wide = torch.full((groups * beams, vocab + 8), math.nan, dtype=t, device="cuda")
+    x = wide[:, offset:offset + vocab]
+    x.copy_(logits_of(rng, groups * beams, vocab, dtype))
+    score = dev((-rng.random(groups * beams) * 3).astype(np.float32))
+    some = torch.from_numpy(rng.random((beams, vocab)) < 0.99).cuda()
+    x[0:2][some] = -math.inf
+    x[2:4][some] = low
+    x[4:6] = -math.inf
+    x[6:8] = low
+    x[8, ::7] = math.nan
+    x[9] = math.nan
+    x[10, [3, 400]] = math.inf
+    x[12, :vocab // 2] = -1000.0
+    x[13, 5:] = -math.inf
+    x[14] -= 200
+    x[15, vocab // 2:] += 300
+    score[16] = -math.inf
+    score[17] = math.nan
+    score[18:20] = -math.inf
+    x[20:22, 1:] = -math.inf
+    x[22:24] = torch.arange(vocab, device="cuda").to(t) * 1e-3
+    x[24:26] = (-torch.arange(vocab, device="cuda") * 1e-3).to(t)
+    x[26:28] = torch.where((torch.arange(vocab, device="cuda") // 4) % 32 < 1, 6.0, -1.0).to(t)
+    check_select(x, score, beams, keep, run_select(wf, x, score, beams, keep))
+    # Equal rows, equal values: by beam, then by token.
+    x[:] = 1.5
+    score[:] = -2.0
+    out = run_select(wf, x, score, beams, keep)
+    assert (host(out.parent) == np.arange(groups)[:, None] * beams).all()
+    assert (host(out.token) == np.arange(keep)).all()
+
+
 # ---------------------------------------------------------------------------
 # Reorder
 # ---------------------------------------------------------------------------
