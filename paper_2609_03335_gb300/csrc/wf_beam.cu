@@ -21,7 +21,7 @@
 // reach it, unless many are equal (a mask of one low value); then the keys that
 // order equal sums by their place make the bound.
 //
-// Measured: 64 searches of 8 beams over 131,072 bf16 tokens (134 MB) take 32.6
+// Measured: 64 searches of 8 beams over 131,072 bf16 tokens (134 MB) take 32.1
 // us; the last warp of step 1 ends at 22 us (6.1 TB/s; 68 warp instructions a
 // line, 40 % of the issue slots: bound by HBM), the join takes 7 us more, the
 // launch 2.  The join is bound by its chain (arrival, parts and units, the units
@@ -43,7 +43,7 @@ constexpr uint32_t kFull = 0xFFFFFFFFu;
 constexpr int kCap = 512;      // keys gathered before they are ranked
 constexpr int kStep = 4;       // lines that a warp has in flight, and as many in work
 constexpr int kSum = 64;       // steps whose exponentials are summed before that sum joins the warp's
-constexpr int kUnits = 4096;   // units of a search, but for one a row more
+constexpr int kUnits = 4096 + kMaxGroup;  // units of a search, at most: shared memory holds their maxima
 constexpr int kPick = 128;     // units that the join reads again, at most, before it orders them by key
 
 // CTAs of 256 threads, three an SM (80 registers; with four and 64, spills:
@@ -121,7 +121,7 @@ struct Shared {
     Key got[kCap];           // gathered keys
     Key sorted[kMaxKeep];    // the best, in order; hi = 0 past the last
     union {
-        float unit[kUnits + kMaxGroup];  // the units' maxima, then their sums
+        float unit[kUnits];  // the units' maxima, then their sums
         struct {
             uint4 aside[kCap];           // vectors with a candidate that reaches the bound
             int2 aside_of[kCap];         // ... their beam and the token of their first element
@@ -314,13 +314,14 @@ struct SelectArgs {
     wf_beam in;
     wf_beam_out out;
     int row_lines, unit_lines, row_units;
+    int group_units;        // a search's units, and up to three more: a multiple of 16 bytes
     int ctas;               // of a search
     bool live_rows;         // the warps share the search's live rows, else all
     uint32_t unit_magic;    // i / row_units = (i * unit_magic) >> 32 for the units of a search
     int most_of_row;        // warps of a row, at most: each has the lines that it loads at once
     int parts;              // places for parts of a search
     float4 *part;           // [groups][parts] {reference, sum of exponentials, maximum}
-    float *most;            // [rows][row_units] the units' maxima
+    float *most;            // [groups][group_units] the units' maxima, a row's row_units side by side
     uint32_t *ticket;       // [groups]
 };
 
@@ -365,7 +366,7 @@ __device__ __forceinline__ float warp_max(float x)  // NaN passed over
 // exponentials.  kUnit: lines of a unit (1 or 2), or kStep for one or more
 // steps.
 template <int kType, int kUnit>
-__device__ __forceinline__ void take_part(const SelectArgs &a, int row, int u0, int u1, float4 *part)
+__device__ __forceinline__ void take_part(const SelectArgs &a, int row, int u0, int u1, float4 *part, float *most)
 {
     using E = Elems<kType>;
     constexpr int kLine = 32 * E::n;
@@ -389,7 +390,6 @@ __device__ __forceinline__ void take_part(const SelectArgs &a, int row, int u0, 
             }
         }
     };
-    float *most = a.most + (int64_t)row * a.row_units + u0;
     uint4 v[kStep], next[kStep];
     load(v, i0);
     // exp(x - ref) = 2^(x log2e - c), c = ref log2e rounded: one operation each; what the rounding shifts is known to
@@ -488,9 +488,10 @@ __device__ __forceinline__ void row_stats(const SelectArgs &a, Shared<kThreads> 
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) q[u] = lane + 32 * u < at.y ? __ldcg(&parts[at.x + lane + 32 * u]) : none;
     const int units = K * a.row_units;
-    const float *most = a.most + (int64_t)group * units;
-#pragma unroll 4
-    for (int i = tid; i < units; i += kThreads) sm.unit[i] = __ldcg(&most[i]);
+    const float *most = a.most + (int64_t)group * a.group_units;
+    for (int i = 4 * tid; i < units; i += 4 * kThreads)  // (all under way together: 0.2 to 0.5 us less than loads in fours)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(&sm.unit[i])), "l"(most + i) : "memory");
+    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
 #pragma unroll 1
     for (int k = warp; k < K; k += kWarps) {
@@ -634,7 +635,7 @@ __device__ __forceinline__ void join(const SelectArgs &a, Shared<kThreads> &sm, 
     using E = Elems<kType>;
     constexpr int kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = a.in.keep, units = a.in.beams * a.row_units;
-    const float *most = a.most + (int64_t)group * units;
+    const float *most = a.most + (int64_t)group * a.group_units;
     row_stats<kType>(a, sm, group);
     // The bound, and the units that reach it.
     float top = -INFINITY;
@@ -839,10 +840,11 @@ __global__ void __launch_bounds__(kThreads, per_sm(kThreads)) select_kernel(cons
     }
     const Share share = share_rows<kThreads>(a, rows);
     float4 *parts = a.part + (int64_t)group * a.parts;
+    float *most = a.most + (int64_t)group * a.group_units;
     const int u0 = share.of_row > 1 ? w % share.of_row * share.units : 0, u1 = min(u0 + share.units, a.row_units);
     for (int j = share.of_row > 1 ? w / share.of_row : w; j < rows && u0 < u1; j += a.ctas * kWarps) {
         const int k = a.live_rows ? (int)__fns(live, 0, j + 1) : j;
-        take_part<kType, kUnit>(a, group * K + k, u0, u1, &parts[share.of_row > 1 ? w : j]);
+        take_part<kType, kUnit>(a, group * K + k, u0, u1, &parts[share.of_row > 1 ? w : j], most + k * a.row_units + u0);
     }
     if (warp == 0) {
         sm.score[lane] = score;
@@ -858,10 +860,12 @@ __global__ void __launch_bounds__(kThreads, per_sm(kThreads)) select_kernel(cons
 // of two; no more in all than the machine holds at once (300 searches of 4
 // beams over 32,000 tokens take 23 us on 300 CTAs, 29 on 600).  Warps: as many
 // a row as that gives, rounded down (parts to be taken in two or three turns,
-// which would leave fewer warps idle, cost 0.3 to 1 us more).  Units: a line where a warp has
-// few, two where it has at least kLong (half the reductions), steps where a
-// search would have more than kUnits.
-constexpr int kLong = 8;
+// which would leave fewer warps idle, cost 0.3 to 1 us more).  Units: a line
+// where a warp has few; two where it has at least kLong and four from kLonger
+// on, for half and a quarter of the reductions (four for two: 400 searches of 4
+// over 32,000 26.8 -> 26.2 us, 64 of 5 over 100,000 20.7 -> 20.1, but 40 of 8
+// over 131,072 24.3 -> 24.7); more where a search would have more than kUnits.
+constexpr int kLong = 8, kLonger = 32;
 // CTAs of 512 threads where every search has an SM and the logits are at most
 // kShort lines (33 MB): twice the warps for the join, half the parts to join.
 // us of 256 threads -> of 512: one search of 4 beams over 32,000 tokens 9.0 ->
@@ -880,9 +884,10 @@ bool deal(SelectArgs &a, int es, int sms, int &threads)
     threads = groups <= sms && rows * row_lines <= kShort ? kBig : kSmall;
     const int64_t most = (int64_t)sms * per_sm(threads), kWarps = threads / 32;
     int64_t ctas = std::max<int64_t>(1, most / groups);
-    int64_t unit = (lines + kUnits - 1) / kUnits;
-    if (unit == 1 && lines >= kLong * ctas * kWarps) unit = 2;
+    const int64_t of_warp = lines / (ctas * kWarps);
+    int64_t unit = std::max<int64_t>(of_warp >= kLonger ? 4 : of_warp >= kLong ? 2 : 1, (lines + kUnits - 1) / kUnits);
     if (unit > 2) unit = (unit + kStep - 1) / kStep * kStep;
+    while (K * ((row_lines + unit - 1) / unit) > kUnits) unit = unit < kStep ? 2 * unit : unit + kStep;
     const int64_t row_units = (row_lines + unit - 1) / unit;
     // The warps that the rows, each cut alike, have a use for.
     const int64_t most_of_row = (row_lines + kStep - 1) / kStep;
@@ -891,11 +896,12 @@ bool deal(SelectArgs &a, int es, int sms, int &threads)
     a.row_lines = (int)row_lines;
     a.unit_lines = (int)unit;
     a.row_units = (int)row_units;
+    a.group_units = (int)((K * row_units + 3) / 4 * 4);
     a.ctas = (int)ctas;
     a.most_of_row = (int)most_of_row;
     a.parts = (int)std::max<int64_t>(ctas * kWarps, K);
     a.live_rows = warp_units * unit >= kLong;
-    // i * (2^32 / row_units, rounded up) is off by less than 1 / row_units for the units of a search, kUnits + kMaxGroup at most.
+    // i * (2^32 / row_units, rounded up) is off by less than 1 / row_units for the units of a search, kUnits at most.
     a.unit_magic = (uint32_t)(((1ull << 32) + (uint64_t)row_units - 1) / (uint64_t)row_units);  // (row_units = 1: not used)
     return groups * a.ctas < INT32_MAX;
 }
@@ -920,11 +926,11 @@ int launch(const SelectArgs &a, int threads, cudaStream_t st)
 
 // Scratch of any call of at most these sizes.  Parts: a search's warps, or its
 // rows; the searches' CTAs are at most what the machine holds of either size, or
-// one each.  Units: a row's share of kUnits and one for the rounding up, or its lines.
+// one each.  Units: a row's lines, or all that a search may have; up to three more a search.
 void wf_beam_scratch(int64_t rows, int64_t vocab, int sms, int64_t *parts, int64_t *units)
 {
     *parts = std::max({(int64_t)sms * per_sm(kSmall) * (kSmall / 32), rows * (kSmall / 32), (int64_t)sms * per_sm(kBig) * (kBig / 32)});
-    *units = rows * std::min<int64_t>((vocab + 6) / 128 + 1, kUnits + 1);
+    *units = rows * (std::min<int64_t>((vocab + 6) / 128 + 1, kUnits) + 3);
 }
 
 int wf_launch_select(wf_decode *d, const wf_beam *in, const wf_beam_out *out, cudaStream_t st)
@@ -938,7 +944,7 @@ int wf_launch_select(wf_decode *d, const wf_beam *in, const wf_beam_out *out, cu
     a.most = d->most;
     a.ticket = d->ticket + 1;
     const int64_t parts = (int64_t)in->groups * a.parts;
-    const int64_t units = (int64_t)in->groups * in->beams * a.row_units;
+    const int64_t units = (int64_t)in->groups * a.group_units;
     if (!ok || parts > d->parts || units > d->units)
         return wf_set_error(WF_EINVAL, "wf_beam_select: %lld parts and %lld units exceed the scratch", (long long)parts, (long long)units);
     if (in->dtype == WF_F32) return launch<WF_F32>(a, threads, st);
