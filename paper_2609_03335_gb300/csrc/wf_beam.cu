@@ -22,8 +22,8 @@
 // order equal sums by their place make the bound.
 //
 // Measured: 64 searches of 8 beams over 131,072 bf16 tokens (134 MB) take 32.1
-// us; the last warp of step 1 ends at 22 us (6.1 TB/s; 68 warp instructions a
-// line, 40 % of the issue slots: bound by HBM), the join takes 7 us more, the
+// us; the last warp of step 1 ends at 22 us (6.1 TB/s; 63 warp instructions a
+// line, 38 % of the issue slots: bound by HBM), the join takes 7 us more, the
 // launch 2.  The join is bound by its chain (arrival, parts and units, the units
 // read again: trips to L2 or HBM of 1,100 to 1,900 cycles) and by code that runs
 // once a CTA, so what is not on its path stays out of line.  One search of 4
