@@ -1,0 +1,83 @@
+"""Calls on a replica's rows: what one prepared input gives in both forms of the measured calls, and the edges of sizes,
+sums, devices and captures."""
+import ctypes
+import importlib.util
+import math
+import os
+import random
+import threading
+
+import numpy as np
+import pytest
+
+import decode_ref as ref
+from gpu_util import lib
+
+pytestmark = pytest.mark.gpu
+
+
+def dev(x):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(x)).cuda()
+
+
+def host(t):
+    return t.cpu().numpy()
+
+
+def equal(a, b):
+    return bool(((a == b) | ((a != a) & (b != b))).all())
+
+
+# ---------------------------------------------------------------------------
+# The measured calls on one input
+# ---------------------------------------------------------------------------
+
+@pytest.fixture(scope="module")
+def measured():
+    lib()
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    spec = importlib.util.spec_from_file_location("measured_operators", os.path.join(root, "perf", "operators.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    yield m
+    m.own = False
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_both_forms_agree_on_one_prepared_input(measured, seed):
+    """Drawn cases: the library's calls, three passes that nothing waits between, and the plain form on the same
+    tensors (two preparations of one seed need not be the same where likely tokens fall on one place).  Whole numbers
+    and copies are equal.  A selection's are those of the 64-bit form too, and its sums near that form's: the inputs keep
+    different sums at least 2^-8 / 17 apart, and 32-bit ones are off by less than 2^-16 there (values below 32:
+    three roundings of up to 2^-19; log Z by up to 100 * 2^-24)."""
+    import torch
+    m, rng = measured, random.Random(seed)
+    cases = [m.draw(rng) for _ in range(12)]
+    for case in cases:
+        m.own = True
+        s, other = m.prepare(case, seed + 50), m.prepare(case, seed + 90)
+        before = {k: v.clone() if torch.is_tensor(v) else v for k, v in s.items()}
+        m.run(s)
+        m.run(other)
+        got = {k: v.clone() for k, v in m.run(s).items()}
+        m.own = False
+        want = m.run(before)
+        for k, w in want.items():
+            if case["kind"] != "select" or not w.is_floating_point():
+                assert equal(got[k], w), (case, k, int((got[k] != w).sum()))
+        if case["kind"] != "select":
+            continue
+        prepared, m._prepare_select = m._prepare_select, lambda c, g: before
+        try:
+            exact = m.exact(case, 0)
+        finally:
+            m._prepare_select = prepared
+        for k, e in exact.items():
+            g = got[k].cpu().reshape(e.shape)
+            if not k.endswith("score"):
+                assert equal(g, e), (case, k)
+                continue
+            there = torch.isfinite(e)
+            assert equal(g.double()[~there], e[~there]), (case, k)
+            assert not there.any() or float((g.double() - e)[there].abs().max()) < 2.0 ** -16, (case, k)
