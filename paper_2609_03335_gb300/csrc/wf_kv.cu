@@ -776,7 +776,8 @@ __global__ void __launch_bounds__(kFinishThreads) reorder_finish_kernel(const __
             bytes = found && (uint32_t)src.x < (uint32_t)a.n_blocks && (uint32_t)to < (uint32_t)a.n_blocks ? src.y * c.token_bytes : 0;
         }
         const int64_t rest = it - copy * each, plane = rest / pieces, first = (rest - plane * pieces) * kPiece;
-        const int n = (int)((min(bytes, first + kPiece) - first) / (int64_t)sizeof(T));  // (no more than 0: nothing to copy)
+        // (A piece past the copied bytes has nothing to copy; in 64 bits, since a block may have more than 2^31 bytes.)
+        const int n = (int)(min(max(bytes - first, (int64_t)0), (int64_t)kPiece) / (int64_t)sizeof(T));
         uint8_t *base = (uint8_t *)c.base + plane * c.plane_stride + first;
         const T *from_at = (const T *)(base + src.x * block_bytes);
         T *to_at = (T *)(base + to * block_bytes);

@@ -81,3 +81,27 @@ def test_both_forms_agree_on_one_prepared_input(measured, seed):
             there = torch.isfinite(e)
             assert equal(g.double()[~there], e[~there]), (case, k)
             assert not there.any() or float((g.double() - e)[there].abs().max()) < 2.0 ** -16, (case, k)
+
+
+# ---------------------------------------------------------------------------
+# Reorder: sizes of blocks, places of the cache
+# ---------------------------------------------------------------------------
+
+def test_reorder_copies_a_few_tokens_of_blocks_beyond_2_gib():
+    """What lies past a copy's last byte is further than 31 bits from it, at one byte an access."""
+    import torch
+    wf = lib()
+    bs, token, n = 70_001, 32_769, 3  # 2.29e9 bytes a block, on no 4-byte boundary
+    assert bs * token > 2 ** 31 + 5 * token
+    cache = torch.zeros((1, n, bs, token), dtype=torch.uint8, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    cache[0, 2, :7] = torch.randint(1, 256, (7, token), generator=gen, device="cuda", dtype=torch.uint8)
+    d = wf.Decode(max_rows=2, max_row_blocks=1)
+    kv = wf.Kv(dev(np.array([[2], [-1]], np.int32)), dev(np.array([5, 0], np.int32)), dev(np.array([1, 0, -1], np.int32)),
+               dev(np.array([0, 2])), bs)
+    out = wf.KvMoves(2)
+    wf.wf_kv_reorder(d, kv, 2, dev(np.array([0, 0], np.int32)), kv, out, cache=cache)
+    wf.wf_decode_status(d)
+    assert host(out.copies).tolist() == [[-1, -1], [2, 1]] and host(kv.len).tolist() == [5, 5]
+    assert torch.equal(cache[0, 1, :5], cache[0, 2, :5])
+    assert not cache[0, 1, 5:].any() and not cache[0, 0].any() and not cache[0, 2, 7:].any()
