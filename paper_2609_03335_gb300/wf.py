@@ -529,6 +529,11 @@ def _tensor(t, name: str, dtype: str, n: int, device: int):
     return t
 
 
+def _apart(where: str, *objects):
+    """The refusal of objects that a call hands over together and that are not all on one device."""
+    return WfError(WF_EINVAL, where, "on different devices: " + ", ".join(f"{type(o).__name__} {o.device}" for o in objects))
+
+
 class Decode:
     """Owns a wf_decode: the scratch of the calls below, for calls of up to these sizes."""
 
@@ -552,7 +557,7 @@ class Decode:
 
 
 def wf_decode_status(decode: Decode, stream=None):
-    _check(load_library().wf_decode_status(decode.ptr, _stream_handle(stream)), "wf_decode_status")
+    _check(load_library().wf_decode_status(decode.ptr, _stream_handle(stream, decode.device)), "wf_decode_status")
 
 
 class Kv:
@@ -566,6 +571,8 @@ class Kv:
         if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.dtype != torch.int32 \
                 or table.device.type != "cuda" or table.stride(1) != 1:
             raise WfError(WF_EINVAL, "table", "is not a device int32 tensor [rows, blocks] with contiguous rows")
+        if not isinstance(ring, torch.Tensor):
+            raise WfError(WF_EINVAL, "ring", f"is {type(ring).__name__}; expected a device int32 tensor")
         rows, dev = table.shape[0], table.device.index
         if row_blocks is not None and not 1 <= row_blocks <= table.shape[1]:
             raise WfError(WF_EINVAL, "row_blocks", f"{row_blocks} of a table {table.shape[1]} wide")
@@ -598,6 +605,12 @@ class KvStep:
         self.max_tokens, self.rows = int(max_tokens), int(rows)
         self.slot, self.pos, self.row = mk(max_tokens, torch.int64), mk(max_tokens, torch.int32), mk(max_tokens, torch.int32)
         self.start, self.status = mk(rows + 1, torch.int32), mk(rows, torch.int32)
+        self.device = self.slot.get_device()
+        if kv:
+            if kv.device != self.device:
+                raise _apart("KvStep", self, kv)
+            if kv.rows != self.rows:
+                raise WfError(WF_EINVAL, "KvStep", f"outputs for {rows} rows, {kv.rows} given")
         self.len = kv.len if kv else mk(rows, torch.int32)
         self.ends = kv.ends if kv else mk(2, torch.int64)
         self.c = wf_kv_step(self.max_tokens, self.slot.data_ptr(), self.pos.data_ptr(), self.row.data_ptr(),
@@ -608,6 +621,8 @@ def wf_kv_extend(decode: Decode, kv: Kv, add, out: KvStep, stream=None):
     """A step's tokens: block tables and slots.  add: device int32 [rows]."""
     if out.rows != kv.rows:
         raise WfError(WF_EINVAL, "wf_kv_extend", f"outputs for {out.rows} rows, {kv.rows} given")
+    if not kv.device == decode.device == out.device:
+        raise _apart("wf_kv_extend", kv, decode, out)
     _tensor(add, "add", "int32", kv.rows, kv.device)
     _check(load_library().wf_kv_extend(decode.ptr, ctypes.byref(kv.c), add.data_ptr(), ctypes.byref(out.c),
                                        _stream_handle(stream, kv.device)), "wf_kv_extend")
@@ -624,8 +639,9 @@ class BeamOut:
         self.groups, self.beams, self.keep = int(groups), int(beams), int(keep)
         self.score, self.parent, self.token = mk(keep, torch.float32), mk(keep, torch.int32), mk(keep, torch.int32)
         self.next_score = mk(beams, torch.float32)
+        self.device = self.score.get_device()
         if score is not None:
-            _tensor(score, "score", "float32", groups * beams, self.score.get_device())
+            _tensor(score, "score", "float32", groups * beams, self.device)
             self.next_score = score.view(groups, beams)
         self.next_parent, self.next_token = mk(beams, torch.int32), mk(beams, torch.int32)
         self.c = wf_beam_out(self.score.data_ptr(), self.parent.data_ptr(), self.token.data_ptr(),
@@ -646,12 +662,15 @@ def wf_beam_select(decode: Decode, logits, score, out: BeamOut, eos: int = -1, s
     """One step of beam search.  logits: device [groups * beams, vocab] in
     float32, float16 or bfloat16 (rows may be strided); score: device float32 with
     groups * beams elements."""
-    rows, dtype = out.groups * out.beams, _dtype_code(logits.dtype)
+    rows, dtype = out.groups * out.beams, _dtype_code(getattr(logits, "dtype", None))
     if dtype is None or not logits.is_cuda or logits.dim() != 2 or logits.shape[0] != rows \
             or (logits.stride(1) != 1 and logits.shape[1] > 1):
-        raise WfError(WF_EINVAL, "logits", f"{logits.dtype} {tuple(logits.shape)}; expected {rows} rows of float32, "
+        what = f"{logits.dtype} {tuple(logits.shape)}" if hasattr(logits, "shape") else type(logits).__name__
+        raise WfError(WF_EINVAL, "logits", f"{what}; expected {rows} rows of float32, "
                                            "float16 or bfloat16 with contiguous elements on the device")
     device = logits.get_device()
+    if not device == decode.device == out.device:
+        raise _apart("wf_beam_select", logits, decode, out)
     _tensor(score, "score", "float32", rows, device)
     c = wf_beam(out.groups, out.beams, logits.shape[1], out.keep, dtype, eos, logits.data_ptr(),
                 logits.stride(0) * logits.element_size(), score.data_ptr())
@@ -667,17 +686,22 @@ class KvMoves:
         self.rows = int(rows)
         self.copies = torch.empty((rows, 2), dtype=torch.int32, device=device)
         self.status = torch.empty(rows, dtype=torch.int32, device=device)
+        self.device = self.status.get_device()
 
 
 def wf_kv_reorder(decode: Decode, kv: Kv, group: int, parent, to: Kv, out: KvMoves, cache=None, stream=None):
     """The rows in the order of a selection.  parent: device int32 with a row
     (or -1) for each row; to: the rows afterwards (kv itself, or another Kv on the same ring);
     cache: a contiguous device tensor [planes, n_blocks, block_tokens, ...] or None."""
+    if not kv.device == decode.device == to.device == out.device:
+        raise _apart("wf_kv_reorder", kv, decode, to, out)
     _tensor(parent, "parent", "int32", kv.rows, kv.device)
     if out.rows != kv.rows:
         raise WfError(WF_EINVAL, "wf_kv_reorder", f"outputs for {out.rows} rows, {kv.rows} given")
     cc = None
     if cache is not None:
+        if not hasattr(cache, "get_device"):
+            raise WfError(WF_EINVAL, "cache", f"is {type(cache).__name__}; expected a device tensor")
         if not (cache.get_device() == kv.device and cache.is_contiguous() and cache.dim() >= 3
                 and cache.size(1) == kv.n_blocks and cache.size(2) == kv.block_tokens):
             raise WfError(WF_EINVAL, "cache", f"{tuple(cache.shape)}; expected contiguous [planes, {kv.n_blocks}, "

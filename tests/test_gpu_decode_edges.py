@@ -105,3 +105,45 @@ def test_reorder_copies_a_few_tokens_of_blocks_beyond_2_gib():
     assert host(out.copies).tolist() == [[-1, -1], [2, 1]] and host(kv.len).tolist() == [5, 5]
     assert torch.equal(cache[0, 1, :5], cache[0, 2, :5])
     assert not cache[0, 1, 5:].any() and not cache[0, 0].any() and not cache[0, 2, 7:].any()
+
+
+# ---------------------------------------------------------------------------
+# Refusals of the binding
+# ---------------------------------------------------------------------------
+
+def test_binding_refuses_outputs_and_scratch_of_another_device_or_size():
+    """Nothing is launched for any of these: what the library would get are pointers of other memory."""
+    import torch
+    wf = lib()
+    d = wf.Decode(max_rows=8, max_row_blocks=4, max_vocab=100, max_keep=8)
+    kv, small = wf.Kv.empty(8, 4, 16, 40), wf.Kv.empty(4, 4, 16, 40)
+    step, moves, out = wf.KvStep(8, 16), wf.KvMoves(8), wf.BeamOut(2, 4, 8)
+    add = torch.ones(8, dtype=torch.int32, device="cuda")
+    parent = torch.full((8,), -1, dtype=torch.int32, device="cuda")
+    logits, score = torch.zeros((8, 100), device="cuda"), torch.zeros(8, device="cuda")
+    elsewhere = wf.Decode(max_rows=8, max_row_blocks=4, max_vocab=100, max_keep=8)
+    elsewhere.device = 1  # as if made there
+    far = wf.Kv.empty(8, 4, 16, 40)
+    far.device = 1
+    for call in (lambda: wf.KvStep(8, 16, small),
+                 lambda: wf.KvStep(8, 16, kv, device="cpu"),
+                 lambda: wf.wf_kv_extend(d, kv, add, wf.KvStep(8, 16, device="cpu")),
+                 lambda: wf.wf_kv_extend(elsewhere, kv, add, step),
+                 lambda: wf.wf_beam_select(elsewhere, logits, score, out),
+                 lambda: wf.wf_beam_select(d, logits, score, wf.BeamOut(2, 4, 8, device="cpu")),
+                 lambda: wf.wf_beam_select(d, logits.cpu().numpy(), score, out),
+                 lambda: wf.wf_kv_reorder(elsewhere, kv, 4, parent, kv, moves),
+                 lambda: wf.wf_kv_reorder(d, kv, 4, parent, far, moves),
+                 lambda: wf.wf_kv_reorder(d, kv, 4, parent, kv, wf.KvMoves(8, device="cpu")),
+                 lambda: wf.wf_kv_reorder(d, kv, 4, parent, kv, moves, cache=np.zeros((1, 40, 16, 4), np.uint8)),
+                 lambda: wf.wf_kv_reorder(d, kv, 4, parent, kv, moves, cache=torch.zeros((1, 40, 16, 4))),
+                 lambda: wf.Kv(kv.table, kv.len, host(kv.ring), kv.ends, 16)):
+        with pytest.raises(wf.WfError) as e:
+            call()
+        assert e.value.code == wf.WF_EINVAL
+    # What fits goes through as before.
+    wf.wf_kv_extend(d, kv, add, wf.KvStep(8, 16, kv))
+    wf.wf_beam_select(d, logits, score, out)
+    wf.wf_kv_reorder(d, kv, 4, parent, kv, moves)
+    wf.wf_decode_status(d)
+    assert int(kv.ends[1] - kv.ends[0]) == 40
