@@ -562,7 +562,7 @@ typedef struct {
 
 /* Status bits of a row (wf_kv_step.status, wf_kv_reorder). */
 enum {
-    WF_KV_LONG = 1u,     /* a negative length or more tokens than a table row holds: the row is left out */
+    WF_KV_LONG = 1u,     /* a negative length, or more tokens than a table row holds or 2^31 - 1: the row is left out */
     WF_KV_BLOCKS = 2u,   /* waits: the free blocks end before it (extend); its last tokens were lost (reorder) */
     WF_KV_TOKENS = 4u,   /* waits: max_tokens ends before it */
     WF_KV_PARENT = 1u    /* reorder: the parent is no row of the group; treated as -1 */
@@ -586,7 +586,7 @@ typedef struct {
  * Rows are admitted in their order until the blocks that they need exceed
  * the free ones or their tokens exceed max_tokens; that row and those
  * after it wait (a line: the caller orders rows by priority).  A row that a
- * table row cannot hold is passed over (WF_KV_LONG).  For the admitted
+ * table row or a 32-bit length cannot hold is passed over (WF_KV_LONG).  For the admitted
  * rows, missing blocks are taken from the ring in the order of rows and
  * appended to kv->table; every new token's slot, position and row are
  * written, and the places up to max_tokens are filled (-1, 0, -1), so that a

@@ -82,7 +82,7 @@ __device__ __forceinline__ uint32_t blocks_of(uint32_t x, uint32_t bs, int shift
 // What a row asks for: tokens (-1: the row is passed over) and blocks.
 __device__ __forceinline__ int2 row_needs(const ExtendArgs &a, int32_t len, int32_t add)
 {
-    if (len < 0 || add < 0) return make_int2(-1, 0);
+    if (len < 0 || add < 0 || add > INT32_MAX - len) return make_int2(-1, 0);  // (a table row may hold more than a length counts)
     const uint32_t had = blocks_of((uint32_t)len, a.bs, a.shift), then = blocks_of((uint32_t)len + (uint32_t)add, a.bs, a.shift);
     return then <= (uint32_t)a.width ? make_int2(add, (int)(then - had)) : make_int2(-1, 0);
 }

@@ -147,3 +147,33 @@ def test_binding_refuses_outputs_and_scratch_of_another_device_or_size():
     wf.wf_kv_reorder(d, kv, 4, parent, kv, moves)
     wf.wf_decode_status(d)
     assert int(kv.ends[1] - kv.ends[0]) == 40
+
+
+# ---------------------------------------------------------------------------
+# Extend: lengths, launches
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows", [5, 17_000])
+def test_extend_passes_over_lengths_beyond_31_bits(rows):
+    """A table row may hold more tokens than a 32-bit length counts: a row that would pass 2^31 - 1 is WF_KV_LONG, the
+    others go on."""
+    import torch
+    wf = lib()
+    most, bs = 2 ** 31 - 1, 1 << 30  # a table row of 4 blocks holds 2^32 tokens
+    length, add = np.zeros(rows, np.int32), np.zeros(rows, np.int32)
+    length[:5], add[:5] = [most - 5, most - 5, 0, most, most], [5, 6, 3, 0, most]
+    table = np.full((rows, 4), -1, np.int32)
+    table[[0, 1, 3, 4], :2] = np.arange(8).reshape(4, 2)
+    ring, ends = np.arange(12, dtype=np.int32)[::-1].copy(), np.array([0, 4], np.int64)
+    left_out = add.copy()
+    left_out[[1, 4]] = -1  # the plain form passes these over for another reason, with the same outcome
+    want = ref.extend(table, length, left_out, ring, ends, bs, 64)
+    assert want["status"][:5].tolist() == [0, wf.KV_LONG, 0, 0, wf.KV_LONG] and want["len"][0] == most
+    d = wf.Decode(max_rows=rows)
+    kv, step = wf.Kv(dev(table), dev(length), dev(ring), dev(ends), bs), wf.KvStep(rows, 64)
+    wf.wf_kv_extend(d, kv, dev(add), step)
+    torch.cuda.synchronize()
+    got = dict(table=kv.table, slot=step.slot, pos=step.pos, row=step.row, start=step.start, len=step.len, ends=step.ends,
+               status=step.status)
+    for k, w in want.items():
+        assert np.array_equal(host(got[k]), w), k
