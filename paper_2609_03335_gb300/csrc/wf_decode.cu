@@ -32,6 +32,7 @@ extern "C" int wf_decode_create(const wf_decode_limits *lim, int device, wf_deco
     d->device = device;
     d->lim = *lim;
     rc = wf_cuda_check(cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, device), "device attributes");
+    if (!rc) rc = wf_extend_setup();
     if (rc) { wf_decode_destroy(d); return rc; }
 
     const int64_t rows = lim->max_rows;

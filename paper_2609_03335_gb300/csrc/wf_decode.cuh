@@ -40,6 +40,7 @@ constexpr int kMaxGroup = 32;      // rows of a group, beams
 constexpr int kMaxKeep = 64;
 
 void wf_beam_scratch(int64_t rows, int64_t vocab, int sms, int64_t *parts, int64_t *units);
+int wf_extend_setup();
 int wf_launch_extend(wf_decode *d, const wf_kv *kv, const int32_t *add, const wf_kv_step *out, cudaStream_t st);
 int wf_launch_reorder(wf_decode *d, const wf_kv *kv, int32_t group, const int32_t *parent, const wf_kv *to,
                       const wf_kv_cache *cache, int32_t *copies, uint32_t *status, cudaStream_t st);

@@ -73,6 +73,9 @@ struct RowSums {
     int32_t *base;   // [rows]
 };
 
+// Their bytes.
+constexpr size_t extend_smem(int rows) { return 4 * (3 * (size_t)rows + 1); }
+
 __device__ __forceinline__ uint32_t blocks_of(uint32_t x, uint32_t bs, int shift)
 {
     const uint32_t q = shift >= 0 ? x >> shift : x / bs;
@@ -857,6 +860,14 @@ int wf_launch_reorder(wf_decode *d, const wf_kv *kv, int32_t group, const int32_
     return launch_finish<uint8_t>(a, *cache, block, pieces, copiers, st);
 }
 
+// The most shared memory that extend_kernel takes, allowed once for a device: the limit is the kernel's there, not a
+// call's, so one that a call set for its own rows would refuse the launches of handles on other threads.
+int wf_extend_setup()
+{
+    return wf_cuda_check(cudaFuncSetAttribute(extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)extend_smem(kSmemRows)),
+                         "extend smem attribute");
+}
+
 int wf_launch_extend(wf_decode *d, const wf_kv *kv, const int32_t *add, const wf_kv_step *out, cudaStream_t st)
 {
     ExtendArgs a;
@@ -883,12 +894,6 @@ int wf_launch_extend(wf_decode *d, const wf_kv *kv, const int32_t *add, const wf
         extend_fill_kernel<<<grid, kExtThreads, 0, st>>>(a, d->sums);
         return wf_cuda_check(cudaGetLastError(), "extend launch");
     }
-    const size_t smem = 4 * (3 * (size_t)a.rows + 1);
-    if (smem > 40 << 10) {
-        const int rc = wf_cuda_check(cudaFuncSetAttribute(extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem),
-                                     "extend smem attribute");
-        if (rc) return rc;
-    }
-    extend_kernel<<<grid, kExtThreads, smem, st>>>(a);
+    extend_kernel<<<grid, kExtThreads, extend_smem(a.rows), st>>>(a);
     return wf_cuda_check(cudaGetLastError(), "extend launch");
 }

@@ -177,3 +177,35 @@ def test_extend_passes_over_lengths_beyond_31_bits(rows):
                status=step.status)
     for k, w in want.items():
         assert np.array_equal(host(got[k]), w), k
+
+
+def test_extend_of_different_sizes_from_two_threads():
+    """Two handles on two host threads and streams: the rows' sums of one take four times the shared memory of the
+    other's, and neither's call changes what the other may launch."""
+    import torch
+    wf = lib()
+    failed, threads = [], []
+    rng = np.random.default_rng(4)
+
+    def work(rows, stream, d, kv, add, step, want):
+        try:
+            for _ in range(1500):
+                wf.wf_kv_extend(d, kv, add, step, stream=stream)
+            stream.synchronize()
+            for k in ("slot", "start", "len", "ends", "status"):
+                assert np.array_equal(host(getattr(step, k)), want[k]), (rows, k)
+        except Exception as e:  # (an assertion of a thread is no failure of the test)
+            failed.append(f"{rows} rows: {e!r}")
+
+    for rows in (16_384, 4_000):
+        add = rng.integers(0, 3, rows).astype(np.int32)
+        kv = wf.Kv.empty(rows, 2, 16, rows)
+        want = ref.extend(host(kv.table), host(kv.len), add, host(kv.ring), host(kv.ends), 16, 2 * rows)
+        args = (rows, torch.cuda.Stream(), wf.Decode(max_rows=rows), kv, dev(add), wf.KvStep(rows, 2 * rows), want)
+        threads.append(threading.Thread(target=work, args=args))
+    torch.cuda.synchronize()
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
