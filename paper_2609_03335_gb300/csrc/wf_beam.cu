@@ -529,20 +529,21 @@ __device__ __forceinline__ void row_stats(const SelectArgs &a, Shared<kThreads> 
     }
     __syncthreads();
     // Summed again, in the order of the tokens: rows with infinities, NaN or sums that left a float's range; and rows
-    // that may be equal to another (same score and maximum) if their sums are near each other but not the same, as where
-    // the rows' places in their 16 bytes differ.
+    // that may be equal to another (same score and maximum) if that one is summed again, or if their sums are near each
+    // other but not the same: where the rows' places in their 16 bytes differ, so do their parts' references and sums.
     uint32_t rows = sm.again;
     {
         // Each with every other, by rotation (a matching instruction takes longer for values that all differ).
         const float4 stat = sm.stat[lane < K ? lane : 0];
-        const uint32_t mark = __float_as_uint(stat.z) * 0x9E3779B1u ^ __float_as_uint(stat.x);
+        const uint32_t mark = __float_as_uint(stat.z + 0.0f) * 0x9E3779B1u ^ __float_as_uint(stat.x + 0.0f);  // (-0 is 0)
+        const float y = rows >> lane & 1u ? NAN : stat.y;  // (a row that is summed again takes its equals along)
         bool off = false;
 #pragma unroll 1
         for (int d = 1; d < K; ++d) {
             const int from = lane + d < K ? lane + d : lane + d - K;
             const uint32_t its = __shfl_sync(kFull, mark, from);
-            const float z = __shfl_sync(kFull, stat.y, from);
-            off |= its == mark && z != stat.y && fabsf(z - stat.y) < 1e-3f;
+            const float z = __shfl_sync(kFull, y, from);
+            off |= its == mark && z != y && !(fabsf(z - y) >= 1e-3f);
         }
         rows |= __ballot_sync(kFull, off && lane < K && stat.x > -INFINITY);
     }

@@ -209,3 +209,59 @@ def test_extend_of_different_sizes_from_two_threads():
     for t in threads:
         t.join()
     assert not failed, failed
+
+
+# ---------------------------------------------------------------------------
+# Select: equal beams, sums
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("low,level,spread", [(-1000.0, 85.0, 7.0), (-1000.0, -62.0, 2.0), (-200.0, 95.0, 4.0)])
+@pytest.mark.parametrize("groups,beams,vocab", [(64, 2, 30_001), (40, 3, 50_257), (1, 5, 32_003)])
+def test_select_equal_rows_have_equal_sums_where_one_leaves_a_floats_range(groups, beams, vocab, low, level, spread):
+    """Equal rows that lie differently in their 16 bytes.  The first 1,023 tokens have a finite mask, so the four
+    lines that give a part its reference hold the first token that says something in some rows and not in others:
+    relative to that the sum fits a float, relative to 0 it passes its range (or nearly vanishes)."""
+    import torch
+    wf = lib()
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    x = (level + spread * (torch.rand((groups, vocab), generator=gen, device="cuda") - 0.5)).half()
+    x[:, :1023] = low
+    x[:, 1023] = level + 8  # so far above the others that log Z is small: a sum shows its last bits
+    x = x.repeat_interleave(beams, 0).contiguous()
+    assert vocab % 8 and x.stride(0) == vocab
+    score = torch.zeros(groups * beams, device="cuda")
+    keep = 2 * beams
+    d = wf.Decode(max_rows=groups * beams, max_vocab=vocab, max_keep=keep)
+    out = wf.BeamOut(groups, beams, keep)
+    wf.wf_beam_select(d, x, score, out)
+    parent, token, got = host(out.parent) % beams, host(out.token), host(out.score)
+    for g in range(groups):
+        row = host(x[g * beams].float())
+        want = []
+        for value in np.unique(row)[::-1]:
+            want += [(k, int(t)) for k in range(beams) for t in np.flatnonzero(row == value)]
+            if len(want) >= keep:
+                break
+        assert list(zip(parent[g].tolist(), token[g].tolist())) == want[:keep], g
+        at = row[token[g]]
+        assert all(len(set(got[g][at == v].tolist())) == 1 for v in np.unique(at)), g
+
+
+def test_select_equal_rows_with_zeros_of_both_signs():
+    """Scores and maxima of -0 and 0 are equal."""
+    import torch
+    wf = lib()
+    vocab, beams, groups = 9001, 4, 30
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = (-20 * torch.rand((groups, vocab), generator=gen, device="cuda")).half()
+    x[:, 77] = 0.0
+    x = x.repeat_interleave(beams, 0).contiguous()
+    x[1::2, 77] = -0.0
+    score = torch.zeros(groups * beams, device="cuda")
+    score[::3] = -0.0
+    d = wf.Decode(max_rows=groups * beams, max_vocab=vocab, max_keep=beams)
+    out = wf.BeamOut(groups, beams, beams)
+    wf.wf_beam_select(d, x, score, out)
+    assert (host(out.token) == 77).all() and (host(out.parent) % beams == np.arange(beams)).all()
+    got = host(out.score)
+    assert (got == got[:, :1]).all()
