@@ -42,7 +42,7 @@ namespace {
 constexpr uint32_t kFull = 0xFFFFFFFFu;
 constexpr int kCap = 512;      // keys gathered before they are ranked
 constexpr int kStep = 4;       // lines that a warp has in flight, and as many in work
-constexpr int kSum = 64;       // steps whose exponentials are summed before that sum joins the warp's
+constexpr int kSum = 64;       // steps whose sums are added up before that sum joins the warp's
 constexpr int kUnits = 4096 + kMaxGroup;  // units of a search, at most: shared memory holds their maxima
 constexpr int kPick = 128;     // units that the join reads again, at most, before it orders them by key
 
@@ -302,6 +302,28 @@ __device__ __forceinline__ float exp2_fast(float x)
     return y;
 }
 
+// Sum: what is added to it passes through two roundings, however many additions follow (Kahan's compensated sum).
+struct Sum {
+    float s = 0, low = 0;
+    __device__ __forceinline__ void add(float x)
+    {
+        const float y = x - low, t = s + y;
+        low = (t - s) - y;
+        s = t;
+    }
+};
+
+// x[0] + ... + x[n - 1], pairs first: log2(n) roundings a term.
+template <int n>
+__device__ __forceinline__ float sum_pairs(float *x)
+{
+#pragma unroll
+    for (int w = n / 2; w > 0; w >>= 1)
+#pragma unroll
+        for (int i = 0; i < w; ++i) x[i] += x[i + w];
+    return x[0];
+}
+
 template <int kType>
 __device__ __forceinline__ float element(const typename Elems<kType>::type *p)
 {
@@ -400,27 +422,28 @@ __device__ __forceinline__ void take_part(const SelectArgs &a, int row, int u0, 
     for (int u = 0; u < kStep; ++u) first = fmaxf(first, E::most(v[u]));
     first = warp_max(first);
     const float c = first > -80.0f && first < 1e4f ? first * kLog2e : 0.0f;
-    float sum = 0, all = -INFINITY, unit = -INFINITY;
+    // A term's way into the sum: 5 additions in its step (4 in 32 bits), kSum of steps, the compensated sum over those.
+    Sum sum;
+    float all = -INFINITY, unit = -INFINITY;
     int left = unit_lines;
     for (int i = i0; i < i1;) {
-        float s0 = 0, s1 = 0;
+        float steps = 0;
         const int until = min(i1, i + kSum * kStep);
 #pragma unroll 1
         for (; i < until; i += kStep) {
             load(next, i + kStep);
-            float top[kStep];
+            float top[kStep], line[kStep];
 #pragma unroll
             for (int u = 0; u < kStep; ++u) {
                 float x[E::n];
                 E::get(v[u], x);
 #pragma unroll
-                for (int e = 0; e < E::n; e += 2) {
-                    s0 += exp2_fast(fmaf(x[e], kLog2e, -c));
-                    s1 += exp2_fast(fmaf(x[e + 1], kLog2e, -c));
-                }
+                for (int e = 0; e < E::n; ++e) x[e] = exp2_fast(fmaf(x[e], kLog2e, -c));
+                line[u] = sum_pairs<E::n>(x);
                 top[u] = E::most(v[u]);
                 v[u] = next[u];
             }
+            steps += sum_pairs<kStep>(line);
             if (kUnit < kStep) {
                 constexpr int kHere = kStep / kUnit;  // units of a step
                 float put = -INFINITY;
@@ -447,11 +470,11 @@ __device__ __forceinline__ void take_part(const SelectArgs &a, int row, int u0, 
                 }
             }
         }
-        sum += s0 + s1;
+        sum.add(steps);
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
-    if (lane == 0) *part = make_float4(c, sum, all, 0.0f);
+    for (int o = 16; o > 0; o >>= 1) sum.s += __shfl_xor_sync(kFull, sum.s, o);
+    if (lane == 0) *part = make_float4(c, sum.s, all, 0.0f);
 }
 
 // The beam of a search's unit.
@@ -553,14 +576,16 @@ __device__ __forceinline__ void row_stats(const SelectArgs &a, Shared<kThreads> 
         int lead;
         const auto *base = row_base<kType>(a, group * K + k, lead);
         const float m = sm.stat[k].x;
-        float s = 0;
+        Sum sum;
         for (int t0 = tid; t0 < V; t0 += 8 * kThreads) {
             float x[8];
 #pragma unroll
             for (int u = 0; u < 8; ++u) x[u] = t0 + u * kThreads < V ? element<kType>(base + t0 + u * kThreads) : -INFINITY;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) s += x[u] == m ? 1.0f : x[u] > -INFINITY ? exp2f((x[u] - m) * kLog2e) : 0.0f;
+            for (int u = 0; u < 8; ++u) x[u] = x[u] == m ? 1.0f : x[u] > -INFINITY ? exp2f((x[u] - m) * kLog2e) : 0.0f;
+            sum.add(sum_pairs<8>(x));  // (up to 65,536 logits a thread)
         }
+        float s = sum.s;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
         if (lane == 0) sm.sum[warp] = s;

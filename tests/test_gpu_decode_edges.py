@@ -265,3 +265,63 @@ def test_select_equal_rows_with_zeros_of_both_signs():
     assert (host(out.token) == 77).all() and (host(out.parent) % beams == np.arange(beams)).all()
     got = host(out.score)
     assert (got == got[:, :1]).all()
+
+
+def z_bound(chain, levels, sizes):
+    """How far a selection's sums may be from the 64-bit form's, by what is done in 32 bits (u = 2^-24):
+      chain       additions that a term passes through on its way to Z, u each
+      levels      distance of the terms that count from the maximum: the argument log2(e) x of 2^x is rounded
+                  (u of it) and so is its factor log2(e) (2^-26 of it), twice, for a part's reference and the maximum's
+      2^x         2^-22 for each of the two
+      log, sum    an ulp of log Z, and half of one for each of two additions."""
+    u = 2.0 ** -24
+    log_z = math.log(sizes)
+    ulp = 2.0 ** (math.floor(math.log2(max(log_z + levels, 1.0))) - 23)
+    return chain * u + 2 * levels * (u + 2.0 ** -26) + 2 * 2.0 ** -22 + 2 * ulp
+
+
+def check_two_levels(wf, x, score, keep, chain):
+    """Rows of 5s and 0s (NaN masked): the best are the 5s, then the 0s."""
+    import torch
+    rows, vocab = x.shape
+    d = wf.Decode(max_rows=rows, max_vocab=vocab, max_keep=keep)
+    out = wf.BeamOut(rows, 1, keep)
+    wf.wf_beam_select(d, x, score, out)
+    got, token = host(out.score).astype(np.float64), host(out.token)
+    high, none = host((x == 5).sum(1)), host(torch.isnan(x).sum(1))
+    log_z = np.log(high + (vocab - high - none) * math.exp(-5.0))
+    first = host(torch.where(torch.isnan(x), -1.0, x.float()).sort(dim=1, descending=True, stable=True).indices[:, :keep]) if vocab < 1 << 20 else None
+    for r in range(rows):
+        want = np.where(np.arange(keep) < high[r], 0.0, -5.0) - log_z[r]
+        assert np.abs(got[r] - want).max() <= z_bound(chain, 5, vocab), (r, got[r] - want)
+        if first is not None:
+            assert token[r].tolist() == first[r].tolist()
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
+def test_select_sums_of_long_parts(dtype):
+    """More searches than are resident at once: a warp sums an eighth of a row.  Each step of a part holds one 5, so that is
+    the part's reference; the others are 0, each term e^-5, and the roundings of its additions go one way.
+    Chain: 5 additions to a step's sum, 64 steps, 2 for the compensated sum over those, 5 over the lanes, 1 part a lane,
+    5 over the lanes of the join."""
+    import torch
+    wf = lib()
+    vocab = 1 << (18 if dtype == "float32" else 19)
+    x = torch.zeros((500, vocab), dtype=getattr(torch, dtype), device="cuda")
+    x[:, ::512 if dtype == "float32" else 1024] = 5  # a step's tokens
+    check_two_levels(wf, x, torch.zeros(500, device="cuda"), 12, 5 + 64 + 2 + 5 + 1 + 5)
+
+
+@pytest.mark.parametrize("vocab", [600_001, 1 << 24])
+@pytest.mark.parametrize("beams", [2])
+def test_select_sums_of_rows_with_a_nan(vocab, beams):
+    """A row with a NaN is summed again by the join, up to 65,536 logits a thread.  Chain: 3 additions to eight
+    logits' sum, 2 for the compensated sum over those, 5 over the lanes, 16 over the warps; and for the row without, one
+    step a part, 76 parts a lane at most."""
+    import torch
+    wf = lib()
+    x = torch.zeros((beams, vocab), dtype=torch.float16, device="cuda")
+    x[:, 1234] = 5
+    x[0, vocab // 2 + 3] = math.nan
+    for row, chain in ((0, 3 + 2 + 5 + 16), (1, 5 + 64 + 2 + 5 + 76 + 5)):
+        check_two_levels(wf, x[row:row + 1], torch.zeros(1, device="cuda"), 4, chain)
