@@ -8,9 +8,10 @@ replica's paged KV cache, and decodes it with beam search:
   wf_kv_extend                                 admission by free blocks, block tables, slots of the prompts
   wf_beam_select, wf_kv_reorder, wf_kv_extend  a step: selection, rows in its order, slots of the new tokens
 
-The language model is a stand-in of random weights (the mean of the row's
-cached vectors through an output matrix), so that what is decoded depends on every
-cached token being where its block table says.
+The language model is a stand-in of random weights: the mean of the row's
+cached vectors, read through its block table, times an output matrix.  So what is
+decoded depends on every cached token being where the table says.  Sums that
+are kept beside the cache, from the parents and tokens alone, check it at the end.
 
     python examples/decode_window.py [window] [beams] [steps]
 """
@@ -54,14 +55,23 @@ def first_batch(prob, n_plans=256, most=8):
     return device, batch
 
 
-def decode(prob, device, batch, beams=4, steps=16, seed=0):
-    """Beam search of `steps` tokens for the activations of the batch that fit the device."""
+def cached_sums(vectors, kv):
+    """The sum of each row's cached vectors, by its block table."""
+    p = torch.arange(int(kv.len.max()), device="cuda")
+    slots = kv.table.long()[:, p // BLOCK_TOKENS] * BLOCK_TOKENS + p % BLOCK_TOKENS
+    there = p < kv.len[:, None]
+    return torch.where(there[:, :, None], vectors[torch.where(there, slots, 0)], 0.0).sum(1)
+
+
+def decode(prob, device, batch, beams=4, steps=16, seed=0, n_blocks=None):
+    """Beam search of `steps` tokens for the activations of the batch that fit the device (n_blocks: with so many blocks
+    in place of the device's).  A search that finds no block left in some step, or waits behind one that does, ends there."""
     D = int(prob.D)
     peak, weight = np.asarray(prob.peak_mib).reshape(-1, D), np.asarray(prob.weight_mib)
     kv_mib = np.array([peak[n, device] - weight[prob.model[n]] for n in batch])
     prompt = np.maximum(1, kv_mib // TOKEN_MIB)
     free_mib = int(np.asarray(prob.cap_mib)[device] - weight[prob.model[batch[0]]])
-    n_blocks = free_mib // (BLOCK_TOKENS * TOKEN_MIB)
+    n_blocks = n_blocks or free_mib // (BLOCK_TOKENS * TOKEN_MIB)
     groups, rows = len(batch), len(batch) * beams
     width = -(-(int(prompt.max()) + steps) // BLOCK_TOKENS)
     gen = torch.Generator(device="cuda").manual_seed(seed)
@@ -87,14 +97,16 @@ def decode(prob, device, batch, beams=4, steps=16, seed=0):
     vectors[prefill.slot[used]] = embed[tokens[:int(used.sum())]]
     taken_at_first = int(kv.ends[0])
 
-    # The stand-in model: the sum of a row's cached vectors, kept as a running state.
+    # Beside the cache: the sum of the vectors that each row's tokens have.
     state = torch.zeros((rows, WIDTH), device="cuda")
     state.index_add_(0, prefill.row[used].long(), vectors[prefill.slot[used]])
     score[heads] = torch.where(kv.len[heads] > 0, 0.0, -torch.inf)
     step = wf.KvStep(rows, rows, kv)
     parents, tokens = [], []
+    lasted = torch.zeros(groups, dtype=torch.int32, device="cuda")  # steps of each search
+    going = kv.len[heads] > 0
     for _ in range(steps):
-        logits = (state / kv.len.clamp(min=1)[:, None]) @ out_matrix
+        logits = (cached_sums(vectors, kv) / kv.len.clamp(min=1)[:, None]) @ out_matrix
         wf.wf_beam_select(scratch, logits, score, found, eos=EOS)
         wf.wf_kv_reorder(scratch, kv, beams, found.next_parent.view(-1), kv, moves, cache=cache)
         alive = found.next_parent.view(-1) >= 0
@@ -105,28 +117,29 @@ def decode(prob, device, batch, beams=4, steps=16, seed=0):
         state = torch.where(alive[:, None], state[found.next_parent.view(-1).clamp(min=0).long()] + embed[new.clamp(min=0).long()], 0.0)
         parents.append(found.next_parent.view(-1).clone())
         tokens.append(new)
+        # A row that lost its last tokens, or that waits: its cache is no longer its hypothesis's.  Without scores its search
+        # has no candidates, so the next reordering gives its blocks back.
+        going &= ((moves.status | step.status) == 0).view(groups, beams).all(1)
+        score.masked_fill_(~going.repeat_interleave(beams), -torch.inf)
+        lasted += going.int()
     wf.wf_decode_status(scratch)
 
     # The best hypothesis of each search, from its last row back.
-    texts = []
+    texts, lasted = [], lasted.tolist()
     for g in range(groups):
         row, text = g * beams, []
-        for parent, token in zip(reversed(parents), reversed(tokens)):
+        for parent, token in zip(reversed(parents[:lasted[g]]), reversed(tokens[:lasted[g]])):
             if row < 0:
                 break
             text.append(int(token[row]))
             row = int(parent[row])
         texts.append(text[::-1] if admitted[g] else [])
     # What the block tables hold is what the running state summed.
-    length, table = kv.len.cpu().numpy(), kv.table.long()
-    held = torch.zeros_like(state)
-    for r in range(rows):
-        p = torch.arange(int(length[r]), device="cuda")
-        held[r] = vectors[table[r, p // BLOCK_TOKENS] * BLOCK_TOKENS + p % BLOCK_TOKENS].sum(0)
-    error = float((held - state).abs().max() / state.abs().max().clamp(min=1))
+    off = torch.where(going.repeat_interleave(beams)[:, None], cached_sums(vectors, kv) - state, 0.0)
+    error = float(off.abs().max() / state.abs().max().clamp(min=1))
     blocks = int(kv.ends[0] - (kv.ends[1] - n_blocks))
     wf.wf_kv_reorder(scratch, kv, beams, torch.full((rows,), -1, dtype=torch.int32, device="cuda"), kv, moves)  # all end
-    return dict(admitted=admitted, prompt=prompt, texts=texts, score=score.view(groups, beams)[:, 0].tolist(), error=error,
+    return dict(admitted=admitted, prompt=prompt, texts=texts, steps=lasted, score=score.view(groups, beams)[:, 0].tolist(), error=error,
                 prompt_blocks=taken_at_first, blocks=blocks, n_blocks=n_blocks, left=int(kv.ends[1] - kv.ends[0]))
 
 
@@ -138,7 +151,10 @@ def main(window="mix", beams=4, steps=16):
     print(f"{got['n_blocks']} blocks of {BLOCK_TOKENS} tokens; {got['prompt_blocks']} for the prompts, "
           f"{got['blocks']} held after {steps} tokens on {beams} beams")
     for n, ok, length, text, score in zip(batch, got["admitted"], got["prompt"], got["texts"], got["score"]):
-        print(f"  activation {n}: {length} tokens, " + (f"log p {score:.2f}, {text[:8]} ..." if ok else "waits for blocks"))
+        end = f"log p {score:.2f}, {text[:8]} ..." if len(text) == steps else f"no block left after {len(text)} tokens, {text[:8]} ..."
+        print(f"  activation {n}: {length} tokens, " + (end if ok else "waits for blocks"))
+    if not got["error"] < 1e-4:
+        raise SystemExit(f"what the block tables hold is off by {got['error']:.1e}")
 
 
 if __name__ == "__main__":

@@ -325,3 +325,48 @@ def test_select_sums_of_rows_with_a_nan(vocab, beams):
     x[0, vocab // 2 + 3] = math.nan
     for row, chain in ((0, 3 + 2 + 5 + 16), (1, 5 + 64 + 2 + 5 + 76 + 5)):
         check_two_levels(wf, x[row:row + 1], torch.zeros(1, device="cuda"), 4, chain)
+
+
+# ---------------------------------------------------------------------------
+# The example
+# ---------------------------------------------------------------------------
+
+@pytest.fixture(scope="module")
+def example():
+    import sys
+    lib()
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    sys.path.insert(0, os.path.join(root, "examples"))
+    import decode_window
+    import wfgen
+    prob = wfgen.config("tiny").problem
+    return decode_window, prob, *decode_window.first_batch(prob, n_plans=64)
+
+
+def test_example_decodes_what_lies_in_the_cache(example, monkeypatch):
+    """With every cached vector's sign changed once, after the first step, other tokens follow."""
+    ex, prob, device, batch = example
+    plain = ex.decode(prob, device, batch, beams=3, steps=6)
+    reorder, calls = ex.wf.wf_kv_reorder, []
+
+    def and_change_signs(scratch, kv, group, parent, to, moves, cache=None, **kw):
+        reorder(scratch, kv, group, parent, to, moves, cache=cache, **kw)
+        calls.append(cache)
+        if len(calls) == 1:
+            cache.neg_()
+    monkeypatch.setattr(ex.wf, "wf_kv_reorder", and_change_signs)
+    other = ex.decode(prob, device, batch, beams=3, steps=6)
+    assert plain["error"] < 1e-4 < other["error"]
+    assert any(a[1:] != b[1:] for a, b in zip(plain["texts"], other["texts"]))
+
+
+def test_example_ends_searches_that_find_no_block(example):
+    """Blocks for the prompts and a few steps: searches end where a row finds none or waits, and all blocks come back."""
+    ex, prob, device, batch = example
+    all_of_it = ex.decode(prob, device, batch, beams=3, steps=40)
+    assert all_of_it["steps"] == [40 if ok else 0 for ok in all_of_it["admitted"]]
+    few = ex.decode(prob, device, batch, beams=3, steps=40, n_blocks=all_of_it["prompt_blocks"] + 2)
+    assert few["admitted"].any() and few["left"] == few["n_blocks"] and few["error"] < 1e-4
+    assert min(n for n, ok in zip(few["steps"], few["admitted"]) if ok) < 40
+    assert [len(t) for t in few["texts"]] == [n if ok else 0 for n, ok in zip(few["steps"], few["admitted"])]
+    assert all(0 < t < ex.VOCAB for text in few["texts"] for t in text)
