@@ -370,3 +370,94 @@ def test_example_ends_searches_that_find_no_block(example):
     assert min(n for n, ok in zip(few["steps"], few["admitted"]) if ok) < 40
     assert [len(t) for t in few["texts"]] == [n if ok else 0 for n, ok in zip(few["steps"], few["admitted"])]
     assert all(0 < t < ex.VOCAB for text in few["texts"] for t in text)
+
+
+# ---------------------------------------------------------------------------
+# Captures, streams
+# ---------------------------------------------------------------------------
+
+def test_a_decoding_step_captured_and_on_a_stream_of_its_own():
+    """Selection, reordering with copies and extension in place, as one step: eagerly on a side stream, then replayed
+    from a graph; each step against the plain forms from the step's own state."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(12)
+    groups, beams, vocab, bs, width = 6, 4, 3001, 4, 12
+    rows, n = groups * beams, groups * beams * width + 4
+    d = wf.Decode(max_rows=rows, max_row_blocks=width, max_vocab=vocab, max_keep=2 * beams)
+    kv, moves, step = wf.Kv.empty(rows, width, bs, n), wf.KvMoves(rows), None
+    step, first = wf.KvStep(rows, rows, kv), wf.KvStep(rows, rows * 10, kv)
+    score = torch.full((rows,), -math.inf, device="cuda")
+    score[::beams] = 0
+    out = wf.BeamOut(groups, beams, 2 * beams, score)
+    logits = torch.zeros((rows, vocab), device="cuda")
+    one = torch.ones(rows, dtype=torch.int32, device="cuda")
+    cache = dev(rng.integers(0, 256, (3, n, bs, 24)).astype(np.uint8))
+    prompt = np.zeros(rows, np.int32)
+    prompt[::beams] = rng.integers(1, 10, groups)
+    wf.wf_kv_extend(d, kv, dev(prompt), first)
+
+    def one_step():
+        wf.wf_beam_select(d, logits, score, out, eos=2)
+        wf.wf_kv_reorder(d, kv, beams, out.next_parent.view(-1), kv, moves, cache=cache)
+        wf.wf_kv_extend(d, kv, one, step)
+
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    for i in range(12):
+        x = rng.standard_normal((rows, vocab)).astype(np.float32) * 2
+        logits.copy_(dev(x))
+        torch.cuda.synchronize()
+        if i == 6:
+            with torch.cuda.graph(graph):  # (captured, not run)
+                one_step()
+        before = {k: host(v) for k, v in dict(table=kv.table, len=kv.len, ring=kv.ring, ends=kv.ends, cache=cache, score=score).items()}
+        if i < 6:
+            with torch.cuda.stream(side):
+                one_step()
+            side.synchronize()
+        else:
+            graph.replay()
+            torch.cuda.synchronize()
+        best = ref.select(x, before["score"], beams, 2 * beams)
+        parent = host(out.next_parent).reshape(-1)
+        for g, want in enumerate(best):  # (normal values: no two sums within their rounding)
+            onward = [(p, t) for _, p, t in want if t != 2][:beams]
+            assert list(zip(host(out.next_parent)[g].tolist(), host(out.next_token)[g].tolist())) == onward, (i, g)
+        mid = ref.reorder(before["table"], before["len"], before["ring"], before["ends"], bs, beams, parent, before["table"], before["cache"])
+        end = ref.extend(mid["table"], mid["len"], np.ones(rows, np.int32), mid["ring"], mid["ends"], bs, rows)
+        got = dict(table=kv.table, len=kv.len, ends=kv.ends, slot=step.slot, pos=step.pos, row=step.row, start=step.start, status=step.status)
+        for k, v in got.items():
+            assert np.array_equal(host(v), end[k]), (i, k)
+        assert np.array_equal(host(moves.copies), mid["copies"]) and np.array_equal(host(cache), mid["cache"]), i
+        assert np.array_equal(host(kv.ring), mid["ring"]) and not host(moves.status).any()
+    wf.wf_decode_status(d)
+
+
+@pytest.mark.parametrize("offset,token_bytes,gap", [(0, 48, 0), (0, 48, 80), (4, 48, 4), (1, 48, 0), (8, 20, 16), (3, 7, 5)])
+def test_reorder_of_a_cache_whose_planes_lie_apart_or_anywhere(offset, token_bytes, gap):
+    """Planes further apart than their blocks, bases on no boundary: nothing between the planes changes."""
+    import torch
+    wf = lib()
+    L, rng = wf.load_library(), np.random.default_rng(offset + gap)
+    planes, n, bs, rows = 3, 9, 5, 4
+    plane = n * bs * token_bytes
+    raw = rng.integers(0, 256, offset + planes * (plane + gap) + 64).astype(np.uint8)
+    buf = dev(raw)
+    table = np.array([[0, 1, -1], [0, 2, -1], [0, 1, 3], [4, -1, -1]], np.int32)
+    length, parent = np.array([8, 9, 11, 3], np.int32), np.array([1, 1, 3, 3], np.int32)
+    ring, ends = np.array([5, 6, 7, 8, -1, -1, -1, -1, -1], np.int32), np.array([0, 4], np.int64)
+    view = lambda a: np.stack([a[offset + p * (plane + gap):][:plane] for p in range(planes)]).reshape(planes, n, bs, token_bytes)
+    want = ref.reorder(table, length, ring, ends, bs, rows, parent, table, view(raw))
+    kv, out = wf.Kv(dev(table), dev(length), dev(ring), dev(ends), bs), wf.KvMoves(rows)
+    d = wf.Decode(max_rows=rows, max_row_blocks=3)
+    cc = wf.wf_kv_cache(buf.data_ptr() + offset, planes, 0, plane + gap, token_bytes)
+    p = dev(parent)
+    assert L.wf_kv_reorder(d.ptr, ctypes.byref(kv.c), rows, p.data_ptr(), ctypes.byref(kv.c), ctypes.byref(cc),
+                           out.copies.data_ptr(), out.status.data_ptr(), torch.cuda.current_stream().cuda_stream or None) == wf.WF_OK
+    wf.wf_decode_status(d)
+    got = host(buf)
+    assert np.array_equal(view(got), want["cache"]) and np.array_equal(host(out.copies), want["copies"])
+    between = np.ones(raw.size, bool)
+    for q in range(planes):
+        between[offset + q * (plane + gap):][:plane] = False
+    assert np.array_equal(got[between], raw[between])
