@@ -523,8 +523,9 @@ typedef struct {
 
 /*
  * Scratch for the calls below on device `device`: about 4 bytes per table
- * cell of the limits and, for the selection, 4 bytes per row and 128 tokens of
- * vocabulary (at most 16 KiB a row).  The calls allocate nothing more.
+ * cell of the limits (a row's cells rounded up to 256) and, for the selection,
+ * 128 bytes per row and 4 per row and 128 tokens of vocabulary (at most about
+ * 16 KiB a row).  The calls allocate nothing more.
  * One wf_decode serves one stream at a time.  Returns WF_OK, WF_EINVAL,
  * WF_ENOMEM or WF_ECUDA.
  */
@@ -630,7 +631,8 @@ typedef struct {
  *   score[k] + log softmax(logits[k])[v]
  * in 32-bit floating point, (x - max) - log(sum of exp(x - max)) added to the
  * score; best first.  Equal sums: the lower beam first, in a beam the larger
- * logit, then the lower token; beams with equal logits and scores have equal sums.  A logit of -inf or NaN is masked: no
+ * logit, then the lower token; beams with equal logits and scores have equal sums,
+ * wherever their rows lie.  A logit of -inf or NaN is masked: no
  * candidate, no part of the sum; a row with a logit of +inf shares its
  * probability among those.  A row that is masked throughout, or whose score
  * is -inf or NaN, has no candidates.  Places without a candidate hold score

@@ -14,20 +14,22 @@
 // The exponentials are summed relative to a value near the start of the
 // warp's part: a sum relative to any value is as exact as one relative to
 // the maximum as long as it stays within a float's range, and a row where it
-// did not is summed again by the join.
+// did not is summed again by the join.  Additions go in pairs and, where they
+// are many, are compensated, so that a term passes through some 80 roundings in
+// the streaming pass and 26 in the join's.
 //
 // The bound: the threads' maxima, over 32 or 64 classes of threads, have a
 // keep-th largest.  The classes hold interleaved units, so few more than `keep`
 // reach it, unless many are equal (a mask of one low value); then the keys that
 // order equal sums by their place make the bound.
 //
-// Measured: 64 searches of 8 beams over 131,072 bf16 tokens (134 MB) take 32.1
+// Measured: 64 searches of 8 beams over 131,072 bf16 tokens (134 MB) take 32.2
 // us; the last warp of step 1 ends at 22 us (6.1 TB/s; 63 warp instructions a
 // line, 38 % of the issue slots: bound by HBM), the join takes 7 us more, the
 // launch 2.  The join is bound by its chain (arrival, parts and units, the units
 // read again: trips to L2 or HBM of 1,100 to 1,900 cycles) and by code that runs
 // once a CTA, so what is not on its path stays out of line.  One search of 4
-// beams over 32,000 tokens, all join, takes 8.6 us.  Lists of candidates that
+// beams over 32,000 tokens, all join, takes 8.7 to 9.0 us.  Lists of candidates that
 // each CTA's part of a row kept, with a running bound, took 46 us for the large
 // case: 10 K warp instructions a part, and barriers that leave the loads waiting.
 #include <algorithm>

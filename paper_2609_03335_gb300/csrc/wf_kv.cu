@@ -11,7 +11,7 @@
 // It has to move 16 bytes a token (slot, position, row) and little else.  So
 // the sums are made by every CTA for itself in shared memory (the rows'
 // lengths come from L2) instead of by a kernel before: one launch.  2,000 rows
-// decoding take 6.1 us and 12 rows 3.6, bound by the launch and two or three trips to L2 in
+// decoding take 6.3 us and 12 rows 4.0, bound by the launch and two or three trips to L2 in
 // turn; 35 M tokens of 2,000 rows 97 us, 5.96 TB/s, bound by the writes (a
 // fill of the same arrays reaches 6.9), about 5 us of it the sums.
 #include <algorithm>
@@ -415,10 +415,10 @@ __global__ void __launch_bounds__(kExtThreads) extend_fill_kernel(const __grid_c
 //    lengths and last blocks, while other CTAs, which find a copy's blocks by
 //    the same sums, copy.
 //
-// One group of 4 rows takes 7.6 us, 64 groups of 8 rows of 1,024 blocks 14.5:
+// One group of 4 rows takes 7.8 us, 64 groups of 8 rows of 1,024 blocks 13.7 to 15.2:
 // bound by L2 trips in turn (lengths, entries, arrivals, sums, lists), about
 // 1,100 cycles each, and by code that is fetched once; 64 groups of 8 with 61 MB
-// of tokens to copy 36 us, the copies near 5.5 TB/s of reads and writes.  The
+// of tokens to copy 35.4 us, 27 of them the copies, 4.5 TB/s of reads and writes.  The
 // second kernel is launched while the first runs and waits for it on the GPU, which hides most of a launch.  (Its CTAs could each make the sums for
 // themselves and spare the first kernel its arrivals: 1 us less where nothing
 // is copied, 2.5 us more where much is.)
