@@ -37,6 +37,10 @@
  *   wf_kv_extend            admission by free blocks, block tables and slots of a step's tokens
  *   wf_beam_select          beam search's selection over beams and vocabulary
  *   wf_kv_reorder           rows put in the selection's order: tables, last blocks, freed blocks
+ *   wf_kv_write             a layer's keys and values of a step's tokens into the cache, with rotary positions
+ *   wf_kv_copy_scales       an 8-bit cache's scales after wf_kv_reorder's copies
+ *   wf_attn_create, wf_attn_status, wf_attn_destroy
+ *   wf_attend               a layer's attention of a step's tokens over their rows' cached keys and values
  *
  * Conventions.
  *   - Times are int64 microseconds, memory int32 MiB; every output is an
@@ -533,8 +537,8 @@ int wf_decode_create(const wf_decode_limits *limits, int device, wf_decode **out
 
 /*
  * Synchronize `stream` and report (then clear) what earlier calls found on
- * the device: WF_EINVAL when a table or the ring named a block outside the
- * cache (its copy was left out), else WF_OK.
+ * the device: WF_EINVAL when a table, the ring, a slot or a copy named a block outside the
+ * cache (what was to be written there was left out), else WF_OK.
  */
 int wf_decode_status(wf_decode *d, void *stream);
 
@@ -598,8 +602,13 @@ typedef struct {
  */
 int wf_kv_extend(wf_decode *d, const wf_kv *kv, const int32_t *add, const wf_kv_step *out, void *stream);
 
-/* Element types of the logits (wf_beam.dtype). */
-enum { WF_F32 = 0, WF_F16 = 1, WF_BF16 = 2 };
+/* Element types: of the logits (wf_beam.dtype: the first three), of a layer's tensors and cache. */
+enum {
+    WF_F32 = 0,
+    WF_F16 = 1,
+    WF_BF16 = 2,
+    WF_E4M3 = 3  /* 8 bits: sign, 4 of exponent, 3 of mantissa; up to 448, no infinity */
+};
 
 /*
  * One step of beam search: `groups` searches of `beams` rows each; row
@@ -682,6 +691,87 @@ typedef struct {
  */
 int wf_kv_reorder(wf_decode *d, const wf_kv *kv, int32_t group, const int32_t *parent, const wf_kv *to,
                   const wf_kv_cache *cache, int32_t *copies, uint32_t *status, void *stream);
+
+/*
+ * One layer's part of the cache; DEVICE pointers, caller-owned.  Element d of
+ * head h of the token at place i of block b lies at
+ *   b * block_stride + i * token_stride + h * head_stride + d * element size
+ * bytes from k (its key) and v (its value).  In WF_E4M3 what an element
+ * stands for is its value times the scale of its block and head.
+ */
+typedef struct {
+    int32_t dtype;         /* WF_F16, WF_BF16 or WF_E4M3 */
+    int32_t heads;         /* key / value heads, 1..1024 */
+    int32_t dim;           /* elements of a head: 64 or 128 */
+    int32_t reserved;      /* 0 */
+    void *k, *v;           /* on 16-byte boundaries */
+    int64_t block_stride;  /* bytes, and the next two: multiples of 16, >= 0 */
+    int64_t token_stride;
+    int64_t head_stride;
+    float *k_scale;        /* [n_blocks][heads], and v_scale: WF_E4M3 only, else NULL */
+    float *v_scale;
+} wf_kv_layer;
+
+/*
+ * Rotary positions: of a head's first `dim` elements the pairs (i, i + dim/2),
+ * or with `interleaved` (2i, 2i + 1), turn by pos * turn[i] / 2^64 turns and
+ * grow by `magnitude`; the elements behind them stay as they are.  Turns are
+ * whole numbers of 2^-64 (a rate f in radians a position is f / 2 pi * 2^64), so the
+ * product modulo a turn is exact at every position.
+ */
+typedef struct {
+    int32_t dim;           /* even, 0 (no rotation) up to the head's */
+    int32_t interleaved;   /* 0 or 1 */
+    const uint64_t *turn;  /* DEVICE [dim / 2] */
+    float magnitude;
+    int32_t reserved;      /* 0 */
+} wf_rope;
+
+/* A step's tensors of a layer; DEVICE pointers, row t is the step's token t, strides in bytes, elements of a head together. */
+typedef struct {
+    int32_t dtype;                 /* of all: WF_F16 or WF_BF16 */
+    int32_t q_heads;               /* 0: no queries; up to 1024 */
+    const void *k, *v;             /* [max_tokens][layer heads][layer dim] */
+    const void *q;                 /* [max_tokens][q_heads][layer dim] */
+    void *q_out;                   /* the turned queries: q itself (with its strides) or apart from every input */
+    int64_t k_token, k_head;       /* bytes between tokens, between heads; multiples of the element size */
+    int64_t v_token, v_head;
+    int64_t q_token, q_head;
+    int64_t q_out_token, q_out_head;
+} wf_kv_new;
+
+/*
+ * A layer's keys and values of a step's tokens into the cache: the key of token t,
+ * turned to its position step->pos[t] and rounded to its type, and its value, in
+ * slot step->slot[t] (wf_kv_extend's; -1: none, the token and its query are passed over), and the
+ * queries turned likewise into q_out.  rope may be NULL (no rotation).
+ * A layer in 16 bits has the type of the step's tensors.  In WF_E4M3, for each block that
+ * gets tokens and each head, of keys and of values apart: need is the
+ * least 2^e, -64 <= e <= 63, with 448 * 2^e at least the largest finite
+ * magnitude of the new tokens.  A block whose first new token is at place 0 gets the scale `need`;
+ * one that holds tokens before that gets the larger of its scale and `need`,
+ * and where that is `need` the tokens before are scaled and rounded anew (with scales
+ * that are powers of two that changes only what falls below 2^-6 times the new scale).  The new elements are
+ * their value over the scale, rounded to nearest, even; beyond 448 they are
+ * +-448 (infinities too), NaN stays NaN.
+ * The new tokens of a block are consecutive in the step, as wf_kv_extend gives them; places
+ * behind the last one written are left as they were.  Asynchronous on `stream`; no allocation.
+ * A slot outside the cache is passed over and reported by
+ * wf_decode_status (in WF_E4M3 what its row's blocks then hold is unspecified).  WF_EINVAL as above.
+ */
+int wf_kv_write(wf_decode *d, const wf_kv *kv, const wf_kv_step *step, const wf_kv_layer *layer, const wf_rope *rope,
+                const wf_kv_new *in, void *stream);
+
+/*
+ * scale[p][to] = scale[p][from] for every plane p and every copy {from, to} of wf_kv_reorder (copies: DEVICE int32
+ * [rows][2]; {-1, -1}: none), `heads` floats each: the scales of an 8-bit cache
+ * whose blocks wf_kv_reorder has copied.  scale: DEVICE [planes][n_blocks][heads], plane_stride floats
+ * between planes.  No block is in two copies' `to`, or in one's `to` and another's
+ * `from` (as wf_kv_reorder gives them).  A block outside the cache is passed over and reported
+ * by wf_decode_status.
+ */
+int wf_kv_copy_scales(wf_decode *d, const wf_kv *kv, const int32_t *copies, float *scale, int32_t planes,
+                      int64_t plane_stride, int32_t heads, void *stream);
 
 /* Release every device and host allocation of the context (NULL is a no-op). */
 void wf_ctx_destroy(wf_ctx *ctx);

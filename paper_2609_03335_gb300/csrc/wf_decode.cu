@@ -101,12 +101,12 @@ extern "C" int wf_decode_status(wf_decode *d, void *stream)
         const int zero = 0;
         rc = wf_cuda_check(cudaMemcpy(d->err, &zero, sizeof(int), cudaMemcpyHostToDevice), "clear error word");
         if (rc) return rc;
-        return wf_set_error(WF_EINVAL, "a table or the ring names a block outside the cache; its copy was left out");
+        return wf_set_error(WF_EINVAL, "a table, the ring, a slot or a copy names a block outside the cache; what was to be written there was left out");
     }
     return WF_OK;
 }
 
-static bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+static bool aligned(const void *p, size_t a) { return wf_aligned(p, a); }
 
 // Two ranges are the same memory or have none in common.
 static bool same_or_apart(const void *a, const void *b, size_t bytes)
@@ -115,10 +115,10 @@ static bool same_or_apart(const void *a, const void *b, size_t bytes)
     return x == y || x + bytes <= y || y + bytes <= x;
 }
 
-static int check_kv(const wf_decode *d, const wf_kv *kv, const char *what)
+int wf_check_rows(const wf_kv *kv, int32_t max_rows, const char *what)
 {
     REQUIRE(kv, "%s: the rows are NULL", what);
-    REQUIRE(kv->rows >= 1 && kv->rows <= d->lim.max_rows, "%s: rows %d outside 1..%d", what, kv->rows, d->lim.max_rows);
+    REQUIRE(kv->rows >= 1 && kv->rows <= max_rows, "%s: rows %d outside 1..%d", what, kv->rows, max_rows);
     REQUIRE(kv->row_blocks >= 1, "%s: row_blocks %d", what, kv->row_blocks);
     REQUIRE(kv->block_tokens >= 1, "%s: block_tokens %d", what, kv->block_tokens);
     REQUIRE(kv->n_blocks >= 1 && kv->n_blocks <= INT32_MAX - 1, "%s: n_blocks %d", what, kv->n_blocks);
@@ -129,6 +129,8 @@ static int check_kv(const wf_decode *d, const wf_kv *kv, const char *what)
             "%s: misaligned table, len, ring or ends", what);
     return WF_OK;
 }
+
+static int check_kv(const wf_decode *d, const wf_kv *kv, const char *what) { return wf_check_rows(kv, d->lim.max_rows, what); }
 
 extern "C" int wf_kv_extend(wf_decode *d, const wf_kv *kv, const int32_t *add, const wf_kv_step *out, void *stream)
 {

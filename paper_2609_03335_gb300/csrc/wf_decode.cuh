@@ -1,5 +1,5 @@
 // Internal definitions of the calls on a replica's rows: cache bookkeeping
-// (wf_kv.cu) and beam selection (wf_beam.cu).
+// (wf_kv.cu), beam selection (wf_beam.cu), a layer's keys and values (wf_write.cu).
 #pragma once
 
 #include "wf_internal.cuh"
@@ -39,9 +39,15 @@ constexpr int kTileCols = 256;     // columns of the tables that a CTA of the re
 constexpr int kMaxGroup = 32;      // rows of a group, beams
 constexpr int kMaxKeep = 64;
 
+inline bool wf_aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+int wf_check_rows(const wf_kv *kv, int32_t max_rows, const char *what);
 void wf_beam_scratch(int64_t rows, int64_t vocab, int sms, int64_t *parts, int64_t *units);
 int wf_extend_setup();
 int wf_launch_extend(wf_decode *d, const wf_kv *kv, const int32_t *add, const wf_kv_step *out, cudaStream_t st);
 int wf_launch_reorder(wf_decode *d, const wf_kv *kv, int32_t group, const int32_t *parent, const wf_kv *to,
                       const wf_kv_cache *cache, int32_t *copies, uint32_t *status, cudaStream_t st);
 int wf_launch_select(wf_decode *d, const wf_beam *in, const wf_beam_out *out, cudaStream_t st);
+int wf_launch_write(wf_decode *d, const wf_kv *kv, const wf_kv_step *step, const wf_kv_layer *layer, const wf_rope *rope,
+                    const wf_kv_new *in, cudaStream_t st);
+int wf_launch_copy_scales(wf_decode *d, const wf_kv *kv, const int32_t *copies, float *scale, int32_t planes, int64_t plane_stride,
+                          int32_t heads, cudaStream_t st);

@@ -28,7 +28,7 @@ EXPORTS = ("wf_problem_check", "wf_ctx_create", "wf_forecast_readiness", "wf_eva
            "wf_topk_phi", "wf_static_status", "wf_ctx_set_eval_path",
            "wf_ctx_set_batch", "wf_eval_topk_host", "wf_ctx_reserve_host",
            "wf_decode_create", "wf_decode_status", "wf_decode_destroy", "wf_kv_extend", "wf_beam_select",
-           "wf_kv_reorder")
+           "wf_kv_reorder", "wf_kv_write", "wf_kv_copy_scales")
 
 
 class WfError(RuntimeError):
@@ -97,6 +97,25 @@ class wf_kv_cache(ctypes.Structure):
                 ("plane_stride", ctypes.c_int64), ("token_bytes", ctypes.c_int64)]
 
 
+class wf_kv_layer(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("block_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p)]
+
+
+class wf_rope(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("turn", ctypes.c_void_p),
+                ("magnitude", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class wf_kv_new(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("k_token", ctypes.c_int64), ("k_head", ctypes.c_int64),
+                ("v_token", ctypes.c_int64), ("v_head", ctypes.c_int64), ("q_token", ctypes.c_int64),
+                ("q_head", ctypes.c_int64), ("q_out_token", ctypes.c_int64), ("q_out_head", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -139,6 +158,8 @@ def load_library():
         "wf_kv_extend": ([p, p, p, p, p], ctypes.c_int),
         "wf_beam_select": ([p, p, p, p], ctypes.c_int),
         "wf_kv_reorder": ([p, p, i32, p, p, p, p, p, p], ctypes.c_int),
+        "wf_kv_write": ([p, p, p, p, p, p, p], ctypes.c_int),
+        "wf_kv_copy_scales": ([p, p, p, p, i32, i64, i32, p], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
@@ -689,15 +710,37 @@ class KvMoves:
         self.device = self.status.get_device()
 
 
-def wf_kv_reorder(decode: Decode, kv: Kv, group: int, parent, to: Kv, out: KvMoves, cache=None, stream=None):
+def _check_scales(scale, kv: Kv):
+    import torch
+    if not (isinstance(scale, torch.Tensor) and scale.dtype is torch.float32 and scale.get_device() == kv.device and scale.dim() == 3
+            and scale.is_contiguous() and scale.size(1) == kv.n_blocks and scale.numel()):
+        what = f"{scale.dtype} {tuple(scale.shape)} on {scale.device}" if isinstance(scale, torch.Tensor) else type(scale).__name__
+        raise WfError(WF_EINVAL, "scale", f"is {what}; expected contiguous float32 [planes, {kv.n_blocks}, heads] on cuda:{kv.device}")
+
+
+def wf_kv_copy_scales(decode: Decode, kv: Kv, copies, scale, stream=None):
+    """The scales of an 8-bit cache (device float32 [planes, n_blocks, heads]) after the copies (KvMoves.copies) of a reordering."""
+    if kv.device != decode.device:
+        raise _apart("wf_kv_copy_scales", kv, decode)
+    _tensor(copies, "copies", "int32", 2 * kv.rows, kv.device)
+    _check_scales(scale, kv)
+    _check(load_library().wf_kv_copy_scales(decode.ptr, ctypes.byref(kv.c), copies.data_ptr(), scale.data_ptr(), scale.shape[0],
+                                            scale.stride(0), scale.shape[2], _stream_handle(stream, kv.device)),
+           "wf_kv_copy_scales")
+
+
+def wf_kv_reorder(decode: Decode, kv: Kv, group: int, parent, to: Kv, out: KvMoves, cache=None, stream=None, scale=None):
     """The rows in the order of a selection.  parent: device int32 with a row
     (or -1) for each row; to: the rows afterwards (kv itself, or another Kv on the same ring);
-    cache: a contiguous device tensor [planes, n_blocks, block_tokens, ...] or None."""
+    cache: a contiguous device tensor [planes, n_blocks, block_tokens, ...] or None; scale: the scales of a cache in
+    8 bits, a contiguous device float32 tensor [planes, n_blocks, heads], or None (wf_kv_copy_scales follows)."""
     if not kv.device == decode.device == to.device == out.device:
         raise _apart("wf_kv_reorder", kv, decode, to, out)
     _tensor(parent, "parent", "int32", kv.rows, kv.device)
     if out.rows != kv.rows:
         raise WfError(WF_EINVAL, "wf_kv_reorder", f"outputs for {out.rows} rows, {kv.rows} given")
+    if scale is not None:
+        _check_scales(scale, kv)
     cc = None
     if cache is not None:
         if not hasattr(cache, "get_device"):
@@ -712,3 +755,120 @@ def wf_kv_reorder(decode: Decode, kv: Kv, group: int, parent, to: Kv, out: KvMov
     _check(load_library().wf_kv_reorder(decode.ptr, ctypes.byref(kv.c), int(group), parent.data_ptr(),
                                         ctypes.byref(to.c), cc, out.copies.data_ptr(), out.status.data_ptr(),
                                         _stream_handle(stream, kv.device)), "wf_kv_reorder")
+    if scale is not None:
+        wf_kv_copy_scales(decode, kv, out.copies, scale, stream)
+
+
+# ---------------------------------------------------------------------------
+# A layer's tensors
+# ---------------------------------------------------------------------------
+
+class KvLayer:
+    """One layer's part of the cache (a wf_kv_layer): device tensors k, v [n_blocks, block_tokens, heads, dim] with the same
+    strides and contiguous elements, in float16 or bfloat16, or in float8_e4m3fn with a scale for each
+    block and head: k_scale, v_scale [n_blocks, heads] float32, contiguous."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        import torch
+        for name, t in (("k", k), ("v", v)):
+            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 4 and t.dtype in (torch.float16, torch.bfloat16, torch.float8_e4m3fn)
+                    and (t.stride(3) == 1 or t.size(3) == 1) and t.numel()):
+                what = f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
+                raise WfError(WF_EINVAL, name, f"is {what}; expected device [n_blocks, block_tokens, heads, dim] with contiguous "
+                                               "elements in float16, bfloat16 or float8_e4m3fn")
+        if k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.device != v.device:
+            raise WfError(WF_EINVAL, "v", f"{v.dtype} {tuple(v.shape)} with strides {v.stride()} on {v.device}; k has {k.dtype} "
+                                          f"{tuple(k.shape)}, {k.stride()}, {k.device}")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_blocks, self.block_tokens, self.heads, self.dim = k.shape
+        self.dtype, self.device = k.dtype, k.get_device()
+        if (k.dtype is torch.float8_e4m3fn) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
+            raise WfError(WF_EINVAL, "k_scale", "scales belong to layers of 8 bits, and to all of those")
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if t is not None:
+                _tensor(t, name, "float32", self.n_blocks * self.heads, self.device)
+        size = k.element_size()
+        self.c = wf_kv_layer(3 if k_scale is not None else _dtype_code(k.dtype), self.heads, self.dim, 0, k.data_ptr(), v.data_ptr(),
+                             k.stride(0) * size, k.stride(1) * size, k.stride(2) * size,
+                             None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr())
+
+
+_PI_192 = 0x3243F6A8885A308D313198A2E03707344A4093822299F31D0  # pi * 2^192, its first 194 bits
+
+
+class Rope:
+    """Rotary positions of the first `dim` elements of a head (a wf_rope): pair i turns by base^(-2i / dim) radians a position,
+    pairs (i, i + dim / 2), or with interleaved (2i, 2i + 1); turned elements grow by `magnitude`.
+    For contexts `factor` times as long as those of the training: rates are divided by the factor (positions interpolated); with
+    `context` (tokens of the training's contexts) given, those that turn more than `fast` times in it stay,
+    those that turn fewer than `slow` times are divided, and between them it goes over linearly.
+    freq: rates in radians a position [dim / 2] in place of all that."""
+
+    def __init__(self, dim: int, base: float = 10000.0, interleaved: bool = False, factor: float = 1.0, context: int = 0,
+                 slow: float = 1.0, fast: float = 32.0, magnitude: float = 1.0, freq=None, device="cuda"):
+        import math
+        import torch
+        dim = int(dim)
+        if dim < 0 or dim % 2 or dim > 128:
+            raise WfError(WF_EINVAL, "Rope", f"{dim} elements turn; an even number up to 128")
+        if not (base > 0 and factor > 0 and context >= 0 and 0 <= slow < fast and math.isfinite(magnitude)):
+            raise WfError(WF_EINVAL, "Rope", f"base {base}, factor {factor}, context {context}, slow {slow}, fast {fast}, magnitude {magnitude}")
+        if freq is None:
+            freq = [base ** (-2 * i / dim) for i in range(dim // 2)]
+            keep = [min(1.0, max(0.0, (context * f / (2 * math.pi) - slow) / (fast - slow))) if context else 0.0 for f in freq]
+            freq = [f * (k + (1 - k) / factor) for f, k in zip(freq, keep)]
+        freq = [float(f) for f in freq]
+        if len(freq) != dim // 2 or not all(math.isfinite(f) for f in freq):
+            raise WfError(WF_EINVAL, "freq", f"{len(freq)} rates; expected {dim // 2} finite ones")
+        self.dim, self.interleaved, self.magnitude, self.freq = dim, bool(interleaved), float(magnitude), freq
+        turns = []
+        for f in freq:  # f / 2 pi * 2^64, rounded down, in whole numbers
+            num, den = f.as_integer_ratio()
+            t = ((num << 192 + 63) // (den * _PI_192)) & ((1 << 64) - 1)
+            turns.append(t - (1 << 64) if t >> 63 else t)
+        self.turn = torch.tensor(turns, dtype=torch.int64, device=device)
+        self.device = self.turn.get_device()
+        self.c = wf_rope(dim, int(self.interleaved), self.turn.data_ptr() if dim else None, self.magnitude, 0)
+
+
+def _heads(t, name: str, dtype, tokens: int, heads: int, dim: int, device: int):
+    """(address, bytes between tokens, bytes between heads) of a tensor [tokens, heads, dim] with contiguous elements."""
+    shape = t.shape if hasattr(t, "stride") else ()
+    if len(shape) != 3 or shape[0] != tokens or shape[1] != heads or shape[2] != dim or t.dtype is not dtype or t.get_device() != device \
+            or t.stride(2) != 1:
+        what = f"{t.dtype} {tuple(t.shape)} on {t.device}" if hasattr(t, "stride") else type(t).__name__
+        raise WfError(WF_EINVAL, name, f"is {what}; expected {dtype} [{tokens}, {heads}, {dim}] with contiguous elements on cuda:{device}")
+    return t.data_ptr(), 2 * t.stride(0), 2 * t.stride(1)
+
+
+def _check_layer(where: str, kv: Kv, step: KvStep, layer: KvLayer, *others):
+    if not kv.device == step.device == layer.device or any(o.device != kv.device for o in others):
+        raise _apart(where, kv, step, layer, *others)
+    if step.rows != kv.rows:
+        raise WfError(WF_EINVAL, where, f"a step of {step.rows} rows, {kv.rows} given")
+    if layer.n_blocks != kv.n_blocks or layer.block_tokens != kv.block_tokens:
+        raise WfError(WF_EINVAL, where, f"a layer of {layer.n_blocks} blocks of {layer.block_tokens} tokens; the rows' are "
+                                        f"{kv.n_blocks} of {kv.block_tokens}")
+
+
+def wf_kv_write(decode: Decode, kv: Kv, step: KvStep, layer: KvLayer, k, v, q=None, q_out=None, rope: Rope | None = None, stream=None):
+    """A step's keys and values [max_tokens, heads, dim] into the layer's cache, keys (and queries q [max_tokens,
+    q_heads, dim], into q_out or in place) turned to their positions by `rope`.  Tensors in float16 or
+    bfloat16, of the layer's type where that has 16 bits; tokens and heads may be strided."""
+    _check_layer("wf_kv_write", kv, step, layer, decode, *(() if rope is None else (rope,)))
+    dtype, n, dim, dev = getattr(k, "dtype", None), step.max_tokens, layer.dim, kv.device
+    code = _dtype_code(dtype)
+    kp = _heads(k, "k", dtype, n, layer.heads, dim, dev)
+    vp = _heads(v, "v", dtype, n, layer.heads, dim, dev)
+    q_heads, qp, op = 0, (None, 0, 0), (None, 0, 0)
+    if q is not None:
+        q_heads = q.shape[1] if hasattr(q, "shape") and len(q.shape) == 3 else 1
+        qp = op = _heads(q, "q", dtype, n, q_heads, dim, dev)
+        if q_out is not None:
+            op = _heads(q_out, "q_out", dtype, n, q_heads, dim, dev)
+    elif q_out is not None:
+        raise WfError(WF_EINVAL, "q_out", "given without q")
+    c = wf_kv_new(-1 if code is None else code, q_heads, kp[0], vp[0], qp[0], op[0], kp[1], kp[2], vp[1], vp[2], qp[1], qp[2], op[1], op[2])
+    _check(load_library().wf_kv_write(decode.ptr, ctypes.byref(kv.c), ctypes.byref(step.c), ctypes.byref(layer.c),
+                                      None if rope is None else ctypes.byref(rope.c), ctypes.byref(c),
+                                      _stream_handle(stream, dev)), "wf_kv_write")
