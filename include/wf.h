@@ -708,7 +708,7 @@ typedef struct {
     int64_t block_stride;  /* bytes, and the next two: multiples of 16, >= 0 */
     int64_t token_stride;
     int64_t head_stride;
-    float *k_scale;        /* [n_blocks][heads], and v_scale: WF_E4M3 only, else NULL */
+    float *k_scale;        /* [n_blocks][heads], and v_scale: WF_E4M3 only, else NULL; numbers >= 0, of values 2^-64..2^63 (or 0) */
     float *v_scale;
 } wf_kv_layer;
 
@@ -772,6 +772,66 @@ int wf_kv_write(wf_decode *d, const wf_kv *kv, const wf_kv_step *step, const wf_
  */
 int wf_kv_copy_scales(wf_decode *d, const wf_kv *kv, const int32_t *copies, float *scale, int32_t planes,
                       int64_t plane_stride, int32_t heads, void *stream);
+
+typedef struct wf_attn wf_attn;
+
+/* Largest sizes of the calls on a wf_attn. */
+typedef struct {
+    int32_t max_rows;   /* 1..65536 */
+    int32_t max_heads;  /* query heads, 1..1024 */
+    int32_t dim;        /* elements of a head: 64 or 128 */
+    int32_t reserved;   /* 0 */
+} wf_attn_limits;
+
+/*
+ * Scratch of wf_attend on device `device`: the parts of rows whose positions are
+ * split among the GPU's blocks, at most 64 MiB whatever the lengths.  The calls allocate
+ * nothing more.  One wf_attn serves one stream at a time.  Returns
+ * WF_OK, WF_EINVAL, WF_ENOMEM or WF_ECUDA.
+ */
+int wf_attn_create(const wf_attn_limits *limits, int device, wf_attn **out);
+
+/*
+ * Synchronize `stream` and report (then clear) what earlier calls found on
+ * the device: WF_EINVAL when a table named a block outside the cache or a row's
+ * lengths contradict each other, WF_ETIMEOUT when a bounded wait expired, else WF_OK.
+ */
+int wf_attn_status(wf_attn *a, void *stream);
+
+/* Release the scratch (NULL is a no-op). */
+void wf_attn_destroy(wf_attn *a);
+
+/* wf_attend's tensors; DEVICE pointers on 16-byte boundaries, row t is the step's token t, strides in bytes and multiples of 16. */
+typedef struct {
+    int32_t dtype;       /* of q and out: WF_F16 or WF_BF16, the layer's type where that has 16 bits */
+    int32_t heads;       /* query heads, a multiple of the layer's: head h reads the layer's head h / (heads / layer heads) */
+    float scale;         /* of the products, usually dim^-0.5 */
+    int32_t new_tokens;  /* the most new tokens that a row is expected to have, 0: unknown.  A hint: it chooses how
+                            the call is launched (1 for a step of decoding), never what it computes */
+    const void *q;       /* [max_tokens][heads][dim] */
+    void *out;           /* [max_tokens][heads][dim], apart from every input */
+    int64_t q_token, q_head;
+    int64_t out_token, out_head;
+} wf_attn_in;
+
+/*
+ * Attention of a step's tokens over their rows' cached keys and values (as
+ * wf_kv_write has put them, the step's own among them), causal.  Row r has step->len[r] tokens cached, its
+ * new ones, step->start[r] .. step->start[r + 1] - 1 in the step, at its last positions; for a token at position p and
+ * head h
+ *   out = sum over j <= p of softmax(scale * q . k[j])[j] * v[j]
+ * with products and sums in 32 bits; the weights of a sum are rounded to the type of the values that they
+ * multiply (over a layer in 8 bits: to 16-bit floats), and out once.  Rows with one new
+ * token (decoding), with a prompt's chunk and with a whole prompt may be in one step, in any order.
+ * Rows without new tokens have no output, and places of out behind the step's last
+ * token are left as they were.  What the cache holds behind a row's tokens does not count, whatever
+ * it is.  A value of the row's step that is no finite number may reach the outputs of all its tokens in the step.
+ * Tables of a row name blocks of the cache; one that does not is read as block 0 and reported by wf_attn_status, as are
+ * rows whose lengths contradict each other (fewer tokens than new ones, more than the table holds, more than the step), which are passed over.
+ * The result does not depend on the order of arrival of the GPU's blocks; the last bits of a row's
+ * may depend on the other rows' lengths.  Asynchronous on `stream`; no allocation.  WF_EINVAL as above.
+ */
+int wf_attend(wf_attn *a, const wf_kv *kv, const wf_kv_step *step, const wf_kv_layer *layer, const wf_attn_in *in, void *stream);
 
 /* Release every device and host allocation of the context (NULL is a no-op). */
 void wf_ctx_destroy(wf_ctx *ctx);

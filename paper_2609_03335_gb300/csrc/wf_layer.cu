@@ -1,6 +1,8 @@
 // The calls on a layer's tensors, host side: the checks of their arguments.
 #include <cmath>
+#include <cstdlib>
 
+#include "wf_attend.cuh"
 #include "wf_decode.cuh"
 #include "wf_layer.cuh"
 
@@ -91,4 +93,110 @@ extern "C" int wf_kv_copy_scales(wf_decode *d, const wf_kv *kv, const int32_t *c
             (long long)plane_stride, (long long)kv->n_blocks * heads);
     rc = wf_cuda_check(cudaSetDevice(d->device), "cudaSetDevice");
     return rc ? rc : wf_launch_copy_scales(d, kv, copies, scale, planes, plane_stride, heads, (cudaStream_t)stream);
+}
+
+extern "C" int wf_attn_create(const wf_attn_limits *lim, int device, wf_attn **out)
+{
+    REQUIRE(out, "out is NULL");
+    *out = nullptr;
+    REQUIRE(lim, "limits is NULL");
+    REQUIRE(lim->max_rows >= 1 && lim->max_rows <= 65536, "max_rows %d outside 1..65536", lim->max_rows);
+    REQUIRE(lim->max_heads >= 1 && lim->max_heads <= 1024, "max_heads %d outside 1..1024", lim->max_heads);
+    REQUIRE(lim->dim == 64 || lim->dim == 128, "heads of %d elements; 64 or 128", lim->dim);
+    REQUIRE(lim->reserved == 0, "reserved %d", lim->reserved);
+    REQUIRE(device >= 0, "device %d", device);
+    int rc = wf_cuda_check(cudaSetDevice(device), "cudaSetDevice");
+    if (rc) return rc;
+    wf_attn *a = (wf_attn *)calloc(1, sizeof(wf_attn));
+    if (!a) return wf_set_error(WF_ENOMEM, "host allocation of the attention scratch");
+    a->device = device;
+    a->lim = *lim;
+    rc = wf_cuda_check(cudaDeviceGetAttribute(&a->sms, cudaDevAttrMultiProcessorCount, device), "device attributes");
+    if (!rc) rc = wf_attend_setup(a);
+    if (rc) { wf_attn_destroy(a); return rc; }
+    int ctas = 0;
+    wf_attend_scratch(a, &a->part_bytes, &ctas);
+    const size_t zeroed = 256 + (4 * (size_t)ctas + 255) / 256 * 256;
+    rc = wf_cuda_check(cudaMalloc(&a->mem, zeroed + a->part_bytes), "cudaMalloc(attention scratch)");
+    if (!rc) rc = wf_cuda_check(cudaMemset(a->mem, 0, zeroed), "clear the attention scratch");
+    // The clearing runs on the default stream; the calls may use any other.
+    if (!rc) rc = wf_cuda_check(cudaDeviceSynchronize(), "cudaDeviceSynchronize");
+    if (rc) { wf_attn_destroy(a); return rc; }
+    a->err = (int *)a->mem;
+    a->arrive = (uint32_t *)((uint8_t *)a->mem + 256);
+    a->part = (float *)((uint8_t *)a->mem + zeroed);
+    *out = a;
+    return WF_OK;
+}
+
+extern "C" void wf_attn_destroy(wf_attn *a)
+{
+    if (!a) return;
+    if (a->mem) {
+        cudaSetDevice(a->device);
+        cudaFree(a->mem);
+    }
+    free(a);
+}
+
+extern "C" int wf_attn_status(wf_attn *a, void *stream)
+{
+    REQUIRE(a, "NULL attention scratch");
+    int rc = wf_cuda_check(cudaSetDevice(a->device), "cudaSetDevice");
+    if (!rc) rc = wf_cuda_check(cudaStreamSynchronize((cudaStream_t)stream), "cudaStreamSynchronize");
+    int err = 0;
+    if (!rc) rc = wf_cuda_check(cudaMemcpy(&err, a->err, sizeof(int), cudaMemcpyDeviceToHost), "read error word");
+    if (rc || !err) return rc;
+    rc = wf_cuda_check(cudaMemset(a->err, 0, sizeof(int)), "clear error word");
+    if (!rc) rc = wf_cuda_check(cudaDeviceSynchronize(), "cudaDeviceSynchronize");
+    if (rc) return rc;
+    if (err == 2) return wf_set_error(WF_ETIMEOUT, "a bounded wait expired; outputs are invalid");
+    return wf_set_error(WF_EINVAL, "a table names a block outside the cache, or a row's lengths contradict each other");
+}
+
+static int check_attn(const void *p, int64_t token, int64_t head, const char *what, const char *name)
+{
+    REQUIRE(p, "%s: NULL %s", what, name);
+    REQUIRE(wf_aligned(p, 16) && token % 16 == 0 && head % 16 == 0, "%s: %s or its strides %lld, %lld not on 16 bytes", what, name,
+            (long long)token, (long long)head);
+    return WF_OK;
+}
+
+extern "C" int wf_attend(wf_attn *at, const wf_kv *kv, const wf_kv_step *step, const wf_kv_layer *layer, const wf_attn_in *in, void *stream)
+{
+    const char *what = "wf_attend";
+    REQUIRE(at, "NULL attention scratch");
+    int rc = wf_check_rows(kv, at->lim.max_rows, what);
+    if (!rc) rc = check_step(kv, step, what);
+    if (rc) return rc;
+    REQUIRE(in, "%s: the tensors are NULL", what);
+    rc = check_layer(layer, in->dtype, what);
+    if (rc) return rc;
+    REQUIRE(layer->dim == at->lim.dim, "%s: heads of %d elements, scratch for %d", what, layer->dim, at->lim.dim);
+    REQUIRE(in->heads >= 1 && in->heads <= at->lim.max_heads && in->heads % layer->heads == 0,
+            "%s: %d query heads; a multiple of %d, up to %d", what, in->heads, layer->heads, at->lim.max_heads);
+    REQUIRE(step->max_tokens * in->heads <= INT32_MAX, "%s: %lld tokens of %d heads", what, (long long)step->max_tokens, in->heads);
+    REQUIRE(std::isfinite(in->scale), "%s: scale %g", what, in->scale);
+    REQUIRE(in->new_tokens >= 0, "%s: new_tokens %d", what, in->new_tokens);
+    REQUIRE(step->start && step->len && wf_aligned(step->start, 4) && wf_aligned(step->len, 4), "%s: NULL or misaligned start or len", what);
+    rc = check_attn(in->q, in->q_token, in->q_head, what, "queries");
+    if (!rc) rc = check_attn(in->out, in->out_token, in->out_head, what, "outputs");
+    if (!rc) rc = wf_cuda_check(cudaSetDevice(at->device), "cudaSetDevice");
+    if (rc) return rc;
+
+    AttendArgs a{};
+    a.table = kv->table, a.start = step->start, a.len = step->len;
+    a.table_stride = kv->table_stride / 4, a.max_tokens = step->max_tokens;
+    a.rows = kv->rows, a.row_blocks = kv->row_blocks, a.bs = kv->block_tokens, a.n_blocks = kv->n_blocks;
+    a.k = (const uint8_t *)layer->k, a.v = (const uint8_t *)layer->v;
+    a.block_stride = layer->block_stride, a.token_stride = layer->token_stride, a.head_stride = layer->head_stride;
+    a.k_scale = layer->k_scale, a.v_scale = layer->v_scale, a.kv = layer->heads;
+    a.q = (const uint8_t *)in->q, a.out = (uint8_t *)in->out;
+    a.q_token = in->q_token, a.q_head = in->q_head, a.o_token = in->out_token, a.o_head = in->out_head;
+    a.group = in->heads / layer->heads;
+    a.by_bs = wf_make_div(a.bs), a.by_group = wf_make_div(a.group);
+    a.scale = in->scale * 1.4426950408889634f;
+    a.above = 0, a.most = INT64_MAX;
+    a.part = at->part, a.arrive = at->arrive, a.err = at->err;
+    return wf_launch_attend(at, a, in->dtype, layer->dim, layer->dtype == WF_E4M3, (cudaStream_t)stream);
 }

@@ -28,7 +28,8 @@ EXPORTS = ("wf_problem_check", "wf_ctx_create", "wf_forecast_readiness", "wf_eva
            "wf_topk_phi", "wf_static_status", "wf_ctx_set_eval_path",
            "wf_ctx_set_batch", "wf_eval_topk_host", "wf_ctx_reserve_host",
            "wf_decode_create", "wf_decode_status", "wf_decode_destroy", "wf_kv_extend", "wf_beam_select",
-           "wf_kv_reorder", "wf_kv_write", "wf_kv_copy_scales")
+           "wf_kv_reorder", "wf_kv_write", "wf_kv_copy_scales",
+           "wf_attn_create", "wf_attn_status", "wf_attn_destroy", "wf_attend")
 
 
 class WfError(RuntimeError):
@@ -116,6 +117,16 @@ class wf_kv_new(ctypes.Structure):
                 ("q_head", ctypes.c_int64), ("q_out_token", ctypes.c_int64), ("q_out_head", ctypes.c_int64)]
 
 
+class wf_attn_limits(ctypes.Structure):
+    _fields_ = [("max_rows", ctypes.c_int32), ("max_heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class wf_attn_in(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("heads", ctypes.c_int32), ("scale", ctypes.c_float), ("new_tokens", ctypes.c_int32),
+                ("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("q_token", ctypes.c_int64), ("q_head", ctypes.c_int64),
+                ("out_token", ctypes.c_int64), ("out_head", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -159,6 +170,10 @@ def load_library():
         "wf_beam_select": ([p, p, p, p], ctypes.c_int),
         "wf_kv_reorder": ([p, p, i32, p, p, p, p, p, p], ctypes.c_int),
         "wf_kv_write": ([p, p, p, p, p, p, p], ctypes.c_int),
+        "wf_attn_create": ([p, ctypes.c_int, p], ctypes.c_int),
+        "wf_attn_status": ([p, p], ctypes.c_int),
+        "wf_attn_destroy": ([p], None),
+        "wf_attend": ([p, p, p, p, p, p], ctypes.c_int),
         "wf_kv_copy_scales": ([p, p, p, p, i32, i64, i32, p], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
@@ -872,3 +887,44 @@ def wf_kv_write(decode: Decode, kv: Kv, step: KvStep, layer: KvLayer, k, v, q=No
     _check(load_library().wf_kv_write(decode.ptr, ctypes.byref(kv.c), ctypes.byref(step.c), ctypes.byref(layer.c),
                                       None if rope is None else ctypes.byref(rope.c), ctypes.byref(c),
                                       _stream_handle(stream, dev)), "wf_kv_write")
+
+
+class Attn:
+    """Owns a wf_attn: the scratch of wf_attend, for calls of up to these rows and query heads, of heads of `dim` elements (64 or 128)."""
+
+    def __init__(self, max_rows: int, heads: int, dim: int, device: int = 0):
+        self.limits = wf_attn_limits(int(max_rows), int(heads), int(dim), 0)
+        self.device, self.dim = int(device), int(dim)
+        self.ptr = ctypes.c_void_p()
+        _check(load_library().wf_attn_create(ctypes.byref(self.limits), self.device, ctypes.byref(self.ptr)), "wf_attn_create")
+
+    def close(self):
+        if self.ptr:
+            load_library().wf_attn_destroy(self.ptr)
+            self.ptr = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def wf_attn_status(attn: Attn, stream=None):
+    _check(load_library().wf_attn_status(attn.ptr, _stream_handle(stream, attn.device)), "wf_attn_status")
+
+
+def wf_attend(attn: Attn, kv: Kv, step: KvStep, layer: KvLayer, q, out, scale: float | None = None, new: int = 0, stream=None):
+    """Causal attention of a step's tokens over their rows' cached keys and values (the step's own among them): q, out
+    [max_tokens, heads, dim] in float16 or bfloat16, tokens and heads strided by multiples of 16 bytes.
+    scale: of the products (None: dim^-0.5); new: the most new tokens that a row is expected to have, a hint for the
+    launch (1: a step of decoding; 0: unknown)."""
+    _check_layer("wf_attend", kv, step, layer, attn)
+    dtype, n, dim, dev = getattr(q, "dtype", None), step.max_tokens, layer.dim, kv.device
+    code = _dtype_code(dtype)
+    heads = q.shape[1] if hasattr(q, "shape") and len(q.shape) == 3 else 1
+    qp = _heads(q, "q", dtype, n, heads, dim, dev)
+    op = _heads(out, "out", dtype, n, heads, dim, dev)
+    c = wf_attn_in(-1 if code is None else code, heads, dim ** -0.5 if scale is None else scale, new, qp[0], op[0], qp[1], qp[2], op[1], op[2])
+    _check(load_library().wf_attend(attn.ptr, ctypes.byref(kv.c), ctypes.byref(step.c), ctypes.byref(layer.c), ctypes.byref(c),
+                                    _stream_handle(stream, dev)), "wf_attend")

@@ -58,10 +58,11 @@ def write8(cache, scale, slot, bs, x):
                 cache[b, first + i, h] = eight(x[t, h] / now)
 
 
-def attend(q, k, v, table, start, length, bs, scale, out):
-    """q [tokens, heads, dim]; k, v [n_blocks, bs, kv heads, dim] values; out is filled in place and returned, with the sum over
-    a row's positions of |softmax| |v| beside it (what errors are relative to)."""
-    size = np.zeros(out.shape)
+def attend(q, k, v, table, start, length, bs, scale, out, v_scale=None):
+    """q [tokens, heads, dim]; k, v [n_blocks, bs, kv heads, dim] values; out is filled in place and returned, and beside it what
+    errors are relative to: the sum over a row's positions of |softmax| |v|, and the largest softmax times scale of the value's block
+    (v_scale [n_blocks, kv heads] or 1) times the sum of |v| over that scale."""
+    size, small = np.zeros(out.shape), np.zeros(out.shape)
     group = q.shape[1] // k.shape[2]
     for r in range(len(length)):
         n = int(start[r + 1] - start[r])
@@ -72,6 +73,8 @@ def attend(q, k, v, table, start, length, bs, scale, out):
         blocks, place = table[r, p // bs], p % bs
         for h in range(q.shape[1]):
             kh, vh = k[blocks, place, h // group], v[blocks, place, h // group]
+            f = np.ones(total) if v_scale is None else v_scale[blocks, h // group]
+            bare = np.cumsum(np.abs(vh) / f[:, None], 0)
             for i in range(n):
                 last = total - n + i + 1
                 x = scale * (kh[:last] @ q[start[r] + i, h])
@@ -79,4 +82,5 @@ def attend(q, k, v, table, start, length, bs, scale, out):
                 w /= w.sum()
                 out[start[r] + i, h] = w @ vh[:last]
                 size[start[r] + i, h] = w @ np.abs(vh[:last])
-    return out, size
+                small[start[r] + i, h] = (w * f[:last]).max() * bare[last - 1]
+    return out, size, small

@@ -22,6 +22,20 @@ def test_calls_refuse_a_null_handle(wf):
     L = wf.load_library()
     assert L.wf_kv_write(None, None, None, None, None, None, None) == wf.WF_EINVAL
     assert L.wf_kv_copy_scales(None, None, None, None, 1, 0, 1, None) == wf.WF_EINVAL
+    assert L.wf_attend(None, None, None, None, None, None) == wf.WF_EINVAL
+    assert L.wf_attn_status(None, None) == wf.WF_EINVAL
+    L.wf_attn_destroy(None)
+
+
+def test_attn_create_refuses_sizes_out_of_range(wf):
+    L, out = wf.load_library(), ctypes.c_void_p()
+    for bad in ((0, 4, 64, 0), (65537, 4, 64, 0), (1, 0, 64, 0), (1, 1025, 64, 0), (1, 4, 96, 0), (1, 4, 64, 1)):
+        assert L.wf_attn_create(ctypes.byref(wf.wf_attn_limits(*bad)), 0, ctypes.byref(out)) == wf.WF_EINVAL, bad
+        assert wf.wf_last_error() and not out
+    lim = wf.wf_attn_limits(1, 1, 64, 0)
+    assert L.wf_attn_create(None, 0, ctypes.byref(out)) == wf.WF_EINVAL
+    assert L.wf_attn_create(ctypes.byref(lim), 0, None) == wf.WF_EINVAL
+    assert L.wf_attn_create(ctypes.byref(lim), -1, ctypes.byref(out)) == wf.WF_EINVAL
 
 
 def test_turns_are_rates_in_whole_numbers(wf):
@@ -82,5 +96,5 @@ def test_plain_rotation_by_hand():
 def test_plain_attention_by_hand():
     k = np.zeros((2, 2, 1, 1))
     v = np.array([[1.0, 2.0], [3.0, 5.0]]).reshape(2, 2, 1, 1)
-    out, _ = ref.attend(np.ones((3, 1, 1)), k, v, np.array([[1, 0], [0, 1]]), [0, 2, 2], [3, 0], 2, 1.0, np.full((3, 1, 1), 9.0))
+    out = ref.attend(np.ones((3, 1, 1)), k, v, np.array([[1, 0], [0, 1]]), [0, 2, 2], [3, 0], 2, 1.0, np.full((3, 1, 1), 9.0))[0]
     assert np.allclose(out[:, 0, 0], [4.0, 3.0, 9.0])  # positions 0..1, then 0..2 of blocks 1, 0; the rest stays
