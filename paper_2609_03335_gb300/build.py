@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libwf.so")
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["wf_ctx.cu", "wf_slots.cpp", "wf_forecast.cu", "wf_eval.cu", "wf_sweep.cu", "wf_batch.cu", "wf_stoch.cu", "wf_topk.cu",
            "wf_search.cu", "wf_construct.cu", "wf_host.cu", "wf_decode.cu", "wf_kv.cu", "wf_beam.cu", "wf_layer.cu",
-           "wf_write.cu", "wf_attend.cu"]
+           "wf_write.cu", "wf_attend.cu", "wf_prompt.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
          "--expt-relaxed-constexpr", "-I", os.path.join(ROOT, "include")]

@@ -76,3 +76,6 @@ __device__ __forceinline__ int32_t block_at(const AttendArgs &a, const int32_t *
 int wf_attend_setup(wf_attn *a);
 void wf_attend_scratch(const wf_attn *a, size_t *part_bytes, int *ctas);
 int wf_launch_attend(wf_attn *at, const AttendArgs &args, int dtype, int dim, bool eight, cudaStream_t st);
+int wf_prompt_setup(wf_attn *a);
+size_t wf_prompt_scratch(const wf_attn *a);
+int wf_launch_prompt(wf_attn *at, const AttendArgs &args, int dtype, int dim, bool eight, cudaStream_t st);

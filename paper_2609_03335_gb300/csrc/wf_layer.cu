@@ -1,4 +1,5 @@
 // The calls on a layer's tensors, host side: the checks of their arguments.
+#include <algorithm>
 #include <cmath>
 #include <cstdlib>
 
@@ -113,9 +114,12 @@ extern "C" int wf_attn_create(const wf_attn_limits *lim, int device, wf_attn **o
     a->lim = *lim;
     rc = wf_cuda_check(cudaDeviceGetAttribute(&a->sms, cudaDevAttrMultiProcessorCount, device), "device attributes");
     if (!rc) rc = wf_attend_setup(a);
+    if (!rc) rc = wf_prompt_setup(a);
     if (rc) { wf_attn_destroy(a); return rc; }
     int ctas = 0;
     wf_attend_scratch(a, &a->part_bytes, &ctas);
+    ctas = std::max(ctas, a->sms);
+    a->part_bytes = std::max(a->part_bytes, wf_prompt_scratch(a));
     const size_t zeroed = 256 + (4 * (size_t)ctas + 255) / 256 * 256;
     rc = wf_cuda_check(cudaMalloc(&a->mem, zeroed + a->part_bytes), "cudaMalloc(attention scratch)");
     if (!rc) rc = wf_cuda_check(cudaMemset(a->mem, 0, zeroed), "clear the attention scratch");
@@ -154,6 +158,8 @@ extern "C" int wf_attn_status(wf_attn *a, void *stream)
     return wf_set_error(WF_EINVAL, "a table names a block outside the cache, or a row's lengths contradict each other");
 }
 
+constexpr int64_t kFew = 32;
+
 static int check_attn(const void *p, int64_t token, int64_t head, const char *what, const char *name)
 {
     REQUIRE(p, "%s: NULL %s", what, name);
@@ -176,7 +182,7 @@ extern "C" int wf_attend(wf_attn *at, const wf_kv *kv, const wf_kv_step *step, c
     REQUIRE(in->heads >= 1 && in->heads <= at->lim.max_heads && in->heads % layer->heads == 0,
             "%s: %d query heads; a multiple of %d, up to %d", what, in->heads, layer->heads, at->lim.max_heads);
     REQUIRE(step->max_tokens * in->heads <= INT32_MAX, "%s: %lld tokens of %d heads", what, (long long)step->max_tokens, in->heads);
-    REQUIRE(std::isfinite(in->scale), "%s: scale %g", what, in->scale);
+    REQUIRE(std::isfinite(in->scale) && in->scale >= 0, "%s: scale %g", what, in->scale);
     REQUIRE(in->new_tokens >= 0, "%s: new_tokens %d", what, in->new_tokens);
     REQUIRE(step->start && step->len && wf_aligned(step->start, 4) && wf_aligned(step->len, 4), "%s: NULL or misaligned start or len", what);
     rc = check_attn(in->q, in->q_token, in->q_head, what, "queries");
@@ -196,7 +202,17 @@ extern "C" int wf_attend(wf_attn *at, const wf_kv *kv, const wf_kv_step *step, c
     a.group = in->heads / layer->heads;
     a.by_bs = wf_make_div(a.bs), a.by_group = wf_make_div(a.group);
     a.scale = in->scale * 1.4426950408889634f;
-    a.above = 0, a.most = INT64_MAX;
     a.part = at->part, a.arrive = at->arrive, a.err = at->err;
-    return wf_launch_attend(at, a, in->dtype, layer->dim, layer->dtype == WF_E4M3, (cudaStream_t)stream);
+    // Rows of up to kFew queries to a key head go to the kernel of 16-query tiles, the others to that of 128-query tiles.  Where no row is
+    // expected to have more (or none can), one launch takes them all.
+    const bool eight = layer->dtype == WF_E4M3;
+    const int64_t expected = in->new_tokens ? std::min<int64_t>(in->new_tokens, step->max_tokens) : step->max_tokens;
+    a.above = 0, a.most = INT64_MAX;
+    if (expected * a.group > kFew) {
+        AttendArgs b = a;
+        b.above = kFew, a.most = kFew;
+        rc = wf_launch_prompt(at, b, in->dtype, layer->dim, eight, (cudaStream_t)stream);
+        if (rc) return rc;
+    }
+    return wf_launch_attend(at, a, in->dtype, layer->dim, eight, (cudaStream_t)stream);
 }
