@@ -35,6 +35,7 @@ struct AttendArgs {
     float scale;         // log2(e) times the caller's
     // the rows that a launch takes: more than `above` and at most `most` new tokens times group
     int64_t above, most;
+    int32_t tile_q;      // queries of a tile of wf_prompt.cu: whole tokens of the group, up to 128
     float *part;
     uint32_t *arrive;
     int *err;

@@ -7,7 +7,8 @@
 //
 //   warps 0-3, 4-7   a thread per query of A, B: scores from TMEM, maximum, powers, weights back as 16-bit numbers;
 //                    where a maximum has grown by more than 2^8, O is shrunk (not before: weights up to 2^8 lose nothing)
-//   warps 8-11       copies of K, V and Q: the blocks' table, then 16 bytes at a time (8 bits: through registers, to halves)
+//   warp 14          copies of K, V and Q by tensor maps: the blocks' table, then a box of positions of one block at a time
+//   warps 8-11       copies 16 bytes at a time where boxes do not fit (blocks that are no multiple of 8 positions), and 8 bits to halves
 //   warp 13          which units come next
 //   warp 12          the products, in the order  S_A(0) S_B(0) | PV_A(j) S_A(j+1) PV_B(j) S_B(j+1) | ...
 //                    so that one tile's powers run beside the other's products
@@ -20,6 +21,8 @@
 #include <algorithm>
 #include <type_traits>
 
+#include <cuda.h>
+
 #include "wf_attend.cuh"
 #include "wf_decode.cuh"
 
@@ -29,6 +32,7 @@ constexpr int kThreads = 512;
 constexpr int kQ = 128, kPair = 2 * kQ;   // queries of a tile, of a unit
 constexpr int kKeys = 128;                // positions of a tile
 constexpr int kLoaders = 128;
+constexpr int kRaw = 3;                   // tiles in 8 bits under way
 constexpr int kFixed = 2;                 // tiles that a unit's beginning and end are worth
 constexpr float kSlack = 8.f;             // log2 of what a maximum may grow by before O is shrunk
 constexpr float kLeastScale = 0x1p-64f;
@@ -37,20 +41,33 @@ template <bool E, int D> struct Shape {
     static constexpr int kRow = 2 * D;                       // bytes of a key or query in shared memory
     static constexpr int kHalf = kKeys * 128;                // bytes of 64 elements of a tile
     static constexpr int kTile = kKeys * kRow;
-    static constexpr int kStages = E ? 4 : D == 128 ? 5 : 8;
+    static constexpr int kStages = D == 64 ? 8 : E ? 3 : 5;
     static constexpr int kScales = E ? 3 * kKeys * 4 : 0;    // of a stage: keys' scales, log2 and reciprocal of values'
     static constexpr int kQBytes = 2 * kTile;
-    static constexpr int kSmem = 1024 + kQBytes + kStages * (kTile + kScales) + kKeys * 8;
+    static constexpr int kRawBytes = E ? kRaw * kKeys * D : 0;
+    static constexpr int kSmem = 1024 + kQBytes + kRawBytes + kStages * (kTile + kScales) + kKeys * 8;
     static_assert(kSmem + 1024 <= 227 * 1024, "shared memory");  // with what is static
+};
+
+struct PromptArgs {
+    AttendArgs a;
+    int32_t box;     // positions of a box of the maps k and v, 0: they are not used
+    int32_t map_q;   // whether q is
+    CUtensorMap k, v, q;
 };
 
 constexpr int kUnits = 4;  // that the roles may be apart
 
-enum { kBarQFull, kBarQEmpty, kBarS, kBarP = kBarS + 2, kBarO = kBarP + 2, kBarDrain = kBarO + 2, kBarFull, kBarUnit = kBarFull + 16, kBars = kBarUnit + 2 * kUnits };
+enum { kBarQFull, kBarQEmpty, kBarS, kBarP = kBarS + 2, kBarO = kBarP + 4, kBarDrain = kBarO + 2, kBarFull, kBarUnit = kBarFull + 16, kBarRaw = kBarUnit + 2 * kUnits,
+       kBars = kBarRaw + 2 * kRaw };
 
 __device__ __forceinline__ uint32_t smem_of(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(n) : "memory"); }
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
@@ -77,6 +94,17 @@ __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile
 __device__ __forceinline__ void copy16(uint32_t to, const void *from, bool there)
 {
     asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+// A box of a tensor map from these coordinates; its bytes arrive at bar.
+__device__ __forceinline__ void copy_box4(uint32_t to, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2, int c3)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(to), "l"(map),
+                 "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+__device__ __forceinline__ void copy_box3(uint32_t to, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(to), "l"(map),
+                 "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -137,23 +165,43 @@ __device__ __forceinline__ float power(float x)
     return r;
 }
 
+// Two at once.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 r;
+    asm("{ .reg .b64 a, b, c, d;\n"
+        "  mov.b64 a, {%2, %3};\n  mov.b64 b, {%4, %5};\n  mov.b64 c, {%6, %7};\n"
+        "  fma.rn.f32x2 d, a, b, c;\n"
+        "  mov.b64 {%0, %1}, d; }" : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 r;
+    asm("{ .reg .b64 a, b, d;\n"
+        "  mov.b64 a, {%2, %3};\n  mov.b64 b, {%4, %5};\n"
+        "  add.rn.f32x2 d, a, b;\n"
+        "  mov.b64 {%0, %1}, d; }" : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+
 // ---------------------------------------------------------------------------
 // The line of work
 // ---------------------------------------------------------------------------
 
-// Weights in 1 / (128 group) of a tile: unit i of a row's key head (queries 256 i ..) sees `have` cached positions and up to
-// 256 (i + 1) / group of the step's; the sum over units 0 .. i - 1 is i W + 128 i (i + 1), W = group (128 kFixed + have).
+// Weights in 1 / (128 group) of a tile: unit i of a row's key head (queries 2 t i .., t = tile_q) sees `have` cached positions and up to
+// 2 t (i + 1) / group of the step's; the sum over units 0 .. i - 1 is i W + t i (i + 1), W = group (128 kFixed + have).
 struct Line {
-    int64_t w;
+    int64_t w, tile_q;
     int64_t units;
-    __device__ __forceinline__ int64_t upto(int64_t i) const { return i * w + 128 * i * (i + 1); }
+    __device__ __forceinline__ int64_t upto(int64_t i) const { return i * w + tile_q * i * (i + 1); }
     __device__ __forceinline__ int64_t head() const { return upto(units); }
 };
 
 __device__ __forceinline__ Line line_of(const AttendArgs &a, const Row &row)
 {
     const int64_t m = taken(a, row);
-    return {(int64_t)a.group * (kKeys * kFixed + row.len - row.n), (m + kPair - 1) / kPair};
+    return {(int64_t)a.group * (kKeys * kFixed + row.len - row.n), a.tile_q, (m + 2 * a.tile_q - 1) / (2 * a.tile_q)};
 }
 
 struct Span {
@@ -225,7 +273,7 @@ struct Unit {
     Row row;
     int32_t r, head;        // row of the tables, key head
     int64_t q0;             // the first query: token * group + head of the group
-    int32_t queries;        // up to 256
+    int32_t queries;        // up to 2 tile_q
     int32_t t0, n;          // first tile of positions, tiles
     int32_t na, nb;         // of them those that A, B see
     int32_t seen;           // positions that the last query sees
@@ -258,19 +306,19 @@ struct Walk {
             u.row = row, u.r = r;
             u.head = (int32_t)((at - row_begin) / head);
             const int64_t base = row_begin + u.head * head, x = at - base;
-            // The unit that holds place x: i W + 128 i (i + 1) <= x.
-            const double b = (double)line.w + 128.0;
-            int64_t i = (int64_t)((sqrt(b * b + 512.0 * (double)x) - b) / 256.0);
+            // The unit that holds place x: i W + t i (i + 1) <= x.
+            const double t = (double)line.tile_q, b = (double)line.w + t;
+            int64_t i = (int64_t)((sqrt(b * b + 4.0 * t * (double)x) - b) / (2.0 * t));
             i = max((int64_t)0, min(line.units - 1, i));
             while (i > 0 && line.upto(i) > x) i--;
             while (i + 1 < line.units && line.upto(i + 1) <= x) i++;
             const int64_t begin = base + line.upto(i), end = base + line.upto(i + 1), m = (int64_t)row.n * a.group;
             const int32_t have = row.len - row.n;
-            u.q0 = i * kPair;
-            u.queries = (int32_t)min((int64_t)kPair, m - u.q0);
+            u.q0 = i * 2 * a.tile_q;
+            u.queries = (int32_t)min((int64_t)2 * a.tile_q, m - u.q0);
             auto sees = [&](int64_t q) { return have + (int32_t)wf_quot((uint32_t)q, a.by_group) + 1; };
             u.seen = sees(u.q0 + u.queries - 1);
-            const int32_t tiles_a = (sees(u.q0 + min(u.queries, kQ) - 1) + kKeys - 1) / kKeys, tiles = (u.seen + kKeys - 1) / kKeys;
+            const int32_t tiles_a = (sees(u.q0 + min(u.queries, a.tile_q) - 1) + kKeys - 1) / kKeys, tiles = (u.seen + kKeys - 1) / kKeys;
             const int64_t each = (int64_t)kKeys * a.group;
             auto tile = [&](int64_t p) { return p >= end ? tiles : (int32_t)max((int64_t)0, min((int64_t)tiles, (p - begin) / each - kFixed)); };
             const int32_t t0 = tile(max(at, begin)), t1 = tile(min(stop, end));
@@ -278,7 +326,7 @@ struct Walk {
             at = min(stop, end);
             if (t1 <= t0) continue;
             u.t0 = t0, u.n = t1 - t0;
-            u.na = max(0, min(t1, tiles_a) - t0), u.nb = u.queries > kQ ? u.n : 0;
+            u.na = max(0, min(t1, tiles_a) - t0), u.nb = u.queries > a.tile_q ? u.n : 0;
             u.first = blockIdx.x, u.parts = 1;
             if (here != begin || at != end) {
                 int32_t first = span.owner(begin), last = span.owner(end - 1);
@@ -298,7 +346,7 @@ struct Walk {
 
 struct Shared {
     Unit *units;           // [kUnits]
-    uint8_t *q, *kv;       // on 1,024 bytes
+    uint8_t *q, *kv, *raw; // on 1,024 bytes; raw: tiles in 8 bits as the cache has them
     float *scales;
     int64_t *offset;       // [kKeys] of a tile's keys in the cache, -1: none
     uint32_t bars;         // address
@@ -352,9 +400,94 @@ template <typename T> __device__ __forceinline__ float largest(const uint4 &x)
     return fmaxf(fmaxf(fmaxf(fabsf(a.x), fabsf(a.y)), fmaxf(fabsf(b.x), fabsf(b.y))), fmaxf(fmaxf(fabsf(c.x), fabsf(c.y)), fmaxf(fabsf(d.x), fabsf(d.y))));
 }
 
-template <typename T, bool E, int D> __device__ __forceinline__ void load_role(const AttendArgs &a, const Shared &sh)
+// A tile's positions p .. by boxes of `box` positions of one block, element group by element group: one copy a lane.  Boxes behind
+// `end` come from a block that is not there: zeros.
+template <int D, int GROUP, int ROW>
+__device__ __forceinline__ void copy_boxes(const AttendArgs &a, const Unit &u, const CUtensorMap *map, uint32_t to, uint32_t bar, int32_t p, int32_t end, int box,
+                                           int lane)
+{
+    constexpr int kGroups = D / GROUP;
+    const int i = lane / kGroups, g = lane % kGroups;
+    if (lane == 0) bar_expect(bar, kKeys * ROW * kGroups);
+    __syncwarp();
+    if (i * box < kKeys) {
+        const int32_t at = p + i * box;
+        const uint32_t j = wf_quot(min(at, end - 1), a.by_bs);
+        const int32_t block = at < end ? block_at(a, a.table + u.r * a.table_stride, j) : a.n_blocks;
+        copy_box4(to + g * (kKeys * ROW) + i * box * ROW, map, bar, g * GROUP, at < end ? at - (int32_t)j * a.bs : 0, u.head, block);
+    }
+}
+
+// Warp 14: copies by the tensor maps, where the layout allows them.
+template <typename T, bool E, int D> __device__ __forceinline__ void box_role(const PromptArgs &pa, const Shared &sh)
 {
     using S = Shape<E, D>;
+    const AttendArgs &a = pa.a;
+    const int lane = threadIdx.x % 32;
+    const uint32_t kv = smem_of(sh.kv), raw = smem_of(sh.raw);
+    uint32_t it = 0, units = 0;
+    for (;; units++) {
+        const Unit &u = sh.unit(units);
+        if (!u.n) break;
+        if (pa.map_q) {
+            sh.wait(kBarQEmpty, (units & 1) ^ 1);
+            const int tiles = u.nb ? 2 : 1;
+            if (lane == 0) bar_expect(sh.bar(kBarQFull), tiles * (D / 64) * a.tile_q * 128);
+            __syncwarp();
+            if (lane < tiles * (D / 64)) {
+                const int x = lane / (D / 64), g = lane % (D / 64);
+                copy_box3(smem_of(sh.q) + x * S::kTile + g * S::kHalf, &pa.q, sh.bar(kBarQFull), g * 64, u.head * a.group,
+                          u.row.first + (int32_t)wf_quot((uint32_t)u.q0 + x * a.tile_q, a.by_group));
+            }
+        }
+        if (pa.box) {
+            const int32_t end = min(u.seen, (u.t0 + u.n) * kKeys);
+            for (int32_t j = 0; j < u.n; j++) {
+                const int32_t p = (u.t0 + j) * kKeys;
+                // A box that the row ends in holds what lies behind the row, and a weight of 0 does not undo a NaN there.
+                const bool ends = !E && u.row.len % pa.box && p + kKeys > u.row.len;
+#pragma unroll 1
+                for (int side = 0; side < 2; side++, it++) {
+                    const CUtensorMap *map = side ? &pa.v : &pa.k;
+                    if constexpr (E) {
+                        const uint32_t s = it % kRaw;
+                        sh.wait(kBarRaw + kRaw + s, (it / kRaw & 1) ^ 1);
+                        copy_boxes<D, D, D>(a, u, map, raw + s * (kKeys * D), sh.bar(kBarRaw + s), p, end, pa.box, lane);
+                    } else {
+                        const uint32_t s = it % S::kStages, to = kv + s * S::kTile;
+                        sh.wait(kBarFull + 8 + s, (it / S::kStages & 1) ^ 1);
+                        if (!ends || !side) {
+                            copy_boxes<D, 64, 128>(a, u, map, to, sh.bar(kBarFull + s), p, end, pa.box, lane);
+                        } else {
+                            constexpr int kPer = D / 8;
+                            const uint8_t *v = a.v + u.head * a.head_stride;
+                            const int32_t *table = a.table + u.r * a.table_stride;
+#pragma unroll 1
+                            for (int i = lane / kPer; i < kKeys; i += 32 / kPer) {
+                                const int32_t at = min(p + i, u.row.len - 1);
+                                const uint32_t b = wf_quot(at, a.by_bs);
+                                const uint8_t *from = v + block_at(a, table, b) * a.block_stride + (at - (int32_t)b * a.bs) * a.token_stride;
+                                copy16(to + place(i, lane % kPer), from + lane % kPer * 16, p + i < u.row.len);
+                            }
+                            copies_commit();
+                            copies_wait<0>();
+                            to_async();
+                            __syncwarp();
+                            if (lane == 0) bar_arrive(sh.bar(kBarFull + s));
+                        }
+                    }
+                }
+            }
+        }
+        sh.unit_done(units);
+    }
+}
+
+// Warps 8 - 11: what tensor maps cannot copy: any blocks and alignment, queries of any group, and 8 bits to halves.
+template <typename T, bool E, int D> __device__ __forceinline__ void load_role(const PromptArgs &pa, const Shared &sh)
+{
+    using S = Shape<E, D>;
+    const AttendArgs &a = pa.a;
     const int tid = threadIdx.x - 256;
     const uint32_t kv = smem_of(sh.kv), q = smem_of(sh.q);
     uint32_t it = 0, units = 0;
@@ -374,57 +507,76 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
             const int32_t p = min((u.t0 + j) * kKeys + tid, end - 1);
             return block_at(a, table, wf_quot(p, a.by_bs));
         };
-        int32_t next = block(0);
+        const bool tiles = E || !pa.box;
+        int32_t next = tiles ? block(0) : 0;
+        float next_k = 1.f, next_v = 1.f;
+        if (E) next_k = a.k_scale[(int64_t)next * a.kv + u.head], next_v = a.v_scale[(int64_t)next * a.kv + u.head];
         // What is under way belongs to the unit before, which must have it to come to its end.
         copies_wait<0>();
         for (; waiting; waiting--) announce(it - waiting);
-        // Queries, once the products of the unit before have read theirs.
-        sh.wait(kBarQEmpty, (units & 1) ^ 1);
-        {
+        if (!pa.map_q) {  // queries, once the products of the unit before have read theirs
+            sh.wait(kBarQEmpty, (units & 1) ^ 1);
             constexpr int kPer = D / 8, kRows = kLoaders / kPer;  // 16-byte chunks of a query; queries at once
             const int c = tid % kPer;
-            if (!E || std::is_same_v<T, __half>) {
+#pragma unroll 1
+            for (int x = 0; x < (u.nb ? 2 : 1); x++) {
+                const int queries = min(a.tile_q, u.queries - x * a.tile_q);
+                if (!E || std::is_same_v<T, __half>) {
 #pragma unroll 4
-                for (int i = tid / kPer; i < kPair; i += kRows) {
-                    const bool there = i < u.queries;
-                    copy16(q + i / kQ * S::kTile + place(i % kQ, c), query(a, u, there ? i : 0) + 16 * c, there);
-                }
-                copies_commit();
-                copies_wait<0>();
-            } else {
-#pragma unroll 4
-                for (int i = tid / kPer; i < kPair; i += kRows) {
-                    const bool there = i < u.queries;
-                    uint4 x = there ? *reinterpret_cast<const uint4 *>(query(a, u, i) + 16 * c) : make_uint4(0, 0, 0, 0);
-                    float most = largest<T>(x);
-#pragma unroll
-                    for (int s = 1; s < kPer; s *= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, s));
-                    const float down = __int_as_float((127 - query_exponent(most)) << 23);
-                    uint32_t *w = &x.x;
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        const float2 y = wf_pair<T>::to_float(w[j]);
-                        w[j] = wf_pair<__half>::of_float(y.x * down, y.y * down);
+                    for (int i = tid / kPer; i < kQ; i += kRows) {
+                        const bool there = i < queries;
+                        copy16(q + x * S::kTile + place(i, c), query(a, u, x * a.tile_q + (there ? i : 0)) + 16 * c, there);
                     }
-                    *reinterpret_cast<uint4 *>(sh.q + i / kQ * S::kTile + place(i % kQ, c)) = x;
+                } else {
+#pragma unroll 4
+                    for (int i = tid / kPer; i < kQ; i += kRows) {
+                        const bool there = i < queries;
+                        uint4 y = there ? *reinterpret_cast<const uint4 *>(query(a, u, x * a.tile_q + i) + 16 * c) : make_uint4(0, 0, 0, 0);
+                        float most = largest<T>(y);
+#pragma unroll
+                        for (int s = 1; s < kPer; s *= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, s));
+                        const float down = __int_as_float((127 - query_exponent(most)) << 23);
+                        uint32_t *w = &y.x;
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            const float2 z = wf_pair<T>::to_float(w[j]);
+                            w[j] = wf_pair<__half>::of_float(z.x * down, z.y * down);
+                        }
+                        *reinterpret_cast<uint4 *>(sh.q + x * S::kTile + place(i, c)) = y;
+                    }
                 }
             }
+            copies_commit();
+            copies_wait<0>();
             to_async();
             bar_arrive(sh.bar(kBarQFull));
         }
-        for (int32_t j = 0; j < u.n; j++) {
+        for (int32_t j = 0; tiles && j < u.n; j++) {
             const int32_t p = (u.t0 + j) * kKeys + tid;
             int64_t *offset = sh.offset;
-            sync_some<1, kLoaders>();
-            offset[tid] = p < end ? next * a.block_stride + (int64_t)(p - (int32_t)wf_quot(p, a.by_bs) * a.bs) * a.token_stride : -1;
-            const int32_t now = next;
-            if (j + 1 < u.n) next = block(j + 1);
-            sync_some<1, kLoaders>();
+            if (!E || !pa.box) {
+                sync_some<1, kLoaders>();
+                offset[tid] = p < end ? next * a.block_stride + (int64_t)(p - (int32_t)wf_quot(p, a.by_bs) * a.bs) * a.token_stride : -1;
+                sync_some<1, kLoaders>();
+            }
+            const float now_k = p < end ? next_k : 1.f, now_v = p < end ? fmaxf(next_v, kLeastScale) : 1.f;
+            if (j + 1 < u.n) {
+                next = block(j + 1);
+                if (E) next_k = a.k_scale[(int64_t)next * a.kv + u.head], next_v = a.v_scale[(int64_t)next * a.kv + u.head];
+            }
 #pragma unroll 1
             for (int side = 0; side < 2; side++, it++) {  // keys, values
                 const uint32_t s = it % S::kStages, to = kv + s * S::kTile;
                 const uint8_t *from = side ? v : k;
-                sh.wait(kBarFull + 8 + s, ((it / S::kStages) & 1) ^ 1);
+                const uint32_t freed = ((it / S::kStages) & 1) ^ 1;
+                // While there is no room, what has landed is announced at once.
+                while (waiting && !bar_try(sh.bar(kBarFull + 8 + s), freed)) {
+                    if (waiting == 2) copies_wait<1>();
+                    else copies_wait<0>();
+                    announce(it - waiting);
+                    waiting--;
+                }
+                sh.wait(kBarFull + 8 + s, freed);
                 if constexpr (!E) {
                     constexpr int kPer = D / 8, kRows = kLoaders / kPer;
                     const int c = tid % kPer;
@@ -444,17 +596,26 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
                 } else {
                     constexpr int kPer = D / 16, kRows = kLoaders / kPer, kTimes = kKeys / kRows;
                     const int c = tid % kPer;
+                    const uint32_t rs = it % kRaw;
                     uint4 x[kTimes];
+                    if (pa.box) {
+                        sh.wait(kBarRaw + rs, it / kRaw & 1);
 #pragma unroll
-                    for (int i = 0; i < kTimes; i++) {
-                        const int64_t o = offset[i * kRows + tid / kPer];
-                        x[i] = o >= 0 ? *reinterpret_cast<const uint4 *>(from + o + 16 * c) : make_uint4(0, 0, 0, 0);
+                        for (int i = 0; i < kTimes; i++) {
+                            const int row = i * kRows + tid / kPer;
+                            x[i] = *reinterpret_cast<const uint4 *>(sh.raw + rs * (kKeys * D) + row * D + 16 * c);
+                            if (p - tid + row >= end) x[i] = make_uint4(0, 0, 0, 0);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kTimes; i++) {
+                            const int64_t o = offset[i * kRows + tid / kPer];
+                            x[i] = o >= 0 ? *reinterpret_cast<const uint4 *>(from + o + 16 * c) : make_uint4(0, 0, 0, 0);
+                        }
                     }
                     if (side) {  // the scales of this tile, with its values: both stay until the weights are made
-                        const int64_t at = (int64_t)now * a.kv + u.head;
-                        const float f = p < end ? fmaxf(a.v_scale[at], kLeastScale) : 1.f;
                         float *sc = sh.scales + s * (S::kScales / 4) + tid;
-                        sc[0] = p < end ? a.k_scale[at] : 1.f, sc[kKeys] = __log2f(f), sc[2 * kKeys] = __frcp_rn(f);
+                        sc[0] = now_k, sc[kKeys] = __log2f(now_v), sc[2 * kKeys] = __frcp_rn(now_v);
                     }
 #pragma unroll
                     for (int i = 0; i < kTimes; i++) {
@@ -465,6 +626,7 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
                         *reinterpret_cast<uint4 *>(dst + place(row, 2 * c + 1)) = make_uint4(h2.x, h2.y, h3.x, h3.y);
                     }
                     announce(it);
+                    if (pa.box) bar_arrive(sh.bar(kBarRaw + kRaw + rs));
                 }
             }
         }
@@ -495,10 +657,10 @@ template <typename T, bool E, int D> __device__ __forceinline__ void product_rol
         }
         commit_to(sh.bar(kBarS + x));
     };
-    auto sums = [&](int x, uint32_t i, bool more) {
+    auto sums = [&](int x, int half, uint32_t i, bool more) {
         const uint32_t value = kv + i % S::kStages * S::kTile;
 #pragma unroll
-        for (int s = 0; s < kKeys / 16; s++)
+        for (int s = half * kKeys / 32; s < (half + 1) * kKeys / 32; s++)
             mma_ts(tmem + 2 * kKeys + x * D, tmem + x * kKeys + 8 * s, matrix(value + s * 2048, S::kHalf), kDescO, more || s > 0);
     };
     for (;; units++) {
@@ -517,18 +679,25 @@ template <typename T, bool E, int D> __device__ __forceinline__ void product_rol
         for (int j = 0; j < most; j++) {
             const bool go = j + 1 < most;
             full(it + 2 * j + 1);
-            if (go) full(it + 2 * j + 2);
 #pragma unroll
             for (int x = 0; x < 2; x++) {
-                if (j >= n[x]) continue;
-                sh.wait(kBarP + x, np[x] & 1);
-                np[x]++;
-                after_sync();
-                sums(x, it + 2 * j + 1, j > 0);
-                if (j + 1 < n[x]) scores(x, it + 2 * j + 2);
-                else commit_to(sh.bar(kBarO + x));
+                if (j < n[x]) {
+                    sh.wait(kBarP + x, np[x] & 1);
+                    after_sync();
+                    sums(x, 0, it + 2 * j + 1, j > 0);
+                    sh.wait(kBarP + 2 + x, np[x] & 1);
+                    np[x]++;
+                    after_sync();
+                    sums(x, 1, it + 2 * j + 1, true);
+                }
+                if (x == 1) done(it + 2 * j + 1);
+                if (j + 1 < n[x]) {
+                    full(it + 2 * j + 2);
+                    scores(x, it + 2 * j + 2);
+                } else if (j < n[x]) {
+                    commit_to(sh.bar(kBarO + x));
+                }
             }
-            done(it + 2 * j + 1);
             if (go) done(it + 2 * j + 2);
             if (j + 2 == most) commit_to(sh.bar(kBarQEmpty));
         }
@@ -547,17 +716,17 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
 {
     using S = Shape<E, D>;
     using M = std::conditional_t<E, __half, T>;
-    const int x = threadIdx.x / kQ, q = threadIdx.x % kQ, qq = threadIdx.x;  // tile, query of the tile, of the unit
+    const int x = threadIdx.x / kQ, q = threadIdx.x % kQ, qq = x * a.tile_q + q;  // tile, query of the tile, of the unit
     const uint32_t lane = tmem + ((uint32_t)(q / 32 * 32) << 16), st = lane + x * kKeys, ot = lane + 2 * kKeys + x * D;
     uint32_t ns = 0, no = 0, it = 0, units = 0;
     for (;; units++) {
         const Unit &u = sh.unit(units);
         if (!u.n) break;
         const int n = x ? u.nb : u.na;
-        const bool there = qq < u.queries;
+        const bool there = q < a.tile_q && qq < u.queries;
         const uint32_t flat = (uint32_t)(u.q0 + (there ? qq : 0)), tok = wf_quot(flat, a.by_group);
         const int32_t seen = u.row.len - u.row.n + (int32_t)tok + 1;
-        const int32_t least = u.row.len - u.row.n + (int32_t)wf_quot((uint32_t)(u.q0 + min(u.queries - 1, qq / 32 * 32)), a.by_group) + 1;  // of the warp
+        const int32_t least = u.row.len - u.row.n + (int32_t)wf_quot((uint32_t)(u.q0 + min(u.queries - 1, x * a.tile_q + q / 32 * 32)), a.by_group) + 1;  // of the warp
         float scale = a.scale;
         if constexpr (E && std::is_same_v<T, __nv_bfloat16>) {
             const uint4 *p = reinterpret_cast<const uint4 *>(query(a, u, there ? qq : 0));
@@ -596,11 +765,11 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
                 for (int i = 0; i < kKeys; i++)
                     if (p + i >= seen) s[i] = -INFINITY;
             }
-            float most[4] = {s[0], s[1], s[2], s[3]};
+            float most[4] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3]), fmaxf(s[4], s[5]), fmaxf(s[6], s[7])};
 #pragma unroll
-            for (int i = 4; i < kKeys; i += 4)
+            for (int i = 8; i < kKeys; i += 8)
 #pragma unroll
-                for (int k = 0; k < 4; k++) most[k] = fmaxf(most[k], s[i + k]);
+                for (int k = 0; k < 4; k++) most[k] = fmaxf(fmaxf(most[k], s[i + 2 * k]), s[i + 2 * k + 1]);
             float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
             if (!E) top *= scale;
             if (j == 0) {
@@ -621,24 +790,25 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
                 }
             }
             const float base = ref == -INFINITY ? 0.f : ref;
-            float sums[4] = {0.f, 0.f, 0.f, 0.f};
+            float2 sums[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            const float2 by = make_float2(scale, scale), less = make_float2(-base, -base);
 #pragma unroll
-            for (int i = 0; i < kKeys; i += 2) {
-                const float y = power(E ? s[i] - base : fmaf(s[i], scale, -base)), z = power(E ? s[i + 1] - base : fmaf(s[i + 1], scale, -base));
-                if constexpr (E) {
-                    const float2 inv = *reinterpret_cast<const float2 *>(sc + 2 * kKeys + i);
-                    sums[i % 4] = fmaf(y, inv.x, sums[i % 4]), sums[i % 4 + 1] = fmaf(z, inv.y, sums[i % 4 + 1]);
-                } else {
-                    sums[i % 4] += y, sums[i % 4 + 1] += z;
+            for (int half = 0; half < 2; half++) {
+#pragma unroll
+                for (int i = half * kKeys / 2; i < (half + 1) * kKeys / 2; i += 2) {
+                    float2 y = make_float2(s[i], s[i + 1]);
+                    y = E ? add2(y, less) : fma2(y, by, less);
+                    y = make_float2(power(y.x), power(y.y));
+                    sums[i / 2 % 2] = E ? fma2(y, *reinterpret_cast<const float2 *>(sc + 2 * kKeys + i), sums[i / 2 % 2]) : add2(y, sums[i / 2 % 2]);
+                    w[i / 2] = wf_pair<M>::of_float(y.x, y.y);
                 }
-                w[i / 2] = wf_pair<M>::of_float(y, z);
+                tm_store(st + half * 32, w + half * 32);
+                tm_stored();
+                before_sync();
+                bar_arrive(sh.bar(kBarP + 2 * half + x));
             }
-            sum += (sums[0] + sums[1]) + (sums[2] + sums[3]);
-            tm_store(st, w);
-            tm_store(st + 32, w + 32);
-            tm_stored();
-            before_sync();
-            bar_arrive(sh.bar(kBarP + x));
+            sums[0] = add2(sums[0], sums[1]);
+            sum += sums[0].x + sums[0].y;
         }
         it += 2 * u.n;
         if (n > 0) {
@@ -670,13 +840,13 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
             } else {
 #pragma unroll
                 for (int k = 0; k < 32; k += 4)
-                    __stcg(reinterpret_cast<float4 *>(part) + (i + k) / 4 * kPair + qq, make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]));
+                    __stcg(reinterpret_cast<float4 *>(part) + (i + k) / 4 * kPair + (int)threadIdx.x, make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]));
             }
         }
         before_sync();
         if (u.parts > 1) {
-            __stcg(part + kPair * D + qq, ref);
-            __stcg(part + kPair * (D + 1) + qq, sum);
+            __stcg(part + kPair * D + (int)threadIdx.x, ref);
+            __stcg(part + kPair * (D + 1) + (int)threadIdx.x, sum);
             __threadfence();
             sync_some<2, 256>();
             if (threadIdx.x == 0) {
@@ -691,9 +861,9 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
                 __threadfence();
                 auto part_of = [&](int i) { return a.part + (2 * (int64_t)(u.first + i) + (i == 0)) * kPart<D>; };
                 float top = -INFINITY, all = 0.f;
-                for (int i = 0; i < u.parts; i++) top = fmaxf(top, __ldcg(part_of(i) + kPair * D + qq));
+                for (int i = 0; i < u.parts; i++) top = fmaxf(top, __ldcg(part_of(i) + kPair * D + (int)threadIdx.x));
                 const float base = top == -INFINITY ? 0.f : top;
-                for (int i = 0; i < u.parts; i++) all += power(__ldcg(part_of(i) + kPair * D + qq) - base) * __ldcg(part_of(i) + kPair * (D + 1) + qq);
+                for (int i = 0; i < u.parts; i++) all += power(__ldcg(part_of(i) + kPair * D + (int)threadIdx.x) - base) * __ldcg(part_of(i) + kPair * (D + 1) + (int)threadIdx.x);
 #pragma unroll 1
                 for (int i = 0; i < D; i += 32) {
                     float y[32];
@@ -701,10 +871,10 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
                     for (int k = 0; k < 32; k++) y[k] = 0.f;
                     for (int c = 0; c < u.parts; c++) {
                         const float *from = part_of(c);
-                        const float g = power(__ldcg(from + kPair * D + qq) - base);
+                        const float g = power(__ldcg(from + kPair * D + (int)threadIdx.x) - base);
 #pragma unroll
                         for (int k = 0; k < 32; k += 4) {
-                            const float4 z = __ldcg(reinterpret_cast<const float4 *>(from) + (i + k) / 4 * kPair + qq);
+                            const float4 z = __ldcg(reinterpret_cast<const float4 *>(from) + (i + k) / 4 * kPair + (int)threadIdx.x);
                             y[k] += g * z.x, y[k + 1] += g * z.y, y[k + 2] += g * z.z, y[k + 3] += g * z.w;
                         }
                     }
@@ -716,8 +886,9 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
     }
 }
 
-template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttendArgs a)
+template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_constant__ PromptArgs pa)
 {
+    const AttendArgs &a = pa.a;
     using S = Shape<E, D>;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[kBars];
@@ -729,15 +900,22 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
     Shared sh;
     sh.q = raw + (1024 - smem_of(raw) % 1024) % 1024;
     sh.kv = sh.q + S::kQBytes;
-    sh.offset = reinterpret_cast<int64_t *>(sh.kv + S::kStages * S::kTile);
+    sh.raw = sh.kv + S::kStages * S::kTile;
+    sh.offset = reinterpret_cast<int64_t *>(sh.raw + S::kRawBytes);
     sh.scales = reinterpret_cast<float *>(sh.offset + kKeys);
     sh.units = units, sh.bars = smem_of(bars), sh.gave_up = &gave_up, sh.err = a.err;
     const int warp = threadIdx.x / 32;
     if (threadIdx.x == 0) {
         gave_up = 0;
+        const bool loaders = E || !pa.box || !pa.map_q, boxes = pa.box || pa.map_q;
         for (int i = 0; i < kBars; i++) {
-            const bool many = i == kBarQFull || (i >= kBarP && i < kBarO) || (i >= kBarFull && i < kBarFull + 8);
-            bar_init(sh.bar(i), many ? 128 : i >= kBarUnit + kUnits ? 385 : 1);  // of a unit's end: 256 + 128 threads and the products'
+            uint32_t n = 1;
+            if (i == kBarQFull) n = pa.map_q ? 1 : kLoaders;
+            if (i >= kBarP && i < kBarO) n = kQ;
+            if (i >= kBarFull && i < kBarFull + 8) n = E || !pa.box ? kLoaders : 1;
+            if (i >= kBarUnit + kUnits && i < kBarUnit + 2 * kUnits) n = 2 * kQ + 1 + (loaders ? kLoaders : 0) + (boxes ? 32 : 0);
+            if (i >= kBarRaw + kRaw) n = kLoaders;
+            bar_init(sh.bar(i), n);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -755,11 +933,12 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
         power_role<T, E, D>(a, sh, tmem, &last_one);
     } else if (warp < 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        load_role<T, E, D>(a, sh);
+        if (E || !pa.box || !pa.map_q) load_role<T, E, D>(pa, sh);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == 12 && threadIdx.x % 32 == 0) product_role<T, E, D>(sh, tmem);
         if (warp == 13 && threadIdx.x % 32 == 0) unit_role(a, f, sh);
+        if (warp == 14 && (pa.box || pa.map_q)) box_role<T, E, D>(pa, sh);
         __syncwarp();
     }
     before_sync();
@@ -773,9 +952,62 @@ template <typename T, bool E, int D> int setup()
     return wf_cuda_check(cudaFuncSetAttribute(prompt_kernel<T, E, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<E, D>::kSmem), "prompt_kernel");
 }
 
-template <typename T, bool E, int D> int launch(const wf_attn *at, const AttendArgs &a, cudaStream_t st)
+using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                            const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// cuTensorMapEncodeTiled, or null; looked up once.
+Encode encoder()
 {
-    prompt_kernel<T, E, D><<<at->sms, kThreads, Shape<E, D>::kSmem, st>>>(a);
+    static const Encode found = [] {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult how;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &how) != cudaSuccess ||
+            how != cudaDriverEntryPointSuccess)
+            fn = nullptr;
+        cudaGetLastError();
+        return (Encode)fn;
+    }();
+    return found;
+}
+
+// Whether these arrays can be read by boxes; else they are copied otherwise.
+bool encode(CUtensorMap *map, CUtensorMapDataType type, int rank, const void *base, const cuuint64_t *sizes, const cuuint64_t *strides,
+            const cuuint32_t *box, bool swizzle)
+{
+    const Encode f = encoder();
+    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    for (int i = 0; i + 1 < rank; i++)
+        if (!strides[i] || strides[i] >= 1ull << 40) return false;
+    return f && f(map, type, rank, const_cast<void *>(base), sizes, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, bool E, int D> int launch(const wf_attn *at, const AttendArgs &args, cudaStream_t st)
+{
+    PromptArgs pa{};
+    AttendArgs &a = pa.a;
+    a = args;
+    const auto half = std::is_same_v<T, __half> ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    // Boxes of positions of one block, in whole rows of eight of the swizzle: the largest power of two up to 128 that divides a block, from 8 on.
+    const int box = std::min(kKeys, a.bs & -a.bs);
+    if (box >= 8) {
+        const cuuint64_t sizes[4] = {D, (cuuint64_t)a.bs, (cuuint64_t)a.kv, (cuuint64_t)a.n_blocks};
+        const cuuint64_t strides[3] = {(cuuint64_t)a.token_stride, (cuuint64_t)a.head_stride, (cuuint64_t)a.block_stride};
+        const cuuint32_t shape[4] = {E ? D : 64, (cuuint32_t)box, 1, 1};
+        const auto type = E ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : half;
+        if (encode(&pa.k, type, 4, a.k, sizes, strides, shape, !E) && encode(&pa.v, type, 4, a.v, sizes, strides, shape, !E)) pa.box = box;
+    }
+    // Queries of whole tokens: a group's heads, then the next token's.  Over 8 bits bfloat16 queries are scaled first.
+    if (a.group <= kQ && !(E && std::is_same_v<T, __nv_bfloat16>)) {
+        const int tokens = kQ / a.group;
+        const cuuint64_t sizes[3] = {D, (cuuint64_t)a.group * a.kv, (cuuint64_t)a.max_tokens};
+        const cuuint64_t strides[2] = {(cuuint64_t)a.q_head, (cuuint64_t)a.q_token};
+        const cuuint32_t shape[3] = {64, (cuuint32_t)a.group, (cuuint32_t)tokens};
+        pa.map_q = a.q_head > 0 && a.q_token > 0 && encode(&pa.q, half, 3, a.q, sizes, strides, shape, true);
+    }
+    a.tile_q = a.group <= kQ ? kQ / a.group * a.group : kQ;
+    prompt_kernel<T, E, D><<<at->sms, kThreads, Shape<E, D>::kSmem, st>>>(pa);
     return wf_cuda_check(cudaGetLastError(), "prompt_kernel");
 }
 

@@ -75,6 +75,59 @@ def test_attend(have, add, bs, heads, kv, dim, dtype, eight):
     assert torch.equal(got, attend(wf, st, cache, scale, q))
 
 
+LONG = [  # have, add, block size, heads, key heads, dim
+    ([0], [700], 16, 1, 1, 128), ([0, 40], [300, 129], 7, 4, 2, 64), ([1000, 3], [64, 400], 100, 5, 1, 128), ([10] * 9, [33, 1, 40, 2, 90, 0, 127, 128, 129], 8, 6, 2, 64),
+    ([0, 300], [40, 3], 64, 130, 1, 64), ([5], [260], 128, 7, 1, 128), ([2000], [64], 32, 64, 1, 128), ([130], [513], 1, 2, 1, 64), ([900], [37], 24, 24, 8, 128),
+    ([0, 0, 0], [256, 255, 257], 48, 2, 2, 128)]
+
+
+@pytest.mark.parametrize("eight", (False, True), ids=("16", "8"))
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("have,add,bs,heads,kv,dim", LONG, ids=range(len(LONG)))
+def test_attend_prompts(have, add, bs, heads, kv, dim, dtype, eight):
+    """Groups that fill a tile or do not, blocks of any size, chunks that end anywhere, NaN behind every row."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(len(have) * 1000 + bs)
+    st = Step(wf, rng, have, add, bs, spare=5)
+    cache, scale = cache_of(rng, st, kv, dim, "float8_e4m3fn" if eight else dtype)
+    used = np.concatenate([st.table[r, np.arange(n) // bs].astype(np.int64) * bs + np.arange(n) % bs for r, n in enumerate(st.len)])
+    rest = torch.from_numpy(np.setdiff1d(np.arange(st.n_blocks * bs), used)).cuda()
+    raw = cache.view(torch.uint8 if eight else torch.int16)
+    raw.flatten(1, 2)[:, rest] = 0x7F if eight else (0x7E00 if dtype == "float16" else 0x7FC0)
+    q = tensor(rng, (st.room, heads, dim), dtype, 1.5)
+    got = attend(wf, st, cache, scale, q)
+    clean = cache.clone()
+    clean.view(torch.uint8).flatten(1, 2)[:, rest] = 0
+    check(st, clean, scale, q, got)
+    assert torch.equal(got, attend(wf, st, cache, scale, q))
+
+
+@pytest.mark.parametrize("eight", (False, True), ids=("16", "8"))
+def test_long_prompts_in_torch(eight):
+    """Longer prompts, whose positions several blocks of the GPU share, against products in 64 bits on the GPU."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(31)
+    for have, add, heads, kv, dim, bs in (([0, 3000], [3000, 700], 8, 2, 128, 16), ([20000], [130], 4, 1, 64, 32), ([11, 0, 5000], [1500, 2100, 1], 6, 2, 128, 24)):
+        st = Step(wf, rng, have, add, bs)
+        dtype = "bfloat16"
+        cache, scale = cache_of(rng, st, kv, dim, "float8_e4m3fn" if eight else dtype)
+        q = tensor(rng, (st.room, heads, dim), dtype, 1.5)
+        got = attend(wf, st, cache, scale, q).double()
+        x = cache.double() if scale is None else cache.double() * scale.double()[:, :, None, :, None]
+        for r, n in enumerate(st.len):
+            blocks = torch.from_numpy(st.table[r, :-(-int(n) // bs)].astype(np.int64)).cuda()
+            k, v = (x[i][blocks].flatten(0, 1)[:int(n)] for i in (0, 1))
+            a, b = int(st.start[r]), int(st.start[r + 1])
+            later = torch.arange(int(n), device="cuda") > torch.arange(int(have[r]), int(n), device="cuda")[:, None]
+            for h in range(heads):
+                w = torch.softmax((q[a:b, h].double() @ k[:, h * kv // heads].T * dim ** -0.5).masked_fill(later, -torch.inf), 1)
+                want, size = w @ v[:, h * kv // heads], w @ v[:, h * kv // heads].abs()
+                # As in bound(), with 2^-9 more for scores (dim 2^-24 times products up to 2^9 here) and for the subnormal weights over 8 bits.
+                assert ((got[a:b, h] - want).abs() <= 2.0 ** -8 * want.abs() + size * (2 * 2.0 ** -8 + 2.0 ** -9)).all(), (r, h)
+
+
 @pytest.mark.parametrize("eight", (False, True), ids=("16", "8"))
 @pytest.mark.parametrize("have,heads,kv,dim", [([40000], 8, 1, 128), ([20000, 3, 9000, 1], 4, 2, 64), ([30000, 30000], 12, 4, 128)])
 def test_long_rows_are_split(have, heads, kv, dim, eight):
