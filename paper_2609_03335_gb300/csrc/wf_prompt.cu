@@ -39,7 +39,8 @@ constexpr float kLeastScale = 0x1p-64f;
 
 template <bool E, int D> struct Shape {
     static constexpr int kRow = 2 * D;                       // bytes of a key or query in shared memory
-    static constexpr int kHalf = kKeys * 128;                // bytes of 64 elements of a tile
+    static constexpr int kHalf = kQ * 128;                   // bytes of 64 elements of the queries
+    static constexpr int kEight = 8 * kRow;                  // bytes of eight keys: 64 elements of all, then the other 64
     static constexpr int kTile = kKeys * kRow;
     static constexpr int kStages = D == 64 ? 8 : E ? 3 : 5;
     static constexpr int kScales = E ? 3 * kKeys * 4 : 0;    // of a stage: keys' scales, log2 and reciprocal of values'
@@ -53,6 +54,8 @@ struct PromptArgs {
     AttendArgs a;
     int32_t box;     // positions of a box of the maps k and v, 0: they are not used
     int32_t map_q;   // whether q is
+    int32_t heads;   // the maps' last coordinate: block * heads + head
+    int32_t beyond;  // the first that is not there
     CUtensorMap k, v, q;
 };
 
@@ -96,10 +99,10 @@ __device__ __forceinline__ void copy16(uint32_t to, const void *from, bool there
     asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
 // A box of a tensor map from these coordinates; its bytes arrive at bar.
-__device__ __forceinline__ void copy_box4(uint32_t to, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2, int c3)
+__device__ __forceinline__ void copy_box5(uint32_t to, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2, int c3, int c4)
 {
-    asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(to), "l"(map),
-                 "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+    asm volatile("cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(to),
+                 "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4) : "memory");
 }
 __device__ __forceinline__ void copy_box3(uint32_t to, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2)
 {
@@ -116,6 +119,16 @@ __device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::bef
 __device__ __forceinline__ void commit_to(uint32_t bar)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// One lane of a whole warp: what it issues has operands that are the same in every lane, as the products' instructions want them.
+__device__ __forceinline__ bool elected()
+{
+    uint32_t one;
+    asm volatile("{ .reg .pred p;\n"
+                 "  elect.sync _|p, 0xFFFFFFFF;\n"
+                 "  selp.u32 %0, 1, 0, p; }" : "=r"(one)::"memory");
+    return one;
 }
 
 // Both operands in shared memory.
@@ -152,10 +165,11 @@ __device__ __forceinline__ void tm_store(uint32_t at, const uint32_t *x)
 __device__ __forceinline__ void tm_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Rows of 128 bytes, swizzled: eight rows are 1,024 bytes, `lead` the bytes to the next 64 elements where these run along rows.
-__device__ __forceinline__ uint64_t matrix(uint32_t at, uint32_t lead)
+// Rows of 128 bytes, swizzled, eight of them 1,024 bytes: `next` the bytes to the next eight rows, `lead` to the next 64 elements where these
+// run along rows.
+__device__ __forceinline__ uint64_t matrix(uint32_t at, uint32_t lead, uint32_t next)
 {
-    return (uint64_t)(at >> 4 & 0x3FFF) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+    return (uint64_t)(at >> 4 & 0x3FFF) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(next >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
 
 __device__ __forceinline__ float power(float x)
@@ -378,8 +392,9 @@ __device__ __forceinline__ void unit_role(const AttendArgs &a, const Found &f, c
     }
 }
 
-// Bytes of 16-byte chunk c of row i in a tile.
-__device__ __forceinline__ uint32_t place(int i, int c) { return c / 8 * (kKeys * 128) + i * 128 + ((c ^ i) & 7) * 16; }
+// Bytes of 16-byte chunk c of query i in its tile, of key i.
+__device__ __forceinline__ uint32_t query_place(int i, int c) { return c / 8 * (kQ * 128) + i * 128 + ((c ^ i) & 7) * 16; }
+template <int D> __device__ __forceinline__ uint32_t place(int i, int c) { return i / 8 * (16 * D) + c / 8 * 1024 + i % 8 * 128 + ((c ^ i) & 7) * 16; }
 
 // log2 of the power of two that a query of 8-bit products is divided by, so that halves hold it: its largest element becomes
 // 2^13 .. 2^14.  0 where the queries are halves.
@@ -400,21 +415,23 @@ template <typename T> __device__ __forceinline__ float largest(const uint4 &x)
     return fmaxf(fmaxf(fmaxf(fabsf(a.x), fabsf(a.y)), fmaxf(fabsf(b.x), fabsf(b.y))), fmaxf(fmaxf(fabsf(c.x), fabsf(c.y)), fmaxf(fabsf(d.x), fabsf(d.y))));
 }
 
-// A tile's positions p .. by boxes of `box` positions of one block, element group by element group: one copy a lane.  Boxes behind
-// `end` come from a block that is not there: zeros.
-template <int D, int GROUP, int ROW>
-__device__ __forceinline__ void copy_boxes(const AttendArgs &a, const Unit &u, const CUtensorMap *map, uint32_t to, uint32_t bar, int32_t p, int32_t end, int box,
-                                           int lane)
+// A tile's positions p .. by boxes of `box` positions of one block: one copy a lane.  Boxes behind `end` come from a block that is not
+// there: zeros.
+template <bool E, int D>
+__device__ __forceinline__ void copy_boxes(const PromptArgs &pa, const Unit &u, const CUtensorMap *map, uint32_t to, uint32_t bar, int32_t p, int32_t end, int lane)
 {
-    constexpr int kGroups = D / GROUP;
-    const int i = lane / kGroups, g = lane % kGroups;
-    if (lane == 0) bar_expect(bar, kKeys * ROW * kGroups);
+    constexpr int kRow = E ? D : 2 * D;
+    const AttendArgs &a = pa.a;
+    const int box = pa.box;
+    if (lane == 0) bar_expect(bar, kKeys * kRow);
     __syncwarp();
-    if (i * box < kKeys) {
-        const int32_t at = p + i * box;
+    if (lane * box < kKeys) {
+        const int32_t at = p + lane * box;
         const uint32_t j = wf_quot(min(at, end - 1), a.by_bs);
-        const int32_t block = at < end ? block_at(a, a.table + u.r * a.table_stride, j) : a.n_blocks;
-        copy_box4(to + g * (kKeys * ROW) + i * box * ROW, map, bar, g * GROUP, at < end ? at - (int32_t)j * a.bs : 0, u.head, block);
+        const int32_t block = at < end ? block_at(a, a.table + u.r * a.table_stride, j) * pa.heads + u.head : pa.beyond;
+        const int32_t place = at < end ? at - (int32_t)j * a.bs : 0;
+        if constexpr (E) copy_box3(to + lane * box * kRow, map, bar, 0, place, block);
+        else copy_box5(to + lane * box * kRow, map, bar, 0, 0, 0, place / 8, block);
     }
 }
 
@@ -452,12 +469,12 @@ template <typename T, bool E, int D> __device__ __forceinline__ void box_role(co
                     if constexpr (E) {
                         const uint32_t s = it % kRaw;
                         sh.wait(kBarRaw + kRaw + s, (it / kRaw & 1) ^ 1);
-                        copy_boxes<D, D, D>(a, u, map, raw + s * (kKeys * D), sh.bar(kBarRaw + s), p, end, pa.box, lane);
+                        copy_boxes<E, D>(pa, u, map, raw + s * (kKeys * D), sh.bar(kBarRaw + s), p, end, lane);
                     } else {
                         const uint32_t s = it % S::kStages, to = kv + s * S::kTile;
                         sh.wait(kBarFull + 8 + s, (it / S::kStages & 1) ^ 1);
                         if (!ends || !side) {
-                            copy_boxes<D, 64, 128>(a, u, map, to, sh.bar(kBarFull + s), p, end, pa.box, lane);
+                            copy_boxes<E, D>(pa, u, map, to, sh.bar(kBarFull + s), p, end, lane);
                         } else {
                             constexpr int kPer = D / 8;
                             const uint8_t *v = a.v + u.head * a.head_stride;
@@ -467,7 +484,7 @@ template <typename T, bool E, int D> __device__ __forceinline__ void box_role(co
                                 const int32_t at = min(p + i, u.row.len - 1);
                                 const uint32_t b = wf_quot(at, a.by_bs);
                                 const uint8_t *from = v + block_at(a, table, b) * a.block_stride + (at - (int32_t)b * a.bs) * a.token_stride;
-                                copy16(to + place(i, lane % kPer), from + lane % kPer * 16, p + i < u.row.len);
+                                copy16(to + place<D>(i, lane % kPer), from + lane % kPer * 16, p + i < u.row.len);
                             }
                             copies_commit();
                             copies_wait<0>();
@@ -525,7 +542,7 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
 #pragma unroll 4
                     for (int i = tid / kPer; i < kQ; i += kRows) {
                         const bool there = i < queries;
-                        copy16(q + x * S::kTile + place(i, c), query(a, u, x * a.tile_q + (there ? i : 0)) + 16 * c, there);
+                        copy16(q + x * S::kTile + query_place(i, c), query(a, u, x * a.tile_q + (there ? i : 0)) + 16 * c, there);
                     }
                 } else {
 #pragma unroll 4
@@ -542,7 +559,7 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
                             const float2 z = wf_pair<T>::to_float(w[j]);
                             w[j] = wf_pair<__half>::of_float(z.x * down, z.y * down);
                         }
-                        *reinterpret_cast<uint4 *>(sh.q + x * S::kTile + place(i, c)) = y;
+                        *reinterpret_cast<uint4 *>(sh.q + x * S::kTile + query_place(i, c)) = y;
                     }
                 }
             }
@@ -583,7 +600,7 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
 #pragma unroll 8
                     for (int i = tid / kPer; i < kKeys; i += kRows) {
                         const int64_t o = offset[i];
-                        copy16(to + place(i, c), from + (o < 0 ? 0 : o) + 16 * c, o >= 0);
+                        copy16(to + place<D>(i, c), from + (o < 0 ? 0 : o) + 16 * c, o >= 0);
                     }
                     copies_commit();
                     // Two tiles under way; the one before them has landed.
@@ -622,8 +639,8 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
                         const int row = i * kRows + tid / kPer;
                         const uint2 h0 = wf_e4m3_halves(x[i].x), h1 = wf_e4m3_halves(x[i].y), h2 = wf_e4m3_halves(x[i].z), h3 = wf_e4m3_halves(x[i].w);
                         uint8_t *dst = sh.kv + s * S::kTile;
-                        *reinterpret_cast<uint4 *>(dst + place(row, 2 * c)) = make_uint4(h0.x, h0.y, h1.x, h1.y);
-                        *reinterpret_cast<uint4 *>(dst + place(row, 2 * c + 1)) = make_uint4(h2.x, h2.y, h3.x, h3.y);
+                        *reinterpret_cast<uint4 *>(dst + place<D>(row, 2 * c)) = make_uint4(h0.x, h0.y, h1.x, h1.y);
+                        *reinterpret_cast<uint4 *>(dst + place<D>(row, 2 * c + 1)) = make_uint4(h2.x, h2.y, h3.x, h3.y);
                     }
                     announce(it);
                     if (pa.box) bar_arrive(sh.bar(kBarRaw + kRaw + rs));
@@ -647,27 +664,35 @@ template <typename T, bool E, int D> __device__ __forceinline__ void product_rol
     const uint32_t kv = smem_of(sh.kv), q = smem_of(sh.q);
     uint32_t it = 0, units = 0, np[2] = {0, 0};
     auto full = [&](uint32_t i) { sh.wait(kBarFull + i % S::kStages, (i / S::kStages) & 1); };
-    auto done = [&](uint32_t i) { commit_to(sh.bar(kBarFull + 8 + i % S::kStages)); };
+    auto commit = [&](int i) {
+        if (elected()) commit_to(sh.bar(i));
+    };
+    auto done = [&](uint32_t i) { commit(kBarFull + 8 + i % S::kStages); };
     auto scores = [&](int x, uint32_t i) {
-        const uint32_t key = kv + i % S::kStages * S::kTile;
+        const uint64_t key = matrix(kv + i % S::kStages * S::kTile, 16, S::kEight), query = matrix(q + x * S::kTile, 16, 1024);
+        if (elected()) {
 #pragma unroll
-        for (int s = 0; s < D / 16; s++) {
-            const uint32_t at = s / 4 * S::kHalf + s % 4 * 32;
-            mma_ss(tmem + x * kKeys, matrix(q + x * S::kTile + at, 16), matrix(key + at, 16), kDescS, s > 0);
+            for (int s = 0; s < D / 16; s++) {
+                mma_ss(tmem + x * kKeys, query + ((s / 4 * S::kHalf + s % 4 * 32) >> 4), key + ((s / 4 * 1024 + s % 4 * 32) >> 4), kDescS, s > 0);
+            }
+            commit_to(sh.bar(kBarS + x));
         }
-        commit_to(sh.bar(kBarS + x));
     };
     auto sums = [&](int x, int half, uint32_t i, bool more) {
-        const uint32_t value = kv + i % S::kStages * S::kTile;
+        const uint64_t value = matrix(kv + i % S::kStages * S::kTile, 1024, S::kEight);
+        if (elected()) {
 #pragma unroll
-        for (int s = half * kKeys / 32; s < (half + 1) * kKeys / 32; s++)
-            mma_ts(tmem + 2 * kKeys + x * D, tmem + x * kKeys + 8 * s, matrix(value + s * 2048, S::kHalf), kDescO, more || s > 0);
+            for (int s = 0; s < kKeys / 32; s++) {
+                const int k = half * kKeys / 32 + s;
+                mma_ts(tmem + 2 * kKeys + x * D, tmem + x * kKeys + 8 * k, value + k * (2 * S::kEight >> 4), kDescO, more || s > 0);
+            }
+        }
     };
     for (;; units++) {
         const Unit &u = sh.unit(units);
         const int n[2] = {u.na, u.nb}, most = u.n;
         if (!most) break;
-        sh.unit_done(units);
+        if (elected()) sh.unit_done(units);
         sh.wait(kBarQFull, units & 1);
         full(it);
         after_sync();
@@ -675,9 +700,8 @@ template <typename T, bool E, int D> __device__ __forceinline__ void product_rol
         for (int x = 0; x < 2; x++)
             if (n[x] > 0) scores(x, it);
         done(it);
-        if (most == 1) commit_to(sh.bar(kBarQEmpty));
+        if (most == 1) commit(kBarQEmpty);
         for (int j = 0; j < most; j++) {
-            const bool go = j + 1 < most;
             full(it + 2 * j + 1);
 #pragma unroll
             for (int x = 0; x < 2; x++) {
@@ -692,19 +716,19 @@ template <typename T, bool E, int D> __device__ __forceinline__ void product_rol
                 }
                 if (x == 1) done(it + 2 * j + 1);
                 if (j + 1 < n[x]) {
-                    full(it + 2 * j + 2);
+                    if (!x || j + 1 >= n[0]) full(it + 2 * j + 2);
                     scores(x, it + 2 * j + 2);
                 } else if (j < n[x]) {
-                    commit_to(sh.bar(kBarO + x));
+                    commit(kBarO + x);
                 }
             }
-            if (go) done(it + 2 * j + 2);
-            if (j + 2 == most) commit_to(sh.bar(kBarQEmpty));
+            if (j + 1 < most) done(it + 2 * j + 2);
+            if (j + 2 == most) commit(kBarQEmpty);
         }
         it += 2 * most;
     }
     // Nothing is under way when TMEM is given back.
-    commit_to(sh.bar(kBarDrain));
+    commit(kBarDrain);
     for (int i = 0; i < 1 << 20 && !bar_try(sh.bar(kBarDrain), 0); i++) {}
 }
 
@@ -760,18 +784,36 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
                 }
             }
             const int32_t p = (u.t0 + j) * kKeys;
+            auto largest_of = [&] {
+                float most[4] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3]), fmaxf(s[4], s[5]), fmaxf(s[6], s[7])};
+#pragma unroll
+                for (int i = 8; i < kKeys; i += 8)
+#pragma unroll
+                    for (int k = 0; k < 4; k++) most[k] = fmaxf(fmaxf(most[k], s[i + 2 * k]), s[i + 2 * k + 1]);
+                const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+                return E ? top : top * scale;
+            };
+            float2 sums[2];
+            const float2 by = make_float2(scale, scale);
+            auto powers = [&](int half) {  // of 64 scores, packed in place
+                const float base = ref == -INFINITY ? 0.f : ref;
+                const float2 off = make_float2(-base, -base);
+#pragma unroll
+                for (int i = half * kKeys / 2; i < (half + 1) * kKeys / 2; i += 2) {
+                    float2 y = make_float2(s[i], s[i + 1]);
+                    y = E ? add2(y, off) : fma2(y, by, off);
+                    y = make_float2(power(y.x), power(y.y));
+                    sums[i / 2 % 2] = E ? fma2(y, *reinterpret_cast<const float2 *>(sc + 2 * kKeys + i), sums[i / 2 % 2]) : add2(y, sums[i / 2 % 2]);
+                    w[i / 2] = wf_pair<M>::of_float(y.x, y.y);
+                }
+            };
+            sums[0] = sums[1] = make_float2(0.f, 0.f);
             if (p + kKeys > least) {
 #pragma unroll
                 for (int i = 0; i < kKeys; i++)
                     if (p + i >= seen) s[i] = -INFINITY;
             }
-            float most[4] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3]), fmaxf(s[4], s[5]), fmaxf(s[6], s[7])};
-#pragma unroll
-            for (int i = 8; i < kKeys; i += 8)
-#pragma unroll
-                for (int k = 0; k < 4; k++) most[k] = fmaxf(fmaxf(most[k], s[i + 2 * k]), s[i + 2 * k + 1]);
-            float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-            if (!E) top *= scale;
+            const float top = largest_of();
             if (j == 0) {
                 ref = top;
             } else if (__any_sync(~0u, top > ref + kSlack)) {
@@ -789,19 +831,9 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
                     tm_store(ot + i, o);
                 }
             }
-            const float base = ref == -INFINITY ? 0.f : ref;
-            float2 sums[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-            const float2 by = make_float2(scale, scale), less = make_float2(-base, -base);
 #pragma unroll
             for (int half = 0; half < 2; half++) {
-#pragma unroll
-                for (int i = half * kKeys / 2; i < (half + 1) * kKeys / 2; i += 2) {
-                    float2 y = make_float2(s[i], s[i + 1]);
-                    y = E ? add2(y, less) : fma2(y, by, less);
-                    y = make_float2(power(y.x), power(y.y));
-                    sums[i / 2 % 2] = E ? fma2(y, *reinterpret_cast<const float2 *>(sc + 2 * kKeys + i), sums[i / 2 % 2]) : add2(y, sums[i / 2 % 2]);
-                    w[i / 2] = wf_pair<M>::of_float(y.x, y.y);
-                }
+                powers(half);
                 tm_store(st + half * 32, w + half * 32);
                 tm_stored();
                 before_sync();
@@ -936,7 +968,7 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
         if (E || !pa.box || !pa.map_q) load_role<T, E, D>(pa, sh);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        if (warp == 12 && threadIdx.x % 32 == 0) product_role<T, E, D>(sh, tmem);
+        if (warp == 12) product_role<T, E, D>(sh, tmem);
         if (warp == 13 && threadIdx.x % 32 == 0) unit_role(a, f, sh);
         if (warp == 14 && (pa.box || pa.map_q)) box_role<T, E, D>(pa, sh);
         __syncwarp();
@@ -975,7 +1007,7 @@ bool encode(CUtensorMap *map, CUtensorMapDataType type, int rank, const void *ba
             const cuuint32_t *box, bool swizzle)
 {
     const Encode f = encoder();
-    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
     for (int i = 0; i + 1 < rank; i++)
         if (!strides[i] || strides[i] >= 1ull << 40) return false;
     return f && f(map, type, rank, const_cast<void *>(base), sizes, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -989,14 +1021,23 @@ template <typename T, bool E, int D> int launch(const wf_attn *at, const AttendA
     AttendArgs &a = pa.a;
     a = args;
     const auto half = std::is_same_v<T, __half> ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-    // Boxes of positions of one block, in whole rows of eight of the swizzle: the largest power of two up to 128 that divides a block, from 8 on.
+    // Boxes of positions of one block, in whole rows of eight of the swizzle: the largest power of two up to 128 that divides a block, from 8
+    // on.  A box is one request, [position / 8][64 elements' group][position % 8][64 elements], since requests are what the copies cost: with one
+    // for each 64 elements blocks of 16 took 1,772 us where those of 128 took 1,496 (one prompt of 16,384).  Block and head share a
+    // coordinate in steps of a head, which takes blocks that lie whole numbers of such steps apart.
     const int box = std::min(kKeys, a.bs & -a.bs);
-    if (box >= 8) {
-        const cuuint64_t sizes[4] = {D, (cuuint64_t)a.bs, (cuuint64_t)a.kv, (cuuint64_t)a.n_blocks};
-        const cuuint64_t strides[3] = {(cuuint64_t)a.token_stride, (cuuint64_t)a.head_stride, (cuuint64_t)a.block_stride};
-        const cuuint32_t shape[4] = {E ? D : 64, (cuuint32_t)box, 1, 1};
+    const int64_t step = a.kv == 1 ? a.block_stride : a.head_stride;
+    const int64_t heads = step > 0 && a.block_stride % step == 0 ? a.block_stride / step : 0, places = (a.n_blocks - 1) * heads + a.kv;
+    if (box >= 8 && heads && places < INT32_MAX) {
         const auto type = E ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : half;
-        if (encode(&pa.k, type, 4, a.k, sizes, strides, shape, !E) && encode(&pa.v, type, 4, a.v, sizes, strides, shape, !E)) pa.box = box;
+        const cuuint64_t tok = (cuuint64_t)a.token_stride, sizes8[3] = {D, (cuuint64_t)a.bs, (cuuint64_t)places}, strides8[2] = {tok, (cuuint64_t)step};
+        const cuuint32_t shape8[3] = {D, (cuuint32_t)box, 1};
+        const cuuint64_t sizes[5] = {64, 8, D / 64, (cuuint64_t)a.bs / 8, (cuuint64_t)places}, strides[4] = {tok, 128, 8 * tok, (cuuint64_t)step};
+        const cuuint32_t shape[5] = {64, 8, D / 64, (cuuint32_t)box / 8, 1};
+        auto map = [&](CUtensorMap *m, const uint8_t *base) {
+            return E ? encode(m, type, 3, base, sizes8, strides8, shape8, false) : encode(m, type, 5, base, sizes, strides, shape, true);
+        };
+        if (map(&pa.k, a.k) && map(&pa.v, a.v)) pa.box = box, pa.heads = (int32_t)heads, pa.beyond = (int32_t)places;
     }
     // Queries of whole tokens: a group's heads, then the next token's.  Over 8 bits bfloat16 queries are scaled first.
     if (a.group <= kQ && !(E && std::is_same_v<T, __nv_bfloat16>)) {
