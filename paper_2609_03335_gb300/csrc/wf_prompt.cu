@@ -42,7 +42,7 @@ template <bool E, int D> struct Shape {
     static constexpr int kHalf = kQ * 128;                   // bytes of 64 elements of the queries
     static constexpr int kEight = 8 * kRow;                  // bytes of eight keys: 64 elements of all, then the other 64
     static constexpr int kTile = kKeys * kRow;
-    static constexpr int kStages = D == 64 ? 8 : E ? 3 : 5;
+    static constexpr int kStages = D == 64 ? 8 : E ? 3 : 4;
     static constexpr int kScales = E ? 3 * kKeys * 4 : 0;    // of a stage: keys' scales, log2 and reciprocal of values'
     static constexpr int kQBytes = 2 * kTile;
     static constexpr int kRawBytes = E ? kRaw * kKeys * D : 0;
@@ -735,6 +735,33 @@ template <typename T, bool E, int D> __device__ __forceinline__ void product_rol
 // Parts in scratch: D / 4 columns of [256 queries] four sums, then [256] references, [256] sums of weights.
 template <int D> constexpr int kPart = kPair * (D + 2);
 
+// Elements i .. i + 31 of the warp's queries, one a lane, times `by`.  Four lanes swap their 16-byte pieces (piece c of each query to lane c),
+// so that a store fills 64 bytes of 8 queries in place of 16 bytes of 32: with those the end of a unit took 4,500 cycles.
+template <typename T> __device__ __forceinline__ void put(uint8_t *const (&out)[4], int i, const float *y, float by)
+{
+    const int c = threadIdx.x % 4;
+    uint32_t w[4][4];
+#pragma unroll
+    for (int k = 0; k < 16; k++) w[k / 4][k % 4] = wf_pair<T>::of_float(y[2 * k] * by, y[2 * k + 1] * by);
+    // Two rounds: lanes 1 apart swap pieces whose numbers differ in bit 0, then lanes 2 apart those that differ in bit 1.
+#pragma unroll
+    for (int bit = 1; bit < 4; bit *= 2)
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+            if (!(k & bit)) {
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const bool up = c & bit;
+                    const uint32_t got = __shfl_xor_sync(~0u, up ? w[k][j] : w[k | bit][j], bit);
+                    if (up) w[k][j] = got;
+                    else w[k | bit][j] = got;
+                }
+            }
+#pragma unroll
+    for (int k = 0; k < 4; k++)  // piece c of query k of the four
+        if (out[k]) *reinterpret_cast<uint4 *>(out[k] + 2 * i + 16 * c) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+}
+
 template <typename T, bool E, int D>
 __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh, uint32_t tmem, int *last_one)
 {
@@ -848,14 +875,12 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
             no++;
             after_sync();
         }
-        uint8_t *out = a.out + (int64_t)(u.row.first + tok) * a.o_token + (int64_t)(u.head * a.group + (flat - tok * a.group)) * a.o_head;
-        auto put = [&](int i, const float *y, float inv) {  // 32 elements
+        uint8_t *mine = there ? a.out + (int64_t)(u.row.first + tok) * a.o_token + (int64_t)(u.head * a.group + (flat - tok * a.group)) * a.o_head : nullptr;
+        uint8_t *out[4];  // of the four queries whose elements this lane writes
 #pragma unroll
-            for (int k = 0; k < 32; k += 8)
-                *reinterpret_cast<uint4 *>(out + 2 * (i + k)) =
-                    make_uint4(wf_pair<T>::of_float(y[k] * inv, y[k + 1] * inv), wf_pair<T>::of_float(y[k + 2] * inv, y[k + 3] * inv),
-                               wf_pair<T>::of_float(y[k + 4] * inv, y[k + 5] * inv), wf_pair<T>::of_float(y[k + 6] * inv, y[k + 7] * inv));
-        };
+        for (int i = 0; i < 4; i++)
+            out[i] = reinterpret_cast<uint8_t *>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(mine), threadIdx.x % 32 / 4 * 4 + i));
+        const int at = threadIdx.x;
         float *part = a.part + (2 * (int64_t)blockIdx.x + (blockIdx.x == u.first)) * kPart<D>;
 #pragma unroll 1
         for (int i = 0; i < D; i += 32) {
@@ -868,17 +893,17 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
                 for (int k = 0; k < 32; k++) y[k] = 0.f;
             }
             if (u.parts == 1) {
-                if (there) put(i, y, 1.f / sum);
+                put<T>(out, i, y, 1.f / sum);
             } else {
 #pragma unroll
                 for (int k = 0; k < 32; k += 4)
-                    __stcg(reinterpret_cast<float4 *>(part) + (i + k) / 4 * kPair + (int)threadIdx.x, make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]));
+                    __stcg(reinterpret_cast<float4 *>(part) + (i + k) / 4 * kPair + at, make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]));
             }
         }
         before_sync();
         if (u.parts > 1) {
-            __stcg(part + kPair * D + (int)threadIdx.x, ref);
-            __stcg(part + kPair * (D + 1) + (int)threadIdx.x, sum);
+            __stcg(part + kPair * D + at, ref);
+            __stcg(part + kPair * (D + 1) + at, sum);
             __threadfence();
             sync_some<2, 256>();
             if (threadIdx.x == 0) {
@@ -893,9 +918,9 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
                 __threadfence();
                 auto part_of = [&](int i) { return a.part + (2 * (int64_t)(u.first + i) + (i == 0)) * kPart<D>; };
                 float top = -INFINITY, all = 0.f;
-                for (int i = 0; i < u.parts; i++) top = fmaxf(top, __ldcg(part_of(i) + kPair * D + (int)threadIdx.x));
+                for (int i = 0; i < u.parts; i++) top = fmaxf(top, __ldcg(part_of(i) + kPair * D + at));
                 const float base = top == -INFINITY ? 0.f : top;
-                for (int i = 0; i < u.parts; i++) all += power(__ldcg(part_of(i) + kPair * D + (int)threadIdx.x) - base) * __ldcg(part_of(i) + kPair * (D + 1) + (int)threadIdx.x);
+                for (int i = 0; i < u.parts; i++) all += power(__ldcg(part_of(i) + kPair * D + at) - base) * __ldcg(part_of(i) + kPair * (D + 1) + at);
 #pragma unroll 1
                 for (int i = 0; i < D; i += 32) {
                     float y[32];
@@ -903,14 +928,14 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
                     for (int k = 0; k < 32; k++) y[k] = 0.f;
                     for (int c = 0; c < u.parts; c++) {
                         const float *from = part_of(c);
-                        const float g = power(__ldcg(from + kPair * D + (int)threadIdx.x) - base);
+                        const float g = power(__ldcg(from + kPair * D + at) - base);
 #pragma unroll
                         for (int k = 0; k < 32; k += 4) {
-                            const float4 z = __ldcg(reinterpret_cast<const float4 *>(from) + (i + k) / 4 * kPair + (int)threadIdx.x);
+                            const float4 z = __ldcg(reinterpret_cast<const float4 *>(from) + (i + k) / 4 * kPair + at);
                             y[k] += g * z.x, y[k + 1] += g * z.y, y[k + 2] += g * z.z, y[k + 3] += g * z.w;
                         }
                     }
-                    if (there) put(i, y, 1.f / all);
+                    put<T>(out, i, y, 1.f / all);
                 }
             }
         }
