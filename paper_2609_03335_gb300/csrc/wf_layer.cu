@@ -210,9 +210,10 @@ extern "C" int wf_attend(wf_attn *at, const wf_kv *kv, const wf_kv_step *step, c
     a.above = 0, a.most = INT64_MAX;
     if (expected * a.group > kFew) {
         AttendArgs b = a;
-        b.above = kFew, a.most = kFew;
+        b.above = kFew;
         rc = wf_launch_prompt(at, b, in->dtype, layer->dim, eight, (cudaStream_t)stream);
-        if (rc) return rc;
+        if (rc > 0) return rc;
+        if (!rc) a.most = kFew;
     }
     return wf_launch_attend(at, a, in->dtype, layer->dim, eight, (cudaStream_t)stream);
 }

@@ -9,6 +9,7 @@
 //                    where a maximum has grown by more than 2^8, O is shrunk (not before: weights up to 2^8 lose nothing)
 //   warp 14          copies of K, V and Q by tensor maps: the blocks' table, then a box of positions of one block at a time
 //   warps 8-11       copies 16 bytes at a time where boxes do not fit (blocks that are no multiple of 8 positions), and 8 bits to halves
+//   warp 15          8 bits: the scales
 //   warp 13          which units come next
 //   warp 12          the products, in the order  S_A(0) S_B(0) | PV_A(j) S_A(j+1) PV_B(j) S_B(j+1) | ...
 //                    so that one tile's powers run beside the other's products
@@ -33,6 +34,7 @@ constexpr int kQ = 128, kPair = 2 * kQ;   // queries of a tile, of a unit
 constexpr int kKeys = 128;                // positions of a tile
 constexpr int kLoaders = 128;
 constexpr int kRaw = 3;                   // tiles in 8 bits under way
+constexpr int kFours = kKeys / 4, kSlots = 4;  // scales of a tile; tiles whose scales are held
 constexpr int kFixed = 2;                 // tiles that a unit's beginning and end are worth
 constexpr float kSlack = 8.f;             // log2 of what a maximum may grow by before O is shrunk
 constexpr float kLeastScale = 0x1p-64f;
@@ -43,10 +45,10 @@ template <bool E, int D> struct Shape {
     static constexpr int kEight = 8 * kRow;                  // bytes of eight keys: 64 elements of all, then the other 64
     static constexpr int kTile = kKeys * kRow;
     static constexpr int kStages = D == 64 ? 8 : E ? 3 : 4;
-    static constexpr int kScales = E ? 3 * kKeys * 4 : 0;    // of a stage: keys' scales, log2 and reciprocal of values'
+    static constexpr int kScales = E ? kSlots * 3 * kFours * 4 : 0;  // keys' scales, log2 and reciprocal of values', for each four positions
     static constexpr int kQBytes = 2 * kTile;
     static constexpr int kRawBytes = E ? kRaw * kKeys * D : 0;
-    static constexpr int kSmem = 1024 + kQBytes + kRawBytes + kStages * (kTile + kScales) + kKeys * 8;
+    static constexpr int kSmem = 1024 + kQBytes + kRawBytes + kStages * kTile + kScales + kKeys * 8;
     static_assert(kSmem + 1024 <= 227 * 1024, "shared memory");  // with what is static
 };
 
@@ -62,7 +64,7 @@ struct PromptArgs {
 constexpr int kUnits = 4;  // that the roles may be apart
 
 enum { kBarQFull, kBarQEmpty, kBarS, kBarP = kBarS + 2, kBarO = kBarP + 4, kBarDrain = kBarO + 2, kBarFull, kBarUnit = kBarFull + 16, kBarRaw = kBarUnit + 2 * kUnits,
-       kBars = kBarRaw + 2 * kRaw };
+       kBarScale = kBarRaw + 2 * kRaw, kBars = kBarScale + 2 * kSlots };
 
 __device__ __forceinline__ uint32_t smem_of(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -294,58 +296,68 @@ struct Unit {
     int32_t first, parts;   // the unit's CTAs
 };
 
-// Walks the CTA's stretch.
+// Walks the CTA's stretch: from its first place (found by division and a root) unit by unit.
 struct Walk {
     Span span;
-    int64_t at, stop, row_begin;
-    int32_t r;
+    int64_t at, stop;
+    int64_t begin;      // of the unit
+    int64_t i;          // the unit of its key head
+    int32_t r, head;
     Row row;
     Line line;
 
-    __device__ __forceinline__ Walk(const AttendArgs &a, const Found &f) : span(span_of(a, f.total)), row_begin(f.row_begin), r(f.row)
+    __device__ __forceinline__ Walk(const AttendArgs &a, const Found &f) : span(span_of(a, f.total)), r(f.row)
     {
         at = span.begin(blockIdx.x), stop = span.begin(blockIdx.x + 1);
         row = row_of(a, r), line = line_of(a, row);
+        const int64_t each = line.head();
+        head = (int32_t)((at - f.row_begin) / each);
+        const int64_t base = f.row_begin + head * each, x = at - base;
+        // The unit that holds place x: i W + t i (i + 1) <= x.
+        const double t = (double)line.tile_q, b = (double)line.w + t;
+        i = max((int64_t)0, min(line.units - 1, (int64_t)((sqrt(b * b + 4.0 * t * (double)x) - b) / (2.0 * t))));
+        while (i > 0 && line.upto(i) > x) i--;
+        while (i + 1 < line.units && line.upto(i + 1) <= x) i++;
+        begin = base + line.upto(i);
     }
 
     __device__ __forceinline__ bool next(const AttendArgs &a, Unit &u)
     {
         while (at < stop) {
-            const int64_t head = line.head();
-            if (at >= row_begin + a.kv * head) {
-                row_begin += a.kv * head;
+            while (i >= line.units) {  // the next key head, or the next row that has units
+                i = 0;
+                if (++head < a.kv && line.units) break;
+                head = 0;
                 row = row_of(a, ++r), line = line_of(a, row);
-                continue;
             }
-            u.row = row, u.r = r;
-            u.head = (int32_t)((at - row_begin) / head);
-            const int64_t base = row_begin + u.head * head, x = at - base;
-            // The unit that holds place x: i W + t i (i + 1) <= x.
-            const double t = (double)line.tile_q, b = (double)line.w + t;
-            int64_t i = (int64_t)((sqrt(b * b + 4.0 * t * (double)x) - b) / (2.0 * t));
-            i = max((int64_t)0, min(line.units - 1, i));
-            while (i > 0 && line.upto(i) > x) i--;
-            while (i + 1 < line.units && line.upto(i + 1) <= x) i++;
-            const int64_t begin = base + line.upto(i), end = base + line.upto(i + 1), m = (int64_t)row.n * a.group;
+            const int64_t end = begin + line.w + 2 * line.tile_q * (i + 1);
             const int32_t have = row.len - row.n;
+            u.row = row, u.r = r, u.head = head;
             u.q0 = i * 2 * a.tile_q;
-            u.queries = (int32_t)min((int64_t)2 * a.tile_q, m - u.q0);
+            u.queries = (int32_t)min((int64_t)2 * a.tile_q, (int64_t)row.n * a.group - u.q0);
             auto sees = [&](int64_t q) { return have + (int32_t)wf_quot((uint32_t)q, a.by_group) + 1; };
             u.seen = sees(u.q0 + u.queries - 1);
             const int32_t tiles_a = (sees(u.q0 + min(u.queries, a.tile_q) - 1) + kKeys - 1) / kKeys, tiles = (u.seen + kKeys - 1) / kKeys;
             const int64_t each = (int64_t)kKeys * a.group;
-            auto tile = [&](int64_t p) { return p >= end ? tiles : (int32_t)max((int64_t)0, min((int64_t)tiles, (p - begin) / each - kFixed)); };
-            const int32_t t0 = tile(max(at, begin)), t1 = tile(min(stop, end));
-            const int64_t here = max(at, begin);
+            auto tile = [&](int64_t p) {
+                return p >= end ? tiles : p <= begin ? 0 : (int32_t)max((int64_t)0, min((int64_t)tiles, (p - begin) / each - kFixed));
+            };
+            const int32_t t0 = tile(at), t1 = tile(stop);
+            const bool split = at > begin || stop < end;
+            const int64_t unit_begin = begin;
             at = min(stop, end);
+            if (at == end) begin = end, i++;
             if (t1 <= t0) continue;
             u.t0 = t0, u.n = t1 - t0;
             u.na = max(0, min(t1, tiles_a) - t0), u.nb = u.queries > a.tile_q ? u.n : 0;
             u.first = blockIdx.x, u.parts = 1;
-            if (here != begin || at != end) {
-                int32_t first = span.owner(begin), last = span.owner(end - 1);
-                while (tile(span.begin(first + 1)) <= 0) first++;
-                while (tile(span.begin(last)) >= tiles) last--;
+            if (split) {
+                int32_t first = span.owner(unit_begin), last = span.owner(end - 1);
+                auto part = [&](int64_t p) {
+                    return p >= end ? tiles : p <= unit_begin ? 0 : (int32_t)max((int64_t)0, min((int64_t)tiles, (p - unit_begin) / each - kFixed));
+                };
+                while (part(span.begin(first + 1)) <= 0) first++;
+                while (part(span.begin(last)) >= tiles) last--;
                 u.first = first, u.parts = last - first + 1;
             }
             return true;
@@ -500,6 +512,36 @@ template <typename T, bool E, int D> __device__ __forceinline__ void box_role(co
     }
 }
 
+// Warp 15, 8 bits: the scales of each four positions, which lie in one block.
+__device__ __forceinline__ void scale_role(const AttendArgs &a, const Shared &sh)
+{
+    const int lane = threadIdx.x % 32;
+    uint32_t t = 0;
+    for (uint32_t units = 0;; units++) {
+        const Unit &u = sh.unit(units);
+        if (!u.n) break;
+        const int32_t *table = a.table + u.r * a.table_stride;
+        const int32_t end = min(u.seen, (u.t0 + u.n) * kKeys), n = u.n, p0 = u.t0 * kKeys + 4 * lane;
+        const float *ks = a.k_scale + u.head, *vs = a.v_scale + u.head;
+        // Blocks two tiles ahead, scales one.
+        auto block = [&](int32_t j) { return (int64_t)block_at(a, table, wf_quot(min(p0 + j * kKeys, end - 1), a.by_bs)) * a.kv; };
+        int64_t b = block(0);
+        float k = ks[b], v = vs[b];
+        b = block(min(1, n - 1));
+        for (int32_t j = 0; j < n; j++, t++) {
+            const float now_k = k, now_v = fmaxf(v, kLeastScale);
+            if (j + 1 < n) k = ks[b], v = vs[b];
+            if (j + 2 < n) b = block(j + 2);
+            const uint32_t s = t % kSlots;
+            sh.wait(kBarScale + kSlots + s, (t / kSlots & 1) ^ 1);
+            float *to = sh.scales + s * 3 * kFours + lane;
+            to[0] = now_k, to[kFours] = __log2f(now_v), to[2 * kFours] = __frcp_rn(now_v);
+            bar_arrive(sh.bar(kBarScale + s));
+        }
+        sh.unit_done(units);
+    }
+}
+
 // Warps 8 - 11: what tensor maps cannot copy: any blocks and alignment, queries of any group, and 8 bits to halves.
 template <typename T, bool E, int D> __device__ __forceinline__ void load_role(const PromptArgs &pa, const Shared &sh)
 {
@@ -525,9 +567,7 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
             return block_at(a, table, wf_quot(p, a.by_bs));
         };
         const bool tiles = E || !pa.box;
-        int32_t next = tiles ? block(0) : 0;
-        float next_k = 1.f, next_v = 1.f;
-        if (E) next_k = a.k_scale[(int64_t)next * a.kv + u.head], next_v = a.v_scale[(int64_t)next * a.kv + u.head];
+        int32_t next = !E && tiles ? block(0) : 0;
         // What is under way belongs to the unit before, which must have it to come to its end.
         copies_wait<0>();
         for (; waiting; waiting--) announce(it - waiting);
@@ -571,16 +611,12 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
         for (int32_t j = 0; tiles && j < u.n; j++) {
             const int32_t p = (u.t0 + j) * kKeys + tid;
             int64_t *offset = sh.offset;
-            if (!E || !pa.box) {
+            if (!E) {
                 sync_some<1, kLoaders>();
                 offset[tid] = p < end ? next * a.block_stride + (int64_t)(p - (int32_t)wf_quot(p, a.by_bs) * a.bs) * a.token_stride : -1;
                 sync_some<1, kLoaders>();
             }
-            const float now_k = p < end ? next_k : 1.f, now_v = p < end ? fmaxf(next_v, kLeastScale) : 1.f;
-            if (j + 1 < u.n) {
-                next = block(j + 1);
-                if (E) next_k = a.k_scale[(int64_t)next * a.kv + u.head], next_v = a.v_scale[(int64_t)next * a.kv + u.head];
-            }
+            if (!E && j + 1 < u.n) next = block(j + 1);
 #pragma unroll 1
             for (int side = 0; side < 2; side++, it++) {  // keys, values
                 const uint32_t s = it % S::kStages, to = kv + s * S::kTile;
@@ -593,8 +629,8 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
                     announce(it - waiting);
                     waiting--;
                 }
-                sh.wait(kBarFull + 8 + s, freed);
                 if constexpr (!E) {
+                    sh.wait(kBarFull + 8 + s, freed);
                     constexpr int kPer = D / 8, kRows = kLoaders / kPer;
                     const int c = tid % kPer;
 #pragma unroll 8
@@ -615,25 +651,15 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
                     const int c = tid % kPer;
                     const uint32_t rs = it % kRaw;
                     uint4 x[kTimes];
-                    if (pa.box) {
-                        sh.wait(kBarRaw + rs, it / kRaw & 1);
+                    sh.wait(kBarRaw + rs, it / kRaw & 1);
 #pragma unroll
-                        for (int i = 0; i < kTimes; i++) {
-                            const int row = i * kRows + tid / kPer;
-                            x[i] = *reinterpret_cast<const uint4 *>(sh.raw + rs * (kKeys * D) + row * D + 16 * c);
-                            if (p - tid + row >= end) x[i] = make_uint4(0, 0, 0, 0);
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < kTimes; i++) {
-                            const int64_t o = offset[i * kRows + tid / kPer];
-                            x[i] = o >= 0 ? *reinterpret_cast<const uint4 *>(from + o + 16 * c) : make_uint4(0, 0, 0, 0);
-                        }
+                    for (int i = 0; i < kTimes; i++) {
+                        const int row = i * kRows + tid / kPer;
+                        x[i] = *reinterpret_cast<const uint4 *>(sh.raw + rs * (kKeys * D) + row * D + 16 * c);
+                        if (p - tid + row >= end) x[i] = make_uint4(0, 0, 0, 0);
                     }
-                    if (side) {  // the scales of this tile, with its values: both stay until the weights are made
-                        float *sc = sh.scales + s * (S::kScales / 4) + tid;
-                        sc[0] = now_k, sc[kKeys] = __log2f(now_v), sc[2 * kKeys] = __frcp_rn(now_v);
-                    }
+                    bar_arrive(sh.bar(kBarRaw + kRaw + rs));
+                    sh.wait(kBarFull + 8 + s, freed);
 #pragma unroll
                     for (int i = 0; i < kTimes; i++) {
                         const int row = i * kRows + tid / kPer;
@@ -643,7 +669,6 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
                         *reinterpret_cast<uint4 *>(dst + place<D>(row, 2 * c + 1)) = make_uint4(h2.x, h2.y, h3.x, h3.y);
                     }
                     announce(it);
-                    if (pa.box) bar_arrive(sh.bar(kBarRaw + kRaw + rs));
                 }
             }
         }
@@ -769,7 +794,7 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
     using M = std::conditional_t<E, __half, T>;
     const int x = threadIdx.x / kQ, q = threadIdx.x % kQ, qq = x * a.tile_q + q;  // tile, query of the tile, of the unit
     const uint32_t lane = tmem + ((uint32_t)(q / 32 * 32) << 16), st = lane + x * kKeys, ot = lane + 2 * kKeys + x * D;
-    uint32_t ns = 0, no = 0, it = 0, units = 0;
+    uint32_t ns = 0, no = 0, ts = 0, units = 0;
     for (;; units++) {
         const Unit &u = sh.unit(units);
         if (!u.n) break;
@@ -797,17 +822,20 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
             for (int i = 0; i < 4; i++) tm_load(w + 32 * i, st + 32 * i);
             const float *sc = nullptr;
             if constexpr (E) {
-                const uint32_t i = it + 2 * j + 1;
-                sh.wait(kBarFull + i % S::kStages, (i / S::kStages) & 1);
-                sc = sh.scales + i % S::kStages * (S::kScales / 4);
+                sh.wait(kBarScale + ts % kSlots, ts / kSlots & 1);
+                sc = sh.scales + ts % kSlots * 3 * kFours;
             }
             tm_loaded();
             if constexpr (E) {
 #pragma unroll
-                for (int i = 0; i < kKeys; i += 4) {
-                    const float4 ks = *reinterpret_cast<const float4 *>(sc + i), lg = *reinterpret_cast<const float4 *>(sc + kKeys + i);
-                    s[i] = fmaf(s[i], scale * ks.x, lg.x), s[i + 1] = fmaf(s[i + 1], scale * ks.y, lg.y);
-                    s[i + 2] = fmaf(s[i + 2], scale * ks.z, lg.z), s[i + 3] = fmaf(s[i + 3], scale * ks.w, lg.w);
+                for (int i = 0; i < kFours; i += 4) {
+                    const float4 ks = *reinterpret_cast<const float4 *>(sc + i), lg = *reinterpret_cast<const float4 *>(sc + kFours + i);
+                    const float by[4] = {scale * ks.x, scale * ks.y, scale * ks.z, scale * ks.w}, plus[4] = {lg.x, lg.y, lg.z, lg.w};
+#pragma unroll
+                    for (int k = 0; k < 16; k += 2) {
+                        const float2 y = fma2(make_float2(s[4 * i + k], s[4 * i + k + 1]), make_float2(by[k / 4], by[k / 4]), make_float2(plus[k / 4], plus[k / 4]));
+                        s[4 * i + k] = y.x, s[4 * i + k + 1] = y.y;
+                    }
                 }
             }
             const int32_t p = (u.t0 + j) * kKeys;
@@ -830,7 +858,12 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
                     float2 y = make_float2(s[i], s[i + 1]);
                     y = E ? add2(y, off) : fma2(y, by, off);
                     y = make_float2(power(y.x), power(y.y));
-                    sums[i / 2 % 2] = E ? fma2(y, *reinterpret_cast<const float2 *>(sc + 2 * kKeys + i), sums[i / 2 % 2]) : add2(y, sums[i / 2 % 2]);
+                    if constexpr (E) {
+                        const float inv = sc[2 * kFours + i / 4];
+                        sums[i / 2 % 2] = fma2(y, make_float2(inv, inv), sums[i / 2 % 2]);
+                    } else {
+                        sums[i / 2 % 2] = add2(y, sums[i / 2 % 2]);
+                    }
                     w[i / 2] = wf_pair<M>::of_float(y.x, y.y);
                 }
             };
@@ -866,10 +899,15 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
                 before_sync();
                 bar_arrive(sh.bar(kBarP + 2 * half + x));
             }
+            if constexpr (E) bar_arrive(sh.bar(kBarScale + kSlots + ts++ % kSlots));
             sums[0] = add2(sums[0], sums[1]);
             sum += sums[0].x + sums[0].y;
         }
-        it += 2 * u.n;
+        if constexpr (E)  // tiles that this one does not see
+            for (int j = n; j < u.n; j++, ts++) {
+                sh.wait(kBarScale + ts % kSlots, ts / kSlots & 1);
+                bar_arrive(sh.bar(kBarScale + kSlots + ts % kSlots));
+            }
         if (n > 0) {
             sh.wait(kBarO + x, no & 1);
             no++;
@@ -970,8 +1008,9 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
             if (i == kBarQFull) n = pa.map_q ? 1 : kLoaders;
             if (i >= kBarP && i < kBarO) n = kQ;
             if (i >= kBarFull && i < kBarFull + 8) n = E || !pa.box ? kLoaders : 1;
-            if (i >= kBarUnit + kUnits && i < kBarUnit + 2 * kUnits) n = 2 * kQ + 1 + (loaders ? kLoaders : 0) + (boxes ? 32 : 0);
-            if (i >= kBarRaw + kRaw) n = kLoaders;
+            if (i >= kBarUnit + kUnits && i < kBarUnit + 2 * kUnits) n = 2 * kQ + 1 + (loaders ? kLoaders : 0) + (boxes ? 32 : 0) + (E ? 32 : 0);
+            if (i >= kBarRaw + kRaw && i < kBarScale) n = kLoaders;
+            if (i >= kBarScale) n = i < kBarScale + kSlots ? 32 : 2 * kQ;
             bar_init(sh.bar(i), n);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -996,6 +1035,7 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
         if (warp == 12) product_role<T, E, D>(sh, tmem);
         if (warp == 13 && threadIdx.x % 32 == 0) unit_role(a, f, sh);
         if (warp == 14 && (pa.box || pa.map_q)) box_role<T, E, D>(pa, sh);
+        if (E && warp == 15) scale_role(a, sh);
         __syncwarp();
     }
     before_sync();
@@ -1053,7 +1093,7 @@ template <typename T, bool E, int D> int launch(const wf_attn *at, const AttendA
     const int box = std::min(kKeys, a.bs & -a.bs);
     const int64_t step = a.kv == 1 ? a.block_stride : a.head_stride;
     const int64_t heads = step > 0 && a.block_stride % step == 0 ? a.block_stride / step : 0, places = (a.n_blocks - 1) * heads + a.kv;
-    if (box >= 8 && heads && places < INT32_MAX) {
+    if (box >= (E ? 4 : 8) && heads && places < INT32_MAX) {
         const auto type = E ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : half;
         const cuuint64_t tok = (cuuint64_t)a.token_stride, sizes8[3] = {D, (cuuint64_t)a.bs, (cuuint64_t)places}, strides8[2] = {tok, (cuuint64_t)step};
         const cuuint32_t shape8[3] = {D, (cuuint32_t)box, 1};
@@ -1064,6 +1104,7 @@ template <typename T, bool E, int D> int launch(const wf_attn *at, const AttendA
         };
         if (map(&pa.k, a.k) && map(&pa.v, a.v)) pa.box = box, pa.heads = (int32_t)heads, pa.beyond = (int32_t)places;
     }
+    if (E && !pa.box) return -1;
     // Queries of whole tokens: a group's heads, then the next token's.  Over 8 bits bfloat16 queries are scaled first.
     if (a.group <= kQ && !(E && std::is_same_v<T, __nv_bfloat16>)) {
         const int tokens = kQ / a.group;
@@ -1094,6 +1135,7 @@ int wf_prompt_setup(wf_attn *at)
 
 size_t wf_prompt_scratch(const wf_attn *at) { return sizeof(float) * 2 * (size_t)at->sms * (at->lim.dim == 64 ? kPart<64> : kPart<128>); }
 
+// WF_OK, an error, or -1: not for this kernel (8 bits whose blocks do not come in fours of positions or lie anyhow).
 int wf_launch_prompt(wf_attn *at, const AttendArgs &a, int dtype, int dim, bool eight, cudaStream_t st)
 {
     if (dtype == WF_F16) {
