@@ -75,6 +75,13 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
 }
 __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
+// One arrival for the warp, once every lane has come.
+__device__ __forceinline__ void warp_arrive(uint32_t bar)
+{
+    __syncwarp();
+    if (threadIdx.x % 32 == 0) bar_arrive(bar);
+}
+
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
@@ -386,7 +393,7 @@ struct Shared {
         wait(kBarUnit + i % kUnits, i / kUnits & 1);
         return units[i % kUnits];
     }
-    __device__ __forceinline__ void unit_done(uint32_t i) const { bar_arrive(bar(kBarUnit + kUnits + i % kUnits)); }
+    __device__ __forceinline__ void unit_done(uint32_t i) const { warp_arrive(bar(kBarUnit + kUnits + i % kUnits)); }
 };
 
 // One thread: the units, as room comes free.
@@ -427,21 +434,15 @@ template <typename T> __device__ __forceinline__ float largest(const uint4 &x)
     return fmaxf(fmaxf(fmaxf(fabsf(a.x), fabsf(a.y)), fmaxf(fabsf(b.x), fabsf(b.y))), fmaxf(fmaxf(fabsf(c.x), fabsf(c.y)), fmaxf(fabsf(d.x), fabsf(d.y))));
 }
 
-// A tile's positions p .. by boxes of `box` positions of one block: one copy a lane.  Boxes behind `end` come from a block that is not
-// there: zeros.
+// A tile by boxes of `box` positions of one block: one copy a lane, whose block (in the maps' last coordinate) and place in it are given.
 template <bool E, int D>
-__device__ __forceinline__ void copy_boxes(const PromptArgs &pa, const Unit &u, const CUtensorMap *map, uint32_t to, uint32_t bar, int32_t p, int32_t end, int lane)
+__device__ __forceinline__ void copy_boxes(const PromptArgs &pa, const CUtensorMap *map, uint32_t to, uint32_t bar, int32_t block, int32_t place, int lane)
 {
     constexpr int kRow = E ? D : 2 * D;
-    const AttendArgs &a = pa.a;
     const int box = pa.box;
     if (lane == 0) bar_expect(bar, kKeys * kRow);
     __syncwarp();
     if (lane * box < kKeys) {
-        const int32_t at = p + lane * box;
-        const uint32_t j = wf_quot(min(at, end - 1), a.by_bs);
-        const int32_t block = at < end ? block_at(a, a.table + u.r * a.table_stride, j) * pa.heads + u.head : pa.beyond;
-        const int32_t place = at < end ? at - (int32_t)j * a.bs : 0;
         if constexpr (E) copy_box3(to + lane * box * kRow, map, bar, 0, place, block);
         else copy_box5(to + lane * box * kRow, map, bar, 0, 0, 0, place / 8, block);
     }
@@ -471,8 +472,15 @@ template <typename T, bool E, int D> __device__ __forceinline__ void box_role(co
         }
         if (pa.box) {
             const int32_t end = min(u.seen, (u.t0 + u.n) * kKeys);
+            const int32_t *table = a.table + u.r * a.table_stride;
+            // This lane's box of tile j: its block in the table, and in the maps.  Boxes behind `end` come from a block that is not there: zeros.
+            auto position = [&](int32_t j) { return (u.t0 + j) * kKeys + min(lane * pa.box, kKeys - 1); };
+            auto block = [&](int32_t j) { return block_at(a, table, wf_quot(min(position(j), end - 1), a.by_bs)); };
+            int32_t next = block(0);
             for (int32_t j = 0; j < u.n; j++) {
-                const int32_t p = (u.t0 + j) * kKeys;
+                const int32_t p = (u.t0 + j) * kKeys, at = position(j);
+                const int32_t b = at < end ? next * pa.heads + u.head : pa.beyond, place_in = at < end ? at - (int32_t)wf_quot(at, a.by_bs) * a.bs : 0;
+                if (j + 1 < u.n) next = block(j + 1);
                 // A box that the row ends in holds what lies behind the row, and a weight of 0 does not undo a NaN there.
                 const bool ends = !E && u.row.len % pa.box && p + kKeys > u.row.len;
 #pragma unroll 1
@@ -481,21 +489,20 @@ template <typename T, bool E, int D> __device__ __forceinline__ void box_role(co
                     if constexpr (E) {
                         const uint32_t s = it % kRaw;
                         sh.wait(kBarRaw + kRaw + s, (it / kRaw & 1) ^ 1);
-                        copy_boxes<E, D>(pa, u, map, raw + s * (kKeys * D), sh.bar(kBarRaw + s), p, end, lane);
+                        copy_boxes<E, D>(pa, map, raw + s * (kKeys * D), sh.bar(kBarRaw + s), b, place_in, lane);
                     } else {
                         const uint32_t s = it % S::kStages, to = kv + s * S::kTile;
                         sh.wait(kBarFull + 8 + s, (it / S::kStages & 1) ^ 1);
                         if (!ends || !side) {
-                            copy_boxes<E, D>(pa, u, map, to, sh.bar(kBarFull + s), p, end, lane);
+                            copy_boxes<E, D>(pa, map, to, sh.bar(kBarFull + s), b, place_in, lane);
                         } else {
                             constexpr int kPer = D / 8;
                             const uint8_t *v = a.v + u.head * a.head_stride;
-                            const int32_t *table = a.table + u.r * a.table_stride;
 #pragma unroll 1
                             for (int i = lane / kPer; i < kKeys; i += 32 / kPer) {
-                                const int32_t at = min(p + i, u.row.len - 1);
-                                const uint32_t b = wf_quot(at, a.by_bs);
-                                const uint8_t *from = v + block_at(a, table, b) * a.block_stride + (at - (int32_t)b * a.bs) * a.token_stride;
+                                const int32_t key = min(p + i, u.row.len - 1);
+                                const uint32_t in = wf_quot(key, a.by_bs);
+                                const uint8_t *from = v + block_at(a, table, in) * a.block_stride + (key - (int32_t)in * a.bs) * a.token_stride;
                                 copy16(to + place<D>(i, lane % kPer), from + lane % kPer * 16, p + i < u.row.len);
                             }
                             copies_commit();
@@ -536,7 +543,7 @@ __device__ __forceinline__ void scale_role(const AttendArgs &a, const Shared &sh
             sh.wait(kBarScale + kSlots + s, (t / kSlots & 1) ^ 1);
             float *to = sh.scales + s * 3 * kFours + lane;
             to[0] = now_k, to[kFours] = __log2f(now_v), to[2 * kFours] = __frcp_rn(now_v);
-            bar_arrive(sh.bar(kBarScale + s));
+            warp_arrive(sh.bar(kBarScale + s));
         }
         sh.unit_done(units);
     }
@@ -553,7 +560,7 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
     int32_t waiting = 0;   // tiles whose copies are under way and not yet announced (16 bits)
     auto announce = [&](uint32_t i) {
         to_async();
-        bar_arrive(sh.bar(kBarFull + i % S::kStages));
+        warp_arrive(sh.bar(kBarFull + i % S::kStages));
     };
     for (;; units++) {
         const Unit &u = sh.unit(units);
@@ -606,7 +613,7 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
             copies_commit();
             copies_wait<0>();
             to_async();
-            bar_arrive(sh.bar(kBarQFull));
+            warp_arrive(sh.bar(kBarQFull));
         }
         for (int32_t j = 0; tiles && j < u.n; j++) {
             const int32_t p = (u.t0 + j) * kKeys + tid;
@@ -658,7 +665,7 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
                         x[i] = *reinterpret_cast<const uint4 *>(sh.raw + rs * (kKeys * D) + row * D + 16 * c);
                         if (p - tid + row >= end) x[i] = make_uint4(0, 0, 0, 0);
                     }
-                    bar_arrive(sh.bar(kBarRaw + kRaw + rs));
+                    warp_arrive(sh.bar(kBarRaw + kRaw + rs));
                     sh.wait(kBarFull + 8 + s, freed);
 #pragma unroll
                     for (int i = 0; i < kTimes; i++) {
@@ -717,7 +724,7 @@ template <typename T, bool E, int D> __device__ __forceinline__ void product_rol
         const Unit &u = sh.unit(units);
         const int n[2] = {u.na, u.nb}, most = u.n;
         if (!most) break;
-        if (elected()) sh.unit_done(units);
+        sh.unit_done(units);
         sh.wait(kBarQFull, units & 1);
         full(it);
         after_sync();
@@ -897,16 +904,16 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
                 tm_store(st + half * 32, w + half * 32);
                 tm_stored();
                 before_sync();
-                bar_arrive(sh.bar(kBarP + 2 * half + x));
+                warp_arrive(sh.bar(kBarP + 2 * half + x));
             }
-            if constexpr (E) bar_arrive(sh.bar(kBarScale + kSlots + ts++ % kSlots));
+            if constexpr (E) warp_arrive(sh.bar(kBarScale + kSlots + ts++ % kSlots));
             sums[0] = add2(sums[0], sums[1]);
             sum += sums[0].x + sums[0].y;
         }
         if constexpr (E)  // tiles that this one does not see
             for (int j = n; j < u.n; j++, ts++) {
                 sh.wait(kBarScale + ts % kSlots, ts / kSlots & 1);
-                bar_arrive(sh.bar(kBarScale + kSlots + ts % kSlots));
+                warp_arrive(sh.bar(kBarScale + kSlots + ts % kSlots));
             }
         if (n > 0) {
             sh.wait(kBarO + x, no & 1);
@@ -1004,13 +1011,13 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
         gave_up = 0;
         const bool loaders = E || !pa.box || !pa.map_q, boxes = pa.box || pa.map_q;
         for (int i = 0; i < kBars; i++) {
-            uint32_t n = 1;
-            if (i == kBarQFull) n = pa.map_q ? 1 : kLoaders;
-            if (i >= kBarP && i < kBarO) n = kQ;
-            if (i >= kBarFull && i < kBarFull + 8) n = E || !pa.box ? kLoaders : 1;
-            if (i >= kBarUnit + kUnits && i < kBarUnit + 2 * kUnits) n = 2 * kQ + 1 + (loaders ? kLoaders : 0) + (boxes ? 32 : 0) + (E ? 32 : 0);
-            if (i >= kBarRaw + kRaw && i < kBarScale) n = kLoaders;
-            if (i >= kBarScale) n = i < kBarScale + kSlots ? 32 : 2 * kQ;
+            uint32_t n = 1;  // a warp arrives once
+            if (i == kBarQFull) n = pa.map_q ? 1 : 4;
+            if (i >= kBarP && i < kBarO) n = 4;
+            if (i >= kBarFull && i < kBarFull + 8) n = E || !pa.box ? 4 : 1;
+            if (i >= kBarUnit + kUnits && i < kBarUnit + 2 * kUnits) n = 8 + 1 + (loaders ? 4 : 0) + (boxes ? 1 : 0) + (E ? 1 : 0);
+            if (i >= kBarRaw + kRaw && i < kBarScale) n = 4;
+            if (i >= kBarScale + kSlots) n = 8;
             bar_init(sh.bar(i), n);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
