@@ -33,7 +33,7 @@ constexpr int kThreads = 512;
 constexpr int kQ = 128, kPair = 2 * kQ;   // queries of a tile, of a unit
 constexpr int kKeys = 128;                // positions of a tile
 constexpr int kLoaders = 128;
-constexpr int kRaw = 3;                   // tiles in 8 bits under way
+constexpr int kRaws = 3;                  // at most
 constexpr int kFours = kKeys / 4, kSlots = 4;  // scales of a tile; tiles whose scales are held
 constexpr int kFixed = 2;                 // tiles that a unit's beginning and end are worth
 constexpr float kSlack = 8.f;             // log2 of what a maximum may grow by before O is shrunk
@@ -44,12 +44,13 @@ template <bool E, int D> struct Shape {
     static constexpr int kHalf = kQ * 128;                   // bytes of 64 elements of the queries
     static constexpr int kEight = 8 * kRow;                  // bytes of eight keys: 64 elements of all, then the other 64
     static constexpr int kTile = kKeys * kRow;
-    static constexpr int kStages = D == 64 ? 8 : E ? 3 : 4;
+    static constexpr int kStages = D == 64 ? 8 : 4;
+    static constexpr int kRaw = D == 64 ? 3 : 2;             // tiles in 8 bits under way
     static constexpr int kScales = E ? kSlots * 3 * kFours * 4 : 0;  // keys' scales, log2 and reciprocal of values', for each four positions
     static constexpr int kQBytes = 2 * kTile;
     static constexpr int kRawBytes = E ? kRaw * kKeys * D : 0;
-    static constexpr int kSmem = 1024 + kQBytes + kRawBytes + kStages * kTile + kScales + kKeys * 8;
-    static_assert(kSmem + 1024 <= 227 * 1024, "shared memory");  // with what is static
+    static constexpr int kSmem = kQBytes + kRawBytes + kStages * kTile + kScales + (E ? 0 : kKeys * 8);
+    static_assert(kSmem + 1024 <= 227 * 1024, "shared memory");  // with what is static, up to the next 1,024 bytes
 };
 
 struct PromptArgs {
@@ -63,8 +64,8 @@ struct PromptArgs {
 
 constexpr int kUnits = 4;  // that the roles may be apart
 
-enum { kBarQFull, kBarQEmpty, kBarS, kBarP = kBarS + 2, kBarO = kBarP + 4, kBarDrain = kBarO + 2, kBarFull, kBarUnit = kBarFull + 16, kBarRaw = kBarUnit + 2 * kUnits,
-       kBarScale = kBarRaw + 2 * kRaw, kBars = kBarScale + 2 * kSlots };
+enum { kBarQFull, kBarQEmpty, kBarS, kBarP = kBarS + 2, kBarO = kBarP + 2, kBarDrain = kBarO + 2, kBarFull, kBarUnit = kBarFull + 16, kBarRaw = kBarUnit + 2 * kUnits,
+       kBarScale = kBarRaw + 2 * kRaws, kBars = kBarScale + 2 * kSlots };
 
 __device__ __forceinline__ uint32_t smem_of(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -487,8 +488,8 @@ template <typename T, bool E, int D> __device__ __forceinline__ void box_role(co
                 for (int side = 0; side < 2; side++, it++) {
                     const CUtensorMap *map = side ? &pa.v : &pa.k;
                     if constexpr (E) {
-                        const uint32_t s = it % kRaw;
-                        sh.wait(kBarRaw + kRaw + s, (it / kRaw & 1) ^ 1);
+                        const uint32_t s = it % S::kRaw;
+                        sh.wait(kBarRaw + kRaws + s, (it / S::kRaw & 1) ^ 1);
                         copy_boxes<E, D>(pa, map, raw + s * (kKeys * D), sh.bar(kBarRaw + s), b, place_in, lane);
                     } else {
                         const uint32_t s = it % S::kStages, to = kv + s * S::kTile;
@@ -656,16 +657,16 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
                 } else {
                     constexpr int kPer = D / 16, kRows = kLoaders / kPer, kTimes = kKeys / kRows;
                     const int c = tid % kPer;
-                    const uint32_t rs = it % kRaw;
+                    const uint32_t rs = it % S::kRaw;
                     uint4 x[kTimes];
-                    sh.wait(kBarRaw + rs, it / kRaw & 1);
+                    sh.wait(kBarRaw + rs, it / S::kRaw & 1);
 #pragma unroll
                     for (int i = 0; i < kTimes; i++) {
                         const int row = i * kRows + tid / kPer;
                         x[i] = *reinterpret_cast<const uint4 *>(sh.raw + rs * (kKeys * D) + row * D + 16 * c);
                         if (p - tid + row >= end) x[i] = make_uint4(0, 0, 0, 0);
                     }
-                    warp_arrive(sh.bar(kBarRaw + kRaw + rs));
+                    warp_arrive(sh.bar(kBarRaw + kRaws + rs));
                     sh.wait(kBarFull + 8 + s, freed);
 #pragma unroll
                     for (int i = 0; i < kTimes; i++) {
@@ -695,14 +696,15 @@ template <typename T, bool E, int D> __device__ __forceinline__ void product_rol
     constexpr uint32_t kDescO = 1u << 4 | kType << 7 | kType << 10 | 1u << 16 | (D / 8) << 17 | (kQ / 16) << 24;
     const uint32_t kv = smem_of(sh.kv), q = smem_of(sh.q);
     uint32_t it = 0, units = 0, np[2] = {0, 0};
+    const bool leader = elected();  // once: elected anew for each turn, one prompt of 16,384 took 1,370 us in place of 1,302
     auto full = [&](uint32_t i) { sh.wait(kBarFull + i % S::kStages, (i / S::kStages) & 1); };
     auto commit = [&](int i) {
-        if (elected()) commit_to(sh.bar(i));
+        if (leader) commit_to(sh.bar(i));
     };
     auto done = [&](uint32_t i) { commit(kBarFull + 8 + i % S::kStages); };
     auto scores = [&](int x, uint32_t i) {
         const uint64_t key = matrix(kv + i % S::kStages * S::kTile, 16, S::kEight), query = matrix(q + x * S::kTile, 16, 1024);
-        if (elected()) {
+        if (leader) {
 #pragma unroll
             for (int s = 0; s < D / 16; s++) {
                 mma_ss(tmem + x * kKeys, query + ((s / 4 * S::kHalf + s % 4 * 32) >> 4), key + ((s / 4 * 1024 + s % 4 * 32) >> 4), kDescS, s > 0);
@@ -710,14 +712,12 @@ template <typename T, bool E, int D> __device__ __forceinline__ void product_rol
             commit_to(sh.bar(kBarS + x));
         }
     };
-    auto sums = [&](int x, int half, uint32_t i, bool more) {
+    auto sums = [&](int x, uint32_t i, bool more) {
         const uint64_t value = matrix(kv + i % S::kStages * S::kTile, 1024, S::kEight);
-        if (elected()) {
+        if (leader) {
 #pragma unroll
-            for (int s = 0; s < kKeys / 32; s++) {
-                const int k = half * kKeys / 32 + s;
-                mma_ts(tmem + 2 * kKeys + x * D, tmem + x * kKeys + 8 * k, value + k * (2 * S::kEight >> 4), kDescO, more || s > 0);
-            }
+            for (int s = 0; s < kKeys / 16; s++)
+                mma_ts(tmem + 2 * kKeys + x * D, tmem + x * kKeys + 8 * s, value + s * (2 * S::kEight >> 4), kDescO, more || s > 0);
         }
     };
     for (;; units++) {
@@ -735,20 +735,17 @@ template <typename T, bool E, int D> __device__ __forceinline__ void product_rol
         if (most == 1) commit(kBarQEmpty);
         for (int j = 0; j < most; j++) {
             full(it + 2 * j + 1);
+            if (j + 1 < most) full(it + 2 * j + 2);
 #pragma unroll
             for (int x = 0; x < 2; x++) {
                 if (j < n[x]) {
                     sh.wait(kBarP + x, np[x] & 1);
-                    after_sync();
-                    sums(x, 0, it + 2 * j + 1, j > 0);
-                    sh.wait(kBarP + 2 + x, np[x] & 1);
                     np[x]++;
                     after_sync();
-                    sums(x, 1, it + 2 * j + 1, true);
+                    sums(x, it + 2 * j + 1, j > 0);
                 }
                 if (x == 1) done(it + 2 * j + 1);
                 if (j + 1 < n[x]) {
-                    if (!x || j + 1 >= n[0]) full(it + 2 * j + 2);
                     scores(x, it + 2 * j + 2);
                 } else if (j < n[x]) {
                     commit(kBarO + x);
@@ -902,10 +899,10 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
             for (int half = 0; half < 2; half++) {
                 powers(half);
                 tm_store(st + half * 32, w + half * 32);
-                tm_stored();
-                before_sync();
-                warp_arrive(sh.bar(kBarP + 2 * half + x));
             }
+            tm_stored();
+            before_sync();
+            warp_arrive(sh.bar(kBarP + x));
             if constexpr (E) warp_arrive(sh.bar(kBarScale + kSlots + ts++ % kSlots));
             sums[0] = add2(sums[0], sums[1]);
             sum += sums[0].x + sums[0].y;
@@ -992,19 +989,23 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
 {
     const AttendArgs &a = pa.a;
     using S = Shape<E, D>;
-    extern __shared__ uint8_t raw[];
+    extern __shared__ __align__(1024) uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[kBars];
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up, last_one;
     __shared__ Unit units[kUnits];
     const Found f = find_row(a);
     if (f.row >= a.rows) return;
+    if (smem_of(raw) % 1024) {  // the swizzle's patterns would not lie as the products read them
+        if (threadIdx.x == 0) *a.err = 2;
+        return;
+    }
     Shared sh;
-    sh.q = raw + (1024 - smem_of(raw) % 1024) % 1024;
+    sh.q = raw;
     sh.kv = sh.q + S::kQBytes;
     sh.raw = sh.kv + S::kStages * S::kTile;
     sh.offset = reinterpret_cast<int64_t *>(sh.raw + S::kRawBytes);
-    sh.scales = reinterpret_cast<float *>(sh.offset + kKeys);
+    sh.scales = reinterpret_cast<float *>(sh.offset);  // 8 bits have no use for the other
     sh.units = units, sh.bars = smem_of(bars), sh.gave_up = &gave_up, sh.err = a.err;
     const int warp = threadIdx.x / 32;
     if (threadIdx.x == 0) {
@@ -1016,7 +1017,7 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
             if (i >= kBarP && i < kBarO) n = 4;
             if (i >= kBarFull && i < kBarFull + 8) n = E || !pa.box ? 4 : 1;
             if (i >= kBarUnit + kUnits && i < kBarUnit + 2 * kUnits) n = 8 + 1 + (loaders ? 4 : 0) + (boxes ? 1 : 0) + (E ? 1 : 0);
-            if (i >= kBarRaw + kRaw && i < kBarScale) n = 4;
+            if (i >= kBarRaw + kRaws && i < kBarScale) n = 4;
             if (i >= kBarScale + kSlots) n = 8;
             bar_init(sh.bar(i), n);
         }
