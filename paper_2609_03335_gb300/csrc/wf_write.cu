@@ -19,14 +19,17 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 32;   // tokens whose angles shared memory holds at once
-constexpr int kMaxPairs = 64;
+constexpr int kChunk = 64;   // tokens whose angles shared memory holds at once
+constexpr int kMost16 = 32;  // tokens of a CTA that writes 16 bits or queries
+constexpr int kMaxHeads = 4; // 8 bits: heads of a CTA
 
 struct WriteArgs {
     const int64_t *slot;
     const int32_t *pos;
     int64_t tokens, n_slots;
-    int32_t bs, kv, q_heads, pairs;  // pairs: of a head that turn
+    wf_div by_bs;
+    int32_t few;        // slots fit 31 bits: a block by a multiplication
+    int32_t rows, bs, kv, q_heads, pairs;  // pairs: of a head that turn
     const uint64_t *turn;
     float magnitude;
     const uint8_t *k, *v, *q;
@@ -136,6 +139,11 @@ __device__ __forceinline__ void turn_any(Pairs &p, const float2 *cs, int u, int 
     else turn_pairs<T, true>(p, cs, u, pairs);
 }
 
+__device__ __forceinline__ int64_t block_of(const WriteArgs &a, int64_t slot)
+{
+    return a.few ? (int64_t)wf_quot((uint32_t)slot, a.by_bs) : slot / a.bs;
+}
+
 // The bytes from the cache's start to a slot's token, or -1.
 __device__ __forceinline__ int64_t slot_offset(const WriteArgs &a, int64_t slot)
 {
@@ -144,12 +152,12 @@ __device__ __forceinline__ int64_t slot_offset(const WriteArgs &a, int64_t slot)
         *a.err = 1;
         return -1;
     }
-    const int64_t block = slot / a.bs;
+    const int64_t block = block_of(a, slot);
     return block * a.block_stride + (slot - block * a.bs) * a.token_stride;
 }
 
 // cos and sin of n tokens from `first`, and where they go.
-__device__ __forceinline__ void load_tokens(const WriteArgs &a, int64_t first, int n, float2 (*cs)[kMaxPairs], int64_t *at)
+__device__ __forceinline__ void load_tokens(const WriteArgs &a, int64_t first, int n, float2 *cs, int64_t *at)
 {
     for (int i = threadIdx.x; i < n; i += kThreads) at[i] = slot_offset(a, a.slot[first + i]);
     for (int i = threadIdx.x; i < n * a.pairs; i += kThreads) {
@@ -157,17 +165,16 @@ __device__ __forceinline__ void load_tokens(const WriteArgs &a, int64_t first, i
         const int32_t part = (int32_t)(((uint64_t)(uint32_t)a.pos[first + t] * a.turn[p]) >> 32);  // of a turn, in 2^-32
         float s, c;
         sincospif((float)part * 0x1p-31f, &s, &c);
-        cs[t][p] = make_float2(c * a.magnitude, s * a.magnitude);
+        cs[i] = make_float2(c * a.magnitude, s * a.magnitude);
     }
 }
 
 // Tokens from `first`, n of them: keys, values (KV) and queries, each read once and written once.
 template <typename T, int D, bool HALF, bool VEC, bool KV>
-__device__ __forceinline__ void write_tokens(const WriteArgs &a, int64_t first, int n)
+__device__ __forceinline__ void write_tokens(const WriteArgs &a, int64_t first, int n, float2 *cs)
 {
-    __shared__ float2 cs[kChunk][kMaxPairs];
-    __shared__ int64_t at[kChunk];
-    constexpr int kGroups = kThreads / kLanes<D>, kDeep = 4;  // heads at once; rounds whose loads are under way together
+    __shared__ int64_t at[kMost16];
+    constexpr int kGroups = kThreads / kLanes<D>, kDeep = 2;  // heads at once; rounds whose loads are under way together
     const int u = threadIdx.x % kLanes<D>, heads = a.q_heads + (KV ? 2 * a.kv : 0);
     load_tokens(a, first, n, cs, at);
     __syncthreads();
@@ -192,7 +199,7 @@ __device__ __forceinline__ void write_tokens(const WriteArgs &a, int64_t first, 
         for (int i = 0; i < kDeep; i++) {
             if (tt[i] >= n || at[tt[i]] < 0) continue;
             const bool q = hh[i] < a.q_heads, v = hh[i] >= a.q_heads + a.kv;
-            if (!v) turn_any<T, HALF, VEC>(p[i], cs[tt[i]], u, a.pairs);
+            if (!v) turn_any<T, HALF, VEC>(p[i], cs + tt[i] * a.pairs, u, a.pairs);
             const int kh = hh[i] - a.q_heads - (v ? a.kv : 0);
             uint8_t *to = q ? a.q_out + (first + tt[i]) * a.o_token + hh[i] * a.o_head
                             : (v ? a.cv : a.ck) + at[tt[i]] + kh * a.head_stride;
@@ -204,8 +211,9 @@ __device__ __forceinline__ void write_tokens(const WriteArgs &a, int64_t first, 
 
 template <typename T, int D, bool HALF, bool VEC> __global__ void __launch_bounds__(kThreads) write16_kernel(const WriteArgs a)
 {
+    extern __shared__ float2 angles[];
     const int64_t first = (int64_t)blockIdx.x * a.per;
-    write_tokens<T, D, HALF, VEC, true>(a, first, (int)min((int64_t)a.per, a.tokens - first));
+    write_tokens<T, D, HALF, VEC, true>(a, first, (int)min((int64_t)a.per, a.tokens - first), angles);
 }
 
 // ---------------------------------------------------------------------------
@@ -223,23 +231,51 @@ __device__ __forceinline__ float scale_of(float x)
 // A token is the first of its block's part in this step.
 __device__ __forceinline__ bool begins(const WriteArgs &a, int64_t t, int64_t slot)
 {
-    return t == 0 || a.slot[t - 1] != slot - 1 || slot % a.bs == 0;
+    return t == 0 || a.slot[t - 1] != slot - 1 || slot - block_of(a, slot) * a.bs == 0;
 }
 
 __device__ __forceinline__ float largest(float m, float x) { return fabsf(x) <= 3.402823466e38f ? fmaxf(m, fabsf(x)) : m; }
 
-// A window of a.per <= 32 tokens, heads h0 .. h0 + n_heads: the parts of blocks that begin in it.
-template <typename T, int D, bool HALF, bool VEC> __device__ __forceinline__ void write8_window(const WriteArgs &a, int64_t first, int h0)
+// The lane's 16 elements over a scale, to a token's head in the cache.
+template <typename T, bool HALF, bool VEC> __device__ __forceinline__ void store8(const WriteArgs &a, const Pairs &p, float scale, uint8_t *to, int u)
 {
-    constexpr int kL = kLanes<D>, kGroups = kThreads / kL;
-    extern __shared__ float dyn[];
-    __shared__ float2 cs[kChunk][kMaxPairs];
-    __shared__ int64_t at[kChunk], part_slot[32];
+    uint32_t w[8];  // a's 8 elements, b's 8, in twos
+    const bool two = (__float_as_int(scale) & 0x7FFFFF) == 0;  // a power of two: the product with its inverse is the quotient
+    const float inv = 1.f / scale;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        float2 f = wf_pair<T>::to_float(p.a[j]), g = wf_pair<T>::to_float(p.b[j]);
+        if (two) f.x *= inv, f.y *= inv, g.x *= inv, g.y *= inv;
+        else f.x /= scale, f.y /= scale, g.x /= scale, g.y /= scale;
+        w[j] = wf_e4m3_of(f.x, f.y);
+        w[4 + j] = wf_e4m3_of(g.x, g.y);
+    }
+    if (VEC) {
+        const bool apart = halves_apart(HALF, u, a.pairs);
+        *reinterpret_cast<uint2 *>(to + (apart ? 8 * u : 16 * u)) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+        *reinterpret_cast<uint2 *>(to + (apart ? 8 * u + a.pairs : 16 * u + 8)) = make_uint2(w[4] | w[5] << 16, w[6] | w[7] << 16);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            to[first_of(HALF, 8 * u + j, a.pairs)] = (uint8_t)(w[j / 2] >> (8 * (j % 2)));
+            to[second_of(HALF, 8 * u + j, a.pairs)] = (uint8_t)(w[4 + j / 2] >> (8 * (j % 2)));
+        }
+    }
+}
+
+// A window of a.per <= 32 tokens, heads h0 .. h0 + n_heads: the parts of blocks that begin in it.  Largest magnitudes first, by part and
+// head, then the scales, then the elements; where the parts are short (kKeep heads of a token for each group of lanes) these stay in registers
+// between.
+template <typename T, int D, bool HALF, bool VEC> __device__ __forceinline__ void write8_window(const WriteArgs &a, int64_t first, int h0, float2 *cs)
+{
+    constexpr int kL = kLanes<D>, kGroups = kThreads / kL, kKeep = 4;
+    __shared__ int64_t at[kChunk], part_block[32];
+    __shared__ int part_held[32];                    // tokens of the block before the part
+    __shared__ int amax[32 * 2 * kMaxHeads];         // [32][combos], then the scales
+    __shared__ float ratio[32 * 2 * kMaxHeads];      // [32][combos] old scale over new, 1: nothing to do
     __shared__ uint32_t s_begin;
     __shared__ int s_end;
     const int n_heads = min(a.heads_per, a.kv - h0), combos = 2 * n_heads;
-    int *amax = reinterpret_cast<int *>(dyn);         // [32][combos], then the scales
-    float *ratio = dyn + 32 * combos;                 // [32][combos] old scale over new, 1: nothing to do
     const int u = threadIdx.x % kL, group = threadIdx.x / kL;
     const int n = (int)min((int64_t)a.per, a.tokens - first);
     // The parts that begin here, and the end of the last one.
@@ -249,7 +285,11 @@ template <typename T, int D, bool HALF, bool VEC> __device__ __forceinline__ voi
         const bool live = slot >= 0 && slot < a.n_slots;
         if (slot >= a.n_slots) *a.err = 1;
         const uint32_t begin = __ballot_sync(~0u, live && begins(a, t, slot)), dead = __ballot_sync(~0u, !live && threadIdx.x < n);
-        if (live && (begin >> threadIdx.x & 1)) part_slot[__popc(begin & ((1u << threadIdx.x) - 1))] = slot;
+        if (live && (begin >> threadIdx.x & 1)) {
+            const int i = __popc(begin & ((1u << threadIdx.x) - 1));
+            part_block[i] = block_of(a, slot);
+            part_held[i] = (int)(slot - part_block[i] * a.bs);
+        }
         if (threadIdx.x == 0) {
             s_begin = begin;
             const uint32_t after = begin ? dead & ~((2u << (31 - __clz(begin))) - 1) : 0;  // the last part ends in the window
@@ -279,42 +319,73 @@ template <typename T, int D, bool HALF, bool VEC> __device__ __forceinline__ voi
         const int h = h0 + (v ? combo - n_heads : combo);
         return load_any<T, HALF, VEC>(v ? a.v + tok * a.v_token + h * a.v_head : a.k + tok * a.k_token + h * a.k_head, u, a.pairs);
     };
-    // The largest magnitudes, by part and head.
-    for (int base = from; base < end; base += kChunk) {
-        const int m = min(kChunk, end - base);
-        __syncthreads();
-        load_tokens(a, first + base, m, cs, at);
-        __syncthreads();
-        for (int i = group; i - group < m * combos; i += kGroups) {
-            const bool live = i < m * combos && at[min(i / combos, m - 1)] >= 0;
-            const int t = i / combos, combo = i - t * combos;
-            float most = 0.f;
-            if (live) {
-                Pairs p = load(base + t, combo);
-                if (combo < n_heads) turn_any<T, HALF, VEC>(p, cs[t], u, a.pairs);
+    auto head_at = [&](int combo) { return (combo >= n_heads ? a.cv : a.ck) + (h0 + (combo >= n_heads ? combo - n_heads : combo)) * a.head_stride; };
+    auto scale_at = [&](int part, int combo) {
+        const bool v = combo >= n_heads;
+        return (v ? a.v_scale : a.k_scale) + part_block[part] * a.kv + h0 + (v ? combo - n_heads : combo);
+    };
+    auto most_of = [](const Pairs &p) {
+        float most = 0.f;
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    const float2 x = wf_pair<T>::to_float(p.a[j]), y = wf_pair<T>::to_float(p.b[j]);
-                    most = largest(largest(largest(largest(most, x.x), x.y), y.x), y.y);
+        for (int j = 0; j < 4; j++) {
+            const float2 x = wf_pair<T>::to_float(p.a[j]), y = wf_pair<T>::to_float(p.b[j]);
+            most = largest(largest(largest(largest(most, x.x), x.y), y.x), y.y);
+        }
+        return most;
+    };
+    // Every group of the warp comes; live: with a token and head of its own.
+    auto put_most = [&](bool live, float most, int t, int combo) {
+#pragma unroll
+        for (int s = kL / 2; s; s /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, s));
+        if (live && u == 0) atomicMax(&amax[part_of(t) * combos + combo], __float_as_int(most));
+    };
+    const float old = threadIdx.x < parts * combos ? *scale_at(threadIdx.x / combos, threadIdx.x % combos) : 0.f;  // under way early
+    const int items = (end - from) * combos;
+    const bool kept = end - from <= kChunk && items <= kKeep * kGroups;
+    Pairs keep[kKeep];
+    if (kept) {
+#pragma unroll
+        for (int r = 0; r < kKeep; r++) {
+            const int i = group + r * kGroups, t = i / combos;
+            if (i < items) keep[r] = load(from + t, i - t * combos);
+        }
+        load_tokens(a, first + from, end - from, cs, at);
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kKeep; r++) {
+            const int i = group + r * kGroups, t = i / combos, combo = i - t * combos;
+            const bool live = i < items && at[t] >= 0;
+            if (live && combo < n_heads) turn_any<T, HALF, VEC>(keep[r], cs + t * a.pairs, u, a.pairs);
+            if (r * kGroups < items) put_most(live, live ? most_of(keep[r]) : 0.f, from + t, combo);
+        }
+    } else {
+        for (int base = from; base < end; base += kChunk) {
+            const int m = min(kChunk, end - base);
+            __syncthreads();
+            load_tokens(a, first + base, m, cs, at);
+            __syncthreads();
+            for (int i = group; i - group < m * combos; i += kGroups) {
+                const int t = i / combos, combo = i - t * combos;
+                const bool live = i < m * combos && at[t] >= 0;
+                Pairs p = {};
+                if (live) {
+                    p = load(base + t, combo);
+                    if (combo < n_heads) turn_any<T, HALF, VEC>(p, cs + t * a.pairs, u, a.pairs);
                 }
+                put_most(live, most_of(p), base + t, combo);
             }
-#pragma unroll
-            for (int s = kL / 2; s; s /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, s));
-            if (live && u == 0) atomicMax(&amax[part_of(base + t) * combos + combo], __float_as_int(most));
         }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < parts * combos; i += kThreads) {
         const int part = i / combos, combo = i - part * combos;
-        const bool v = combo >= n_heads;
-        const int64_t slot = part_slot[part], block = slot / a.bs;
-        float *scale = (v ? a.v_scale : a.k_scale) + block * a.kv + h0 + (v ? combo - n_heads : combo);
-        const float need = scale_of(__int_as_float(amax[i])), old = *scale;
-        const bool held = slot - block * a.bs > 0;
-        const float now = held && old > need ? old : need;
+        float *scale = scale_at(part, combo);
+        const float need = scale_of(__int_as_float(amax[i])), was = i == threadIdx.x ? old : *scale;
+        const bool held = part_held[part] > 0;
+        const float now = held && was > need ? was : need;
         *scale = now;
         amax[i] = __float_as_int(now);
-        ratio[i] = held ? old / now : 1.f;
+        ratio[i] = held ? was / now : 1.f;
     }
     __syncthreads();
     // What the blocks held before, where a scale has grown.
@@ -322,72 +393,62 @@ template <typename T, int D, bool HALF, bool VEC> __device__ __forceinline__ voi
         const float r = ratio[i];
         if (r == 1.f) continue;
         const int part = i / combos, combo = i - part * combos;
-        const bool v = combo >= n_heads;
-        const int64_t block = part_slot[part] / a.bs;
-        const int held = (int)(part_slot[part] - block * a.bs);
-        uint8_t *p = (v ? a.cv : a.ck) + block * a.block_stride + (h0 + (v ? combo - n_heads : combo)) * a.head_stride + 16 * u;
-        for (int j = 0; j < held; j++, p += a.token_stride) {
-            uint4 x = *reinterpret_cast<uint4 *>(p);
-            uint32_t *w = &x.x;
+        const int held = part_held[part];
+        uint8_t *p = head_at(combo) + part_block[part] * a.block_stride + 16 * u;
+        for (int j = 0; j < held; j += 4) {
+            uint4 x[4];
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                if (j + k < held) x[k] = *reinterpret_cast<const uint4 *>(p + (j + k) * a.token_stride);
 #pragma unroll
             for (int k = 0; k < 4; k++) {
-                const uint2 hv = wf_e4m3_halves(w[k]);
-                const float2 lo = wf_pair<__half>::to_float(hv.x), hi = wf_pair<__half>::to_float(hv.y);
-                w[k] = wf_e4m3_of(lo.x * r, lo.y * r) | wf_e4m3_of(hi.x * r, hi.y * r) << 16;
+                if (j + k >= held) break;
+                uint32_t *w = &x[k].x;
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    const uint2 hv = wf_e4m3_halves(w[c]);
+                    const float2 lo = wf_pair<__half>::to_float(hv.x), hi = wf_pair<__half>::to_float(hv.y);
+                    w[c] = wf_e4m3_of(lo.x * r, lo.y * r) | wf_e4m3_of(hi.x * r, hi.y * r) << 16;
+                }
+                *reinterpret_cast<uint4 *>(p + (j + k) * a.token_stride) = x[k];
             }
-            *reinterpret_cast<uint4 *>(p) = x;
         }
     }
     // The new tokens.
-    const bool once = end - from <= kChunk;  // the angles are still there
+    if (kept) {
+#pragma unroll
+        for (int r = 0; r < kKeep; r++) {
+            const int i = group + r * kGroups, t = i / combos, combo = i - t * combos;
+            if (i < items && at[t] >= 0)
+                store8<T, HALF, VEC>(a, keep[r], __int_as_float(amax[part_of(from + t) * combos + combo]), head_at(combo) + at[t], u);
+        }
+        return;
+    }
     for (int base = from; base < end; base += kChunk) {
         const int m = min(kChunk, end - base);
-        if (!once) {
-            __syncthreads();
-            load_tokens(a, first + base, m, cs, at);
-            __syncthreads();
-        }
+        __syncthreads();
+        load_tokens(a, first + base, m, cs, at);
+        __syncthreads();
         for (int i = group; i < m * combos; i += kGroups) {
             const int t = i / combos, combo = i - t * combos;
             if (at[t] < 0) continue;
             Pairs p = load(base + t, combo);
-            const bool v = combo >= n_heads;
-            if (!v) turn_any<T, HALF, VEC>(p, cs[t], u, a.pairs);
-            const float scale = __int_as_float(amax[part_of(base + t) * combos + combo]);
-            uint2 x, y;  // 8 elements of a, 8 of b
-            uint32_t w[8];
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const float2 f = wf_pair<T>::to_float(p.a[j]), g = wf_pair<T>::to_float(p.b[j]);
-                w[j] = wf_e4m3_of(f.x / scale, f.y / scale);
-                w[4 + j] = wf_e4m3_of(g.x / scale, g.y / scale);
-            }
-            x = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16), y = make_uint2(w[4] | w[5] << 16, w[6] | w[7] << 16);
-            uint8_t *to = (v ? a.cv : a.ck) + at[t] + (h0 + (v ? combo - n_heads : combo)) * a.head_stride;
-            if (VEC) {
-                const bool apart = halves_apart(HALF, u, a.pairs);
-                *reinterpret_cast<uint2 *>(to + (apart ? 8 * u : 16 * u)) = x;
-                *reinterpret_cast<uint2 *>(to + (apart ? 8 * u + a.pairs : 16 * u + 8)) = y;
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    to[first_of(HALF, 8 * u + j, a.pairs)] = (uint8_t)(w[j / 2] >> (8 * (j % 2)));
-                    to[second_of(HALF, 8 * u + j, a.pairs)] = (uint8_t)(w[4 + j / 2] >> (8 * (j % 2)));
-                }
-            }
+            if (combo < n_heads) turn_any<T, HALF, VEC>(p, cs + t * a.pairs, u, a.pairs);
+            store8<T, HALF, VEC>(a, p, __int_as_float(amax[part_of(base + t) * combos + combo]), head_at(combo) + at[t], u);
         }
     }
 }
 
-template <typename T, int D, bool HALF, bool VEC> __global__ void __launch_bounds__(kThreads) write8_kernel(const WriteArgs a)
+template <typename T, int D, bool HALF, bool VEC> __global__ void __launch_bounds__(kThreads, 4) write8_kernel(const WriteArgs a)
 {
+    extern __shared__ float2 angles[];
     const int split = (a.kv + a.heads_per - 1) / a.heads_per;
     const int64_t cta = blockIdx.x;
     if (cta < (int64_t)a.windows * split) {
-        write8_window<T, D, HALF, VEC>(a, cta / split * a.per, (int)(cta % split) * a.heads_per);
+        write8_window<T, D, HALF, VEC>(a, cta / split * a.per, (int)(cta % split) * a.heads_per, angles);
     } else {
         const int64_t first = (cta - (int64_t)a.windows * split) * a.per;
-        write_tokens<T, D, HALF, VEC, false>(a, first, (int)min((int64_t)a.per, a.tokens - first));
+        write_tokens<T, D, HALF, VEC, false>(a, first, (int)min((int64_t)a.per, a.tokens - first), angles);
     }
 }
 
@@ -416,16 +477,21 @@ template <typename T, int D, bool HALF, bool VEC> int launch(const WriteArgs &ar
     // nothing more is saved.
     if (!f8) {
         a.per = (int)std::min<int64_t>(8, std::max<int64_t>(1, a.tokens / (4 * sms)));
-        write16_kernel<T, D, HALF, VEC><<<(unsigned)((a.tokens + a.per - 1) / a.per), kThreads, 0, st>>>(a);
+        write16_kernel<T, D, HALF, VEC><<<(unsigned)((a.tokens + a.per - 1) / a.per), kThreads, a.per * a.pairs * sizeof(float2), st>>>(a);
         return wf_cuda_check(cudaGetLastError(), "write16_kernel");
     }
-    a.per = (int)std::min<int64_t>(16, std::max<int64_t>(1, a.tokens / (2 * sms)));
+    // 8 bits: a block's part is one CTA's, so that blocks, not tokens, are what there is to share out; heads are shared out too until
+    // every SM has CTAs enough.
+    a.per = (int)std::min<int64_t>(kMost16, std::max<int64_t>(1, a.tokens / (2 * sms)));
     a.windows = (int)((a.tokens + a.per - 1) / a.per);
-    a.heads_per = std::min(a.kv, 4);
+    const int64_t parts = std::max((a.tokens + std::max(a.per, a.bs) - 1) / std::max(a.per, a.bs), std::min<int64_t>(a.rows, a.tokens) / a.per);
+    a.heads_per = std::min(a.kv, kMaxHeads);
+    while (a.heads_per > 1 && parts * ((a.kv + a.heads_per - 1) / a.heads_per) < 4 * sms) a.heads_per = (a.heads_per + 1) / 2;
     const int64_t split = (a.kv + a.heads_per - 1) / a.heads_per;
     const int64_t ctas = a.windows * split + (a.q_heads ? a.windows : 0);
     if (ctas > INT32_MAX) return wf_set_error(WF_EINVAL, "wf_kv_write: %lld tokens of %d heads", (long long)a.tokens, a.kv);
-    write8_kernel<T, D, HALF, VEC><<<(unsigned)ctas, kThreads, 2 * 32 * 2 * a.heads_per * sizeof(float), st>>>(a);
+    const int most = (int)std::min<int64_t>(kChunk, (int64_t)a.per + a.bs);  // tokens whose angles a CTA holds
+    write8_kernel<T, D, HALF, VEC><<<(unsigned)ctas, kThreads, most * a.pairs * sizeof(float2), st>>>(a);
     return wf_cuda_check(cudaGetLastError(), "write8_kernel");
 }
 
@@ -443,7 +509,8 @@ int wf_launch_write(wf_decode *d, const wf_kv *kv, const wf_kv_step *step, const
     WriteArgs a{};
     a.slot = step->slot, a.pos = step->pos;
     a.tokens = step->max_tokens, a.n_slots = (int64_t)kv->n_blocks * kv->block_tokens;
-    a.bs = kv->block_tokens, a.kv = l->heads, a.q_heads = in->q_heads;
+    a.by_bs = wf_make_div(kv->block_tokens), a.few = a.n_slots <= INT32_MAX;
+    a.rows = kv->rows, a.bs = kv->block_tokens, a.kv = l->heads, a.q_heads = in->q_heads;
     a.pairs = rope ? rope->dim / 2 : 0;
     a.turn = rope ? rope->turn : nullptr, a.magnitude = rope ? rope->magnitude : 1.f;
     a.k = (const uint8_t *)in->k, a.v = (const uint8_t *)in->v, a.q = (const uint8_t *)in->q, a.q_out = (uint8_t *)in->q_out;

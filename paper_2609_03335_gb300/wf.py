@@ -846,19 +846,25 @@ class Rope:
         self.c = wf_rope(dim, int(self.interleaved), self.turn.data_ptr() if dim else None, self.magnitude, 0)
 
 
-def _heads(t, name: str, dtype, tokens: int, heads: int, dim: int, device: int):
+def _heads(t, name: str, dtype, shape: tuple, device: int):
     """(address, bytes between tokens, bytes between heads) of a tensor [tokens, heads, dim] with contiguous elements."""
-    shape = t.shape if hasattr(t, "stride") else ()
-    if len(shape) != 3 or shape[0] != tokens or shape[1] != heads or shape[2] != dim or t.dtype is not dtype or t.get_device() != device \
-            or t.stride(2) != 1:
-        what = f"{t.dtype} {tuple(t.shape)} on {t.device}" if hasattr(t, "stride") else type(t).__name__
-        raise WfError(WF_EINVAL, name, f"is {what}; expected {dtype} [{tokens}, {heads}, {dim}] with contiguous elements on cuda:{device}")
-    return t.data_ptr(), 2 * t.stride(0), 2 * t.stride(1)
+    try:
+        stride = t.stride()
+        if t.shape == shape and t.dtype is dtype and t.get_device() == device and stride[2] == 1:
+            return t.data_ptr(), 2 * stride[0], 2 * stride[1]
+        what = f"{t.dtype} {tuple(t.shape)} with strides {stride} on {t.device}"
+    except AttributeError:
+        what = type(t).__name__
+    raise WfError(WF_EINVAL, name, f"is {what}; expected {dtype} {list(shape)} with contiguous elements on cuda:{device}")
 
 
 def _check_layer(where: str, kv: Kv, step: KvStep, layer: KvLayer, *others):
-    if not kv.device == step.device == layer.device or any(o.device != kv.device for o in others):
+    dev = kv.device
+    if not dev == step.device == layer.device:
         raise _apart(where, kv, step, layer, *others)
+    for o in others:
+        if o.device != dev:
+            raise _apart(where, kv, step, layer, *others)
     if step.rows != kv.rows:
         raise WfError(WF_EINVAL, where, f"a step of {step.rows} rows, {kv.rows} given")
     if layer.n_blocks != kv.n_blocks or layer.block_tokens != kv.block_tokens:
@@ -870,17 +876,18 @@ def wf_kv_write(decode: Decode, kv: Kv, step: KvStep, layer: KvLayer, k, v, q=No
     """A step's keys and values [max_tokens, heads, dim] into the layer's cache, keys (and queries q [max_tokens,
     q_heads, dim], into q_out or in place) turned to their positions by `rope`.  Tensors in float16 or
     bfloat16, of the layer's type where that has 16 bits; tokens and heads may be strided."""
-    _check_layer("wf_kv_write", kv, step, layer, decode, *(() if rope is None else (rope,)))
+    _check_layer("wf_kv_write", kv, step, layer, decode, decode if rope is None else rope)
     dtype, n, dim, dev = getattr(k, "dtype", None), step.max_tokens, layer.dim, kv.device
     code = _dtype_code(dtype)
-    kp = _heads(k, "k", dtype, n, layer.heads, dim, dev)
-    vp = _heads(v, "v", dtype, n, layer.heads, dim, dev)
+    shape = (n, layer.heads, dim)
+    kp, vp = _heads(k, "k", dtype, shape, dev), _heads(v, "v", dtype, shape, dev)
     q_heads, qp, op = 0, (None, 0, 0), (None, 0, 0)
     if q is not None:
-        q_heads = q.shape[1] if hasattr(q, "shape") and len(q.shape) == 3 else 1
-        qp = op = _heads(q, "q", dtype, n, q_heads, dim, dev)
+        q_heads = q.size(1) if hasattr(q, "dim") and q.dim() == 3 else 1
+        shape = (n, q_heads, dim)
+        qp = op = _heads(q, "q", dtype, shape, dev)
         if q_out is not None:
-            op = _heads(q_out, "q_out", dtype, n, q_heads, dim, dev)
+            op = _heads(q_out, "q_out", dtype, shape, dev)
     elif q_out is not None:
         raise WfError(WF_EINVAL, "q_out", "given without q")
     c = wf_kv_new(-1 if code is None else code, q_heads, kp[0], vp[0], qp[0], op[0], kp[1], kp[2], vp[1], vp[2], qp[1], qp[2], op[1], op[2])
@@ -922,9 +929,9 @@ def wf_attend(attn: Attn, kv: Kv, step: KvStep, layer: KvLayer, q, out, scale: f
     _check_layer("wf_attend", kv, step, layer, attn)
     dtype, n, dim, dev = getattr(q, "dtype", None), step.max_tokens, layer.dim, kv.device
     code = _dtype_code(dtype)
-    heads = q.shape[1] if hasattr(q, "shape") and len(q.shape) == 3 else 1
-    qp = _heads(q, "q", dtype, n, heads, dim, dev)
-    op = _heads(out, "out", dtype, n, heads, dim, dev)
+    heads = q.size(1) if hasattr(q, "dim") and q.dim() == 3 else 1
+    shape = (n, heads, dim)
+    qp, op = _heads(q, "q", dtype, shape, dev), _heads(out, "out", dtype, shape, dev)
     c = wf_attn_in(-1 if code is None else code, heads, dim ** -0.5 if scale is None else scale, new, qp[0], op[0], qp[1], qp[2], op[1], op[2])
     _check(load_library().wf_attend(attn.ptr, ctypes.byref(kv.c), ctypes.byref(step.c), ctypes.byref(layer.c), ctypes.byref(c),
                                     _stream_handle(stream, dev)), "wf_attend")
