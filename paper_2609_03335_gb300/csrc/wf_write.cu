@@ -4,7 +4,7 @@
 // A pair (a, b) of token t at angle x = pos * turn turns to
 // m (a cos x - b sin x, b cos x + a sin x).  Turns are whole numbers of 2^-64,
 // so pos * turn modulo 2^64 is the exact angle modulo a turn, whatever the
-// position; its upper 32 bits go through sincospi.
+// position; its upper 32 bits, less whole quarters, go through sincospi.
 //
 // It has to read the step's tensors and write the queries and the cache, once
 // each, and computes little: HBM bounds it, and launches where tokens are few.
@@ -110,8 +110,9 @@ template <typename T, bool SPLIT> __device__ __forceinline__ void turn_pairs(Pai
         const float2 a = wf_pair<T>::to_float(p.a[j]), b = wf_pair<T>::to_float(p.b[j]);
         const float2 ci = i < pairs ? cs[i] : make_float2(1.f, 0.f), ck = k < pairs ? cs[k] : make_float2(1.f, 0.f);
         const float ix = a.x, iy = SPLIT ? b.x : a.y, kx = SPLIT ? a.y : b.x, ky = b.y;
-        const float i0 = ix * ci.x - iy * ci.y, i1 = iy * ci.x + ix * ci.y;
-        const float k0 = kx * ck.x - ky * ck.y, k1 = ky * ck.x + kx * ck.y;
+        // One rounding of a product, one of the sum, the same in every layout.
+        const float i0 = __fmaf_rn(ix, ci.x, -__fmul_rn(iy, ci.y)), i1 = __fmaf_rn(iy, ci.x, __fmul_rn(ix, ci.y));
+        const float k0 = __fmaf_rn(kx, ck.x, -__fmul_rn(ky, ck.y)), k1 = __fmaf_rn(ky, ck.x, __fmul_rn(kx, ck.y));
         const uint32_t was_a = p.a[j], was_b = p.b[j];
         p.a[j] = SPLIT ? wf_pair<T>::of_float(i0, k0) : wf_pair<T>::of_float(i0, i1);
         p.b[j] = SPLIT ? wf_pair<T>::of_float(i1, k1) : wf_pair<T>::of_float(k0, k1);
@@ -162,9 +163,16 @@ __device__ __forceinline__ void load_tokens(const WriteArgs &a, int64_t first, i
     for (int i = threadIdx.x; i < n; i += kThreads) at[i] = slot_offset(a, a.slot[first + i]);
     for (int i = threadIdx.x; i < n * a.pairs; i += kThreads) {
         const int t = i / a.pairs, p = i - t * a.pairs;
-        const int32_t part = (int32_t)(((uint64_t)(uint32_t)a.pos[first + t] * a.turn[p]) >> 32);  // of a turn, in 2^-32
+        const uint32_t part = (uint32_t)(((uint64_t)(uint32_t)a.pos[first + t] * a.turn[p]) >> 32);  // of a turn, in 2^-32
+        // The nearest quarter, and what is left: at most an eighth of a turn, so that 24 bits hold it to 2^-27 of a turn.
+        const uint32_t quarter = (part + (1u << 29)) >> 30;
         float s, c;
-        sincospif((float)part * 0x1p-31f, &s, &c);
+        sincospif((float)(int32_t)(part - (quarter << 30)) * 0x1p-31f, &s, &c);
+        if (quarter & 1) {
+            const float was = c;
+            c = -s, s = was;
+        }
+        if (quarter & 2) c = -c, s = -s;
         cs[i] = make_float2(c * a.magnitude, s * a.magnitude);
     }
 }
