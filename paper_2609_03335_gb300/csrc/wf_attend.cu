@@ -30,9 +30,9 @@
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kSlice = 16;                // positions of a stage
+constexpr int kSlice = 16;                // positions of a stage, queries of a unit
 constexpr int kTile = kSlice * kWarps;    // positions of a unit of work
-constexpr int kFixed = 2;                 // tiles that a unit's beginning and end are worth
+static_assert(kSlice == kShortQueries && kTile == kShortTile, "the line's units");
 constexpr int kLeast = 6;                 // work that is not split further
 constexpr float kLeastScale = 0x1p-64f;  // what a scale of 0 counts as
 
@@ -113,81 +113,6 @@ __device__ __forceinline__ float one_over(float x)
 }
 
 // ---------------------------------------------------------------------------
-// The line of work
-// ---------------------------------------------------------------------------
-
-struct Span {
-    int64_t total;
-    int32_t ctas;  // that share it
-    __device__ __forceinline__ int64_t begin(int32_t c) const { return total * c / ctas; }
-    // The CTA whose stretch holds place p < total.
-    __device__ __forceinline__ int32_t owner(int64_t p) const
-    {
-        int32_t c = (int32_t)min((int64_t)(ctas - 1), (int64_t)((double)p * ctas / (double)total));
-        while (c > 0 && begin(c) > p) c--;
-        while (c + 1 < ctas && begin(c + 1) <= p) c++;
-        return c;
-    }
-};
-
-__device__ __forceinline__ int64_t unit_work(const Row &row) { return kFixed + (row.len + kTile - 1) / kTile; }
-__device__ __forceinline__ int64_t row_work(const AttendArgs &a, const Row &row)
-{
-    const int64_t m = taken(a, row);
-    return m ? a.kv * ((m + kSlice - 1) / kSlice) * unit_work(row) : 0;
-}
-
-// The whole line, and the row (its number and where it begins) that holds this CTA's first place.
-struct Found {
-    int64_t total, row_begin;
-    int32_t row;
-};
-
-__device__ __forceinline__ Span span_of(int64_t total)
-{
-    return {total, (int32_t)max((int64_t)1, min((int64_t)gridDim.x, total / kLeast))};
-}
-
-__device__ Found find_row(const AttendArgs &a)
-{
-    __shared__ int64_t sums[kWarps];
-    __shared__ Found found;
-    const int32_t per = (a.rows + kThreads - 1) / kThreads, r0 = min(a.rows, (int32_t)threadIdx.x * per), r1 = min(a.rows, r0 + per);
-    int64_t mine = 0;
-    for (int32_t r = r0; r < r1; r++) mine += row_work(a, row_of(a, r));
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    int64_t incl = mine;
-#pragma unroll
-    for (int s = 1; s < 32; s *= 2) {
-        const int64_t x = __shfl_up_sync(~0u, incl, s);
-        if (lane >= s) incl += x;
-    }
-    if (lane == 31) sums[warp] = incl;
-    __syncthreads();
-    int64_t before = incl - mine, total = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; w++) {
-        if (w < warp) before += sums[w];
-        total += sums[w];
-    }
-    const Span span = span_of(total);
-    const int64_t at = blockIdx.x < span.ctas ? span.begin(blockIdx.x) : total;
-    if (threadIdx.x == 0) found = {total, total, a.rows};
-    __syncthreads();
-    if (mine && at >= before && at < before + mine)
-        for (int32_t r = r0; r < r1; r++) {
-            const int64_t w = row_work(a, row_of(a, r));
-            if (at < before + w) {
-                found = {total, before, r};
-                break;
-            }
-            before += w;
-        }
-    __syncthreads();
-    return found;
-}
-
-// ---------------------------------------------------------------------------
 // A unit
 // ---------------------------------------------------------------------------
 
@@ -201,6 +126,51 @@ struct Unit {
     int32_t begin, end;   // positions
     int32_t full;         // positions that every query sees
 };
+
+// A CTA's way along the line, and what it takes of a unit: positions u.begin .. u.end of it, one of `parts` whose first is CTA `first`'s.
+struct Walk {
+    Span span;
+    int64_t at, stop, row_begin;
+    int32_t r;
+    Row row;
+};
+struct Part {
+    Unit u;               // no queries: the end
+    int32_t first, parts;
+};
+
+__device__ __forceinline__ void next_part(const AttendArgs &a, Walk &w, Part &p)
+{
+    Unit u;
+    u.queries = 0;
+    while (w.at < w.stop) {
+        const int64_t work = short_work(a, w.row);
+        if (w.at >= w.row_begin + work) {  // on to the next row
+            w.row_begin += work;
+            w.row = row_of(a, ++w.r);
+            continue;
+        }
+        const int64_t each = unit_work(w.row), index = quotient(w.at - w.row_begin, each), begin = w.row_begin + index * each;
+        const int64_t m = queries_of(a, w.row), tiles = (m + kSlice - 1) / kSlice;
+        const int64_t body = begin + kFixed, t0 = max(w.at, body) - body, t1 = min(w.stop, begin + each) - body;
+        w.at = min(w.stop, begin + each);
+        if (t1 <= t0) continue;
+        u.row = w.row, u.table = a.table + w.r * a.table_stride;
+        u.head = (int32_t)quotient(index, tiles);
+        u.q0 = (index - u.head * tiles) * kSlice;
+        u.queries = (int32_t)min((int64_t)kSlice, m - u.q0);
+        u.full = w.row.len - w.row.n + (int32_t)wf_quot((uint32_t)u.q0, a.by_group) + 1;
+        const int32_t last = w.row.len - w.row.n + (int32_t)wf_quot((uint32_t)(u.q0 + u.queries - 1), a.by_group) + 1;
+        u.begin = (int32_t)min((int64_t)last, t0 * kTile), u.end = (int32_t)min((int64_t)last, t1 * kTile);
+        p.first = 0, p.parts = 1;
+        if (t0 || t1 != each - kFixed) {
+            p.first = w.span.owner(body);
+            p.parts = w.span.owner(begin + each - 1) - p.first + 1;
+        }
+        break;
+    }
+    p.u = u;
+}
 
 template <typename T, bool E, int D> struct Kernel {
     using S = Shape<E, D>;
@@ -471,6 +441,12 @@ __device__ __forceinline__ void put_out(const AttendArgs &a, const Unit &u, int 
                                                wf_pair<T>::of_float(x[4], x[5]), wf_pair<T>::of_float(x[6], x[7]));
 }
 
+// Beside prompt_kernel this kernel ends after it, so that what follows on the stream finds both done.
+__device__ __forceinline__ void leave(const AttendArgs &a)
+{
+    if (a.both && blockIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // Parts in scratch: [16 queries][D] sums, [16] references, [16] sums of weights.
 template <int D> constexpr int kPart = kSlice * (D + 2);
 
@@ -480,36 +456,24 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float s_m[kWarps][kSlice], s_l[kWarps][kSlice], s_ref[kSlice], s_sum[kSlice];
     __shared__ bool s_last;
+    __shared__ Walk s_walk;
+    __shared__ Part s_part;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const Found f = find_row(a);
-    if (f.row >= a.rows) return;
-    const Span span = span_of(f.total);
-    int64_t at = span.begin(blockIdx.x), row_begin = f.row_begin;
-    const int64_t stop = span.begin(blockIdx.x + 1);
-    int32_t r = f.row;
-    Row row = row_of(a, r);
-    while (at < stop) {
-        const int64_t work = row_work(a, row);
-        if (at >= row_begin + work) {  // on to the next row
-            row_begin += work;
-            row = row_of(a, ++r);
-            continue;
-        }
-        const int64_t each = unit_work(row), index = (at - row_begin) / each, begin = row_begin + index * each;
-        const int64_t m = taken(a, row), tiles = (m + kSlice - 1) / kSlice;
-        Unit u;
-        u.row = row, u.table = a.table + r * a.table_stride;
-        u.head = (int32_t)(index / tiles);
-        u.q0 = (index - u.head * tiles) * kSlice;
-        u.queries = (int32_t)min((int64_t)kSlice, m - u.q0);
-        u.full = row.len - row.n + (int32_t)wf_quot((uint32_t)u.q0, a.by_group) + 1;
-        const int32_t last = row.len - row.n + (int32_t)wf_quot((uint32_t)(u.q0 + u.queries - 1), a.by_group) + 1;
-        const int64_t body = begin + kFixed, t0 = max(at, body) - body, t1 = min(stop, begin + each) - body;
-        at = min(stop, begin + each);
-        if (t1 <= t0) continue;
-        u.begin = (int32_t)min((int64_t)last, t0 * kTile), u.end = (int32_t)min((int64_t)last, t1 * kTile);
-        const bool whole = t0 == 0 && t1 == each - kFixed;
-
+    const Found f = find_row<kThreads, false>(a, [&](int64_t total, int64_t rest) {
+        const int64_t room = rest ? gridDim.x / a.sms * (a.sms - prompt_sms(a, total, rest)) : gridDim.x;
+        return (int32_t)max((int64_t)1, min(room, total / kLeast));
+    });
+    if (f.row >= a.rows) {
+        leave(a);
+        return;
+    }
+    // The walk along the line is one thread's, and lies in shared memory: the others' registers are for the products.
+    if (threadIdx.x == 0) s_walk = {f.span, f.span.begin(blockIdx.x), f.span.begin(blockIdx.x + 1), f.row_begin, f.row, row_of(a, f.row)};
+    for (;;) {
+        if (threadIdx.x == 0) next_part(a, s_walk, s_part);
+        __syncthreads();
+        const Unit u = s_part.u;
+        if (!u.queries) break;
         uint8_t *buf = smem + warp * S::kWarpBytes;
         {
             Kernel<T, E, D> k;
@@ -521,7 +485,7 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
         }
         __syncthreads();
         // The warps' results together: 8 elements of a query at a time.
-        const int32_t first = whole ? 0 : span.owner(body), n = whole ? 1 : span.owner(begin + each - 1) - first + 1;
+        const int32_t first = s_part.first, n = s_part.parts;
         float *part = a.part + (2 * (int64_t)blockIdx.x + (blockIdx.x == first)) * kPart<D>;
         for (int i = threadIdx.x; i < u.queries * (D / 8); i += kThreads) {
             const int q = i / (D / 8), e = i % (D / 8) * 8;
@@ -600,6 +564,7 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
         }
         __syncthreads();
     }
+    leave(a);
 }
 
 template <typename T, bool E, int D> int setup(int sms, int *grid)
@@ -616,8 +581,13 @@ template <typename T, bool E, int D> int setup(int sms, int *grid)
 
 template <typename T, bool E, int D> int launch(const wf_attn *at, const AttendArgs &a, cudaStream_t st)
 {
-    attend_kernel<T, E, D><<<at->grid[E][D == 128], kThreads, Shape<E, D>::kSmem, st>>>(a);
-    return wf_cuda_check(cudaGetLastError(), "attend_kernel");
+    cudaLaunchConfig_t c{};
+    c.gridDim = at->grid[E][D == 128], c.blockDim = kThreads, c.dynamicSmemBytes = Shape<E, D>::kSmem, c.stream = st;
+    cudaLaunchAttribute beside{};
+    beside.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    beside.val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = &beside, c.numAttrs = a.both ? 1 : 0;
+    return wf_cuda_check(cudaLaunchKernelEx(&c, attend_kernel<T, E, D>, a), "attend_kernel");
 }
 
 }  // namespace

@@ -10,9 +10,9 @@ struct wf_attn {
     wf_attn_limits lim;
     void *mem;
     int *err;            // device error word (wf_attn_status): 1 a block or a row, 2 a wait
-    uint32_t *arrive;    // arrivals at units that several CTAs share, by the CTA that begins one; every call leaves them 0
-    float *part;         // two parts a CTA
-    size_t part_bytes;
+    // Of attend_kernel, of prompt_kernel, which may run side by side:
+    uint32_t *arrive[2]; // arrivals at units that several CTAs share, by the CTA that begins one; every call leaves them 0
+    float *part[2];      // two parts a CTA
     int grid[2][2];      // CTAs of attend_kernel by 8 bits or not, dim 64 or 128
 };
 
@@ -33,8 +33,12 @@ struct AttendArgs {
     int64_t q_token, q_head, o_token, o_head;
     int32_t group;       // query heads of a key / value head
     float scale;         // log2(e) times the caller's
-    // the rows that a launch takes: more than `above` and at most `most` new tokens times group
-    int64_t above, most;
+    // Rows of up to `few` queries to a key head are attend_kernel's, the others prompt_kernel's; `both`: it runs beside the other.
+    int64_t few;
+    int32_t both, sms;
+    int32_t pair_cost;   // cycles of a prompt_kernel's tile on an SM
+    int32_t tile_cost;   // of an attend_kernel's on an SM of its own, and
+    int32_t tile_share;  // 1 / 16 of the GPU's cycles that its bytes take at least
     int32_t tile_q;      // queries of a tile of wf_prompt.cu: whole tokens of the group, up to 128
     float *part;
     uint32_t *arrive;
@@ -58,11 +62,124 @@ __device__ __forceinline__ Row row_of(const AttendArgs &a, int32_t r)
     return row;
 }
 
-// The new tokens of row r if this launch takes it, times group.
-__device__ __forceinline__ int64_t taken(const AttendArgs &a, const Row &row)
+// Work.  attend_kernel: units of up to 16 queries, in tiles of 64 positions, each worth kFixed tiles more.  prompt_kernel: units of 2 tile_q
+// queries; in 1 / (128 group) of a tile of 128 positions, unit i of a row's key head (queries 2 t i .., t = tile_q) sees `have` cached
+// positions and up to 2 t (i + 1) / group of the step's, so that the sum over units 0 .. i - 1 is i W + t i (i + 1), W = group (128 kFixed + have).
+constexpr int kFixed = 2;         // tiles that a unit's beginning and end are worth
+constexpr int kShortQueries = 16, kShortTile = 64, kKeys = 128;
+
+__device__ __forceinline__ int64_t queries_of(const AttendArgs &a, const Row &row) { return (int64_t)row.n * a.group; }
+
+__device__ __forceinline__ int64_t unit_work(const Row &row) { return kFixed + (row.len + kShortTile - 1) / kShortTile; }
+__device__ __forceinline__ int64_t short_work(const AttendArgs &a, const Row &row)
 {
-    const int64_t m = (int64_t)row.n * a.group;
-    return m > a.above && m <= a.most ? m : 0;
+    const int64_t m = queries_of(a, row);
+    return m <= a.few ? a.kv * ((m + kShortQueries - 1) / kShortQueries) * unit_work(row) : 0;
+}
+
+struct Line {
+    int64_t w, tile_q;
+    int64_t units;
+    __device__ __forceinline__ int64_t upto(int64_t i) const { return i * w + tile_q * i * (i + 1); }
+    __device__ __forceinline__ int64_t head() const { return upto(units); }
+};
+
+__device__ __forceinline__ Line line_of(const AttendArgs &a, const Row &row)
+{
+    const int64_t m = queries_of(a, row);
+    return {(int64_t)a.group * (kKeys * kFixed + row.len - row.n), a.tile_q, m > a.few ? (m + 2 * a.tile_q - 1) / (2 * a.tile_q) : 0};
+}
+__device__ __forceinline__ int64_t long_work(const AttendArgs &a, const Row &row) { return a.kv * line_of(a, row).head(); }
+
+// The SMs that prompt_kernel takes where both kernels run side by side, the others being attend_kernel's: as many as make both end at the
+// same time.  Decoding alone cannot use them all (its bytes take tile_share / 16 of the whole GPU's cycles a tile), nor does a prompt's work shrink its bytes.
+__device__ __forceinline__ int32_t prompt_sms(const AttendArgs &a, int64_t short_total, int64_t long_total)
+{
+    if (!a.both || !short_total) return a.sms;
+    const double p = (double)long_total / ((double)kKeys * a.group) * a.pair_cost, d = (double)short_total * a.tile_cost;
+    const double even = a.sms * p / (p + d), bytes = (double)short_total * a.tile_share / 16.0;  // cycles
+    // With `even` SMs both take (p + d) / sms cycles; if the bytes take longer, prompts need only p / bytes SMs.
+    const double want = (p + d) / a.sms >= bytes ? even : p / bytes;
+    return max(1, min(a.sms - 1, (int32_t)ceil(want)));
+}
+
+// a / b for a >= 0, b > 0; in 32 bits where they fit, as they mostly do (a division in 64 bits is a hundred instructions).
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b)
+{
+    return ((uint64_t)a | (uint64_t)b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
+
+// A line of work in equal stretches.
+struct Span {
+    int64_t total;
+    int32_t ctas;
+    __device__ __forceinline__ int64_t begin(int32_t c) const 
+    {
+        const int64_t q = quotient(total, ctas);
+        return q * c + quotient((total - q * ctas) * c, ctas);
+    }
+    // The CTA whose stretch holds place p < total.
+    __device__ __forceinline__ int32_t owner(int64_t p) const
+    {
+        int32_t c = (int32_t)max((int64_t)0, min((int64_t)(ctas - 1), (int64_t)((double)p * ctas / (double)total)));
+        while (c > 0 && begin(c) > p) c--;
+        while (c + 1 < ctas && begin(c + 1) <= p) c++;
+        return c;
+    }
+};
+
+// The line, how it is cut (by `cut`, from this kernel's and the other's totals), and the row (its number and where it begins) that holds
+// this CTA's first place; row = rows: this CTA has none.
+struct Found {
+    Span span;
+    int64_t row_begin;
+    int32_t row;
+};
+
+template <int THREADS, bool LONG, typename CUT> __device__ Found find_row(const AttendArgs &a, CUT cut)
+{
+    constexpr int kW = THREADS / 32;
+    __shared__ int64_t sums[kW], others[kW];
+    __shared__ Found found;
+    const int32_t per = (a.rows + THREADS - 1) / THREADS, r0 = min(a.rows, (int32_t)threadIdx.x * per), r1 = min(a.rows, r0 + per);
+    int64_t mine = 0, other = 0;
+    for (int32_t r = r0; r < r1; r++) {
+        const Row row = row_of(a, r);
+        mine += LONG ? long_work(a, row) : short_work(a, row);
+        if (a.both) other += LONG ? short_work(a, row) : long_work(a, row);
+    }
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    int64_t incl = mine;
+#pragma unroll
+    for (int s = 1; s < 32; s *= 2) {
+        const int64_t x = __shfl_up_sync(~0u, incl, s);
+        if (lane >= s) incl += x;
+        other += __shfl_xor_sync(~0u, other, s);
+    }
+    if (lane == 31) sums[warp] = incl, others[warp] = other;
+    __syncthreads();
+    int64_t before = incl - mine, total = 0, rest = 0;
+#pragma unroll
+    for (int w = 0; w < kW; w++) {
+        if (w < warp) before += sums[w];
+        total += sums[w], rest += others[w];
+    }
+    const Span span = {total, cut(total, rest)};
+    const int64_t at = blockIdx.x < span.ctas ? span.begin(blockIdx.x) : total;
+    if (threadIdx.x == 0) found = {span, total, a.rows};
+    __syncthreads();
+    if (mine && at >= before && at < before + mine)
+        for (int32_t r = r0; r < r1; r++) {
+            const Row row = row_of(a, r);
+            const int64_t w = LONG ? long_work(a, row) : short_work(a, row);
+            if (at < before + w) {
+                found = {span, before, r};
+                break;
+            }
+            before += w;
+        }
+    __syncthreads();
+    return found;
 }
 
 // A position's block, kept inside the cache.

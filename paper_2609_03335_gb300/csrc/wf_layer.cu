@@ -117,18 +117,20 @@ extern "C" int wf_attn_create(const wf_attn_limits *lim, int device, wf_attn **o
     if (!rc) rc = wf_prompt_setup(a);
     if (rc) { wf_attn_destroy(a); return rc; }
     int ctas = 0;
-    wf_attend_scratch(a, &a->part_bytes, &ctas);
-    ctas = std::max(ctas, a->sms);
-    a->part_bytes = std::max(a->part_bytes, wf_prompt_scratch(a));
-    const size_t zeroed = 256 + (4 * (size_t)ctas + 255) / 256 * 256;
-    rc = wf_cuda_check(cudaMalloc(&a->mem, zeroed + a->part_bytes), "cudaMalloc(attention scratch)");
+    size_t parts = 0;
+    wf_attend_scratch(a, &parts, &ctas);
+    parts = (parts + 255) / 256 * 256;
+    const size_t arrivals = (4 * (size_t)std::max(ctas, a->sms) + 255) / 256 * 256, zeroed = 256 + 2 * arrivals;
+    rc = wf_cuda_check(cudaMalloc(&a->mem, zeroed + parts + wf_prompt_scratch(a)), "cudaMalloc(attention scratch)");
     if (!rc) rc = wf_cuda_check(cudaMemset(a->mem, 0, zeroed), "clear the attention scratch");
     // The clearing runs on the default stream; the calls may use any other.
     if (!rc) rc = wf_cuda_check(cudaDeviceSynchronize(), "cudaDeviceSynchronize");
     if (rc) { wf_attn_destroy(a); return rc; }
     a->err = (int *)a->mem;
-    a->arrive = (uint32_t *)((uint8_t *)a->mem + 256);
-    a->part = (float *)((uint8_t *)a->mem + zeroed);
+    for (int i = 0; i < 2; i++) {
+        a->arrive[i] = (uint32_t *)((uint8_t *)a->mem + 256 + i * arrivals);
+        a->part[i] = (float *)((uint8_t *)a->mem + zeroed + i * parts);
+    }
     *out = a;
     return WF_OK;
 }
@@ -159,6 +161,15 @@ extern "C" int wf_attn_status(wf_attn *a, void *stream)
 }
 
 constexpr int64_t kFew = 32;
+
+// Cycles of a tile of each kernel on an SM, as measured with full SMs (a prompt of 8,192 tokens; 64 rows behind 9,000), from which the SMs are
+// shared out where both run.  tile_share: 64 positions' keys and values at 6.7 TB/s and 1.93 GHz.
+static void wf_costs(bool eight, int dim, AttendArgs *a)
+{
+    a->pair_cost = eight ? (dim == 128 ? 6500 : 4000) : (dim == 128 ? 4000 : 3000);
+    a->tile_cost = eight ? 950 : (dim == 128 ? 1100 : 900);
+    a->tile_share = 16 * (64 * 2 * dim * (eight ? 1 : 2)) / 3470;
+}
 
 static int check_attn(const void *p, int64_t token, int64_t head, const char *what, const char *name)
 {
@@ -202,18 +213,21 @@ extern "C" int wf_attend(wf_attn *at, const wf_kv *kv, const wf_kv_step *step, c
     a.group = in->heads / layer->heads;
     a.by_bs = wf_make_div(a.bs), a.by_group = wf_make_div(a.group);
     a.scale = in->scale * 1.4426950408889634f;
-    a.part = at->part, a.arrive = at->arrive, a.err = at->err;
+    a.part = at->part[0], a.arrive = at->arrive[0], a.err = at->err, a.sms = at->sms;
     // Rows of up to kFew queries to a key head go to the kernel of 16-query tiles, the others to that of 128-query tiles.  Where no row is
     // expected to have more (or none can), one launch takes them all.
     const bool eight = layer->dtype == WF_E4M3;
     const int64_t expected = in->new_tokens ? std::min<int64_t>(in->new_tokens, step->max_tokens) : step->max_tokens;
-    a.above = 0, a.most = INT64_MAX;
+    a.few = INT64_MAX, a.both = 0;
     if (expected * a.group > kFew) {
+        a.tile_q = a.group <= kKeys ? kKeys / a.group * a.group : kKeys;
+        a.few = kFew, a.both = 1;
+        wf_costs(eight, layer->dim, &a);
         AttendArgs b = a;
-        b.above = kFew;
+        b.part = at->part[1], b.arrive = at->arrive[1];
         rc = wf_launch_prompt(at, b, in->dtype, layer->dim, eight, (cudaStream_t)stream);
         if (rc > 0) return rc;
-        if (!rc) a.most = kFew;
+        if (rc < 0) a.few = INT64_MAX, a.both = 0;
     }
     return wf_launch_attend(at, a, in->dtype, layer->dim, eight, (cudaStream_t)stream);
 }

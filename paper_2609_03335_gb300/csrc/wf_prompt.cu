@@ -31,11 +31,9 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kQ = 128, kPair = 2 * kQ;   // queries of a tile, of a unit
-constexpr int kKeys = 128;                // positions of a tile
 constexpr int kLoaders = 128;
 constexpr int kRaws = 3;                  // at most
 constexpr int kFours = kKeys / 4, kSlots = 4;  // scales of a tile; tiles whose scales are held
-constexpr int kFixed = 2;                 // tiles that a unit's beginning and end are worth
 constexpr float kSlack = 8.f;             // log2 of what a maximum may grow by before O is shrunk
 constexpr float kLeastScale = 0x1p-64f;
 
@@ -213,85 +211,6 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
 // The line of work
 // ---------------------------------------------------------------------------
 
-// Weights in 1 / (128 group) of a tile: unit i of a row's key head (queries 2 t i .., t = tile_q) sees `have` cached positions and up to
-// 2 t (i + 1) / group of the step's; the sum over units 0 .. i - 1 is i W + t i (i + 1), W = group (128 kFixed + have).
-struct Line {
-    int64_t w, tile_q;
-    int64_t units;
-    __device__ __forceinline__ int64_t upto(int64_t i) const { return i * w + tile_q * i * (i + 1); }
-    __device__ __forceinline__ int64_t head() const { return upto(units); }
-};
-
-__device__ __forceinline__ Line line_of(const AttendArgs &a, const Row &row)
-{
-    const int64_t m = taken(a, row);
-    return {(int64_t)a.group * (kKeys * kFixed + row.len - row.n), a.tile_q, (m + 2 * a.tile_q - 1) / (2 * a.tile_q)};
-}
-
-struct Span {
-    int64_t total;
-    int32_t ctas;
-    __device__ __forceinline__ int64_t begin(int32_t c) const { return total / ctas * c + total % ctas * c / ctas; }
-    __device__ __forceinline__ int32_t owner(int64_t p) const
-    {
-        int32_t c = (int32_t)max((int64_t)0, min((int64_t)(ctas - 1), (int64_t)((double)p * ctas / (double)total)));
-        while (c > 0 && begin(c) > p) c--;
-        while (c + 1 < ctas && begin(c + 1) <= p) c++;
-        return c;
-    }
-};
-
-// A stretch is worth six tiles at least, so that only a unit's first and last CTA can find no tile in their part of it.
-__device__ __forceinline__ Span span_of(const AttendArgs &a, int64_t total)
-{
-    return {total, (int32_t)max((int64_t)1, min((int64_t)gridDim.x, total / (6 * kKeys * (int64_t)a.group)))};
-}
-
-struct Found {
-    int64_t total, row_begin;
-    int32_t row;
-};
-
-__device__ Found find_row(const AttendArgs &a)
-{
-    constexpr int kW = kThreads / 32;
-    __shared__ int64_t sums[kW];
-    __shared__ Found found;
-    const int32_t per = (a.rows + kThreads - 1) / kThreads, r0 = min(a.rows, (int32_t)threadIdx.x * per), r1 = min(a.rows, r0 + per);
-    int64_t mine = 0;
-    for (int32_t r = r0; r < r1; r++) mine += a.kv * line_of(a, row_of(a, r)).head();
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    int64_t incl = mine;
-#pragma unroll
-    for (int s = 1; s < 32; s *= 2) {
-        const int64_t x = __shfl_up_sync(~0u, incl, s);
-        if (lane >= s) incl += x;
-    }
-    if (lane == 31) sums[warp] = incl;
-    __syncthreads();
-    int64_t before = incl - mine, total = 0;
-#pragma unroll
-    for (int w = 0; w < kW; w++) {
-        if (w < warp) before += sums[w];
-        total += sums[w];
-    }
-    const Span span = span_of(a, total);
-    const int64_t at = blockIdx.x < span.ctas ? span.begin(blockIdx.x) : total;
-    if (threadIdx.x == 0) found = {total, total, a.rows};
-    __syncthreads();
-    if (mine && at >= before && at < before + mine)
-        for (int32_t r = r0; r < r1; r++) {
-            const int64_t w = a.kv * line_of(a, row_of(a, r)).head();
-            if (at < before + w) {
-                found = {total, before, r};
-                break;
-            }
-            before += w;
-        }
-    __syncthreads();
-    return found;
-}
-
 // A CTA's part of a unit; no tiles: the end.
 struct Unit {
     Row row;
@@ -314,12 +233,12 @@ struct Walk {
     Row row;
     Line line;
 
-    __device__ __forceinline__ Walk(const AttendArgs &a, const Found &f) : span(span_of(a, f.total)), r(f.row)
+    __device__ __forceinline__ Walk(const AttendArgs &a, const Found &f) : span(f.span), r(f.row)
     {
         at = span.begin(blockIdx.x), stop = span.begin(blockIdx.x + 1);
         row = row_of(a, r), line = line_of(a, row);
         const int64_t each = line.head();
-        head = (int32_t)((at - f.row_begin) / each);
+        head = (int32_t)quotient(at - f.row_begin, each);
         const int64_t base = f.row_begin + head * each, x = at - base;
         // The unit that holds place x: i W + t i (i + 1) <= x.
         const double t = (double)line.tile_q, b = (double)line.w + t;
@@ -348,7 +267,7 @@ struct Walk {
             const int32_t tiles_a = (sees(u.q0 + min(u.queries, a.tile_q) - 1) + kKeys - 1) / kKeys, tiles = (u.seen + kKeys - 1) / kKeys;
             const int64_t each = (int64_t)kKeys * a.group;
             auto tile = [&](int64_t p) {
-                return p >= end ? tiles : p <= begin ? 0 : (int32_t)max((int64_t)0, min((int64_t)tiles, (p - begin) / each - kFixed));
+                return p >= end ? tiles : p <= begin ? 0 : (int32_t)max((int64_t)0, min((int64_t)tiles, quotient(p - begin, each) - kFixed));
             };
             const int32_t t0 = tile(at), t1 = tile(stop);
             const bool split = at > begin || stop < end;
@@ -362,7 +281,7 @@ struct Walk {
             if (split) {
                 int32_t first = span.owner(unit_begin), last = span.owner(end - 1);
                 auto part = [&](int64_t p) {
-                    return p >= end ? tiles : p <= unit_begin ? 0 : (int32_t)max((int64_t)0, min((int64_t)tiles, (p - unit_begin) / each - kFixed));
+                    return p >= end ? tiles : p <= unit_begin ? 0 : (int32_t)max((int64_t)0, min((int64_t)tiles, quotient(p - unit_begin, each) - kFixed));
                 };
                 while (part(span.begin(first + 1)) <= 0) first++;
                 while (part(span.begin(last)) >= tiles) last--;
@@ -460,7 +379,7 @@ template <typename T, bool E, int D> __device__ __forceinline__ void box_role(co
     for (;; units++) {
         const Unit &u = sh.unit(units);
         if (!u.n) break;
-        if (pa.map_q) {
+        if (pa.map_q && !*sh.gave_up) {
             sh.wait(kBarQEmpty, (units & 1) ^ 1);
             const int tiles = u.nb ? 2 : 1;
             if (lane == 0) bar_expect(sh.bar(kBarQFull), tiles * (D / 64) * a.tile_q * 128);
@@ -471,7 +390,7 @@ template <typename T, bool E, int D> __device__ __forceinline__ void box_role(co
                           u.row.first + (int32_t)wf_quot((uint32_t)u.q0 + x * a.tile_q, a.by_group));
             }
         }
-        if (pa.box) {
+        if (pa.box && !*sh.gave_up) {
             const int32_t end = min(u.seen, (u.t0 + u.n) * kKeys);
             const int32_t *table = a.table + u.r * a.table_stride;
             // This lane's box of tile j: its block in the table, and in the maps.  Boxes behind `end` come from a block that is not there: zeros.
@@ -518,6 +437,14 @@ template <typename T, bool E, int D> __device__ __forceinline__ void box_role(co
         }
         sh.unit_done(units);
     }
+    // Where waiting was given up, copies may still be on their way into this CTA's shared memory: no longer than a while.
+    if (*sh.gave_up && lane == 0) {
+        const int n = E ? S::kRaw : S::kStages, first = E ? kBarRaw : kBarFull;
+        for (uint32_t i = it > (uint32_t)n ? it - n : 0; pa.box && i < it; i++)
+            for (int k = 0; k < 1 << 16 && !bar_try(sh.bar(first + i % n), i / n & 1); k++) {}
+        for (int k = 0; pa.map_q && units && k < 1 << 16 && !bar_try(sh.bar(kBarQFull), (units - 1) & 1); k++) {}
+    }
+    __syncwarp();
 }
 
 // Warp 15, 8 bits: the scales of each four positions, which lie in one block.
@@ -994,7 +921,11 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up, last_one;
     __shared__ Unit units[kUnits];
-    const Found f = find_row(a);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // A stretch is worth six tiles at least, so that only a unit's first and last CTA can find no tile in their part of it.
+    const Found f = find_row<kThreads, true>(a, [&](int64_t total, int64_t rest) {
+        return (int32_t)max((int64_t)1, min((int64_t)prompt_sms(a, rest, total), total / (6 * kKeys * (int64_t)a.group)));
+    });
     if (f.row >= a.rows) return;
     if (smem_of(raw) % 1024) {  // the swizzle's patterns would not lie as the products read them
         if (threadIdx.x == 0) *a.err = 2;
@@ -1121,7 +1052,6 @@ template <typename T, bool E, int D> int launch(const wf_attn *at, const AttendA
         const cuuint32_t shape[3] = {64, (cuuint32_t)a.group, (cuuint32_t)tokens};
         pa.map_q = a.q_head > 0 && a.q_token > 0 && encode(&pa.q, half, 3, a.q, sizes, strides, shape, true);
     }
-    a.tile_q = a.group <= kQ ? kQ / a.group * a.group : kQ;
     prompt_kernel<T, E, D><<<at->sms, kThreads, Shape<E, D>::kSmem, st>>>(pa);
     return wf_cuda_check(cudaGetLastError(), "prompt_kernel");
 }

@@ -356,3 +356,60 @@ def test_a_prompt_in_chunks_is_the_prompt():
     score = np.abs(rounded["q"]).sum(-1, keepdims=True) * np.abs(rounded["k"]).max() * dim ** -0.5
     for got in results:
         assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + size * (2.0 ** -7 + 2 * 2.0 ** -8 * score)).all()
+
+
+@pytest.mark.parametrize("eight", (False, True), ids=("16", "8"))
+def test_beams_on_the_cache(eight):
+    """A search as it runs: a prompt, rows that share its blocks, a reordering with copies of last blocks and their scales, a token each, attention."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(41)
+    bs, heads, kv, dim, beams, prompt = 16, 4, 2, 64, 4, 43
+    dtype = "bfloat16"
+    dec, attn, rope = wf.Decode(max_rows=beams, max_row_blocks=8), wf.Attn(max_rows=beams, heads=heads, dim=dim), wf.Rope(dim)
+    rows, moves = wf.Kv.empty(beams, 8, bs, 40), wf.KvMoves(beams)
+    cache = torch.zeros((2, 40, bs, kv, dim), dtype=torch.float8_e4m3fn if eight else torch.bfloat16, device="cuda")
+    scale = torch.ones((2, 40, kv), device="cuda") if eight else None
+    layer = wf.KvLayer(cache[0], cache[1], *((scale[0], scale[1]) if eight else ()))
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    texts = [[] for _ in range(beams)]  # keys and values of each row, as given
+
+    def step(add, new_max):
+        s = wf.KvStep(beams, sum(add) + 1, rows)
+        wf.wf_kv_extend(dec, rows, dev(add), s)
+        t = {n: tensor(rng, (s.max_tokens, h, dim), dtype, spread) for n, h, spread in (("q", heads, 1.5), ("k", kv, rng.uniform(0.5, 8)), ("v", kv, 1))}
+        q = torch.empty_like(t["q"])
+        wf.wf_kv_write(dec, rows, s, layer, t["k"], t["v"], q=t["q"], q_out=q, rope=rope)
+        out = torch.full_like(q, 7.0)
+        wf.wf_attend(attn, rows, s, layer, q, out, new=new_max)
+        at = 0
+        for r, n in enumerate(add):
+            texts[r] = texts[r] + [(t["k"][at + i], t["v"][at + i]) for i in range(n)]
+            at += n
+        return q, out, at
+
+    step([prompt, 0, 0, 0], prompt)
+    for parents in ([0, 0, 0, 0], [1, 1, 3, 0], [2, 0, 0, 3], [0, 1, 2, 3], [3, 3, 3, 3]):
+        wf.wf_kv_reorder(dec, rows, beams, dev(parents), rows, moves, cache=cache.view(torch.uint8) if eight else cache, scale=scale)
+        texts[:] = [list(texts[p]) for p in parents]
+        q, out, n = step([1] * beams, 1)
+        wf.wf_decode_status(dec)
+        wf.wf_attn_status(attn)
+        x, table, length = values(cache, scale), rows.table.cpu().numpy(), rows.len.cpu().numpy()
+        want, size, small = ref.attend(f64(q), x[0], x[1], table, np.arange(beams + 1), length, bs, dim ** -0.5, np.full(q.shape, 7.0),
+                                       None if scale is None else f64(scale[1]))
+        off = np.abs(f64(out) - want)
+        assert (off[:n] <= bound(size, small, want, f64(q), dtype, eight, dim ** -0.5, int(length.max()), np.abs(x[0]).max())[:n]).all()
+        # What the blocks hold is each hypothesis's own keys and values: a rounding to E4M3 (2^-4, once more each time a block's scale grew; what is
+        # small in its block to 2^-10 of the block's scale) where 8 bits hold them, as given where 16 do.
+        for r in range(beams):
+            p = np.arange(length[r])
+            blocks, place = table[r, p // bs], p % bs
+            held = x[1][blocks, place]
+            given = np.stack([f64(v) for _, v in texts[r]])
+            assert len(given) == length[r]
+            if eight:
+                unit = f64(scale[1])[blocks][:, :, None]
+                assert (np.abs(held - given) <= np.abs(given) * (2 * 2.0 ** -4 + 2.0 ** -8) + 2 * 2.0 ** -10 * unit).all()
+            else:
+                assert np.array_equal(held, given)
