@@ -160,7 +160,9 @@ extern "C" int wf_attn_status(wf_attn *a, void *stream)
     return wf_set_error(WF_EINVAL, "a table names a block outside the cache, or a row's lengths contradict each other");
 }
 
-constexpr int64_t kFew = 32;
+// Queries to a key head (new tokens times the group's heads) up to which a row goes to attend_kernel: one of its tiles.  Two tiles read the
+// row's keys twice: 32 rows of 20 to 32 queries behind 9,000 tokens took 386 us there and 240 in prompt_kernel.
+constexpr int64_t kFew = 16;
 
 // Cycles of a tile of each kernel on an SM, as measured with full SMs (a prompt of 8,192 tokens; 64 rows behind 9,000), from which the SMs are
 // shared out where both run.  tile_share: 64 positions' keys and values at 6.7 TB/s and 1.93 GHz.
