@@ -164,13 +164,14 @@ extern "C" int wf_attn_status(wf_attn *a, void *stream)
 // row's keys twice: 32 rows of 20 to 32 queries behind 9,000 tokens took 386 us there and 240 in prompt_kernel.
 constexpr int64_t kFew = 16;
 
-// Cycles of a tile of each kernel on an SM, as measured with full SMs (a prompt of 8,192 tokens; 64 rows behind 9,000), from which the SMs are
-// shared out where both run.  tile_share: 64 positions' keys and values at 6.7 TB/s and 1.93 GHz.
-static void wf_costs(bool eight, int dim, AttendArgs *a)
+// Cycles of a tile of each kernel on an SM, as measured with full SMs (chunks of 500 behind 2,000 tokens; 161 rows behind 2,000), from which
+// the SMs are shared out where both run.  tile_share: 64 positions' keys and values at 6.7 TB/s and 1.93 GHz.  Over 8 bits instructions bound
+// both kernels, and one after the other is faster (376 us against 387 for chunks of nine prompts beside 51 rows).
+static void wf_costs(int dim, AttendArgs *a)
 {
-    a->pair_cost = eight ? (dim == 128 ? 6500 : 4000) : (dim == 128 ? 4000 : 3000);
-    a->tile_cost = eight ? 950 : (dim == 128 ? 1100 : 900);
-    a->tile_share = 16 * (64 * 2 * dim * (eight ? 1 : 2)) / 3470;
+    a->pair_cost = dim == 128 ? 4000 : 3000;
+    a->tile_cost = dim == 128 ? 1100 : 900;
+    a->tile_share = 16 * (64 * 2 * dim * 2) / 3470;
 }
 
 static int check_attn(const void *p, int64_t token, int64_t head, const char *what, const char *name)
@@ -223,8 +224,8 @@ extern "C" int wf_attend(wf_attn *at, const wf_kv *kv, const wf_kv_step *step, c
     a.few = INT64_MAX, a.both = 0;
     if (expected * a.group > kFew) {
         a.tile_q = a.group <= kKeys ? kKeys / a.group * a.group : kKeys;
-        a.few = kFew, a.both = 1;
-        wf_costs(eight, layer->dim, &a);
+        a.few = kFew, a.both = !eight;
+        wf_costs(layer->dim, &a);
         AttendArgs b = a;
         b.part = at->part[1], b.arrive = at->arrive[1];
         rc = wf_launch_prompt(at, b, in->dtype, layer->dim, eight, (cudaStream_t)stream);

@@ -315,7 +315,7 @@ template <typename T, int D, bool HALF, bool VEC> __device__ __forceinline__ voi
     const uint32_t begin = s_begin;
     if (!begin) return;
     if (n == a.per && s_end > n) {  // on behind the window
-        for (int64_t base = n; base < a.bs + n && s_end == 0x7FFFFFFF; base += kThreads) {
+        for (int64_t base = n; base < (int64_t)a.bs + n && s_end == 0x7FFFFFFF; base += kThreads) {
             __syncthreads();
             const int64_t t = first + base + threadIdx.x;
             const int64_t slot = t < a.tokens ? a.slot[t] : -1;
