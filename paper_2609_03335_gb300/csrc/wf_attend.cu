@@ -466,12 +466,12 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
         const int64_t room = rest ? gridDim.x / a.sms * (a.sms - prompt_sms(a, total, rest)) : gridDim.x;
         return (int32_t)max((int64_t)1, min(room, total / kLeast));
     });
-    if (f.row >= a.rows) {
+    if (f.r >= a.rows) {
         leave(a);
         return;
     }
     // The walk along the line is one thread's, and lies in shared memory: the others' registers are for the products.
-    if (threadIdx.x == 0) s_walk = {f.span, f.span.begin(blockIdx.x), f.span.begin(blockIdx.x + 1), f.row_begin, f.row, row_of(a, f.row)};
+    if (threadIdx.x == 0) s_walk = {f.span, f.span.begin(blockIdx.x), f.span.begin(blockIdx.x + 1), f.row_begin, f.r, f.row};
     for (;;) {
         if (threadIdx.x == 0) next_part(a, s_walk, s_part);
         __syncthreads();

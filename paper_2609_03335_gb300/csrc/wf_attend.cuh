@@ -128,12 +128,13 @@ struct Span {
     }
 };
 
-// The line, how it is cut (by `cut`, from this kernel's and the other's totals), and the row (its number and where it begins) that holds
-// this CTA's first place; row = rows: this CTA has none.
+// The line, how it is cut (by `cut`, from this kernel's and the other's totals), and the row (where it begins, its number, itself) that holds
+// this CTA's first place; r = rows: this CTA has none.
 struct Found {
     Span span;
     int64_t row_begin;
-    int32_t row;
+    int32_t r;
+    Row row;
 };
 
 template <int THREADS, bool LONG, typename CUT> __device__ Found find_row(const AttendArgs &a, CUT cut)
@@ -143,8 +144,9 @@ template <int THREADS, bool LONG, typename CUT> __device__ Found find_row(const 
     __shared__ Found found;
     const int32_t per = (a.rows + THREADS - 1) / THREADS, r0 = min(a.rows, (int32_t)threadIdx.x * per), r1 = min(a.rows, r0 + per);
     int64_t mine = 0, other = 0;
+    Row row = {};
     for (int32_t r = r0; r < r1; r++) {
-        const Row row = row_of(a, r);
+        row = row_of(a, r);
         mine += LONG ? long_work(a, row) : short_work(a, row);
         if (a.both) other += LONG ? short_work(a, row) : long_work(a, row);
     }
@@ -166,18 +168,21 @@ template <int THREADS, bool LONG, typename CUT> __device__ Found find_row(const 
     }
     const Span span = {total, cut(total, rest)};
     const int64_t at = blockIdx.x < span.ctas ? span.begin(blockIdx.x) : total;
-    if (threadIdx.x == 0) found = {span, total, a.rows};
+    if (threadIdx.x == 0) found = {span, total, a.rows, {}};
     __syncthreads();
-    if (mine && at >= before && at < before + mine)
+    if (mine && at >= before && at < before + mine && per == 1) {
+        found = {span, before, r0, row};
+    } else if (mine && at >= before && at < before + mine) {
         for (int32_t r = r0; r < r1; r++) {
-            const Row row = row_of(a, r);
+            row = row_of(a, r);
             const int64_t w = LONG ? long_work(a, row) : short_work(a, row);
             if (at < before + w) {
-                found = {span, before, r};
+                found = {span, before, r, row};
                 break;
             }
             before += w;
         }
+    }
     __syncthreads();
     return found;
 }

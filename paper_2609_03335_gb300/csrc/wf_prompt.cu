@@ -238,10 +238,10 @@ struct Walk {
     Row row;
     Line line;
 
-    __device__ __forceinline__ Walk(const AttendArgs &a, const Found &f) : span(f.span), r(f.row)
+    __device__ __forceinline__ Walk(const AttendArgs &a, const Found &f) : span(f.span), r(f.r)
     {
         at = span.begin(blockIdx.x), stop = span.begin(blockIdx.x + 1);
-        row = row_of(a, r), line = line_of(a, row);
+        row = f.row, line = line_of(a, row);
         const int64_t each = line.head();
         head = (int32_t)quotient(at - f.row_begin, each);
         const int64_t base = f.row_begin + head * each, x = at - base;
@@ -931,7 +931,7 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
     const Found f = find_row<kThreads, true>(a, [&](int64_t total, int64_t rest) {
         return (int32_t)max((int64_t)1, min((int64_t)prompt_sms(a, rest, total), total / (6 * kKeys * (int64_t)a.group)));
     });
-    if (f.row >= a.rows) return;
+    if (f.r >= a.rows) return;
     if (smem_of(raw) % 1024) {  // the swizzle's patterns would not lie as the products read them
         if (threadIdx.x == 0) *a.err = 2;
         return;
