@@ -805,7 +805,7 @@ void wf_attn_destroy(wf_attn *a);
 typedef struct {
     int32_t dtype;       /* of q and out: WF_F16 or WF_BF16, the layer's type where that has 16 bits */
     int32_t heads;       /* query heads, a multiple of the layer's: head h reads the layer's head h / (heads / layer heads) */
-    float scale;         /* of the products, >= 0, usually dim^-0.5 */
+    float scale;         /* of the products, >= 0, usually dim^-0.5; 0 gives the mean of the values that a token sees */
     int32_t new_tokens;  /* the most new tokens that a row is expected to have, 0: unknown.  A hint: it chooses how
                             the call is launched (1 for a step of decoding), never what it computes */
     const void *q;       /* [max_tokens][heads][dim] */

@@ -1,5 +1,6 @@
 // The calls on a layer's tensors, host side: the checks of their arguments.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdlib>
 
@@ -215,7 +216,9 @@ extern "C" int wf_attend(wf_attn *at, const wf_kv *kv, const wf_kv_step *step, c
     a.q_token = in->q_token, a.q_head = in->q_head, a.o_token = in->out_token, a.o_head = in->out_head;
     a.group = in->heads / layer->heads;
     a.by_bs = wf_make_div(a.bs), a.by_group = wf_make_div(a.group);
-    a.scale = in->scale * 1.4426950408889634f;
+    // prompt_kernel masks scores before it scales them, and -inf * 0 is no number.  The least positive number in place of 0 keeps finite scores
+    // within 2^-21 of each other (2^-149 times 2^128), so that the weights are equal; a finite scale stays finite.
+    a.scale = std::clamp(in->scale * 1.4426950408889634f, FLT_TRUE_MIN, FLT_MAX);
     a.part = at->part[0], a.arrive = at->arrive[0], a.err = at->err, a.sms = at->sms;
     // Rows of up to kFew queries to a key head go to the kernel of 16-query tiles, the others to that of 128-query tiles.  Where no row is
     // expected to have more (or none can), one launch takes them all.
