@@ -562,8 +562,8 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
                 const uint32_t s = it % S::kStages, to = kv + s * S::kTile;
                 const uint8_t *from = side ? v : k;
                 const uint32_t freed = ((it / S::kStages) & 1) ^ 1;
-                // While there is no room, what has landed is announced at once.
-                while (waiting && !bar_try(sh.bar(kBarFull + 8 + s), freed)) {
+                // While there is no room, what has landed is announced at once: the warp's decision, as announcements are (its lanes' polls may differ).
+                while (waiting && !__all_sync(~0u, bar_try(sh.bar(kBarFull + 8 + s), freed))) {
                     if (waiting == 2) copies_wait<1>();
                     else copies_wait<0>();
                     announce(it - waiting);

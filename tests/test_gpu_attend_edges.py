@@ -27,3 +27,19 @@ def test_scales(have, add, scaling, dtype, eight):
     q = tensor(rng, (st.room, 6, 64), dtype)
     check(st, cache, scale, q, attend(wf, st, cache, scale, q, scaling=scaling), scaling)
     check(st, cache, scale, q, attend(wf, st, cache, scale, q, scaling=scaling, new=1), scaling)
+
+
+@pytest.mark.parametrize("bs,kv,dim", [(7, 2, 64), (100, 1, 128), (1, 2, 64), (30, 4, 128)])
+def test_blocks_that_no_box_fits_again_and_again(bs, kv, dim):
+    """Prompts over blocks whose positions are copied one by one (no multiple of 8): many tiles under way, every call the same."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(55)
+    st = Step(wf, rng, [900, 0, 40], [200, 700, 65], bs)
+    cache, _ = cache_of(rng, st, kv, dim, "bfloat16")
+    q = tensor(rng, (st.room, 2 * kv, dim), "bfloat16")
+    attn = wf.Attn(max_rows=3, heads=2 * kv, dim=dim)
+    first = attend(wf, st, cache, None, q, attn=attn)
+    check(st, cache, None, q, first)
+    for _ in range(30):
+        assert torch.equal(first, attend(wf, st, cache, None, q, attn=attn))
