@@ -39,7 +39,7 @@
  *   wf_kv_reorder           rows put in the selection's order: tables, last blocks, freed blocks
  *   wf_kv_write             a layer's keys and values of a step's tokens into the cache, with rotary positions
  *   wf_kv_copy_scales       an 8-bit cache's scales after wf_kv_reorder's copies
- *   wf_attn_create, wf_attn_status, wf_attn_destroy
+ *   wf_attn_create, wf_attn_status, wf_attn_limit_waits, wf_attn_destroy
  *   wf_attend               a layer's attention of a step's tokens over their rows' cached keys and values
  *
  * Conventions.
@@ -794,9 +794,16 @@ int wf_attn_create(const wf_attn_limits *limits, int device, wf_attn **out);
 /*
  * Synchronize `stream` and report (then clear) what earlier calls found on
  * the device: WF_EINVAL when a table named a block outside the cache or a row's
- * lengths contradict each other, WF_ETIMEOUT when a bounded wait expired, else WF_OK.
+ * lengths contradict each other, WF_ETIMEOUT when a bounded wait expired (the outputs of all calls since the last status are
+ * invalid then, and the next call finds the scratch as new), else WF_OK.
  */
 int wf_attn_status(wf_attn *a, void *stream);
+
+/*
+ * Polls, of a microsecond or a few each, after which a wait of later calls on the GPU gives up: 0..2^20, 2^20 unless set here.
+ * Diagnostic: with 0 a call over rows with many queries gives up at the first wait that finds nothing, and wf_attn_status returns WF_ETIMEOUT.
+ */
+int wf_attn_limit_waits(wf_attn *a, int32_t polls);
 
 /* Release the scratch (NULL is a no-op). */
 void wf_attn_destroy(wf_attn *a);

@@ -8,10 +8,12 @@ struct wf_attn {
     int device;
     int sms;
     wf_attn_limits lim;
+    int polls;           // of a bounded wait
     void *mem;
-    int *err;            // device error word (wf_attn_status): 1 a block or a row, 2 a wait
+    size_t zeroed;       // bytes at its beginning that are 0 between calls: err and arrive
+    int *err;            // device error words (wf_attn_status): not 0 after a bad block or row; after a wait that ran out
     // Of attend_kernel, of prompt_kernel, which may run side by side:
-    uint32_t *arrive[2]; // arrivals at units that several CTAs share, by the CTA that begins one; every call leaves them 0
+    uint32_t *arrive[2]; // arrivals at units that several CTAs share, by the CTA that begins one; a call whose waits do not run out leaves them 0
     float *part[2];      // two parts a CTA
     int grid[2][2];      // CTAs of attend_kernel by 8 bits or not, dim 64 or 128
 };
@@ -56,7 +58,7 @@ __device__ __forceinline__ Row row_of(const AttendArgs &a, int32_t r)
     Row row = {s0, s1 - s0, len};
     if (s0 == s1) return {s0, 0, len};
     if (s0 < 0 || s1 < s0 || s1 > a.max_tokens || len < row.n || len > (int64_t)a.row_blocks * a.bs) {
-        *a.err = 1;
+        a.err[0] = 1;
         return {0, 0, 0};
     }
     return row;
@@ -192,7 +194,7 @@ __device__ __forceinline__ int32_t block_at(const AttendArgs &a, const int32_t *
 {
     const int32_t b = table[j];
     if ((uint32_t)b < (uint32_t)a.n_blocks) return b;
-    *a.err = 1;
+    a.err[0] = 1;
     return 0;
 }
 

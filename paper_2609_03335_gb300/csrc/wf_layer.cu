@@ -97,6 +97,9 @@ extern "C" int wf_kv_copy_scales(wf_decode *d, const wf_kv *kv, const int32_t *c
     return rc ? rc : wf_launch_copy_scales(d, kv, copies, scale, planes, plane_stride, heads, (cudaStream_t)stream);
 }
 
+// Polls of a bounded wait unless wf_attn_limit_waits says otherwise.
+constexpr int32_t kPolls = 1 << 20;
+
 extern "C" int wf_attn_create(const wf_attn_limits *lim, int device, wf_attn **out)
 {
     REQUIRE(out, "out is NULL");
@@ -113,6 +116,7 @@ extern "C" int wf_attn_create(const wf_attn_limits *lim, int device, wf_attn **o
     if (!a) return wf_set_error(WF_ENOMEM, "host allocation of the attention scratch");
     a->device = device;
     a->lim = *lim;
+    a->polls = kPolls;
     rc = wf_cuda_check(cudaDeviceGetAttribute(&a->sms, cudaDevAttrMultiProcessorCount, device), "device attributes");
     if (!rc) rc = wf_attend_setup(a);
     if (!rc) rc = wf_prompt_setup(a);
@@ -127,7 +131,7 @@ extern "C" int wf_attn_create(const wf_attn_limits *lim, int device, wf_attn **o
     // The clearing runs on the default stream; the calls may use any other.
     if (!rc) rc = wf_cuda_check(cudaDeviceSynchronize(), "cudaDeviceSynchronize");
     if (rc) { wf_attn_destroy(a); return rc; }
-    a->err = (int *)a->mem;
+    a->err = (int *)a->mem, a->zeroed = zeroed;
     for (int i = 0; i < 2; i++) {
         a->arrive[i] = (uint32_t *)((uint8_t *)a->mem + 256 + i * arrivals);
         a->part[i] = (float *)((uint8_t *)a->mem + zeroed + i * parts);
@@ -151,14 +155,23 @@ extern "C" int wf_attn_status(wf_attn *a, void *stream)
     REQUIRE(a, "NULL attention scratch");
     int rc = wf_cuda_check(cudaSetDevice(a->device), "cudaSetDevice");
     if (!rc) rc = wf_cuda_check(cudaStreamSynchronize((cudaStream_t)stream), "cudaStreamSynchronize");
-    int err = 0;
-    if (!rc) rc = wf_cuda_check(cudaMemcpy(&err, a->err, sizeof(int), cudaMemcpyDeviceToHost), "read error word");
-    if (rc || !err) return rc;
-    rc = wf_cuda_check(cudaMemset(a->err, 0, sizeof(int)), "clear error word");
+    int err[2] = {0, 0};
+    if (!rc) rc = wf_cuda_check(cudaMemcpy(err, a->err, sizeof(err), cudaMemcpyDeviceToHost), "read error words");
+    if (rc || !(err[0] | err[1])) return rc;
+    // With the arrivals: those of a call whose waits ran out were not all made.
+    rc = wf_cuda_check(cudaMemset(a->mem, 0, a->zeroed), "clear error words");
     if (!rc) rc = wf_cuda_check(cudaDeviceSynchronize(), "cudaDeviceSynchronize");
     if (rc) return rc;
-    if (err == 2) return wf_set_error(WF_ETIMEOUT, "a bounded wait expired; outputs are invalid");
+    if (err[1]) return wf_set_error(WF_ETIMEOUT, "a bounded wait expired; outputs of the calls since the last status are invalid");
     return wf_set_error(WF_EINVAL, "a table names a block outside the cache, or a row's lengths contradict each other");
+}
+
+extern "C" int wf_attn_limit_waits(wf_attn *a, int32_t polls)
+{
+    REQUIRE(a, "NULL attention scratch");
+    REQUIRE(polls >= 0 && polls <= kPolls, "%d polls outside 0..%d", polls, kPolls);
+    a->polls = polls;
+    return WF_OK;
 }
 
 // Queries to a key head (new tokens times the group's heads) up to which a row goes to attend_kernel: one of its tiles.  Two tiles read the

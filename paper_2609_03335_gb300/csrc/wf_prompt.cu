@@ -22,8 +22,9 @@
 // handed over in halves, to begin sooner, cost 80 us of 1,420, a lane elected anew each turn 68, a second warp for tile B 280.
 //
 // Work is laid on a line and cut into equal stretches as in wf_attend.cu; a unit is the 256 queries, its weight grows with
-// the positions that they see.  Every wait ends: after a limit it is reported (wf_attn_status) and the
-// kernel runs to its end without waiting.
+// the positions that they see.  Every wait ends: after a limit it is reported (wf_attn_status) and the role that waited leaves, as the others of the
+// CTA do at their next wait that finds nothing.  No unit is overwritten, no output joined and no copy or product begun after that; those under
+// way are awaited before the CTA ends, and wf_attn_status clears the arrivals that a join may be left with.
 #include <algorithm>
 #include <type_traits>
 
@@ -52,7 +53,7 @@ template <bool E, int D> struct Shape {
     static constexpr int kScales = E ? kSlots * 3 * kFours * 4 : 0;  // keys' scales, log2 and reciprocal of values', for each four positions
     static constexpr int kQBytes = 2 * kTile;
     static constexpr int kRawBytes = E ? kRaw * kKeys * D : 0;
-    static constexpr int kSmem = kQBytes + kRawBytes + kStages * kTile + kScales + (E ? 0 : kKeys * 8);
+    static constexpr int kSmem = kQBytes + kRawBytes + kStages * kTile + kScales;
     static_assert(kSmem + 1024 <= 227 * 1024, "shared memory");  // with what is static, up to the next 1,024 bytes
 };
 
@@ -62,13 +63,14 @@ struct PromptArgs {
     int32_t map_q;   // whether q is
     int32_t heads;   // the maps' last coordinate: block * heads + head
     int32_t beyond;  // the first that is not there
+    int32_t polls, hint;  // of a wait before it gives up, nanoseconds of one
     CUtensorMap k, v, q;
 };
 
 constexpr int kUnits = 4;  // that the roles may be apart
 
 enum { kBarQFull, kBarQEmpty, kBarS, kBarP = kBarS + 2, kBarO = kBarP + 2, kBarDrain = kBarO + 2, kBarFull, kBarUnit = kBarFull + 16, kBarRaw = kBarUnit + 2 * kUnits,
-       kBarScale = kBarRaw + 2 * kRaws, kBars = kBarScale + 2 * kSlots };
+       kBarScale = kBarRaw + 2 * kRaws, kBarJoin = kBarScale + 2 * kSlots, kBarLast, kBars };
 
 __device__ __forceinline__ uint32_t smem_of(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -86,25 +88,27 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar)
     if (threadIdx.x % 32 == 0) bar_arrive(bar);
 }
 
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
+// Whether the barrier's phase is over; the hardware may wait about `hint` nanoseconds for it.
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity, uint32_t hint = 1000)
 {
     uint32_t done;
     asm volatile("{ .reg .pred p;\n"
-                 "  mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000;\n"
-                 "  selp.u32 %0, 1, 0, p; }" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+                 "  mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
+                 "  selp.u32 %0, 1, 0, p; }" : "=r"(done) : "r"(bar), "r"(parity), "r"(hint) : "memory");
     return done;
 }
 
-// Waits about 2 s at most; then (or when another thread has given up) on without waiting.
-__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up, int *err)
+// Waits for so many polls more than one; false: that ran out, here or in another thread.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, int polls, uint32_t hint, volatile int *gave_up, int *err)
 {
-    if (bar_try(bar, parity)) return;
-    for (int i = 0; i < 1 << 20 && !*gave_up; i++)
-        if (bar_try(bar, parity)) return;
+    if (bar_try(bar, parity, hint)) return true;
+    for (int i = 0; i < polls && !*gave_up; i++)
+        if (bar_try(bar, parity, hint)) return true;
     if (!*gave_up) {
         *gave_up = 1;
-        *err = 2;
+        err[1] = 1;
     }
+    return false;
 }
 
 __device__ __forceinline__ void copy16(uint32_t to, const void *from, bool there)
@@ -125,7 +129,6 @@ __device__ __forceinline__ void copy_box3(uint32_t to, const CUtensorMap *map, u
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void to_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-template <int ID, int N> __device__ __forceinline__ void sync_some() { asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(N) : "memory"); }
 
 __device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -306,17 +309,20 @@ struct Shared {
     Unit *units;           // [kUnits]
     uint8_t *q, *kv, *raw; // on 1,024 bytes; raw: tiles in 8 bits as the cache has them
     float *scales;
-    int64_t *offset;       // [kKeys] of a tile's keys in the cache, -1: none
     uint32_t bars;         // address
+    int polls, hint;
     volatile int *gave_up;
     int *err;
     __device__ __forceinline__ uint32_t bar(int i) const { return bars + 8 * i; }
-    __device__ __forceinline__ void wait(int i, uint32_t parity) const { bar_wait(bar(i), parity, gave_up, err); }
-    // Unit i of the CTA.
-    __device__ __forceinline__ const Unit &unit(uint32_t i) const
+    // False: waiting was given up.  wait: every lane of the warp comes, and the answer is one for all.
+    __device__ __forceinline__ bool wait_alone(int i, uint32_t parity) const { return bar_wait(bar(i), parity, polls, hint, gave_up, err); }
+    __device__ __forceinline__ bool wait(int i, uint32_t parity) const { return __all_sync(~0u, wait_alone(i, parity)); }
+    // Unit i of the CTA; null: there are no more, or waiting was given up.  It stays as it is until every role is done with it.
+    __device__ __forceinline__ const Unit *unit(uint32_t i) const
     {
-        wait(kBarUnit + i % kUnits, i / kUnits & 1);
-        return units[i % kUnits];
+        if (!wait(kBarUnit + i % kUnits, i / kUnits & 1)) return nullptr;
+        const Unit *u = units + i % kUnits;
+        return u->n ? u : nullptr;
     }
     __device__ __forceinline__ void unit_done(uint32_t i) const { warp_arrive(bar(kBarUnit + kUnits + i % kUnits)); }
 };
@@ -328,7 +334,7 @@ __device__ __forceinline__ void unit_role(const AttendArgs &a, const Found &f, c
     Unit u;
     for (uint32_t i = 0;; i++) {
         const bool more = walk.next(a, u);
-        sh.wait(kBarUnit + kUnits + i % kUnits, (i / kUnits & 1) ^ 1);
+        if (!sh.wait_alone(kBarUnit + kUnits + i % kUnits, (i / kUnits & 1) ^ 1)) return;
         if (!more) u.n = 0;
         sh.units[i % kUnits] = u;
         bar_arrive(sh.bar(kBarUnit + i % kUnits));
@@ -359,18 +365,22 @@ template <typename T> __device__ __forceinline__ float largest(const uint4 &x)
     return fmaxf(fmaxf(fmaxf(fabsf(a.x), fabsf(a.y)), fmaxf(fabsf(b.x), fabsf(b.y))), fmaxf(fmaxf(fabsf(c.x), fabsf(c.y)), fmaxf(fabsf(d.x), fabsf(d.y))));
 }
 
-// A tile by boxes of `box` positions of one block: one copy a lane, whose block (in the maps' last coordinate) and place in it are given.
+// A tile by boxes of `box` positions of one block, once there is room: one copy a lane, whose block (in the maps' last coordinate) and place in it are
+// given.  False: waiting was given up.
 template <bool E, int D>
-__device__ __forceinline__ void copy_boxes(const PromptArgs &pa, const CUtensorMap *map, uint32_t to, uint32_t bar, int32_t block, int32_t place, int lane)
+__device__ __forceinline__ bool copy_boxes(const PromptArgs &pa, const Shared &sh, int room, uint32_t parity, const CUtensorMap *map, uint32_t to, int bar,
+                                           int32_t block, int32_t place, int lane)
 {
     constexpr int kRow = E ? D : 2 * D;
     const int box = pa.box;
-    if (lane == 0) bar_expect(bar, kKeys * kRow);
-    __syncwarp();
+    const bool there = sh.wait_alone(room, parity);
+    if (there && lane == 0) bar_expect(sh.bar(bar), kKeys * kRow);
+    if (!__all_sync(~0u, there)) return false;
     if (lane * box < kKeys) {
-        if constexpr (E) copy_box3(to + lane * box * kRow, map, bar, 0, place, block);
-        else copy_box5(to + lane * box * kRow, map, bar, 0, 0, 0, place / 8, block);
+        if constexpr (E) copy_box3(to + lane * box * kRow, map, sh.bar(bar), 0, place, block);
+        else copy_box5(to + lane * box * kRow, map, sh.bar(bar), 0, 0, 0, place / 8, block);
     }
+    return true;
 }
 
 // Warp 14: copies by the tensor maps, where the layout allows them.
@@ -380,12 +390,10 @@ template <typename T, bool E, int D> __device__ __forceinline__ void box_role(co
     const AttendArgs &a = pa.a;
     const int lane = threadIdx.x % 32;
     const uint32_t kv = smem_of(sh.kv), raw = smem_of(sh.raw);
-    uint32_t it = 0, units = 0;
-    for (;; units++) {
-        const Unit &u = sh.unit(units);
-        if (!u.n) break;
-        if (pa.map_q && !*sh.gave_up) {
-            sh.wait(kBarQEmpty, (units & 1) ^ 1);
+    uint32_t it = 0, units = 0, queries = 0;  // tiles, units, units' queries whose copies have begun
+    auto unit = [&](const Unit &u) {
+        if (pa.map_q) {
+            if (!sh.wait(kBarQEmpty, (units & 1) ^ 1)) return false;
             const int tiles = u.nb ? 2 : 1;
             if (lane == 0) bar_expect(sh.bar(kBarQFull), tiles * (D / 64) * a.tile_q * 128);
             __syncwarp();
@@ -394,60 +402,64 @@ template <typename T, bool E, int D> __device__ __forceinline__ void box_role(co
                 copy_box3(smem_of(sh.q) + x * S::kTile + g * S::kHalf, &pa.q, sh.bar(kBarQFull), g * 64, u.head * a.group,
                           u.row.first + (int32_t)wf_quot((uint32_t)u.q0 + x * a.tile_q, a.by_group));
             }
+            queries++;
         }
-        if (pa.box && !*sh.gave_up) {
-            const int32_t end = min(u.seen, (u.t0 + u.n) * kKeys);
-            const int32_t *table = a.table + u.r * a.table_stride;
-            // This lane's box of tile j: its block in the table, and in the maps.  Boxes behind `end` come from a block that is not there: zeros.
-            auto position = [&](int32_t j) { return (u.t0 + j) * kKeys + min(lane * pa.box, kKeys - 1); };
-            auto block = [&](int32_t j) { return block_at(a, table, wf_quot(min(position(j), end - 1), a.by_bs)); };
-            int32_t next = block(0);
-            for (int32_t j = 0; j < u.n; j++) {
-                const int32_t p = (u.t0 + j) * kKeys, at = position(j);
-                const int32_t b = at < end ? next * pa.heads + u.head : pa.beyond, place_in = at < end ? at - (int32_t)wf_quot(at, a.by_bs) * a.bs : 0;
-                if (j + 1 < u.n) next = block(j + 1);
-                // A box that the row ends in holds what lies behind the row, and a weight of 0 does not undo a NaN there.
-                const bool ends = !E && u.row.len % pa.box && p + kKeys > u.row.len;
+        if (!pa.box) return true;
+        const int32_t end = min(u.seen, (u.t0 + u.n) * kKeys);
+        const int32_t *table = a.table + u.r * a.table_stride;
+        // This lane's box of tile j: its block in the table, and in the maps.  Boxes behind `end` come from a block that is not there: zeros.
+        auto position = [&](int32_t j) { return (u.t0 + j) * kKeys + min(lane * pa.box, kKeys - 1); };
+        auto block = [&](int32_t j) { return block_at(a, table, wf_quot(min(position(j), end - 1), a.by_bs)); };
+        int32_t next = block(0);
+        for (int32_t j = 0; j < u.n; j++) {
+            const int32_t p = (u.t0 + j) * kKeys, at = position(j);
+            const int32_t b = at < end ? next * pa.heads + u.head : pa.beyond, place_in = at < end ? at - (int32_t)wf_quot(at, a.by_bs) * a.bs : 0;
+            if (j + 1 < u.n) next = block(j + 1);
+            // A box that the row ends in holds what lies behind the row, and a weight of 0 does not undo a NaN there.
+            const bool ends = !E && u.row.len % pa.box && p + kKeys > u.row.len;
 #pragma unroll 1
-                for (int side = 0; side < 2; side++, it++) {
-                    const CUtensorMap *map = side ? &pa.v : &pa.k;
-                    if constexpr (E) {
-                        const uint32_t s = it % S::kRaw;
-                        sh.wait(kBarRaw + kRaws + s, (it / S::kRaw & 1) ^ 1);
-                        copy_boxes<E, D>(pa, map, raw + s * (kKeys * D), sh.bar(kBarRaw + s), b, place_in, lane);
+            for (int side = 0; side < 2; side++, it++) {
+                const CUtensorMap *map = side ? &pa.v : &pa.k;
+                if constexpr (E) {
+                    const uint32_t s = it % S::kRaw;
+                    if (!copy_boxes<E, D>(pa, sh, kBarRaw + kRaws + s, (it / S::kRaw & 1) ^ 1, map, raw + s * (kKeys * D), kBarRaw + s, b, place_in, lane))
+                        return false;
+                } else {
+                    const uint32_t s = it % S::kStages, to = kv + s * S::kTile, empty = (it / S::kStages & 1) ^ 1;
+                    if (!ends || !side) {
+                        if (!copy_boxes<E, D>(pa, sh, kBarFull + 8 + s, empty, map, to, kBarFull + s, b, place_in, lane)) return false;
                     } else {
-                        const uint32_t s = it % S::kStages, to = kv + s * S::kTile;
-                        sh.wait(kBarFull + 8 + s, (it / S::kStages & 1) ^ 1);
-                        if (!ends || !side) {
-                            copy_boxes<E, D>(pa, map, to, sh.bar(kBarFull + s), b, place_in, lane);
-                        } else {
-                            constexpr int kPer = D / 8;
-                            const uint8_t *v = a.v + u.head * a.head_stride;
+                        if (!sh.wait(kBarFull + 8 + s, empty)) return false;
+                        constexpr int kPer = D / 8;
+                        const uint8_t *v = a.v + u.head * a.head_stride;
 #pragma unroll 1
-                            for (int i = lane / kPer; i < kKeys; i += 32 / kPer) {
-                                const int32_t key = min(p + i, u.row.len - 1);
-                                const uint32_t in = wf_quot(key, a.by_bs);
-                                const uint8_t *from = v + block_at(a, table, in) * a.block_stride + (key - (int32_t)in * a.bs) * a.token_stride;
-                                copy16(to + place<D>(i, lane % kPer), from + lane % kPer * 16, p + i < u.row.len);
-                            }
-                            copies_commit();
-                            copies_wait<0>();
-                            to_async();
-                            __syncwarp();
-                            if (lane == 0) bar_arrive(sh.bar(kBarFull + s));
+                        for (int i = lane / kPer; i < kKeys; i += 32 / kPer) {
+                            const int32_t key = min(p + i, u.row.len - 1);
+                            const uint32_t in = wf_quot(key, a.by_bs);
+                            const uint8_t *from = v + block_at(a, table, in) * a.block_stride + (key - (int32_t)in * a.bs) * a.token_stride;
+                            copy16(to + place<D>(i, lane % kPer), from + lane % kPer * 16, p + i < u.row.len);
                         }
+                        copies_commit();
+                        copies_wait<0>();
+                        to_async();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(sh.bar(kBarFull + s));
                     }
                 }
             }
         }
+        return true;
+    };
+    for (; const Unit *u = sh.unit(units); units++) {
+        if (!unit(*u)) break;
         sh.unit_done(units);
     }
-    // Where waiting was given up, copies may still be on their way into this CTA's shared memory: no longer than a while.
-    if (*sh.gave_up && lane == 0) {
+    // No copy is on its way into this CTA's shared memory when it ends, whatever the other roles have come to.
+    if (lane == 0) {
         const int n = E ? S::kRaw : S::kStages, first = E ? kBarRaw : kBarFull;
         for (uint32_t i = it > (uint32_t)n ? it - n : 0; pa.box && i < it; i++)
             for (int k = 0; k < 1 << 16 && !bar_try(sh.bar(first + i % n), i / n & 1); k++) {}
-        for (int k = 0; pa.map_q && units && k < 1 << 16 && !bar_try(sh.bar(kBarQFull), (units - 1) & 1); k++) {}
+        for (int k = 0; queries && k < 1 << 16 && !bar_try(sh.bar(kBarQFull), (queries - 1) & 1); k++) {}
     }
     __syncwarp();
 }
@@ -457,9 +469,8 @@ __device__ __forceinline__ void scale_role(const AttendArgs &a, const Shared &sh
 {
     const int lane = threadIdx.x % 32;
     uint32_t t = 0;
-    for (uint32_t units = 0;; units++) {
-        const Unit &u = sh.unit(units);
-        if (!u.n) break;
+    for (uint32_t units = 0; const Unit *now = sh.unit(units); units++) {
+        const Unit &u = *now;
         const int32_t *table = a.table + u.r * a.table_stride;
         const int32_t end = min(u.seen, (u.t0 + u.n) * kKeys), n = u.n, p0 = u.t0 * kKeys + 4 * lane;
         const float *ks = a.k_scale + u.head, *vs = a.v_scale + u.head;
@@ -473,7 +484,7 @@ __device__ __forceinline__ void scale_role(const AttendArgs &a, const Shared &sh
             if (j + 1 < n) k = ks[b], v = vs[b];
             if (j + 2 < n) b = block(j + 2);
             const uint32_t s = t % kSlots;
-            sh.wait(kBarScale + kSlots + s, (t / kSlots & 1) ^ 1);
+            if (!sh.wait(kBarScale + kSlots + s, (t / kSlots & 1) ^ 1)) return;
             float *to = sh.scales + s * 3 * kFours + lane;
             to[0] = now_k, to[kFours] = __log2f(now_v), to[2 * kFours] = __frcp_rn(now_v);
             warp_arrive(sh.bar(kBarScale + s));
@@ -487,23 +498,28 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
 {
     using S = Shape<E, D>;
     const AttendArgs &a = pa.a;
-    const int tid = threadIdx.x - 256;
+    const int tid = threadIdx.x - 256, lane = tid % 32;
+    // Of a tile in 16 bits a warp copies kAt keys at once, kRows further on each time: 32 in all, of which each lane looks up one.
+    constexpr int kChunks = D / 8, kAt = 32 / kChunks, kRows = kLoaders / kChunks;  // 16-byte chunks of a key or query; queries at once
+    const int mine = lane / kAt * kRows + tid / 32 * kAt + lane % kAt;
     const uint32_t kv = smem_of(sh.kv), q = smem_of(sh.q);
     uint32_t it = 0, units = 0;
+    bool on = true;
     int32_t waiting = 0;   // tiles whose copies are under way and not yet announced (16 bits)
     auto announce = [&](uint32_t i) {
         to_async();
         warp_arrive(sh.bar(kBarFull + i % S::kStages));
     };
-    for (;; units++) {
-        const Unit &u = sh.unit(units);
-        if (!u.n) break;
+    for (; on; units++) {
+        const Unit *now = sh.unit(units);
+        if (!now) break;
+        const Unit &u = *now;
         const int32_t *table = a.table + u.r * a.table_stride;
         const uint8_t *k = a.k + u.head * a.head_stride, *v = a.v + u.head * a.head_stride;
         const int32_t end = min(u.seen, (u.t0 + u.n) * kKeys);  // positions that count
-        // The block of this thread's key of tile j.
+        // The block of this lane's key of tile j.
         auto block = [&](int32_t j) {
-            const int32_t p = min((u.t0 + j) * kKeys + tid, end - 1);
+            const int32_t p = min((u.t0 + j) * kKeys + mine, end - 1);
             return block_at(a, table, wf_quot(p, a.by_bs));
         };
         const bool tiles = E || !pa.box;
@@ -512,26 +528,26 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
         copies_wait<0>();
         for (; waiting; waiting--) announce(it - waiting);
         if (!pa.map_q) {  // queries, once the products of the unit before have read theirs
-            sh.wait(kBarQEmpty, (units & 1) ^ 1);
-            constexpr int kPer = D / 8, kRows = kLoaders / kPer;  // 16-byte chunks of a query; queries at once
-            const int c = tid % kPer;
+            on = sh.wait(kBarQEmpty, (units & 1) ^ 1);
+            if (!on) break;
+            const int c = tid % kChunks;
 #pragma unroll 1
             for (int x = 0; x < (u.nb ? 2 : 1); x++) {
                 const int queries = min(a.tile_q, u.queries - x * a.tile_q);
                 if (!E || std::is_same_v<T, __half>) {
 #pragma unroll 4
-                    for (int i = tid / kPer; i < kQ; i += kRows) {
+                    for (int i = tid / kChunks; i < kQ; i += kRows) {
                         const bool there = i < queries;
                         copy16(q + x * S::kTile + query_place(i, c), query(a, u, x * a.tile_q + (there ? i : 0)) + 16 * c, there);
                     }
                 } else {
 #pragma unroll 4
-                    for (int i = tid / kPer; i < kQ; i += kRows) {
+                    for (int i = tid / kChunks; i < kQ; i += kRows) {
                         const bool there = i < queries;
                         uint4 y = there ? *reinterpret_cast<const uint4 *>(query(a, u, x * a.tile_q + i) + 16 * c) : make_uint4(0, 0, 0, 0);
                         float most = largest<T>(y);
 #pragma unroll
-                        for (int s = 1; s < kPer; s *= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, s));
+                        for (int s = 1; s < kChunks; s *= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, s));
                         const float down = __int_as_float((127 - query_exponent(most)) << 23);
                         uint32_t *w = &y.x;
 #pragma unroll
@@ -548,17 +564,13 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
             to_async();
             warp_arrive(sh.bar(kBarQFull));
         }
-        for (int32_t j = 0; tiles && j < u.n; j++) {
-            const int32_t p = (u.t0 + j) * kKeys + tid;
-            int64_t *offset = sh.offset;
-            if (!E) {
-                sync_some<1, kLoaders>();
-                offset[tid] = p < end ? next * a.block_stride + (int64_t)(p - (int32_t)wf_quot(p, a.by_bs) * a.bs) * a.token_stride : -1;
-                sync_some<1, kLoaders>();
-            }
+        for (int32_t j = 0; tiles && on && j < u.n; j++) {
+            const int32_t p = (u.t0 + j) * kKeys, key = p + mine;
+            // This lane's key in the cache, -1: none.
+            const int64_t offset = !E && key < end ? next * a.block_stride + (int64_t)(key - (int32_t)wf_quot(key, a.by_bs) * a.bs) * a.token_stride : -1;
             if (!E && j + 1 < u.n) next = block(j + 1);
 #pragma unroll 1
-            for (int side = 0; side < 2; side++, it++) {  // keys, values
+            for (int side = 0; on && side < 2; side++, it++) {  // keys, values
                 const uint32_t s = it % S::kStages, to = kv + s * S::kTile;
                 const uint8_t *from = side ? v : k;
                 const uint32_t freed = ((it / S::kStages) & 1) ^ 1;
@@ -570,13 +582,13 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
                     waiting--;
                 }
                 if constexpr (!E) {
-                    sh.wait(kBarFull + 8 + s, freed);
-                    constexpr int kPer = D / 8, kRows = kLoaders / kPer;
-                    const int c = tid % kPer;
+                    on = sh.wait(kBarFull + 8 + s, freed);
+                    if (!on) break;
+                    const int c = tid % kChunks;
 #pragma unroll 8
-                    for (int i = tid / kPer; i < kKeys; i += kRows) {
-                        const int64_t o = offset[i];
-                        copy16(to + place<D>(i, c), from + (o < 0 ? 0 : o) + 16 * c, o >= 0);
+                    for (int i = 0; i < kKeys / kRows; i++) {
+                        const int64_t o = __shfl_sync(~0u, offset, i * kAt + lane / kChunks);
+                        copy16(to + place<D>(i * kRows + tid / kChunks, c), from + (o < 0 ? 0 : o) + 16 * c, o >= 0);
                     }
                     copies_commit();
                     // Two tiles under way; the one before them has landed.
@@ -587,22 +599,24 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
                         waiting++;
                     }
                 } else {
-                    constexpr int kPer = D / 16, kRows = kLoaders / kPer, kTimes = kKeys / kRows;
+                    constexpr int kPer = D / 16, kStep = kLoaders / kPer, kTimes = kKeys / kStep;
                     const int c = tid % kPer;
                     const uint32_t rs = it % S::kRaw;
                     uint4 x[kTimes];
-                    sh.wait(kBarRaw + rs, it / S::kRaw & 1);
+                    on = sh.wait(kBarRaw + rs, it / S::kRaw & 1);
+                    if (!on) break;
 #pragma unroll
                     for (int i = 0; i < kTimes; i++) {
-                        const int row = i * kRows + tid / kPer;
+                        const int row = i * kStep + tid / kPer;
                         x[i] = *reinterpret_cast<const uint4 *>(sh.raw + rs * (kKeys * D) + row * D + 16 * c);
-                        if (p - tid + row >= end) x[i] = make_uint4(0, 0, 0, 0);
+                        if (p + row >= end) x[i] = make_uint4(0, 0, 0, 0);
                     }
                     warp_arrive(sh.bar(kBarRaw + kRaws + rs));
-                    sh.wait(kBarFull + 8 + s, freed);
+                    on = sh.wait(kBarFull + 8 + s, freed);
+                    if (!on) break;
 #pragma unroll
                     for (int i = 0; i < kTimes; i++) {
-                        const int row = i * kRows + tid / kPer;
+                        const int row = i * kStep + tid / kPer;
                         const uint2 h0 = wf_e4m3_halves(x[i].x), h1 = wf_e4m3_halves(x[i].y), h2 = wf_e4m3_halves(x[i].z), h3 = wf_e4m3_halves(x[i].w);
                         uint8_t *dst = sh.kv + s * S::kTile;
                         *reinterpret_cast<uint4 *>(dst + place<D>(row, 2 * c)) = make_uint4(h0.x, h0.y, h1.x, h1.y);
@@ -612,7 +626,7 @@ template <typename T, bool E, int D> __device__ __forceinline__ void load_role(c
                 }
             }
         }
-        sh.unit_done(units);
+        if (on) sh.unit_done(units);
     }
     copies_wait<0>();
     for (; waiting; waiting--) announce(it - waiting);
@@ -629,7 +643,9 @@ template <typename T, bool E, int D> __device__ __forceinline__ void product_rol
     const uint32_t kv = smem_of(sh.kv), q = smem_of(sh.q);
     uint32_t it = 0, units = 0, np[2] = {0, 0};
     const bool leader = elected();  // once: elected anew for each turn, one prompt of 16,384 took 1,370 us in place of 1,302
-    auto full = [&](uint32_t i) { sh.wait(kBarFull + i % S::kStages, (i / S::kStages) & 1); };
+    // A lane whose wait was given up goes on at the unit's end, so that the warp leaves as one; the leader issues nothing more of the unit then.
+    bool on = true;
+    auto full = [&](uint32_t i) { return sh.wait_alone(kBarFull + i % S::kStages, (i / S::kStages) & 1); };
     auto commit = [&](int i) {
         if (leader) commit_to(sh.bar(i));
     };
@@ -652,13 +668,13 @@ template <typename T, bool E, int D> __device__ __forceinline__ void product_rol
                 mma_ts(tmem + 2 * kKeys + x * D, tmem + x * kKeys + 8 * s, value + s * (2 * S::kEight >> 4), kDescO, more || s > 0);
         }
     };
-    for (;; units++) {
-        const Unit &u = sh.unit(units);
-        const int n[2] = {u.na, u.nb}, most = u.n;
-        if (!most) break;
+    for (; __all_sync(~0u, on); units++) {
+        const Unit *u = sh.unit(units);
+        if (!u) break;
+        const int n[2] = {u->na, u->nb}, most = u->n;
         sh.unit_done(units);
-        sh.wait(kBarQFull, units & 1);
-        full(it);
+        on = false;
+        if (!sh.wait_alone(kBarQFull, units & 1) || !full(it)) continue;
         after_sync();
 #pragma unroll
         for (int x = 0; x < 2; x++)
@@ -666,12 +682,12 @@ template <typename T, bool E, int D> __device__ __forceinline__ void product_rol
         done(it);
         if (most == 1) commit(kBarQEmpty);
         for (int j = 0; j < most; j++) {
-            full(it + 2 * j + 1);
-            if (j + 1 < most) full(it + 2 * j + 2);
+            if (!full(it + 2 * j + 1)) goto next;
+            if (j + 1 < most && !full(it + 2 * j + 2)) goto next;
 #pragma unroll
             for (int x = 0; x < 2; x++) {
                 if (j < n[x]) {
-                    sh.wait(kBarP + x, np[x] & 1);
+                    if (!sh.wait_alone(kBarP + x, np[x] & 1)) goto next;
                     np[x]++;
                     after_sync();
                     sums(x, it + 2 * j + 1, j > 0);
@@ -686,7 +702,8 @@ template <typename T, bool E, int D> __device__ __forceinline__ void product_rol
             if (j + 1 < most) done(it + 2 * j + 2);
             if (j + 2 == most) commit(kBarQEmpty);
         }
-        it += 2 * most;
+        it += 2 * most, on = true;
+    next:;
     }
     // Nothing is under way when TMEM is given back.
     commit(kBarDrain);
@@ -730,10 +747,9 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
     using M = std::conditional_t<E, __half, T>;
     const int x = threadIdx.x / kQ, q = threadIdx.x % kQ, qq = x * a.tile_q + q;  // tile, query of the tile, of the unit
     const uint32_t lane = tmem + ((uint32_t)(q / 32 * 32) << 16), st = lane + x * kKeys, ot = lane + 2 * kKeys + x * D;
-    uint32_t ns = 0, no = 0, ts = 0, units = 0;
-    for (;; units++) {
-        const Unit &u = sh.unit(units);
-        if (!u.n) break;
+    uint32_t ns = 0, no = 0, ts = 0, joins = 0, units = 0;
+    for (; const Unit *now = sh.unit(units); units++) {
+        const Unit &u = *now;
         const int n = x ? u.nb : u.na;
         const bool there = q < a.tile_q && qq < u.queries;
         const uint32_t flat = (uint32_t)(u.q0 + (there ? qq : 0)), tok = wf_quot(flat, a.by_group);
@@ -751,17 +767,19 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
         for (int j = 0; j < n; j++) {
             float s[kKeys];
             uint32_t *w = reinterpret_cast<uint32_t *>(s);
-            sh.wait(kBarS + x, ns & 1);
+            if (!sh.wait(kBarS + x, ns & 1)) return;
             ns++;
             after_sync();
 #pragma unroll
             for (int i = 0; i < 4; i++) tm_load(w + 32 * i, st + 32 * i);
             const float *sc = nullptr;
+            bool on = true;
             if constexpr (E) {
-                sh.wait(kBarScale + ts % kSlots, ts / kSlots & 1);
+                on = sh.wait(kBarScale + ts % kSlots, ts / kSlots & 1);
                 sc = sh.scales + ts % kSlots * 3 * kFours;
             }
             tm_loaded();
+            if (!on) return;
             if constexpr (E) {
 #pragma unroll
                 for (int i = 0; i < kFours; i += 4) {
@@ -841,11 +859,11 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
         }
         if constexpr (E)  // tiles that this one does not see
             for (int j = n; j < u.n; j++, ts++) {
-                sh.wait(kBarScale + ts % kSlots, ts / kSlots & 1);
+                if (!sh.wait(kBarScale + ts % kSlots, ts / kSlots & 1)) return;
                 warp_arrive(sh.bar(kBarScale + kSlots + ts % kSlots));
             }
         if (n > 0) {
-            sh.wait(kBarO + x, no & 1);
+            if (!sh.wait(kBarO + x, no & 1)) return;
             no++;
             after_sync();
         }
@@ -878,17 +896,21 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
         if (u.parts > 1) {
             __stcg(part + kPair * D + at, ref);
             __stcg(part + kPair * (D + 1) + at, sum);
+            // The eight warps' parts are there; then one thread's answer.  Each warp reads it before it comes to the next join.
             __threadfence();
-            sync_some<2, 256>();
-            if (threadIdx.x == 0) {
-                const bool last = atomicAdd(a.arrive + u.first, 1u) == (uint32_t)u.parts - 1;
-                if (last) a.arrive[u.first] = 0;
-                *last_one = last;
+            warp_arrive(sh.bar(kBarJoin));
+            if (threadIdx.x < 32) {
+                if (!sh.wait(kBarJoin, joins & 1)) return;
+                if (threadIdx.x == 0) {
+                    const bool last = atomicAdd(a.arrive + u.first, 1u) == (uint32_t)u.parts - 1;
+                    if (last) a.arrive[u.first] = 0;
+                    *last_one = last;
+                    bar_arrive(sh.bar(kBarLast));
+                }
             }
-            sync_some<2, 256>();
-            const bool last = *last_one;
-            sync_some<2, 256>();
-            if (last) {  // the parts together, in their order
+            if (!sh.wait(kBarLast, joins & 1)) return;
+            joins++;
+            if (*last_one) {  // the parts together, in their order
                 __threadfence();
                 auto part_of = [&](int i) { return a.part + (2 * (int64_t)(u.first + i) + (i == 0)) * kPart<D>; };
                 float top = -INFINITY, all = 0.f;
@@ -933,16 +955,15 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
     });
     if (f.r >= a.rows) return;
     if (smem_of(raw) % 1024) {  // the swizzle's patterns would not lie as the products read them
-        if (threadIdx.x == 0) *a.err = 2;
+        if (threadIdx.x == 0) a.err[1] = 1;
         return;
     }
     Shared sh;
     sh.q = raw;
     sh.kv = sh.q + S::kQBytes;
     sh.raw = sh.kv + S::kStages * S::kTile;
-    sh.offset = reinterpret_cast<int64_t *>(sh.raw + S::kRawBytes);
-    sh.scales = reinterpret_cast<float *>(sh.offset);  // 8 bits have no use for the other
-    sh.units = units, sh.bars = smem_of(bars), sh.gave_up = &gave_up, sh.err = a.err;
+    sh.scales = reinterpret_cast<float *>(sh.raw + S::kRawBytes);
+    sh.units = units, sh.bars = smem_of(bars), sh.polls = pa.polls, sh.hint = pa.hint, sh.gave_up = &gave_up, sh.err = a.err;
     const int warp = threadIdx.x / 32;
     if (threadIdx.x == 0) {
         gave_up = 0;
@@ -954,7 +975,7 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
             if (i >= kBarFull && i < kBarFull + 8) n = E || !pa.box ? 4 : 1;
             if (i >= kBarUnit + kUnits && i < kBarUnit + 2 * kUnits) n = 8 + 1 + (loaders ? 4 : 0) + (boxes ? 1 : 0) + (E ? 1 : 0);
             if (i >= kBarRaw + kRaws && i < kBarScale) n = 4;
-            if (i >= kBarScale + kSlots) n = 8;
+            if (i >= kBarScale + kSlots && i <= kBarJoin) n = 8;
             bar_init(sh.bar(i), n);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -1028,7 +1049,7 @@ template <typename T, bool E, int D> int launch(const wf_attn *at, const AttendA
 {
     PromptArgs pa{};
     AttendArgs &a = pa.a;
-    a = args;
+    a = args, pa.polls = at->polls, pa.hint = at->polls ? 1000 : 0;
     const auto half = std::is_same_v<T, __half> ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     // Boxes of positions of one block, in whole rows of eight of the swizzle: the largest power of two up to 128 that divides a block, from 8
     // on.  A box is one request, [position / 8][64 elements' group][position % 8][64 elements], since requests are what the copies cost: with one

@@ -29,7 +29,7 @@ EXPORTS = ("wf_problem_check", "wf_ctx_create", "wf_forecast_readiness", "wf_eva
            "wf_ctx_set_batch", "wf_eval_topk_host", "wf_ctx_reserve_host",
            "wf_decode_create", "wf_decode_status", "wf_decode_destroy", "wf_kv_extend", "wf_beam_select",
            "wf_kv_reorder", "wf_kv_write", "wf_kv_copy_scales",
-           "wf_attn_create", "wf_attn_status", "wf_attn_destroy", "wf_attend")
+           "wf_attn_create", "wf_attn_status", "wf_attn_limit_waits", "wf_attn_destroy", "wf_attend")
 
 
 class WfError(RuntimeError):
@@ -172,6 +172,7 @@ def load_library():
         "wf_kv_write": ([p, p, p, p, p, p, p], ctypes.c_int),
         "wf_attn_create": ([p, ctypes.c_int, p], ctypes.c_int),
         "wf_attn_status": ([p, p], ctypes.c_int),
+        "wf_attn_limit_waits": ([p, i32], ctypes.c_int),
         "wf_attn_destroy": ([p], None),
         "wf_attend": ([p, p, p, p, p, p], ctypes.c_int),
         "wf_kv_copy_scales": ([p, p, p, p, i32, i64, i32, p], ctypes.c_int),
@@ -919,6 +920,11 @@ class Attn:
 
 def wf_attn_status(attn: Attn, stream=None):
     _check(load_library().wf_attn_status(attn.ptr, _stream_handle(stream, attn.device)), "wf_attn_status")
+
+
+def wf_attn_limit_waits(attn: Attn, polls: int = 1 << 20):
+    """Polls after which a wait of later calls gives up (diagnostic; 0: the first that finds nothing)."""
+    _check(load_library().wf_attn_limit_waits(attn.ptr, polls), "wf_attn_limit_waits")
 
 
 def wf_attend(attn: Attn, kv: Kv, step: KvStep, layer: KvLayer, q, out, scale: float | None = None, new: int = 0, stream=None):

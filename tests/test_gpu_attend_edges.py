@@ -43,3 +43,35 @@ def test_blocks_that_no_box_fits_again_and_again(bs, kv, dim):
     check(st, cache, None, q, first)
     for _ in range(30):
         assert torch.equal(first, attend(wf, st, cache, None, q, attn=attn))
+
+
+@pytest.mark.parametrize("eight,dtype,bs,heads", [(False, "bfloat16", 16, 4), (False, "float16", 100, 4), (False, "bfloat16", 64, 130), (True, "float16", 16, 4),
+                                                  (True, "bfloat16", 64, 4)], ids=("boxes", "no-boxes", "large-group", "8-half", "8-bfloat"))
+def test_waits_that_run_out(eight, dtype, bs, heads):
+    """A call whose waits give up, at the first or some later one, comes to its end and says so; the next one on the same scratch is right."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(56)
+    st = Step(wf, rng, [3000, 0, 40], [300, 700, 65], bs, spare=2)
+    cache, scale = cache_of(rng, st, 1, 64, layer_type(eight, dtype))
+    q = tensor(rng, (st.room, heads, 64), dtype)
+    want = attend(wf, st, cache, scale, q)
+    attn = wf.Attn(max_rows=3, heads=heads, dim=64)
+    layer, out = wf.KvLayer(cache[0], cache[1], *(() if scale is None else (scale[0], scale[1]))), torch.full_like(q, 7.0)
+    for polls in (0, 0, 1, 2, 4, 8):
+        wf.wf_attn_limit_waits(attn, polls)
+        for _ in range(2):
+            wf.wf_attend(attn, st.kv, st.step, layer, q, out)
+        try:
+            wf.wf_attn_status(attn)
+            assert polls
+        except wf.WfError as e:
+            assert e.code == wf.WF_ETIMEOUT
+        wf.wf_attn_status(attn)  # reported once
+        assert (out[st.tokens:] == 7).all()
+        wf.wf_attn_limit_waits(attn)
+        for _ in range(2):
+            assert torch.equal(attend(wf, st, cache, scale, q, attn=attn), want)
+    for bad in (-1, (1 << 20) + 1):
+        with pytest.raises(wf.WfError):
+            wf.wf_attn_limit_waits(attn, bad)
