@@ -22,7 +22,7 @@
 // 64 rows behind 9,000 tokens (32 / 8 heads of 128) take 333 us, 6.9 TB/s; 128 rows over 8 bits 404 us, 5.6 TB/s of the same bytes: there
 // the conversions take half the issue slots.  The walk along the line is one thread's, in shared memory, since registers are what the
 // kernels over 8 bits run short of.
-// Weights are rounded to the values' type for the second product (2^-9 relative in bfloat16, where a second
+// Weights are rounded to the values' type for the second product (by 2^-12 relative in half floats, 2^-9 in bfloat16, where a second
 // product takes the remainder: below 2^-17 then), sums of weights are not.
 #include <algorithm>
 #include <type_traits>
@@ -180,6 +180,9 @@ template <typename T, bool E, int D> struct Kernel {
     using M = std::conditional_t<E, __half, T>;  // of the products
     static constexpr int kSteps = D / 16, kTiles = D / 8;
     static constexpr bool kTwice = !E && std::is_same_v<T, __nv_bfloat16>;
+    // Weights in half floats reach up to 2^15 in place of 1, sums of them likewise: so what is 2^-40 of the largest still counts (2^-25 else, and many
+    // keys behind one that has most of the weight would be lost in the result, not in the sum).
+    static constexpr float kLift = std::is_same_v<M, __half> ? 15.f : 0.f;
 
     float o[kTiles][4], m[2], l[2];
     uint32_t q[kSteps][4];
@@ -330,7 +333,7 @@ template <typename T, bool E, int D> struct Kernel {
         for (int t = 0; t < 2; t++)
 #pragma unroll
             for (int i = 0; i < 2; i++) {
-                const float ref = m[i] == -INFINITY ? 0.f : m[i];  // nothing seen yet
+                const float ref = m[i] == -INFINITY ? 0.f : m[i] - kLift;  // nothing seen yet
                 const float a = power(x[t][2 * i] - ref), b = power(x[t][2 * i + 1] - ref);
                 l[i] += E ? fmaf(a, inv[t].x, b * inv[t].y) : a + b;
                 w[2 * t + i] = wf_pair<M>::of_float(a, b);

@@ -41,6 +41,7 @@ constexpr int kLoaders = 128;
 constexpr int kRaws = 3;                  // at most
 constexpr int kFours = kKeys / 4, kSlots = 4;  // scales of a tile; tiles whose scales are held
 constexpr float kSlack = 8.f;             // log2 of what a maximum may grow by before O is shrunk
+constexpr float kLift = 15.f - kSlack;    // log2 of a half weight at the reference: half floats reach to 2^16, and what is 2^-32 of the reference still counts
 constexpr float kLeastScale = 0x1p-64f;
 
 template <bool E, int D> struct Shape {
@@ -805,7 +806,7 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
             float2 sums[2];
             const float2 by = make_float2(scale, scale);
             auto powers = [&](int half) {  // of 64 scores, packed in place
-                const float base = ref == -INFINITY ? 0.f : ref;
+                const float base = ref == -INFINITY ? 0.f : std::is_same_v<M, __half> ? ref - kLift : ref;
                 const float2 off = make_float2(-base, -base);
 #pragma unroll
                 for (int i = half * kKeys / 2; i < (half + 1) * kKeys / 2; i += 2) {

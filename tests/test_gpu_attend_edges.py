@@ -29,6 +29,34 @@ def test_scales(have, add, scaling, dtype, eight):
     check(st, cache, scale, q, attend(wf, st, cache, scale, q, scaling=scaling, new=1), scaling)
 
 
+@EIGHT
+@pytest.mark.parametrize("n,value", [(200, 96), (60_000, 1)])
+@pytest.mark.parametrize("add", (1, 40), ids=("few", "many"))
+def test_the_tail_behind_one_key(add, n, value, eight):
+    """The first key has nearly all the weight and a value of 0: what is left are n weights of 2^-26 of it.
+
+    Weights in half floats lie 2^-24 apart below 2^-14, and the largest is 2^7 at least, so that each is off by 2^-25 of 2^7 at most, or by half a
+    step; a score of 26 (in base 2) is off by 26 * 2^-23, sums of 60,000 by 2^-16 at most."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(52)
+    st = Step(wf, rng, [n], [add], 16)
+    cache = torch.zeros((2, st.n_blocks, 16, 1, 64), dtype=torch.float16, device="cuda")
+    cache[1] = value
+    first = int(st.table[0, 0])
+    cache[0, first, 0, 0, 0], cache[1, first, 0] = 36, 0
+    scale = torch.ones((2, st.n_blocks, 1), device="cuda") if eight else None
+    if eight:
+        cache = cache.to(torch.float8_e4m3fn)
+    q = torch.zeros((add, 2, 64), dtype=torch.float16, device="cuda")
+    q[:, :, 0] = 4
+    rest = (n + np.arange(add)) * np.exp(-18.0)  # 4 * 36 / 8
+    want = value * (rest / (1 + rest))[:, None, None]
+    got = f64(attend(wf, st, cache, scale, q))
+    least = 2.0 ** -32 * (n + add) * value
+    assert (np.abs(got - want) <= want * (2 * HALF_STEP["float16"] + 26 * 2.0 ** -22 + 2.0 ** -15) + least * (1 + 2.0 ** -8)).all()
+
+
 @pytest.mark.parametrize("bs,kv,dim", [(7, 2, 64), (100, 1, 128), (1, 2, 64), (30, 4, 128)])
 def test_blocks_that_no_box_fits_again_and_again(bs, kv, dim):
     """Prompts over blocks whose positions are copied one by one (no multiple of 8): many tiles under way, every call the same."""
