@@ -832,7 +832,7 @@ typedef struct {
  * token (decoding), with a prompt's chunk and with a whole prompt may be in one step, in any order.
  * Rows without new tokens have no output, and places of out behind the step's last
  * token are left as they were.  What the cache holds behind a row's tokens does not count, whatever
- * it is.  A value of the row's step that is no finite number may reach the outputs of all its tokens in the step.
+ * it is.  A value that is no finite number makes its element infinite or NaN in the outputs of the tokens that see it, and in no others.
  * Tables of a row name blocks of the cache; one that does not is read as block 0 and reported by wf_attn_status, as are
  * rows whose lengths contradict each other (fewer tokens than new ones, more than the table holds, more than the step), which are passed over.
  * The result does not depend on the order of arrival of the GPU's blocks; the last bits of a row's

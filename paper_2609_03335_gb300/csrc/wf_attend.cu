@@ -175,8 +175,16 @@ __device__ __forceinline__ void next_part(const AttendArgs &a, Walk &w, Part &p)
     p.u = u;
 }
 
+// By warp: whether it has taken a value that is no finite number out of its part of the unit.
+__device__ __forceinline__ volatile int *unfit_flags()
+{
+    __shared__ volatile int flags[kWarps];
+    return flags;
+}
+
 template <typename T, bool E, int D> struct Kernel {
     using S = Shape<E, D>;
+    using V = std::conditional_t<E, __nv_fp8_e4m3, T>;  // of the cache
     using M = std::conditional_t<E, __half, T>;  // of the products
     static constexpr int kSteps = D / 16, kTiles = D / 8;
     static constexpr bool kTwice = !E && std::is_same_v<T, __nv_bfloat16>;
@@ -261,9 +269,26 @@ template <typename T, bool E, int D> struct Kernel {
         return block_at(a, u.table, wf_quot(min(p + lane % kSlice, u.end - 1), a.by_bs));
     }
 
-    __device__ __forceinline__ void slice(const Unit &u, const uint8_t *buf, uint32_t stage, int32_t p, int lane)
+    // Values from `from` on of a stage, which some queries do not see: what is no finite number becomes 0, and add_unfit's.
+    __device__ __forceinline__ void take_unfit(uint8_t *buf, int from, int lane)
+    {
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < S::kChunks / 2; i++) {
+            const int id = 32 * i + lane, key = id / S::kChunks, c = id % S::kChunks;
+            if (key < from) continue;
+            uint4 *at = reinterpret_cast<uint4 *>(buf + kSlice * S::kRow + place<S::kRow>(key, c));
+            const uint4 x = *at;
+            if (wf_unfit<V>(x)) *at = wf_fit<V>(x), found = true;
+        }
+        if (found) unfit_flags()[threadIdx.x / 32] = 1;
+        __syncwarp();
+    }
+
+    __device__ __forceinline__ void slice(const Unit &u, uint8_t *buf, uint32_t stage, int32_t p, int lane)
     {
         const int c = lane % 4;
+        if (p + kSlice > u.full && u.full < u.end) take_unfit(buf, u.full - p, lane);
         float x[2][4] = {};
         if (!E) {
             const int key = lane / 16 * 8 + lane % 8, odd = lane / 8 % 2;
@@ -481,6 +506,10 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
         const Unit u = s_part.u;
         if (!u.queries) break;
         uint8_t *buf = smem + warp * S::kWarpBytes;
+        if (u.full < u.end) {
+            if (lane == 0) unfit_flags()[warp] = 0;
+            __syncwarp();
+        }
         {
             Kernel<T, E, D> k;
             k.run(a, u, buf, warp, lane);
@@ -507,6 +536,12 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
                 sum += g * s_l[w][q];
                 x[0] += g * y.x, x[1] += g * y.y, x[2] += g * y.z, x[3] += g * y.w;
                 x[4] += g * z.x, x[5] += g * z.y, x[6] += g * z.z, x[7] += g * z.w;
+            }
+            static_assert(kWarps == 4, "the flags");
+            if (volatile int *f = unfit_flags(); u.full < u.end && (f[0] | f[1] | f[2] | f[3])) {
+                const int32_t seen = u.row.len - u.row.n + (int32_t)wf_quot((uint32_t)(u.q0 + q), a.by_group) + 1;
+                using V = typename Kernel<T, E, D>::V;
+                add_unfit<V>(a, u.table, a.v + u.head * a.head_stride + e * (int)sizeof(V), max(u.begin, u.full), min(u.end, seen), x);
             }
             if (n == 1) {
                 const float inv = 1.f / sum;

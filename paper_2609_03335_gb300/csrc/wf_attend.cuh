@@ -198,6 +198,37 @@ __device__ __forceinline__ int32_t block_at(const AttendArgs &a, const int32_t *
     return 0;
 }
 
+// A weight of 0 does not undo a value that is no finite number.  So where some queries of a tile see a position and others do not, such values are taken
+// out of the tile's products, and added here for the queries that do: positions begin .. end - 1, of N elements of the values v of type V, to x.  Their
+// weights, whatever they are, leave an infinity what it is, and NaN.
+template <typename V, int N>
+__device__ __forceinline__ void add_unfit(const AttendArgs &a, const int32_t *table, const uint8_t *v, int32_t begin, int32_t end, float (&x)[N])
+{
+#pragma unroll 1
+    for (int32_t p = begin; p < end; p++) {
+        const uint32_t j = wf_quot(p, a.by_bs);
+        const uint8_t *from = v + block_at(a, table, j) * a.block_stride + (p - (int32_t)j * a.bs) * a.token_stride;
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            if constexpr (sizeof(V) == 1) {
+                const uint32_t w = wf_unfit<V>(*reinterpret_cast<const uint32_t *>(from + i));
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+                    if (w >> (8 * k + 7) & 1) x[i + k] = NAN;
+            } else {
+                const uint2 w = *reinterpret_cast<const uint2 *>(from + 2 * i);
+                if (wf_unfit<V>(w.x) | wf_unfit<V>(w.y)) {
+                    const float2 lo = wf_pair<V>::to_float(w.x), hi = wf_pair<V>::to_float(w.y);
+                    const float y[4] = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+                    for (int k = 0; k < 4; k++)
+                        if (!isfinite(y[k])) x[i + k] += y[k];
+                }
+            }
+        }
+    }
+}
+
 int wf_attend_setup(wf_attn *a);
 void wf_attend_scratch(const wf_attn *a, size_t *part_bytes, int *ctas);
 int wf_launch_attend(wf_attn *at, const AttendArgs &args, int dtype, int dim, bool eight, cudaStream_t st);

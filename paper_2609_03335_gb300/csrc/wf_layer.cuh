@@ -56,6 +56,41 @@ __device__ __forceinline__ uint2 wf_e4m3_halves(uint32_t x)
     return r;
 }
 
+// Elements that are no finite numbers, in a word of two or four: their topmost bits.  An exponent of all ones (in E4M3 with a mantissa of all ones) carries into it.
+template <typename T> __device__ __forceinline__ uint32_t wf_unfit(uint32_t x);
+template <> __device__ __forceinline__ uint32_t wf_unfit<__half>(uint32_t x) { return ((x & 0x7C007C00u) + 0x04000400u) & 0x80008000u; }
+template <> __device__ __forceinline__ uint32_t wf_unfit<__nv_bfloat16>(uint32_t x) { return ((x & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
+template <> __device__ __forceinline__ uint32_t wf_unfit<__nv_fp8_e4m3>(uint32_t x) { return ((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
+
+template <typename T> __device__ __forceinline__ uint32_t wf_unfit(const uint4 &x)
+{
+    return wf_unfit<T>(x.x) | wf_unfit<T>(x.y) | wf_unfit<T>(x.z) | wf_unfit<T>(x.w);
+}
+
+// The larger magnitude of both halves each; NaN stays.
+template <typename T> __device__ __forceinline__ uint32_t wf_larger(uint32_t most, uint32_t x);
+template <> __device__ __forceinline__ uint32_t wf_larger<__half>(uint32_t most, uint32_t x)
+{
+    const __half2 r = __hmax2_nan(*reinterpret_cast<__half2 *>(&most), __habs2(*reinterpret_cast<__half2 *>(&x)));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+template <> __device__ __forceinline__ uint32_t wf_larger<__nv_bfloat16>(uint32_t most, uint32_t x)
+{
+    const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<__nv_bfloat162 *>(&most), __habs2(*reinterpret_cast<__nv_bfloat162 *>(&x)));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+
+// The word with 0 in their place.
+template <typename T> __device__ __forceinline__ uint32_t wf_fit(uint32_t x)
+{
+    constexpr int kBits = 8 * sizeof(T);
+    return x & ~((wf_unfit<T>(x) >> (kBits - 1)) * ((1u << kBits) - 1));
+}
+template <typename T> __device__ __forceinline__ uint4 wf_fit(const uint4 &x)
+{
+    return make_uint4(wf_fit<T>(x.x), wf_fit<T>(x.y), wf_fit<T>(x.z), wf_fit<T>(x.w));
+}
+
 // Rounded to nearest, even; beyond 448 to +-448; a in the lower byte.
 __device__ __forceinline__ uint32_t wf_e4m3_of(float a, float b)
 {

@@ -311,8 +311,9 @@ struct Shared {
     uint8_t *q, *kv, *raw; // on 1,024 bytes; raw: tiles in 8 bits as the cache has them
     float *scales;
     uint32_t bars;         // address
-    int polls, hint;
+    int polls, hint, box;  // as in PromptArgs
     volatile int *gave_up;
+    int *unfit;            // the last unit, from 1 on, out of whose products values that are no finite numbers were taken
     int *err;
     __device__ __forceinline__ uint32_t bar(int i) const { return bars + 8 * i; }
     // False: waiting was given up.  wait: every lane of the warp comes, and the answer is one for all.
@@ -435,10 +436,10 @@ template <typename T, bool E, int D> __device__ __forceinline__ void box_role(co
                         const uint8_t *v = a.v + u.head * a.head_stride;
 #pragma unroll 1
                         for (int i = lane / kPer; i < kKeys; i += 32 / kPer) {
-                            const int32_t key = min(p + i, u.row.len - 1);
+                            const int32_t key = min(p + i, end - 1);
                             const uint32_t in = wf_quot(key, a.by_bs);
                             const uint8_t *from = v + block_at(a, table, in) * a.block_stride + (key - (int32_t)in * a.bs) * a.token_stride;
-                            copy16(to + place<D>(i, lane % kPer), from + lane % kPer * 16, p + i < u.row.len);
+                            copy16(to + place<D>(i, lane % kPer), from + lane % kPer * 16, p + i < end);
                         }
                         copies_commit();
                         copies_wait<0>();
@@ -463,6 +464,12 @@ template <typename T, bool E, int D> __device__ __forceinline__ void box_role(co
         for (int k = 0; queries && k < 1 << 16 && !bar_try(sh.bar(kBarQFull), (queries - 1) & 1); k++) {}
     }
     __syncwarp();
+}
+
+// Positions that the first query q of the unit sees.
+__device__ __forceinline__ int32_t seen_by(const AttendArgs &a, const Unit &u, int q)
+{
+    return u.row.len - u.row.n + (int32_t)wf_quot((uint32_t)(u.q0 + q), a.by_group) + 1;
 }
 
 // Warp 15, 8 bits: the scales of each four positions, which lie in one block.
@@ -741,6 +748,50 @@ template <typename T> __device__ __forceinline__ void put(uint8_t *const (&out)[
         if (out[k]) *reinterpret_cast<uint4 *>(out[k] + 2 * i + 16 * c) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
 }
 
+// Values of a tile (halves where the cache has 8 bits) from key `from` on, up to `to`, which some queries of the 128 do not see: what is no finite number becomes 0,
+// and give_unfit's.  A thread looks through a key.  False: waiting was given up.  (Sixteen prompts of 512: 92 -> 96 us.)
+template <typename T, bool E, int D> __device__ __forceinline__ bool take_unfit(const Shared &sh, uint32_t it, int32_t from, int32_t to, uint32_t unit)
+{
+    using S = Shape<E, D>;
+    if (!sh.wait(kBarFull + it % S::kStages, it / S::kStages & 1)) return false;
+    const int key = threadIdx.x % kQ;
+    if (key < from || key >= to) return true;
+    uint8_t *tile = sh.kv + it % S::kStages * S::kTile;
+    auto at = [&](int c) { return reinterpret_cast<uint4 *>(tile + place<D>(key, c)); };
+    uint32_t most[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int c = 0; c < D / 8; c++) {
+        const uint4 y = *at(c);
+        most[0] = wf_larger<T>(most[0], y.x), most[1] = wf_larger<T>(most[1], y.y), most[2] = wf_larger<T>(most[2], y.z), most[3] = wf_larger<T>(most[3], y.w);
+    }
+    if (wf_unfit<T>(make_uint4(most[0], most[1], most[2], most[3]))) {
+        atomicMax(sh.unfit, (int)unit + 1);
+        __threadfence_block();
+#pragma unroll 1
+        for (int c = 0; c < D / 8; c++) *at(c) = wf_fit<T>(*at(c));
+        to_async();
+    }
+    return true;
+}
+
+// What take_unfit took, to a query's output or, where that is null, its sums.
+template <typename T, bool E, int D> __device__ __noinline__ void give_unfit(const AttendArgs &a, const Unit &u, int32_t seen, uint8_t *out, float *sums)
+{
+    using V = std::conditional_t<E, __nv_fp8_e4m3, T>;
+    const int32_t begin = max(seen_by(a, u, 0), u.t0 * kKeys), end = min(seen, (u.t0 + u.n) * kKeys);
+#pragma unroll 1
+    for (int i = 0; i < D; i += 4) {
+        uint32_t *w = reinterpret_cast<uint32_t *>(out + 2 * i);
+        float4 *s = reinterpret_cast<float4 *>(sums) + i / 4 * kPair;
+        const float2 lo = out ? wf_pair<T>::to_float(w[0]) : make_float2(0.f, 0.f), hi = out ? wf_pair<T>::to_float(w[1]) : make_float2(0.f, 0.f);
+        const float4 z = out ? make_float4(lo.x, lo.y, hi.x, hi.y) : __ldcg(s);
+        float y[4] = {z.x, z.y, z.z, z.w};
+        add_unfit<V>(a, a.table + u.r * a.table_stride, a.v + u.head * a.head_stride + i * (int)sizeof(V), begin, end, y);
+        if (out) w[0] = wf_pair<T>::of_float(y[0], y[1]), w[1] = wf_pair<T>::of_float(y[2], y[3]);
+        else __stcg(s, make_float4(y[0], y[1], y[2], y[3]));
+    }
+}
+
 template <typename T, bool E, int D>
 __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh, uint32_t tmem, int *last_one)
 {
@@ -748,14 +799,14 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
     using M = std::conditional_t<E, __half, T>;
     const int x = threadIdx.x / kQ, q = threadIdx.x % kQ, qq = x * a.tile_q + q;  // tile, query of the tile, of the unit
     const uint32_t lane = tmem + ((uint32_t)(q / 32 * 32) << 16), st = lane + x * kKeys, ot = lane + 2 * kKeys + x * D;
-    uint32_t ns = 0, no = 0, ts = 0, joins = 0, units = 0;
+    uint32_t ns = 0, no = 0, ts = 0, joins = 0, units = 0;  // ts: tiles of the CTA, whichever are seen
     for (; const Unit *now = sh.unit(units); units++) {
         const Unit &u = *now;
         const int n = x ? u.nb : u.na;
         const bool there = q < a.tile_q && qq < u.queries;
         const uint32_t flat = (uint32_t)(u.q0 + (there ? qq : 0)), tok = wf_quot(flat, a.by_group);
         const int32_t seen = u.row.len - u.row.n + (int32_t)tok + 1;
-        const int32_t least = u.row.len - u.row.n + (int32_t)wf_quot((uint32_t)(u.q0 + min(u.queries - 1, x * a.tile_q + q / 32 * 32)), a.by_group) + 1;  // of the warp
+        const int32_t least = seen_by(a, u, x * a.tile_q);  // what every query of the 128 sees (no more than that if there are none)
         float scale = a.scale;
         if constexpr (E && std::is_same_v<T, __nv_bfloat16>) {
             const uint4 *p = reinterpret_cast<const uint4 *>(query(a, u, there ? qq : 0));
@@ -766,6 +817,9 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
         }
         float ref = -INFINITY, sum = 0.f;
         for (int j = 0; j < n; j++) {
+            const int32_t p = (u.t0 + j) * kKeys;
+            // Tile A's threads do it for both where A sees the positions: B's product comes after A's.
+            if (p + kKeys > least && (x == 0 || j >= u.na) && !take_unfit<M, E, D>(sh, 2 * ts + 1, least - p, u.seen - p + sh.box, units)) return;
             float s[kKeys];
             uint32_t *w = reinterpret_cast<uint32_t *>(s);
             if (!sh.wait(kBarS + x, ns & 1)) return;
@@ -793,7 +847,6 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
                     }
                 }
             }
-            const int32_t p = (u.t0 + j) * kKeys;
             auto largest_of = [&] {
                 float most[4] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3]), fmaxf(s[4], s[5]), fmaxf(s[6], s[7])};
 #pragma unroll
@@ -854,7 +907,8 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
             tm_stored();
             before_sync();
             warp_arrive(sh.bar(kBarP + x));
-            if constexpr (E) warp_arrive(sh.bar(kBarScale + kSlots + ts++ % kSlots));
+            if constexpr (E) warp_arrive(sh.bar(kBarScale + kSlots + ts % kSlots));
+            ts++;
             sums[0] = add2(sums[0], sums[1]);
             sum += sums[0].x + sums[0].y;
         }
@@ -863,6 +917,8 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
                 if (!sh.wait(kBarScale + ts % kSlots, ts / kSlots & 1)) return;
                 warp_arrive(sh.bar(kBarScale + kSlots + ts % kSlots));
             }
+        else
+            ts += u.n - n;
         if (n > 0) {
             if (!sh.wait(kBarO + x, no & 1)) return;
             no++;
@@ -894,6 +950,10 @@ __device__ __forceinline__ void power_role(const AttendArgs &a, const Shared &sh
             }
         }
         before_sync();
+        if (__any_sync(~0u, n > 0 && *static_cast<volatile int *>(sh.unfit) > (int)units)) {
+            __syncwarp();  // others have written this query's output, too
+            if (there) give_unfit<T, E, D>(a, u, seen, u.parts == 1 ? mine : nullptr, part + 4 * at);
+        }
         if (u.parts > 1) {
             __stcg(part + kPair * D + at, ref);
             __stcg(part + kPair * (D + 1) + at, sum);
@@ -947,7 +1007,7 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
     extern __shared__ __align__(1024) uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[kBars];
     __shared__ uint32_t tmem_at;
-    __shared__ int gave_up, last_one;
+    __shared__ int gave_up, last_one, unfit;
     __shared__ Unit units[kUnits];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     // A stretch is worth six tiles at least, so that only a unit's first and last CTA can find no tile in their part of it.
@@ -964,10 +1024,10 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
     sh.kv = sh.q + S::kQBytes;
     sh.raw = sh.kv + S::kStages * S::kTile;
     sh.scales = reinterpret_cast<float *>(sh.raw + S::kRawBytes);
-    sh.units = units, sh.bars = smem_of(bars), sh.polls = pa.polls, sh.hint = pa.hint, sh.gave_up = &gave_up, sh.err = a.err;
+    sh.units = units, sh.bars = smem_of(bars), sh.polls = pa.polls, sh.hint = pa.hint, sh.box = pa.box, sh.gave_up = &gave_up, sh.unfit = &unfit, sh.err = a.err;
     const int warp = threadIdx.x / 32;
     if (threadIdx.x == 0) {
-        gave_up = 0;
+        gave_up = 0, unfit = 0;
         const bool loaders = E || !pa.box || !pa.map_q, boxes = pa.box || pa.map_q;
         for (int i = 0; i < kBars; i++) {
             uint32_t n = 1;  // a warp arrives once

@@ -103,3 +103,65 @@ def test_waits_that_run_out(eight, dtype, bs, heads):
     for bad in (-1, (1 << 20) + 1):
         with pytest.raises(wf.WfError):
             wf.wf_attn_limit_waits(attn, bad)
+
+
+LATER = [  # have, add, block size, heads, key heads, dim, tokens of the first row whose values are no numbers
+    ([20, 5], [4, 1], 16, 4, 2, 64, (2,)), ([20, 5], [4, 1], 7, 8, 2, 128, (3,)), ([500], [16], 16, 1, 1, 64, (1, 9)),
+    ([300, 0], [200, 90], 16, 8, 2, 128, (70,)), ([60], [600], 16, 2, 2, 64, (127, 130, 400)), ([0], [300], 24, 7, 1, 128, (0, 299)),
+    ([90, 3], [250, 40], 7, 6, 2, 64, (33, 34)), ([5000], [80], 32, 4, 1, 128, (0, 41)), ([3], [70], 16, 130, 1, 64, (50,))]
+
+
+def same(got, want):
+    """Finite numbers alike, and the others in the same places."""
+    import torch
+    fine = want.isfinite()
+    return torch.equal(got.isfinite(), fine) and torch.equal(got[fine], want[fine])
+
+
+@EIGHT
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("have,add,bs,heads,kv,dim,at", LATER, ids=range(len(LATER)))
+def test_a_value_reaches_no_earlier_token(have, add, bs, heads, kv, dim, at, dtype, eight):
+    """Values that are infinite or no numbers reach the outputs of their token and those behind it, in their element and of their head, and no others.
+    (Infinite or no number: the second product of attend_kernel in bfloat16 takes a weight's remainder, and 0 times an infinity is no number.)"""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(53)
+    st = Step(wf, rng, have, add, bs, spare=2)
+    cache, scale = cache_of(rng, st, kv, dim, layer_type(eight, dtype))
+    q = tensor(rng, (st.room, heads, dim), dtype, 0.5)
+    for new in (0, 1):
+        want = attend(wf, st, cache, scale, q, new=new)
+        assert want.isfinite().all()
+        for bad in ((float("nan"),) if eight else (float("inf"), float("-inf"), float("nan"))):
+            held, expect = cache.clone(), want.clone()
+            for i, token in enumerate(at):
+                p, head, d = have[0] + token, i % kv, (5 + 9 * i) % dim
+                block, place = int(st.table[0, p // bs]), p % bs
+                if eight:
+                    held.view(torch.uint8)[1, block, place, head, d] = 0xFF
+                else:
+                    held[1, block, place, head, d] = bad
+                group = heads // kv
+                expect[token:add[0], head * group:(head + 1) * group, d] = bad
+            assert same(attend(wf, st, held, scale, q, new=new), expect), (new, bad)
+
+
+def test_infinities_of_both_signs_and_whole_values():
+    """An infinity of each sign in one element make NaN from the later one on; a token whose whole value is infinite leaves those before it alone."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(54)
+    for add, new in ((4, 0), (150, 0), (150, 1)):
+        st = Step(wf, rng, [33], [add], 16)
+        cache, _ = cache_of(rng, st, 1, 64, "bfloat16")
+        q = tensor(rng, (add, 2, 64), "bfloat16", 0.5)
+        expect = attend(wf, st, cache, None, q, new=new)
+        first, second, whole = add // 4, add // 2, add - 1
+        put = lambda token: cache[1, int(st.table[0, (33 + token) // 16]), (33 + token) % 16, 0]
+        put(first)[7], put(second)[7] = float("inf"), float("-inf")
+        put(whole)[:] = float("inf")
+        expect[first:second, :, 7] = float("inf")
+        expect[whole] = float("inf")
+        expect[second:, :, 7] = float("nan")
+        assert same(attend(wf, st, cache, None, q, new=new), expect)
