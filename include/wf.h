@@ -816,7 +816,8 @@ typedef struct {
     int32_t new_tokens;  /* the most new tokens that a row is expected to have, 0: unknown.  A hint: it chooses how
                             the call is launched (1 for a step of decoding), never what it computes */
     const void *q;       /* [max_tokens][heads][dim] */
-    void *out;           /* [max_tokens][heads][dim], apart from every input */
+    void *out;           /* [max_tokens][heads][dim], apart from every input (queries are read while outputs are written: not in place);
+                            where it lies among the queries, as other columns of one product, with their strides */
     int64_t q_token, q_head;
     int64_t out_token, out_head;
 } wf_attn_in;

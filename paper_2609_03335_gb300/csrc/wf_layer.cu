@@ -196,6 +196,24 @@ static int check_attn(const void *p, int64_t token, int64_t head, const char *wh
     return WF_OK;
 }
 
+// Whether queries and outputs have bytes in common.  Tensors that lie among each other (two parts of one product's columns) need the same strides
+// to be told apart; others have to have ranges of their own.
+static bool meet(const wf_attn_in &in, int64_t tokens, int64_t bytes)
+{
+    const int64_t n = tokens - 1, m = in.heads - 1;
+    auto low = [&](int64_t token, int64_t head) { return n * std::min<int64_t>(token, 0) + m * std::min<int64_t>(head, 0); };
+    auto high = [&](int64_t token, int64_t head) { return n * std::max<int64_t>(token, 0) + m * std::max<int64_t>(head, 0) + bytes; };
+    const int64_t apart = (const uint8_t *)in.out - (const uint8_t *)in.q;
+    if (apart + low(in.out_token, in.out_head) >= high(in.q_token, in.q_head) || apart + high(in.out_token, in.out_head) <= low(in.q_token, in.q_head)) return false;
+    if ((n && in.q_token != in.out_token) || (m && in.q_head != in.out_head)) return true;
+    for (int64_t j = -m; j <= m; j++) {  // heads apart; then the token that lies nearest
+        const int64_t at = apart + j * in.q_head, i = in.q_token ? std::clamp(-at / in.q_token, -n, n) : 0;
+        for (int64_t k = std::max(-n, i - 1); k <= std::min(n, i + 1); k++)
+            if (std::abs(at + k * in.q_token) < bytes) return true;
+    }
+    return false;
+}
+
 extern "C" int wf_attend(wf_attn *at, const wf_kv *kv, const wf_kv_step *step, const wf_kv_layer *layer, const wf_attn_in *in, void *stream)
 {
     const char *what = "wf_attend";
@@ -215,7 +233,9 @@ extern "C" int wf_attend(wf_attn *at, const wf_kv *kv, const wf_kv_step *step, c
     REQUIRE(step->start && step->len && wf_aligned(step->start, 4) && wf_aligned(step->len, 4), "%s: NULL or misaligned start or len", what);
     rc = check_attn(in->q, in->q_token, in->q_head, what, "queries");
     if (!rc) rc = check_attn(in->out, in->out_token, in->out_head, what, "outputs");
-    if (!rc) rc = wf_cuda_check(cudaSetDevice(at->device), "cudaSetDevice");
+    if (rc) return rc;
+    REQUIRE(!meet(*in, step->max_tokens, 2 * layer->dim), "%s: outputs in the queries' memory", what);
+    rc = wf_cuda_check(cudaSetDevice(at->device), "cudaSetDevice");
     if (rc) return rc;
 
     AttendArgs a{};

@@ -929,7 +929,7 @@ def wf_attn_limit_waits(attn: Attn, polls: int = 1 << 20):
 
 def wf_attend(attn: Attn, kv: Kv, step: KvStep, layer: KvLayer, q, out, scale: float | None = None, new: int = 0, stream=None):
     """Causal attention of a step's tokens over their rows' cached keys and values (the step's own among them): q, out
-    [max_tokens, heads, dim] in float16 or bfloat16, tokens and heads strided by multiples of 16 bytes.
+    [max_tokens, heads, dim] in float16 or bfloat16, tokens and heads strided by multiples of 16 bytes; out apart from every input (not in place).
     scale: of the products (None: dim^-0.5); new: the most new tokens that a row is expected to have, a hint for the
     launch (1: a step of decoding; 0: unknown)."""
     _check_layer("wf_attend", kv, step, layer, attn)

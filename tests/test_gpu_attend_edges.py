@@ -165,3 +165,22 @@ def test_infinities_of_both_signs_and_whole_values():
         expect[whole] = float("inf")
         expect[second:, :, 7] = float("nan")
         assert same(attend(wf, st, cache, None, q, new=new), expect)
+
+
+def test_outputs_in_the_queries_memory_are_refused():
+    """In place, a head or a token further on, with other strides; two parts of one product's columns are apart."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(57)
+    st = Step(wf, rng, [40, 3], [1, 30], 16)
+    cache, _ = cache_of(rng, st, 2, 64, "float16")
+    layer, attn = wf.KvLayer(cache[0], cache[1]), wf.Attn(max_rows=2, heads=4, dim=64)
+    whole = torch.cat([tensor(rng, (st.room + 1, 4, 64), "float16"), torch.full((st.room + 1, 4, 64), 7.0, dtype=torch.float16, device="cuda")], 1)
+    q = whole[:-1, :4]
+    was = whole.clone()
+    for out in (q, whole[:-1, 1:5], whole[:-1, 3:7], whole[1:, :4], whole.view(-1, 4, 64)[:st.room], whole.view(-1, 4, 64)[1:st.room + 1]):
+        with pytest.raises(wf.WfError, match="queries' memory"):
+            wf.wf_attend(attn, st.kv, st.step, layer, q, out)
+    assert torch.equal(whole, was)
+    check(st, cache, None, q.contiguous(), attend(wf, st, cache, None, q, out=whole[:-1, 4:]))
+    assert torch.equal(whole[:, :4], was[:, :4])
