@@ -729,9 +729,10 @@ class KvMoves:
 def _check_scales(scale, kv: Kv):
     import torch
     if not (isinstance(scale, torch.Tensor) and scale.dtype is torch.float32 and scale.get_device() == kv.device and scale.dim() == 3
-            and scale.is_contiguous() and scale.size(1) == kv.n_blocks and scale.numel()):
+            and scale.is_contiguous() and scale.size(1) == kv.n_blocks and scale.numel() and scale.size(2) <= 1024
+            and scale.size(0) * scale.size(2) < 1 << 31):
         what = f"{scale.dtype} {tuple(scale.shape)} on {scale.device}" if isinstance(scale, torch.Tensor) else type(scale).__name__
-        raise WfError(WF_EINVAL, "scale", f"is {what}; expected contiguous float32 [planes, {kv.n_blocks}, heads] on cuda:{kv.device}")
+        raise WfError(WF_EINVAL, "scale", f"is {what}; expected contiguous float32 [planes, {kv.n_blocks}, heads] of up to 1024 heads on cuda:{kv.device}")
 
 
 def wf_kv_copy_scales(decode: Decode, kv: Kv, copies, scale, stream=None):

@@ -184,3 +184,17 @@ def test_outputs_in_the_queries_memory_are_refused():
     assert torch.equal(whole, was)
     check(st, cache, None, q.contiguous(), attend(wf, st, cache, None, q, out=whole[:-1, 4:]))
     assert torch.equal(whole[:, :4], was[:, :4])
+
+
+def test_a_reordering_whose_scales_are_refused_changes_nothing():
+    """Scales that wf_kv_copy_scales would not take are refused before the rows are reordered."""
+    import torch
+    wf = lib()
+    dec, rows, moves = wf.Decode(max_rows=2, max_row_blocks=4), wf.Kv.empty(2, 4, 8, 20), wf.KvMoves(2)
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    wf.wf_kv_extend(dec, rows, dev([21, 3]), wf.KvStep(2, 24, rows))
+    was = rows.table.clone(), rows.len.clone()
+    for scale in (torch.ones((2, 20, 1025), device="cuda"), torch.ones((2, 19, 4), device="cuda"), torch.ones((2, 20, 4), device="cuda").half()):
+        with pytest.raises(wf.WfError):
+            wf.wf_kv_reorder(dec, rows, 2, dev([1, 0]), rows, moves, scale=scale)
+        assert torch.equal(rows.table, was[0]) and torch.equal(rows.len, was[1])
