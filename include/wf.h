@@ -708,7 +708,7 @@ typedef struct {
     int64_t block_stride;  /* bytes, and the next two: multiples of 16, >= 0 */
     int64_t token_stride;
     int64_t head_stride;
-    float *k_scale;        /* [n_blocks][heads], and v_scale: WF_E4M3 only, else NULL; numbers >= 0, of values 2^-64..2^63 (or 0) */
+    float *k_scale;        /* [n_blocks][heads], and v_scale: WF_E4M3 only, else NULL; numbers >= 0, of values 2^-64..2^63 (wf_attend takes one of 0 for 2^-64) */
     float *v_scale;
 } wf_kv_layer;
 

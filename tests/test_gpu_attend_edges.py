@@ -198,3 +198,162 @@ def test_a_reordering_whose_scales_are_refused_changes_nothing():
         with pytest.raises(wf.WfError):
             wf.wf_kv_reorder(dec, rows, 2, dev([1, 0]), rows, moves, scale=scale)
         assert torch.equal(rows.table, was[0]) and torch.equal(rows.len, was[1])
+
+
+JOINS = [([40_000], [1], 8, 1, 128, 1), ([20_000, 7, 9_000], [1, 1, 2], 6, 2, 64, 0), ([20_000], [40], 8, 1, 64, 0), ([9_000, 30], [500, 2], 4, 2, 128, 0)]
+
+
+
+
+@EIGHT
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("have,add,heads,kv,dim,new", JOINS, ids=("decode", "few", "many", "long"))
+def test_every_tile_counts_once(have, add, heads, kv, dim, new, dtype, eight):
+    """Equal scores, and values of 1 in one element for each 64 positions: an element is the share of the positions whose value it has.  No element has more than
+    six such tiles, so that one that is lost, doubled or stale moves its element by a seventh at least.
+
+    Weights are equal powers of two, their sums exact (whole numbers below 2^24 of them), the joins' factors 1; what is left are a division, a product
+    and a rounding."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(58)
+    st = Step(wf, rng, have, add, 16)
+    cache = torch.zeros((2, st.n_blocks, 16, kv, dim), dtype=getattr(torch, dtype), device="cuda")
+    for r, n in enumerate(st.len):
+        p = np.arange(n)
+        slot = torch.from_numpy(st.table[r, p // 16].astype(np.int64) * 16 + p % 16).cuda()
+        one = torch.zeros((n, dim), dtype=cache.dtype, device="cuda")
+        one[torch.from_numpy(p).cuda(), torch.from_numpy(p // 64 % dim).cuda()] = 1
+        cache[1].flatten(0, 1)[slot] = one[:, None]
+    scale = None
+    if eight:
+        cache, scale = cache.to(torch.float8_e4m3fn), torch.ones((2, st.n_blocks, kv), device="cuda")
+    attn = wf.Attn(max_rows=st.rows, heads=heads, dim=dim)
+    q = torch.zeros((st.room, heads, dim), dtype=getattr(torch, dtype), device="cuda")
+    for _ in range(3):
+        got = f64(attend(wf, st, cache, scale, q, new=new, attn=attn))
+        for r, n in enumerate(st.len):
+            for i in range(int(add[r])):
+                seen = have[r] + i + 1
+                want = np.bincount(np.arange(seen) // 64 % dim, minlength=dim) / seen
+                off = np.abs(got[int(st.start[r]) + i] - want)
+                assert (off <= want * (HALF_STEP[dtype] + 2.0 ** -22) + (2.0 ** -25 if dtype == "float16" else 0)).all(), (r, i)
+
+
+@EIGHT
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("have,add,heads,new", [(20_000, 1, 16, 1), (20_000, 40, 8, 0)], ids=("few", "many"))
+def test_one_key_has_all_the_weight(have, add, heads, new, dtype, eight):
+    """The first and the last position of every tile of 64 (few queries) or 128 (many) in turn: each query's own key there has all the weight, and the output
+    is its value, whichever part of the row it lies in.  The other weights are e^-64 of it."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(59)
+    dim, tile = 64, 64 if add == 1 else 128
+    st = Step(wf, rng, [have], [add], 16)
+    n = have + add
+    p = np.arange(n)
+    slot = torch.from_numpy(st.table[0, p // 16].astype(np.int64) * 16 + p % 16).cuda()
+    cache = torch.zeros((2, st.n_blocks, 16, 1, dim), dtype=getattr(torch, dtype), device="cuda")
+    value = torch.from_numpy((p[:, None] * 7 + np.arange(dim) * 3) % 15 - 7).to(cache.dtype).cuda()
+    cache[1].flatten(0, 1)[slot] = value[:, None]
+    scale = torch.ones((2, st.n_blocks, 1), device="cuda") if eight else None
+    attn = wf.Attn(max_rows=1, heads=heads, dim=dim)
+    axis = np.arange(add * heads).reshape(add, heads) % dim  # a query looks along one element
+    q = torch.zeros((add, heads, dim), dtype=cache.dtype, device="cuda")
+    q.scatter_(2, torch.from_numpy(axis).cuda()[..., None], 8.0)
+    spots = np.unique(np.concatenate([np.arange(0, have, tile), np.arange(tile - 1, have, tile), [have - 1]]))
+    most = min(dim, add * heads)
+    for i in range(0, len(spots), most):
+        at = np.resize(spots[i:i + most], most)  # by element
+        held = cache.clone()
+        held[0].flatten(0, 1)[slot[torch.from_numpy(at).cuda()], 0, torch.arange(most, device="cuda")] = 8.0
+        if eight:
+            held = held.to(torch.float8_e4m3fn)
+        got = attend(wf, st, held, scale, q, scaling=1.0, new=new, attn=attn)
+        want = value[torch.from_numpy(at[axis]).cuda()]
+        assert ((got.float() - want.float()).abs() <= 1e-6).all(), at
+
+
+def test_two_scratches_at_once():
+    """Prompts and decoding on two streams from two threads, each with a scratch of its own."""
+    import threading
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(60)
+    work = []
+    for have, add, heads, dim, eight in (([3000, 0, 900], [200, 500, 1], 8, 128, False), ([8000, 40] * 3, [1, 300] * 3, 4, 64, True)):
+        st = Step(wf, rng, have, add, 16)
+        cache, scale = cache_of(rng, st, 2, dim, layer_type(eight, "bfloat16"))
+        layer = wf.KvLayer(cache[0], cache[1], *(() if scale is None else (scale[0], scale[1])))
+        q = tensor(rng, (st.room, heads, dim), "bfloat16")
+        attn = wf.Attn(max_rows=st.rows, heads=heads, dim=dim)
+        work.append((st, layer, q, attn, attend(wf, st, cache, scale, q, attn=attn), torch.cuda.Stream(), [torch.empty_like(q) for _ in range(20)]))
+    torch.cuda.synchronize()
+
+    def run(st, layer, q, attn, want, stream, outs):
+        for out in outs:
+            wf.wf_attend(attn, st.kv, st.step, layer, q, out, stream=stream)
+    threads = [threading.Thread(target=run, args=w) for w in work]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for st, layer, q, attn, want, stream, outs in work:
+        wf.wf_attn_status(attn)
+        assert all(torch.equal(o, want) for o in outs)
+
+
+def odd_scales(rng, scale):
+    """No powers of two, and some 0."""
+    import torch
+    new = torch.from_numpy(rng.uniform(2.0 ** -9, 2.0 ** -5, scale.shape)).float().cuda()
+    new[torch.from_numpy(rng.random(scale.shape) < 0.1).cuda()] = 0
+    return new
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("have,add,new", [([300, 17], [1, 1], 1), ([300, 17], [40, 200], 0)], ids=("few", "many"))
+def test_attention_over_scales_of_any_value(have, add, new, dtype):
+    """A value's scale of 0 counts as 2^-64, a key's as 0."""
+    wf = lib()
+    rng = np.random.default_rng(61)
+    st = Step(wf, rng, have, add, 16, spare=2)
+    cache, scale = cache_of(rng, st, 2, 64, "float8_e4m3fn")
+    scale = odd_scales(rng, scale)
+    q = tensor(rng, (st.room, 4, 64), dtype, 1.5)
+    got = attend(wf, st, cache, scale, q, new=new)
+    least = scale.clone()
+    least[1].clamp_(min=2.0 ** -64)
+    check(st, cache, least, q, got)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kv,bs,have,add", [(2, 16, [5, 16, 0, 31], [1, 3, 20, 1]), (3, 24, [1000, 23, 24], [1, 2, 60]), (1, 64, [10] * 100, [1] * 100)])
+def test_writing_beside_scales_of_any_value(kv, bs, have, add, dtype):
+    """Scales are the larger of what was and a power of two; elements, new ones and those that are scaled anew, are as near as any of their type to what
+    they stand for, but for 2^-22 of a quotient or product in 32 bits; what need not change does not."""
+    import layer_ref as ref
+    wf = lib()
+    rng = np.random.default_rng(62)
+    st = Step(wf, rng, have, add, bs, spare=2)
+    cache, scale = cache_of(rng, st, kv, 64, "float8_e4m3fn")
+    scale = odd_scales(rng, scale) * 4
+    k, v = (tensor(rng, (st.room, kv, 64), dtype, 2.0 ** rng.integers(-4, 6, (st.room, 1, 1))) for _ in range(2))
+    was, want, want_scale = f64(cache), f64(cache), f64(scale)
+    old_scale = want_scale.copy()
+    wf.wf_kv_write(st.decode, st.kv, st.step, wf.KvLayer(cache[0], cache[1], scale[0], scale[1]), k, v)
+    wf.wf_decode_status(st.decode)
+    got, new_scale = f64(cache), f64(scale)
+    for plane, x in enumerate((f64(k), f64(v))):
+        ref.write8(want[plane], want_scale[plane], st.slot, bs, x)
+        assert np.array_equal(new_scale[plane], want_scale[plane])
+        with np.errstate(invalid="ignore"):  # blocks whose scale was 0 and stays so
+            exact = was[plane] * (old_scale[plane] / new_scale[plane])[:, None, :, None]
+        live = st.slot >= 0
+        blocks = st.slot[live] // bs
+        exact.reshape(-1, kv, 64)[st.slot[live]] = x[live] / new_scale[plane][blocks][:, :, None]
+        changed = want[plane] != was[plane]
+        near = np.abs(got[plane] - exact) <= np.abs(want[plane] - exact) + 2.0 ** -22 * np.abs(exact)
+        assert np.where(changed, near, got[plane] == was[plane])[np.isfinite(exact)].all()
