@@ -485,7 +485,7 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
 {
     using S = Shape<E, D>;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ float s_m[kWarps][kSlice], s_l[kWarps][kSlice], s_ref[kSlice], s_sum[kSlice];
+    __shared__ float s_m[kWarps][kSlice], s_l[kWarps][kSlice], s_sum[kSlice];
     __shared__ bool s_last;
     __shared__ Walk s_walk;
     __shared__ Part s_part;
@@ -568,7 +568,6 @@ template <typename T, bool E, int D> __global__ void __launch_bounds__(kThreads,
                 // Part i: that of CTA first + i, the beginning unit's in its second place, the others' in their first.
                 auto part_of = [&](int i) { return a.part + (2 * (int64_t)(first + i) + (i == 0)) * kPart<D>; };
                 float *weight = reinterpret_cast<float *>(smem);  // [n][16]
-                if (threadIdx.x < kSlice) s_ref[threadIdx.x] = -INFINITY;
                 for (int q = warp; q < u.queries; q += kWarps) {
                     float ref = -INFINITY;
                     for (int i = lane; i < n; i += 32) ref = fmaxf(ref, __ldcg(part_of(i) + kSlice * D + q));

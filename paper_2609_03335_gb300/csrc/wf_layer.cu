@@ -11,11 +11,10 @@
 #define REQUIRE(cond, ...) \
     do { if (!(cond)) return wf_set_error(WF_EINVAL, __VA_ARGS__); } while (0)
 
-static int check_step(const wf_kv *kv, const wf_kv_step *step, const char *what)
+static int check_step(const wf_kv_step *step, const char *what)
 {
     REQUIRE(step, "%s: the step is NULL", what);
     REQUIRE(step->max_tokens >= 1 && step->max_tokens <= INT32_MAX - 1, "%s: max_tokens %lld", what, (long long)step->max_tokens);
-    (void)kv;
     return WF_OK;
 }
 
@@ -53,7 +52,7 @@ extern "C" int wf_kv_write(wf_decode *d, const wf_kv *kv, const wf_kv_step *step
     const char *what = "wf_kv_write";
     REQUIRE(d, "NULL decode scratch");
     int rc = wf_check_rows(kv, d->lim.max_rows, what);
-    if (!rc) rc = check_step(kv, step, what);
+    if (!rc) rc = check_step(step, what);
     if (rc) return rc;
     REQUIRE(in, "%s: the tensors are NULL", what);
     rc = check_layer(layer, in->dtype, what);
@@ -219,7 +218,7 @@ extern "C" int wf_attend(wf_attn *at, const wf_kv *kv, const wf_kv_step *step, c
     const char *what = "wf_attend";
     REQUIRE(at, "NULL attention scratch");
     int rc = wf_check_rows(kv, at->lim.max_rows, what);
-    if (!rc) rc = check_step(kv, step, what);
+    if (!rc) rc = check_step(step, what);
     if (rc) return rc;
     REQUIRE(in, "%s: the tensors are NULL", what);
     rc = check_layer(layer, in->dtype, what);

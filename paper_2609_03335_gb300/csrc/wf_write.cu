@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kChunk = 64;   // tokens whose angles shared memory holds at once
-constexpr int kMost16 = 32;  // tokens of a CTA that writes 16 bits or queries
+constexpr int kMost16 = 32;  // tokens of a window over 8 bits and of a CTA that turns queries beside; 16 bits: 8 at most
 constexpr int kMaxHeads = 4; // 8 bits: heads of a CTA
 
 struct WriteArgs {
