@@ -814,7 +814,8 @@ typedef struct {
     int32_t heads;       /* query heads, a multiple of the layer's: head h reads the layer's head h / (heads / layer heads) */
     float scale;         /* of the products, >= 0, usually dim^-0.5; 0 gives the mean of the values that a token sees */
     int32_t new_tokens;  /* the most new tokens that a row is expected to have, 0: unknown.  A hint: it chooses how
-                            the call is launched (1 for a step of decoding), never what it computes */
+                            the call is launched (1 for a step of decoding).  Any value is right for any step; outputs may
+                            differ by the rounding of weights, which the kernels do differently */
     const void *q;       /* [max_tokens][heads][dim] */
     void *out;           /* [max_tokens][heads][dim], apart from every input (queries are read while outputs are written: not in place);
                             where it lies among the queries, as other columns of one product, with their strides */
@@ -829,7 +830,7 @@ typedef struct {
  * head h
  *   out = sum over j <= p of softmax(scale * q . k[j])[j] * v[j]
  * with products and sums in 32 bits; the weights of a sum are rounded to the type of the values that they
- * multiply (over a layer in 8 bits: to 16-bit floats), and out once.  Rows with one new
+ * multiply (over a layer in 8 bits: to 16-bit floats; in bfloat16 for rows with few queries to 16 bits of mantissa), and out once.  Rows with one new
  * token (decoding), with a prompt's chunk and with a whole prompt may be in one step, in any order.
  * Rows without new tokens have no output, and places of out behind the step's last
  * token are left as they were.  What the cache holds behind a row's tokens does not count, whatever

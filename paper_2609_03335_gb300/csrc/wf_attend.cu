@@ -19,7 +19,7 @@
 // times a power of two of their own (exact but for what is 2^-29 of a row's largest element).  A key's scale multiplies its score.
 // A value's scale f_j goes into the weight's exponent, w_j = 2^(x_j + log2 f_j - m), so that the largest
 // weight of an unscaled value is 1 whatever the scales' range; the sum of weights takes w_j / f_j.
-// 64 rows behind 9,000 tokens (32 / 8 heads of 128) take 333 us, 6.9 TB/s; 128 rows over 8 bits 404 us, 5.6 TB/s of the same bytes: there
+// 64 rows behind 9,200 tokens (32 / 8 heads of 128) take 369 us, 6.6 TB/s; 128 rows over 8 bits 425 us, 5.6 TB/s of the same bytes: there
 // the conversions take half the issue slots.  The walk along the line is one thread's, in shared memory, since registers are what the
 // kernels over 8 bits run short of.
 // Weights are rounded to the values' type for the second product (by 2^-12 relative in half floats, 2^-9 in bfloat16, where a second

@@ -174,12 +174,16 @@ extern "C" int wf_attn_limit_waits(wf_attn *a, int32_t polls)
 }
 
 // Queries to a key head (new tokens times the group's heads) up to which a row goes to attend_kernel: one of its tiles.  Two tiles read the
-// row's keys twice: 32 rows of 20 to 32 queries behind 9,000 tokens took 386 us there and 240 in prompt_kernel.
+// row's keys twice: 32 rows of 20 queries (32 / 8 heads of 128, bfloat16) behind 9,000 tokens take 398 us there and 242 in prompt_kernel, 64 rows of 20
+// (16 / 4 heads of 64, halves) behind 3,000 107 us and 99.  Outputs in bfloat16 are further off there, as weights are rounded once: 2.3e-3 of their root mean square
+// at 20 to 32 queries behind 9,000 tokens, 1.7e-3 in attend_kernel (the outputs' own rounding: 1.7e-3).
 constexpr int64_t kFew = 16;
 
 // Cycles of a tile of each kernel on an SM, as measured with full SMs (chunks of 500 behind 2,000 tokens; 161 rows behind 2,000), from which
-// the SMs are shared out where both run.  tile_share: 64 positions' keys and values at 6.7 TB/s and 1.93 GHz.  Over 8 bits instructions bound
-// both kernels, and one after the other is faster (376 us against 387 for chunks of nine prompts beside 51 rows).
+// the SMs are shared out where both run.  tile_share: 64 positions' keys and values at 6.7 TB/s and 1.93 GHz.  Side by side against one after the other,
+// us: 8 chunks of 500 and 161 rows behind 2,000 (28 / 4 heads of 128, bfloat16) 243, 279; the same over blocks that no box fits 298, 307; 12 of 300 and 108 rows
+// behind 2,000 (24 / 8 of 64, bfloat16) 191, 214; 4 of 700 and 96 rows behind 4,000 (32 / 4 of 128, halves) 263, 318.  Over 8 bits instructions bound
+// both kernels, and one after the other is faster: 9 of 700 and 51 rows behind 3,500 (24 / 8 of 64) 378, 351; 4 of 700 and 96 rows behind 4,000 (32 / 8 of 128) 519, 438.
 static void wf_costs(int dim, AttendArgs *a)
 {
     a->pair_cost = dim == 128 ? 4000 : 3000;

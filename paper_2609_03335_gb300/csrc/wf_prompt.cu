@@ -16,10 +16,16 @@
 //
 // In order of issue is in order of execution: S_A(j+1)'s arrival says that PV_A(j) has read P and written O.
 //
-// The products bound it: 64 cycles for each of a pair's 32 (heads of 128), 2,048 a turn of 128 positions, of about 2,900 that a turn takes.
-// One prompt of 16,384 tokens (32 / 8 heads of 128) takes 1.30 ms, 1.69 PFLOP/s, of 8,192 0.37 ms; heads of 64 345 us for 8,192, over
-// 8 bits 820 us, where the conversions of one warp group bound it.  What the products' warp does between two of them counts most: weights
-// handed over in halves, to begin sooner, cost 80 us of 1,420, a lane elected anew each turn 68, a second warp for tile B 280.
+// The products bound it: 64 cycles for each of a pair's 32 (heads of 128), 2,048 a turn of 128 positions, of about 2,950 that a turn takes.
+// One prompt of 16,384 tokens (32 / 8 heads of 128) takes 1.34 ms, 1.65 PFLOP/s, of 8,192 0.38 ms; heads of 64 335 us for 8,192 (the tensor
+// cores at work 36 % of the time: the powers' warps set the turn), over 8 bits 814 us (37 %: the conversions of one warp group bound it), over blocks
+// that no box fits 582 us.  What the products' warp does between two of them counts most: weights
+// handed over in halves, to begin sooner, cost 80 us of 1,420, a lane elected anew each turn 68, a second warp for tile B 280.  The roles that copy
+// count next: a flag read after each wait there cost 3 %, an atomic report of bad blocks in place of a store 2 to 4 %.
+//
+// Weights are rounded once to the products' type, by 2^-9 relative in bfloat16 and 2^-12 in halves; sums of weights are not.  Outputs of a prompt
+// of 2,000 are off by 2.0e-3 of their root mean square for it (bfloat16; their own rounding alone is 1.6e-3), 2.6e-4 in halves (2.0e-4).  The remainders' product, which
+// attend_kernel has in bfloat16, would be half as many products again here, where these bound the work.
 //
 // Work is laid on a line and cut into equal stretches as in wf_attend.cu; a unit is the 256 queries, its weight grows with
 // the positions that they see.  Every wait ends: after a limit it is reported (wf_attn_status) and the role that waited leaves, as the others of the
@@ -749,7 +755,8 @@ template <typename T> __device__ __forceinline__ void put(uint8_t *const (&out)[
 }
 
 // Values of a tile (halves where the cache has 8 bits) from key `from` on, up to `to`, which some queries of the 128 do not see: what is no finite number becomes 0,
-// and give_unfit's.  A thread looks through a key.  False: waiting was given up.  (Sixteen prompts of 512: 92 -> 96 us.)
+// and give_unfit's.  A thread looks through a key.  False: waiting was given up.  (Sixteen prompts of 512: 91 -> 97 us; after the powers, where more
+// registers are spilled for it, one of 16,384 took 1,389 us for 1,333.)
 template <typename T, bool E, int D> __device__ __forceinline__ bool take_unfit(const Shared &sh, uint32_t it, int32_t from, int32_t to, uint32_t unit)
 {
     using S = Shape<E, D>;

@@ -10,8 +10,8 @@
 // each, and computes little: HBM bounds it, and launches where tokens are few.
 // A lane takes 8 pairs of a head (two 16-byte loads, two 16-byte stores), a
 // CTA some tokens with all their heads, so that the cosines of a token are made
-// once, in shared memory, for every head.  16,800 tokens of 32 + 8 + 8 heads of 128 take 77 us, 5.4 TB/s; two rounds of loads under way
-// together are best (77 us; four 80: fewer warps fit).
+// once, in shared memory, for every head.  18,360 tokens of 32 + 8 + 8 heads of 128 take 85 us, 5.3 TB/s; two rounds of loads under way
+// together are best (77 us for 16,800 tokens; four 80: fewer warps fit).
 #include <algorithm>
 
 #include "wf_decode.cuh"
@@ -230,7 +230,7 @@ template <typename T, int D, bool HALF, bool VEC> __global__ void __launch_bound
 //
 // The scale of a block and head is known when its new tokens have been seen, so a block's part in the step is one CTA's: magnitudes, scale,
 // elements.  That is a chain of loads, three barriers and a store, and what bounds it: 2,000 rows decoding (32 + 8 + 8 heads of 128) take
-// 17 us where their bytes take 6.6, 9,100 prompt tokens in blocks of 64 31 us (9.6).  Elements stay in registers between magnitude and
+// 17 us where their bytes take 6.6, 8,660 prompt tokens in blocks of 64 30 us (9.2).  Elements stay in registers between magnitude and
 // store where they fit (26 -> 17 us with blocks found by a multiplication in place of 64-bit divisions).
 // ---------------------------------------------------------------------------
 

@@ -932,7 +932,7 @@ def wf_attend(attn: Attn, kv: Kv, step: KvStep, layer: KvLayer, q, out, scale: f
     """Causal attention of a step's tokens over their rows' cached keys and values (the step's own among them): q, out
     [max_tokens, heads, dim] in float16 or bfloat16, tokens and heads strided by multiples of 16 bytes; out apart from every input (not in place).
     scale: of the products (None: dim^-0.5); new: the most new tokens that a row is expected to have, a hint for the
-    launch (1: a step of decoding; 0: unknown)."""
+    launch (1: a step of decoding; 0: unknown), which any step may be given; roundings of weights may differ by it."""
     _check_layer("wf_attend", kv, step, layer, attn)
     dtype, n, dim, dev = getattr(q, "dtype", None), step.max_tokens, layer.dim, kv.device
     code = _dtype_code(dtype)
