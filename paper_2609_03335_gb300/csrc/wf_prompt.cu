@@ -29,7 +29,7 @@
 //
 // Work is laid on a line and cut into equal stretches as in wf_attend.cu; a unit is the 256 queries, its weight grows with
 // the positions that they see.  Every wait ends: after a limit it is reported (wf_attn_status) and the role that waited leaves, as the others of the
-// CTA do at their next wait that finds nothing.  No unit is overwritten, no output joined and no copy or product begun after that; those under
+// CTA do at their next wait that finds nothing.  No unit is overwritten then, and no barrier without limit stands between roles; copies and products under
 // way are awaited before the CTA ends, and wf_attn_status clears the arrivals that a join may be left with.
 #include <algorithm>
 #include <type_traits>
@@ -472,7 +472,7 @@ template <typename T, bool E, int D> __device__ __forceinline__ void box_role(co
     __syncwarp();
 }
 
-// Positions that the first query q of the unit sees.
+// Positions that query q of the unit sees.
 __device__ __forceinline__ int32_t seen_by(const AttendArgs &a, const Unit &u, int q)
 {
     return u.row.len - u.row.n + (int32_t)wf_quot((uint32_t)(u.q0 + q), a.by_group) + 1;
