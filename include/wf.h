@@ -733,7 +733,7 @@ typedef struct {
     int32_t q_heads;               /* 0: no queries; up to 1024 */
     const void *k, *v;             /* [max_tokens][layer heads][layer dim] */
     const void *q;                 /* [max_tokens][q_heads][layer dim] */
-    void *q_out;                   /* the turned queries: q itself (with its strides) or apart from every input */
+    void *q_out;                   /* the turned queries: q itself (with its strides) or apart from every input; among one (columns of one product) with its strides */
     int64_t k_token, k_head;       /* bytes between tokens, between heads; multiples of the element size */
     int64_t v_token, v_head;
     int64_t q_token, q_head;

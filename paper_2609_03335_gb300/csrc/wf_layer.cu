@@ -46,6 +46,32 @@ static int check_heads(const void *p, int64_t token, int64_t head, const char *w
     return WF_OK;
 }
 
+// A tensor [tokens][heads][elements], strides in bytes.
+struct Heads {
+    const void *at;
+    int64_t token, head;
+    int32_t heads;
+};
+
+// Whether two of them have bytes in common.  Tensors that lie among each other (parts of one product's columns) need the same strides to be told
+// apart; others have to have ranges of their own.
+static bool meet(const Heads &a, const Heads &b, int64_t tokens, int64_t bytes)
+{
+    const int64_t n = tokens - 1;
+    auto low = [&](const Heads &x) { return n * std::min<int64_t>(x.token, 0) + (x.heads - 1) * std::min<int64_t>(x.head, 0); };
+    auto high = [&](const Heads &x) { return n * std::max<int64_t>(x.token, 0) + (x.heads - 1) * std::max<int64_t>(x.head, 0) + bytes; };
+    const int64_t apart = (const uint8_t *)b.at - (const uint8_t *)a.at;
+    if (apart + low(b) >= high(a) || apart + high(b) <= low(a)) return false;
+    const int64_t head = a.heads == 1 ? b.head : a.head;  // one head's stride does not count
+    if ((n && a.token != b.token) || (a.heads > 1 && b.heads > 1 && a.head != b.head)) return true;
+    for (int64_t j = 1 - a.heads; j < b.heads; j++) {  // heads apart; then the token that lies nearest
+        const int64_t at = apart + j * head, i = a.token ? std::clamp(-at / a.token, -n, n) : 0;
+        for (int64_t k = std::max(-n, i - 1); k <= std::min(n, i + 1); k++)
+            if (std::abs(at + k * a.token) < bytes) return true;
+    }
+    return false;
+}
+
 extern "C" int wf_kv_write(wf_decode *d, const wf_kv *kv, const wf_kv_step *step, const wf_kv_layer *layer, const wf_rope *rope,
                            const wf_kv_new *in, void *stream)
 {
@@ -66,6 +92,12 @@ extern "C" int wf_kv_write(wf_decode *d, const wf_kv *kv, const wf_kv_step *step
         if (rc) return rc;
         REQUIRE(in->q != in->q_out || (in->q_token == in->q_out_token && in->q_head == in->q_out_head),
                 "%s: queries turned in place under other strides", what);
+        const Heads out = {in->q_out, in->q_out_token, in->q_out_head, in->q_heads};
+        const int64_t bytes = 2 * layer->dim;
+        REQUIRE((in->q == in->q_out || !meet(out, {in->q, in->q_token, in->q_head, in->q_heads}, step->max_tokens, bytes)) &&
+                    !meet(out, {in->k, in->k_token, in->k_head, layer->heads}, step->max_tokens, bytes) &&
+                    !meet(out, {in->v, in->v_token, in->v_head, layer->heads}, step->max_tokens, bytes),
+                "%s: turned queries in the memory of keys, values or other queries", what);
     }
     REQUIRE(step->slot && wf_aligned(step->slot, 8), "%s: NULL or misaligned slots", what);
     if (rope) {
@@ -199,24 +231,6 @@ static int check_attn(const void *p, int64_t token, int64_t head, const char *wh
     return WF_OK;
 }
 
-// Whether queries and outputs have bytes in common.  Tensors that lie among each other (two parts of one product's columns) need the same strides
-// to be told apart; others have to have ranges of their own.
-static bool meet(const wf_attn_in &in, int64_t tokens, int64_t bytes)
-{
-    const int64_t n = tokens - 1, m = in.heads - 1;
-    auto low = [&](int64_t token, int64_t head) { return n * std::min<int64_t>(token, 0) + m * std::min<int64_t>(head, 0); };
-    auto high = [&](int64_t token, int64_t head) { return n * std::max<int64_t>(token, 0) + m * std::max<int64_t>(head, 0) + bytes; };
-    const int64_t apart = (const uint8_t *)in.out - (const uint8_t *)in.q;
-    if (apart + low(in.out_token, in.out_head) >= high(in.q_token, in.q_head) || apart + high(in.out_token, in.out_head) <= low(in.q_token, in.q_head)) return false;
-    if ((n && in.q_token != in.out_token) || (m && in.q_head != in.out_head)) return true;
-    for (int64_t j = -m; j <= m; j++) {  // heads apart; then the token that lies nearest
-        const int64_t at = apart + j * in.q_head, i = in.q_token ? std::clamp(-at / in.q_token, -n, n) : 0;
-        for (int64_t k = std::max(-n, i - 1); k <= std::min(n, i + 1); k++)
-            if (std::abs(at + k * in.q_token) < bytes) return true;
-    }
-    return false;
-}
-
 extern "C" int wf_attend(wf_attn *at, const wf_kv *kv, const wf_kv_step *step, const wf_kv_layer *layer, const wf_attn_in *in, void *stream)
 {
     const char *what = "wf_attend";
@@ -237,7 +251,8 @@ extern "C" int wf_attend(wf_attn *at, const wf_kv *kv, const wf_kv_step *step, c
     rc = check_attn(in->q, in->q_token, in->q_head, what, "queries");
     if (!rc) rc = check_attn(in->out, in->out_token, in->out_head, what, "outputs");
     if (rc) return rc;
-    REQUIRE(!meet(*in, step->max_tokens, 2 * layer->dim), "%s: outputs in the queries' memory", what);
+    REQUIRE(!meet({in->q, in->q_token, in->q_head, in->heads}, {in->out, in->out_token, in->out_head, in->heads}, step->max_tokens, 2 * layer->dim),
+            "%s: outputs in the queries' memory", what);
     rc = wf_cuda_check(cudaSetDevice(at->device), "cudaSetDevice");
     if (rc) return rc;
 

@@ -357,3 +357,28 @@ def test_writing_beside_scales_of_any_value(kv, bs, have, add, dtype):
         changed = want[plane] != was[plane]
         near = np.abs(got[plane] - exact) <= np.abs(want[plane] - exact) + 2.0 ** -22 * np.abs(exact)
         assert np.where(changed, near, got[plane] == was[plane])[np.isfinite(exact)].all()
+
+
+def test_turned_queries_in_other_memory_are_refused():
+    """Into keys, values or the queries a head or a token further on; in place and beside them, as columns of one product, they go on."""
+    import torch
+    wf = lib()
+    rng = np.random.default_rng(64)
+    st = Step(wf, rng, [40, 3], [1, 30], 16)
+    cache, _ = cache_of(rng, st, 2, 64, "float16")
+    layer, rope = wf.KvLayer(cache[0], cache[1]), wf.Rope(64)
+    whole = tensor(rng, (st.room + 1, 12, 64), "float16")
+    q, k, v, free = whole[:-1, :4], whole[:-1, 4:6], whole[:-1, 6:8], whole[:-1, 8:]
+    was = whole.clone()
+    run = lambda out, q=q: wf.wf_kv_write(st.decode, st.kv, st.step, layer, k, v, q=q, q_out=out, rope=rope)
+    for out in (whole[:-1, 1:5], whole[:-1, 3:7], whole[:-1, 5:9], whole[:-1, 7:11], whole[1:, :4], whole.view(-1, 4, 64)[:st.room]):
+        with pytest.raises(wf.WfError, match="turned"):
+            run(out)
+    with pytest.raises(wf.WfError, match="turned"):
+        run(whole[:-1, 4:5], q=whole[:-1, 8:9])  # one head, in the first key's place
+    assert torch.equal(whole, was)
+    apart = torch.empty_like(free)
+    run(apart)
+    run(free)
+    run(None)
+    assert torch.equal(free, apart) and torch.equal(q, apart) and torch.equal(whole[:-1, 4:8], was[:-1, 4:8])
